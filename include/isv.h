@@ -68,6 +68,7 @@ extern "C" {
 #define ISV_STATUS_WAIT_EXPIRED  2u   /* a bounded wait inside a kernel gave up                */
 #define ISV_STATUS_BAD_LENGTH    4u   /* a device-side sequence length was negative or exceeded */
                                       /* the table row; it was clamped to what the row covers  */
+#define ISV_STATUS_NO_PAGES      8u   /* isv_pages_*: fewer free pages than were needed        */
 
 typedef struct isv_kv isv_kv;   /* opaque; created by isv_kv_alloc, destroyed by isv_kv_free */
 
@@ -400,6 +401,164 @@ int isv_attn_decode_static(const void *kv_pool_dev, int32_t n_pool_blocks,
                            int32_t q_heads, int32_t kv_heads, int32_t head_dim, int32_t block_tokens,
                            int32_t dtype, int32_t max_ctas, const void *q_dev, void *out_dev,
                            float *out_f32_dev, uint32_t *status_dev, void *stream);
+
+/* ---- a KV cache held in 8 bits -------------------------------------------- */
+
+/* (The paper keeps K and V in the model's 16-bit precision; a cache in 8 bits halves both the memory term
+ * and the bandwidth term of its decode model.  These calls stand beside isv_attn_decode_static: the caller
+ * owns every buffer, nothing is offloaded.)
+ *
+ * A page holds one block of 16 tokens.  Every (page, KV head, K or V) has a scale of its own:
+ *     ISV_Q8_INT8   scale = absmax / 127, code = x / scale rounded to the nearest integer
+ *     ISV_Q8_E4M3   scale = absmax / 448, code = x / scale rounded to the nearest e4m3 value
+ * absmax is taken over the block's 16 x head_dim values; scale is the fp32 rounding of the quotient and the
+ * code is the rounding (ties to even) of the exact quotient x / scale.  A block of zeros has scale 0.  A
+ * block with an infinity or a NaN has scale NaN, and so has every result that reads it.
+ * Only complete blocks are quantised.  The open block of a sequence (its last n mod 16 tokens) stays in 16
+ * bits in the sequence's tail slot until it is complete; it is then rounded once and its page never changes
+ * again, so sequences may share complete pages.
+ *
+ * Page layout: [kv_head][16 * head_dim codes of K | 16 * head_dim codes of V | fp32 scale of K | fp32 scale
+ * of V | 8 unused bytes].  The codes are stored in the order in which a warp's lanes feed them to the tensor
+ * cores.  With D = head_dim and P = D / 32 (rounded down), byte b < 512 * P of a part belongs to
+ *     lane = (b mod 512) / 16, g = lane / 4, c = lane mod 4, p = b / 512, i = (b mod 16) / 8,
+ *     h = (b mod 8) / 4, j = b mod 4;
+ * the last 256 bytes at head_dim 80 belong to lane = (b - 512 * P) / 8, p = P, i = 0 and the same h and j:
+ *     K: token g + 8 * h,                           dim 32 * p + 8 * c + 4 * i + j  (32 * P + 4 * c + j in the last 256)
+ *     V: token 2 * c + (j mod 2) + 8 * (j / 2),     dim g * (D / 8) + 2 * (2 * p + i) + h
+ * Tail slots: [sequence][K|V][kv_head][16][head_dim] 16-bit, rows in order; rows from n mod 16 on are never
+ * read. */
+#define ISV_Q8_INT8  0
+#define ISV_Q8_E4M3  1
+
+typedef struct {
+    int32_t q_heads;             /* query heads; multiple of kv_heads                           */
+    int32_t kv_heads;
+    int32_t head_dim;            /* 64, 80 or 128                                               */
+    int32_t dtype;               /* ISV_F16 or ISV_BF16: q, k, v, tails and the 16-bit output   */
+    int32_t format;              /* ISV_Q8_INT8 or ISV_Q8_E4M3                                  */
+    int32_t max_seqs;            /* sequences per call, <= 4096                                 */
+    int32_t max_ctas;            /* cap on the attention kernel's grid; 0 = one CTA per SM      */
+} isv_q8_desc;
+
+typedef struct isv_q8 isv_q8;
+
+/* Bytes of one page and of one sequence's tail slot.  Needs no GPU. */
+int isv_q8_sizes(int32_t kv_heads, int32_t head_dim, uint64_t *page_bytes, uint64_t *tail_bytes);
+
+/* Allocates the attention's scratch and a status word on the current device (synchronous).  The handle
+ * holds no cache: any number of layers and pools may be used with it.  Calls on one handle share its
+ * scratch: order them on one stream or with events (one handle per stream or captured graph that may
+ * overlap another).  Calls run on the handle's device, whichever is current. */
+int isv_q8_create(isv_q8 **out, const isv_q8_desc *desc);
+int isv_q8_free(isv_q8 *h);
+
+/* Stores new tokens of one layer: a prompt, a chunk of one, or one token per sequence.  Sequence s has
+ * seq_lens_dev[s] tokens after the call; its last new_lens_dev[s] <= T of them are rows 0 .. of
+ *     k_dev, v_dev + s * seq_stride + t * token_stride, each [kv_heads][head_dim] 16-bit
+ * (strides in elements, multiples of 8).  new_lens_dev NULL = T new tokens for every sequence.  Blocks that
+ * are complete afterwards are quantised into the page that block_table_dev ([n_seqs][table_stride],
+ * max_blocks_per_seq <= table_stride entries of a row are used) names; the rest goes to the tail slot
+ * tails_dev[s].  A sequence with no new token keeps everything.  Page ids outside [0, n_pages) are skipped
+ * and flagged (ISV_STATUS_BAD_BLOCK_ID), also ISV_BLOCK_NONE; lengths are clamped to what the table row
+ * and the tail slot hold, 16 * max_blocks_per_seq + 15, and new lengths to [0, min(T, length)], and flagged
+ * (ISV_STATUS_BAD_LENGTH).  Asynchronous on `stream`; may be captured into a CUDA graph. */
+int isv_q8_write(isv_q8 *h, void *pool_dev, int32_t n_pages, void *tails_dev, const int32_t *block_table_dev,
+                 int32_t table_stride, int32_t max_blocks_per_seq, const int32_t *seq_lens_dev,
+                 const int32_t *new_lens_dev, const void *k_dev, const void *v_dev, int64_t seq_stride,
+                 int64_t token_stride, int32_t n_seqs, int32_t T, void *stream);
+
+/* out[s][h][:] = softmax(q[s][h] . K_s^T / sqrt(head_dim)) V_s over the seq_lens_dev[s] tokens of sequence s,
+ * as isv_attn_decode: complete blocks from their pages, the open block from its tail slot.  A sequence of
+ * length 0 yields zeros.  q_dev [n_seqs][q_heads][head_dim] 16-bit; out_dev (16-bit) and out_f32_dev (fp32),
+ * same shape, may each be NULL, not both.  A block without a page (ISV_BLOCK_NONE) is left out and not
+ * flagged; other ids outside [0, n_pages) are left out and flagged.  fp32 arithmetic; the same inputs give
+ * the same bits.  Asynchronous on `stream`; may be captured. */
+int isv_q8_attn(isv_q8 *h, const void *pool_dev, int32_t n_pages, const void *tails_dev,
+                const int32_t *block_table_dev, int32_t table_stride, int32_t max_blocks_per_seq,
+                const int32_t *seq_lens_dev, const void *q_dev, void *out_dev, float *out_f32_dev,
+                int32_t n_seqs, void *stream);
+
+/* Waits for `stream` and returns ISV_EDEVICE_STATUS (and clears the status) if a call on this handle
+ * flagged a problem since the last query. */
+int isv_q8_status(isv_q8 *h, void *stream, uint32_t *status_out);
+
+/* ---- pages of a paged cache ------------------------------------------------ */
+
+/* (The paper has no counterpart: it treats the cache as one growing array per sequence.)  For callers that
+ * own their pool and block table (isv_attn_decode_static, isv_q8_*).  All state is the table and the lengths:
+ * a page is live if some row names it in the blocks its length covers, and free otherwise; there are no
+ * reference counts to keep and nothing to release.  Rows may share pages.
+ *   block_table_dev  int32 [n_rows][table_stride]; the first max_blocks_per_seq entries of a row are used
+ *   lens_dev         int32 [n_rows] tokens; a length covers ceil(n / 16) blocks, or floor(n / 16) where the
+ *                    open block has no page (open_in_pool = 0: the 8-bit cache)
+ *   n_pages          pages of the pool, at most ISV_PAGES_MAX; ids outside [0, n_pages) are kept as they are,
+ *                    and flagged with ISV_STATUS_BAD_BLOCK_ID unless ISV_BLOCK_NONE
+ *   status_dev       optional uint32 into which ISV_STATUS_* bits are ORed
+ * Free pages are handed out lowest id first.  Lengths that are negative or not covered by max_blocks_per_seq
+ * are clamped and flagged (ISV_STATUS_BAD_LENGTH).  n_rows <= 4096.  All calls are asynchronous on `stream`,
+ * use no memory but what they are given, run on the current device, and may be captured into a CUDA graph.
+ * Results do not depend on scheduling. */
+#define ISV_PAGES_MAX (1 << 20)
+
+/* Copies whole pages: src_ids_dev[i] of src_pool to dst_ids_dev[i] of dst_pool (NULL = page i) for i < n, in
+ * each of `layers` slabs that lie a layer stride apart.  page_bytes and the strides are multiples of 16.
+ * n_dev (optional, device) lowers n to *n_dev.  An id of ISV_BLOCK_NONE on either side skips the pair; other
+ * ids outside the pool are skipped and flagged.  The pools may be the same; a page that is both source and
+ * destination of one call, or twice a destination, ends up with unspecified contents. */
+int isv_pages_copy(void *dst_pool_dev, int32_t n_dst_pages, const void *src_pool_dev, int32_t n_src_pages,
+                   uint64_t page_bytes, int32_t layers, uint64_t dst_layer_stride, uint64_t src_layer_stride,
+                   const int32_t *src_ids_dev, const int32_t *dst_ids_dev, int32_t n, const int32_t *n_dev,
+                   uint32_t *status_dev, void *stream);
+
+/* Row s of the new table (table_out_dev, lens_out_dev; n_rows_out rows, same stride) continues old row
+ * parent_dev[s]: the same row again (keep), another one (reorder), one that several rows name (fork), or
+ * ISV_BLOCK_NONE for an empty row.  Old rows that nobody continues are freed.  Entries behind a row's blocks
+ * become ISV_BLOCK_NONE.  Where rows continue the same parent and its last block is open (open_in_pool = 1
+ * and length mod 16 not 0), the first of them keeps that page and every other one gets a fresh page, in row
+ * order; copy_src_dev[s], copy_dst_dev[s] is then the pair for isv_pages_copy, else ISV_BLOCK_NONE twice.
+ * Fresh pages may be pages of freed rows.  Without enough free pages the last rows' entries become
+ * ISV_BLOCK_NONE (ISV_STATUS_NO_PAGES).  A parent outside [0, n_rows) other than ISV_BLOCK_NONE gives an empty
+ * row (ISV_STATUS_BAD_BLOCK_ID).  The arrays must not overlap. */
+int isv_pages_fork(const int32_t *block_table_dev, const int32_t *lens_dev, int32_t n_rows, const int32_t *parent_dev,
+                   int32_t *table_out_dev, int32_t *lens_out_dev, int32_t n_rows_out, int32_t table_stride,
+                   int32_t max_blocks_per_seq, int32_t open_in_pool, int32_t n_pages, int32_t *copy_src_dev,
+                   int32_t *copy_dst_dev, uint32_t *status_dev, void *stream);
+
+/* Grows and shrinks rows in place, from lens_dev to new_lens_dev (neither is written): blocks that a longer
+ * row adds get free pages, in the order of rows and blocks; blocks behind the new length are freed, their
+ * entries become ISV_BLOCK_NONE.  Length 0 frees a row.  Without enough free pages the last blocks in that
+ * order become ISV_BLOCK_NONE (ISV_STATUS_NO_PAGES).  A page freed by this call may be handed out by it. */
+int isv_pages_resize(int32_t *block_table_dev, const int32_t *lens_dev, const int32_t *new_lens_dev, int32_t n_rows,
+                     int32_t table_stride, int32_t max_blocks_per_seq, int32_t open_in_pool, int32_t n_pages,
+                     uint32_t *status_dev, void *stream);
+
+/* Renames live pages so that they are exactly the ids [0, counts[0]): the i-th live page from counts[0] on
+ * takes the i-th free id below it.  table_out_dev (may be block_table_dev itself) gets the new ids, with
+ * ISV_BLOCK_NONE behind every row's blocks; src_ids_dev[i] -> dst_ids_dev[i], i < counts[1], are the moves for
+ * isv_pages_copy (sources and destinations are disjoint), filled up with ISV_BLOCK_NONE to max_moves, which
+ * must be at least n_pages / 2.  counts_dev: int32 [2]. */
+int isv_pages_compact(const int32_t *block_table_dev, const int32_t *lens_dev, int32_t n_rows, int32_t table_stride,
+                      int32_t max_blocks_per_seq, int32_t open_in_pool, int32_t n_pages, int32_t *table_out_dev,
+                      int32_t *src_ids_dev, int32_t *dst_ids_dev, int32_t max_moves, int32_t *counts_dev,
+                      uint32_t *status_dev, void *stream);
+
+/* ---- decode linear layers with 4-bit weights -------------------------------- */
+
+/* y = x . w^T as isv_linear_*, with w[n][k] = (u[n][k] - 8) * scale[n][k / group] and u in 0 .. 15, for M <= max_M
+ * <= 64 tokens: a quarter of the weight bytes that bound a decode step's linear layers at small batches.
+ *   w4_dev      uint8 [N][K / 2]: u[n][2 i] in the low and u[n][2 i + 1] in the high four bits of byte i
+ *   scales_dev  [N][K / group] 16-bit of `dtype`; group 32, 64 or 128, K a multiple of it; N >= 1
+ *   x_dev [M][K] 16-bit;  y_dev [M][N] 16-bit and / or y_f32_dev [M][N] fp32 (one may be NULL)
+ * isv_linear4_create lays the weights out anew in memory of its own (on `stream`, then waits for it): w4_dev and
+ * scales_dev may be freed afterwards.  isv_linear4_forward is asynchronous on the stream it is given, keeps no
+ * state between calls (calls may overlap) and may be captured; it runs on the handle's device.  Products are
+ * exact and summed in fp32; the scale is applied to each group's sum. */
+typedef struct isv_linear4 isv_linear4;
+int isv_linear4_create(isv_linear4 **out, const void *w4_dev, const void *scales_dev, int32_t N, int32_t K,
+                       int32_t group, int32_t dtype, int32_t max_M, void *stream);
+int isv_linear4_forward(isv_linear4 *l, const void *x_dev, void *y_dev, float *y_f32_dev, int32_t M, void *stream);
+int isv_linear4_free(isv_linear4 *l);
 
 /* Text of the calling thread's last error; valid until its next call. */
 const char *isv_last_error(void);

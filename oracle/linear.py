@@ -24,3 +24,25 @@ def linear_flops_per_layer(BS: int, h1: int, h2: int) -> float:
     """Flops of one layer's decode projections: QKV (3 h1^2), output (h1^2) and the two MLP
     matrices (2 h1 h2), two flops per multiply-add: BS * (8 h1^2 + 4 h1 h2)."""
     return 2.0 * BS * (3 * h1 * h1 + h1 * h1 + 2 * h1 * h2)
+
+
+def linear4(x, w4: np.ndarray, scales, group: int) -> np.ndarray:
+    """x [M, K], w4 uint8 [N, K / 2] (even k in the low four bits), scales [N, K / group] -> y [M, N] float64 with
+    w[n][k] = (u[n][k] - 8) * scale[n][k / group]."""
+    u = np.empty((w4.shape[0], 2 * w4.shape[1]), np.float64)
+    u[:, 0::2] = w4 & 15
+    u[:, 1::2] = w4 >> 4
+    w = (u - 8.0) * np.repeat(to_f64(scales), group, axis=1)
+    return np.matmul(to_f64(x), w.T)
+
+
+def linear4_error(x, w4: np.ndarray, scales, group: int) -> np.ndarray:
+    """How far fp32 sums may be from :func:`linear4`: K exact products are summed with at most 2^-23 of the running
+    magnitude lost per addition (2^-24 by rounding, twice that where a sum truncates), and each of the K / group
+    scalings rounds once: (K + K / group + 64) * 2^-23 of the sum of the magnitudes."""
+    u = np.empty((w4.shape[0], 2 * w4.shape[1]), np.float64)
+    u[:, 0::2] = w4 & 15
+    u[:, 1::2] = w4 >> 4
+    K = u.shape[1]
+    w = np.abs(u - 8.0) * np.repeat(np.abs(to_f64(scales)), group, axis=1)
+    return (K + K // group + 64) * 2.0 ** -23 * np.matmul(np.abs(to_f64(x)), w.T)

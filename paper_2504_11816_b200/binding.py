@@ -33,6 +33,10 @@ ISV_BLOCK_HOST_BIT = 1 << 30
 ISV_STATUS_BAD_BLOCK_ID = 1
 ISV_STATUS_WAIT_EXPIRED = 2
 ISV_STATUS_BAD_LENGTH = 4
+ISV_STATUS_NO_PAGES = 8
+ISV_Q8_INT8 = 0
+ISV_Q8_E4M3 = 1
+ISV_PAGES_MAX = 1 << 20
 
 EXPORTS = [
     "isv_kv_alloc", "isv_kv_free", "isv_kv_reset", "isv_kv_info", "isv_kv_fill", "isv_kv_fill_async",
@@ -42,6 +46,9 @@ EXPORTS = [
     "isv_plan_bytes", "isv_set_zero_copy", "isv_set_timing", "isv_step_timing", "isv_sync", "isv_link_probe",
     "isv_set_host_timeout", "isv_set_wait_limit", "isv_inject_lost_copy",
     "isv_attn_decode_static", "isv_linear_create", "isv_linear_forward", "isv_linear_status", "isv_linear_free",
+    "isv_q8_sizes", "isv_q8_create", "isv_q8_free", "isv_q8_write", "isv_q8_attn", "isv_q8_status",
+    "isv_pages_copy", "isv_pages_fork", "isv_pages_resize", "isv_pages_compact",
+    "isv_linear4_create", "isv_linear4_forward", "isv_linear4_free",
     "isv_last_error",
 ]
 
@@ -100,6 +107,11 @@ class FillTimes(ctypes.Structure):
     ]
 
 
+class Q8Desc(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in
+                ("q_heads", "kv_heads", "head_dim", "dtype", "format", "max_seqs", "max_ctas")]
+
+
 _lib = None
 
 
@@ -149,6 +161,20 @@ def lib():
     L.isv_linear_forward.argtypes = [vp, vp, vp, vp, i32]
     L.isv_linear_status.argtypes = [vp, P(ctypes.c_uint32)]
     L.isv_linear_free.argtypes = [vp]
+    i64 = ctypes.c_int64
+    L.isv_q8_sizes.argtypes = [i32, i32, P(u64), P(u64)]
+    L.isv_q8_create.argtypes = [P(vp), P(Q8Desc)]
+    L.isv_q8_free.argtypes = [vp]
+    L.isv_q8_write.argtypes = [vp, vp, i32, vp, vp, i32, i32, vp, vp, vp, vp, i64, i64, i32, i32, vp]
+    L.isv_q8_attn.argtypes = [vp, vp, i32, vp, vp, i32, i32, vp, vp, vp, vp, i32, vp]
+    L.isv_q8_status.argtypes = [vp, vp, P(ctypes.c_uint32)]
+    L.isv_pages_copy.argtypes = [vp, i32, vp, i32, u64, i32, u64, u64, vp, vp, i32, vp, vp, vp]
+    L.isv_pages_fork.argtypes = [vp, vp, i32, vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp]
+    L.isv_pages_resize.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, vp, vp]
+    L.isv_pages_compact.argtypes = [vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, i32, vp, vp, vp]
+    L.isv_linear4_create.argtypes = [P(vp), vp, vp, i32, i32, i32, i32, i32, vp]
+    L.isv_linear4_forward.argtypes = [vp, vp, vp, vp, i32, vp]
+    L.isv_linear4_free.argtypes = [vp]
     L.isv_last_error.argtypes = []
     L.isv_last_error.restype = ctypes.c_char_p
     for name in EXPORTS:
@@ -356,6 +382,92 @@ def isv_linear_status(l: int) -> int:
 
 def isv_linear_free(l: int):
     _check(lib().isv_linear_free(l))
+
+
+def isv_q8_sizes(kv_heads: int, head_dim: int):
+    """(bytes of one page, bytes of one sequence's tail slot) of the 8-bit cache."""
+    page, tail = ctypes.c_uint64(0), ctypes.c_uint64(0)
+    _check(lib().isv_q8_sizes(kv_heads, head_dim, ctypes.byref(page), ctypes.byref(tail)))
+    return page.value, tail.value
+
+
+def isv_q8_create(**kw) -> int:
+    """Fields of ``isv_q8_desc`` as keyword arguments; returns the handle."""
+    h = ctypes.c_void_p()
+    _check(lib().isv_q8_create(ctypes.byref(h), ctypes.byref(Q8Desc(**kw))))
+    return h.value
+
+
+def isv_q8_free(h: int):
+    _check(lib().isv_q8_free(h))
+
+
+def isv_q8_write(h: int, pool, n_pages: int, tails, block_table, table_stride: int, max_blocks_per_seq: int, seq_lens,
+                 new_lens, k, v, seq_stride: int, token_stride: int, n_seqs: int, T: int, stream: int = 0):
+    """Stores up to ``T`` new tokens per sequence; ``seq_lens`` counts them already (see ``include/isv.h``)."""
+    _check(lib().isv_q8_write(h, _ptr(pool), n_pages, _ptr(tails), _ptr(block_table), table_stride, max_blocks_per_seq,
+                              _ptr(seq_lens), _ptr(new_lens), _ptr(k), _ptr(v), seq_stride, token_stride, n_seqs, T,
+                              stream or None))
+
+
+def isv_q8_attn(h: int, pool, n_pages: int, tails, block_table, table_stride: int, max_blocks_per_seq: int, seq_lens, q,
+                out, out_f32, n_seqs: int, stream: int = 0):
+    """Decode attention over the 8-bit cache."""
+    _check(lib().isv_q8_attn(h, _ptr(pool), n_pages, _ptr(tails), _ptr(block_table), table_stride, max_blocks_per_seq,
+                             _ptr(seq_lens), _ptr(q), _ptr(out), _ptr(out_f32), n_seqs, stream or None))
+
+
+def isv_q8_status(h: int, stream: int = 0) -> int:
+    st = ctypes.c_uint32(0)
+    _check(lib().isv_q8_status(h, stream or None, ctypes.byref(st)))
+    return st.value
+
+
+def isv_pages_copy(dst_pool, n_dst_pages: int, src_pool, n_src_pages: int, page_bytes: int, layers: int,
+                   dst_layer_stride: int, src_layer_stride: int, src_ids, dst_ids, n: int, n_dev=None, status=None,
+                   stream: int = 0):
+    """Copies pages ``src_ids[i]`` to ``dst_ids[i]`` (None = page i) in every layer."""
+    _check(lib().isv_pages_copy(_ptr(dst_pool), n_dst_pages, _ptr(src_pool), n_src_pages, page_bytes, layers,
+                                dst_layer_stride, src_layer_stride, _ptr(src_ids), _ptr(dst_ids), n, _ptr(n_dev),
+                                _ptr(status), stream or None))
+
+
+def isv_pages_fork(block_table, lens, n_rows: int, parent, table_out, lens_out, n_rows_out: int, table_stride: int,
+                   max_blocks_per_seq: int, open_in_pool: int, n_pages: int, copy_src, copy_dst, status=None,
+                   stream: int = 0):
+    """Row s of the new table continues old row ``parent[s]``: reorder, fork and free rows."""
+    _check(lib().isv_pages_fork(_ptr(block_table), _ptr(lens), n_rows, _ptr(parent), _ptr(table_out), _ptr(lens_out),
+                                n_rows_out, table_stride, max_blocks_per_seq, open_in_pool, n_pages, _ptr(copy_src),
+                                _ptr(copy_dst), _ptr(status), stream or None))
+
+
+def isv_pages_resize(block_table, lens, new_lens, n_rows: int, table_stride: int, max_blocks_per_seq: int,
+                     open_in_pool: int, n_pages: int, status=None, stream: int = 0):
+    """Hands out and frees the pages that rows need to go from ``lens`` to ``new_lens``, in place."""
+    _check(lib().isv_pages_resize(_ptr(block_table), _ptr(lens), _ptr(new_lens), n_rows, table_stride,
+                                  max_blocks_per_seq, open_in_pool, n_pages, _ptr(status), stream or None))
+
+
+def isv_pages_compact(block_table, lens, n_rows: int, table_stride: int, max_blocks_per_seq: int, open_in_pool: int,
+                      n_pages: int, table_out, src_ids, dst_ids, max_moves: int, counts, status=None, stream: int = 0):
+    """Renames live pages to the lowest ids; the moves are for :func:`isv_pages_copy`."""
+    _check(lib().isv_pages_compact(_ptr(block_table), _ptr(lens), n_rows, table_stride, max_blocks_per_seq, open_in_pool,
+                                   n_pages, _ptr(table_out), _ptr(src_ids), _ptr(dst_ids), max_moves, _ptr(counts),
+                                   _ptr(status), stream or None))
+
+
+def isv_linear4_create(w4, scales, N: int, K: int, group: int, dtype: int, max_M: int, stream: int = 0) -> int:
+    h = ctypes.c_void_p()
+    _check(lib().isv_linear4_create(ctypes.byref(h), _ptr(w4), _ptr(scales), N, K, group, dtype, max_M, stream or None))
+    return h.value
+
+
+def isv_linear4_forward(l: int, x, y, y_f32, M: int, stream: int = 0):
+    _check(lib().isv_linear4_forward(l, _ptr(x), _ptr(y), _ptr(y_f32), M, stream or None))
+
+
+def isv_linear4_free(l: int):
+    _check(lib().isv_linear4_free(l))
 
 
 def desc_from_workload(w, **overrides) -> dict:
