@@ -1,5 +1,5 @@
-// The KV cache held in 8 bits: storing new tokens (quantisation of complete blocks) and decode attention over it.
-// Layout, formats and the treatment of open blocks are described in include/isv.h.
+// The KV cache held in 8 bits: the handle, and storing new tokens (quantisation of complete blocks).  Layout, formats and
+// the treatment of open blocks are described in include/isv.h; the attention kernel is in isv_q8_attn.cu.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
@@ -12,6 +12,8 @@
 #include <new>
 
 #include "../../include/isv.h"
+#include "isv_kernels.cuh"
+#include "isv_q8.cuh"
 
 namespace isv {
 int set_error(int code, const char *msg);
@@ -19,7 +21,11 @@ int set_error(int code, const char *msg);
 
 namespace {
 
-constexpr int kBT = 16;   // tokens of a page
+using isv::q8::AttnParams;
+using isv::q8::CacheParams;
+using isv::q8::kBT;
+using isv::q8::seq_len;
+using isv::q8::unit_bytes;
 
 int err(int code, const char *fmt, ...) {
     char buf[512];
@@ -44,17 +50,6 @@ struct OnDevice {
     }
 };
 
-__host__ __device__ constexpr int unit_bytes(int d) { return 2 * kBT * d + 16; }
-
-struct CacheParams {
-    uint8_t *pool;              // [n_pages][Hkv] units
-    uint8_t *tails;             // [n_seqs][K|V][Hkv][16][D] 16-bit
-    const int32_t *table;       // [n_seqs][table_stride]
-    const int32_t *lens;
-    uint32_t *status;
-    int32_t table_stride, max_blocks, n_pages, n_seqs, Hkv;
-};
-
 struct WriteParams {
     CacheParams c;
     const int32_t *new_lens;    // NULL = T
@@ -63,22 +58,6 @@ struct WriteParams {
     int32_t T, blocks;          // blocks: how many blocks T tokens can touch
     int32_t bf16, e4m3;
 };
-
-struct AttnParams {
-    CacheParams c;
-    const uint16_t *q;
-    void *out;
-    float *out_f32;
-    int32_t Hq, bf16, e4m3;
-    float scale_log2;
-};
-
-// Tokens of sequence s, clamped to what its table row and its tail slot hold.
-__device__ __forceinline__ int seq_len(const CacheParams &c, int s, bool &bad) {
-    const int n = c.lens[s], most = c.max_blocks * kBT + kBT - 1;
-    bad = n < 0 || n > most;
-    return min(max(n, 0), most);
-}
 
 __device__ __forceinline__ float to_f32(uint16_t b, int bf16) {
     return bf16 ? __bfloat162float(__ushort_as_bfloat16(b)) : __half2float(__ushort_as_half(b));
@@ -178,60 +157,17 @@ __global__ void write_kernel(WriteParams p, int D) {
     }
 }
 
-// One warp per (sequence, query head) walks the tokens with a running maximum and sum.
-__global__ void attn_kernel(AttnParams p, int D) {
-    const int h = blockIdx.x, s = blockIdx.y, lane = threadIdx.x;
-    bool bad;
-    const int len = seq_len(p.c, s, bad);
-    if (bad && lane == 0) atomicOr(p.c.status, ISV_STATUS_BAD_LENGTH);
-    const int hk = h / (p.Hq / p.c.Hkv);
-    const uint16_t *q = p.q + ((size_t)s * p.Hq + h) * D;
-    float qv[4], o[4] = {0.f, 0.f, 0.f, 0.f}, m = -INFINITY, l = 0.f;
-    for (int i = 0; i < 4; ++i) qv[i] = lane + 32 * i < D ? to_f32(q[lane + 32 * i], p.bf16) : 0.f;
-    auto value = [&](const uint8_t *unit, const uint16_t *tail, int kv, int t, int x) {
-        if (!unit) return to_f32(tail[(size_t)kv * p.c.Hkv * kBT * D + t * D + x], p.bf16);
-        const uint8_t b = unit[kv * kBT * D + (kv ? v_byte(t, x, D) : k_byte(t, x, D))];
-        const float f = p.e4m3 ? __half2float(__half(__nv_cvt_fp8_to_halfraw(b, __NV_E4M3))) : (float)(int8_t)b;
-        return f * reinterpret_cast<const float *>(unit + 2 * kBT * D)[kv];
-    };
-    const uint16_t *tail = reinterpret_cast<const uint16_t *>(p.c.tails) + ((size_t)s * 2 * p.c.Hkv + hk) * kBT * D;
-    for (int t = 0; t < len; ++t) {
-        const uint8_t *unit = nullptr;
-        if (t / kBT < len / kBT) {
-            const int page = p.c.table[(size_t)s * p.c.table_stride + t / kBT];
-            if (page < 0 || page >= p.c.n_pages) {
-                if (page != ISV_BLOCK_NONE && lane == 0) atomicOr(p.c.status, ISV_STATUS_BAD_BLOCK_ID);
-                continue;
-            }
-            unit = p.c.pool + ((size_t)page * p.c.Hkv + hk) * unit_bytes(D);
-        }
-        float dot = 0.f;
-        for (int i = 0; i < 4; ++i)
-            if (lane + 32 * i < D) dot += qv[i] * value(unit, tail, 0, t % kBT, lane + 32 * i);
-        for (int x = 16; x; x /= 2) dot += __shfl_xor_sync(~0u, dot, x);
-        dot *= p.scale_log2;
-        const float top = fmaxf(m, dot), f = exp2f(m - top), w = exp2f(dot - top);
-        l = l * f + w;
-        for (int i = 0; i < 4; ++i)
-            if (lane + 32 * i < D) o[i] = o[i] * f + w * value(unit, tail, 1, t % kBT, lane + 32 * i);
-        m = top;
-    }
-    for (int i = 0; i < 4; ++i) {
-        const int x = lane + 32 * i;
-        if (x >= D) break;
-        const float r = m == -INFINITY ? 0.f : o[i] / l;
-        const size_t at = ((size_t)s * p.Hq + h) * D + x;
-        if (p.out_f32) p.out_f32[at] = r;
-        if (p.out) static_cast<uint16_t *>(p.out)[at] = p.bf16 ? __bfloat16_as_ushort(__float2bfloat16(r)) : __half_as_ushort(__float2half(r));
-    }
-}
-
 }  // namespace
 
 struct isv_q8 {
     isv_q8_desc d{};
     int device = 0;
+    int GT = 1, P = 1;            // query heads of a visit, visits that share a block
+    int grid = 1;
+    int smem_optin = 0;
     uint32_t *status = nullptr;
+    float *part_o = nullptr, *part_ml = nullptr;   // the attention's partial results
+    int32_t *tickets = nullptr;
 };
 
 namespace {
@@ -277,6 +213,9 @@ int isv_q8_free(isv_q8 *h) {
     OnDevice on(h->device);
     cudaDeviceSynchronize();   // calls may have been made on any stream
     cudaFree(h->status);
+    cudaFree(h->part_o);
+    cudaFree(h->part_ml);
+    cudaFree(h->tickets);
     delete h;
     return ISV_OK;
 }
@@ -297,13 +236,30 @@ int isv_q8_create(isv_q8 **out, const isv_q8_desc *desc) {
     isv_q8 *h = new (std::nothrow) isv_q8();
     if (!h) return err(ISV_EINVAL, "out of host memory");
     h->d = *desc;
+    const int G = desc->q_heads / desc->kv_heads, D = desc->head_dim;
+    h->GT = isv::group_heads(G);
+    h->P = G / h->GT;
+    int sms = 0;
     cudaError_t e = cudaGetDevice(&h->device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, h->device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&h->smem_optin, cudaDevAttrMaxSharedMemoryPerBlockOptin, h->device);
+    h->grid = desc->max_ctas > 0 ? std::min(desc->max_ctas, sms) : sms;   // one CTA per SM
+    if (e == cudaSuccess && isv::q8::attn_smem(D, h->GT, desc->max_seqs) + 1024 > (size_t)h->smem_optin) {
+        delete h;
+        return err(ISV_EINVAL, "isv_q8_create: shared memory too small for this shape");
+    }
+    const size_t rows = (size_t)isv::q8::attn_slots(h->GT, h->grid) * isv::q8::attn_head_rows(h->GT);
+    if (e == cudaSuccess) e = isv::q8::attn_configure(D, h->GT, desc->dtype == ISV_BF16, desc->format == ISV_Q8_E4M3, h->smem_optin - 1024);
     if (e == cudaSuccess) e = cudaMalloc((void **)&h->status, 4);
     if (e == cudaSuccess) e = cudaMemset(h->status, 0, 4);
+    if (e == cudaSuccess) e = cudaMalloc((void **)&h->part_o, rows * D * 4);
+    if (e == cudaSuccess) e = cudaMalloc((void **)&h->part_ml, rows * 2 * 4);
+    if (e == cudaSuccess) e = cudaMalloc((void **)&h->tickets, (size_t)h->grid * 4);
+    if (e == cudaSuccess) e = cudaMemset(h->tickets, 0, (size_t)h->grid * 4);
+    if (e == cudaSuccess) e = cudaDeviceSynchronize();   // the zeros are there before any stream's first call
     if (e != cudaSuccess) {
         cudaGetLastError();
-        if (h->status) cudaFree(h->status);
-        delete h;
+        isv_q8_free(h);
         return err(e == cudaErrorMemoryAllocation ? ISV_ENOMEM_DEVICE : ISV_ECUDA, "isv_q8_create: %s", cudaGetErrorString(e));
     }
     *out = h;
@@ -347,16 +303,20 @@ int isv_q8_attn(isv_q8 *h, const void *pool_dev, int32_t n_pages, const void *ta
     if (misaligned(q_dev) || misaligned(out_dev) || misaligned(out_f32_dev))
         return err(ISV_EINVAL, "isv_q8_attn: q and outputs must be 16-byte aligned");
     if (n_seqs == 0) return ISV_OK;
+    const long long groups = (long long)h->d.kv_heads * h->P;
+    if (((long long)max_blocks_per_seq + 1) * n_seqs * groups >= (1ll << 31))
+        return err(ISV_EINVAL, "isv_q8_attn: n_seqs * blocks * heads too large");
     AttnParams p{};
     p.c = cache_params(h, pool_dev, n_pages, tails_dev, block_table_dev, table_stride, max_blocks_per_seq, seq_lens_dev, n_seqs);
     p.q = static_cast<const uint16_t *>(q_dev);
     p.out = out_dev; p.out_f32 = out_f32_dev;
-    p.Hq = h->d.q_heads; p.bf16 = h->d.dtype == ISV_BF16; p.e4m3 = h->d.format == ISV_Q8_E4M3;
+    p.part_o = h->part_o; p.part_ml = h->part_ml; p.tickets = h->tickets;
+    p.Hq = h->d.q_heads; p.P = h->P; p.GT = h->GT;
     p.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)h->d.head_dim));
     OnDevice on(h->device);
     if (on.e != cudaSuccess) return err(ISV_ECUDA, "isv_q8_attn: %s", cudaGetErrorString(on.e));
-    attn_kernel<<<dim3(h->d.q_heads, n_seqs), 32, 0, static_cast<cudaStream_t>(stream)>>>(p, h->d.head_dim);
-    cudaError_t e = cudaGetLastError();
+    cudaError_t e = isv::q8::launch_attn(p, h->d.head_dim, h->d.dtype == ISV_BF16, h->d.format == ISV_Q8_E4M3, h->grid,
+                                         isv::q8::attn_smem(h->d.head_dim, h->GT, n_seqs), static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? ISV_OK : err(ISV_ECUDA, "isv_q8_attn: %s", cudaGetErrorString(e));
 }
 

@@ -1,0 +1,54 @@
+// Parameter blocks and launchers of the 8-bit cache's kernels.  Plain pointers and sizes; nothing here owns memory.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/isv.h"
+
+namespace isv {
+namespace q8 {
+
+constexpr int kBT = 16;   // tokens of a page
+
+// Bytes of one (page, KV head): codes of K and V, two scales, padding to 16.
+__host__ __device__ constexpr int unit_bytes(int d) { return 2 * kBT * d + 16; }
+
+struct CacheParams {
+    uint8_t *pool;              // [n_pages][Hkv] units
+    uint8_t *tails;             // [n_seqs][K|V][Hkv][16][D] 16-bit
+    const int32_t *table;       // [n_seqs][table_stride]
+    const int32_t *lens;
+    uint32_t *status;
+    int32_t table_stride, max_blocks, n_pages, n_seqs, Hkv;
+};
+
+struct AttnParams {
+    CacheParams c;
+    const uint16_t *q;          // [n_seqs][Hq][D]
+    void *out;
+    float *out_f32;
+    float *part_o;              // partial results: [slot][heads of a visit][D], [slot][heads of a visit][2]
+    float *part_ml;
+    int32_t *tickets;           // [grid], zero between launches
+    int32_t Hq, P, GT;          // Hq = Hkv * P * GT; a visit serves GT query heads
+    float scale_log2;           // log2(e) / sqrt(D)
+};
+
+// Tokens of sequence s, clamped to what its table row and its tail slot hold.
+__device__ __forceinline__ int seq_len(const CacheParams &c, int s, bool &bad) {
+    const int n = c.lens[s], most = c.max_blocks * kBT + kBT - 1;
+    bad = n < 0 || n > most;
+    return min(max(n, 0), most);
+}
+
+// Shape of the attention kernel that serves GT query heads per visit at head_dim D.
+int attn_warps(int GT);
+int attn_head_rows(int GT);                                        // GT rounded up to whole tiles of 8
+int attn_slots(int GT, int grid);                                  // partial results of a launch
+size_t attn_smem(int D, int GT, int max_seqs);
+cudaError_t attn_configure(int D, int GT, bool bf16, bool e4m3, size_t smem);
+cudaError_t launch_attn(const AttnParams &p, int D, bool bf16, bool e4m3, int grid, size_t smem, cudaStream_t st);
+
+}  // namespace q8
+}  // namespace isv

@@ -1,0 +1,724 @@
+// Decode attention over the 8-bit cache (isv_q8_attn; layout and formats: include/isv.h).
+//
+// Per (sequence, KV head) and block of 16 tokens, with q of the GT query heads that share the KV head:
+//     S[token][head] = K q^T * (scale_K * log2(e) / sqrt(D)),  p = 2^(S - m),  l += p,  O[dim][head] += V^T (p * scale_V)
+// with a running reference m per head, everything accumulated in fp32.  Both products run on the tensor cores
+// (mma.m16n8k16, fp16 operands) with the cache as the 16-row operand and the query heads as the 8 columns: a
+// visit of one block costs D / 16 instructions for the scores and D / 8 for the output however many of the 8
+// columns are in use, half of what heads as rows would take.  8-bit codes are exact in fp16; q is brought into fp16
+// by a power of two per head (exact but for elements 2^-14 below the largest); p * scale_V goes in as an fp16 value and its
+// fp16 remainder, so its rounding (2^-22) does not show.  The codes lie in memory in the order of the operand
+// registers, so a lane's operands are 16-byte shared-memory loads without conflicts and nothing is transposed.
+//
+// What bounds it is reading the cache.  All visits of all (sequence, KV head) pairs form one list that is cut into equal ranges,
+// one per warp, whatever the lengths.  A warp streams its visits through a ring of its own (one bulk copy of
+// a unit brings K, V and both scales).  A pair that several warps share leaves partial results that are merged in fixed
+// order, first within the CTA, then, for the pairs that cross CTAs, by the CTA that arrives last.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include "isv_q8.cuh"
+
+namespace isv {
+namespace q8 {
+namespace {
+
+constexpr float kNone = -1.0e30f;            // reference of a head that has no score yet: differences stay finite
+constexpr uint32_t kSpin = 1u << 22;
+constexpr float kSlack = 8.f;                // scores may exceed the reference by this much (log2) before it moves
+constexpr int kRingBytes = 132 << 10;        // per SM
+constexpr int kMinVisits = 2;                // visits of a warp below which fewer warps of a CTA take part
+
+__device__ __forceinline__ uint32_t s32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}\n"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) {
+    if (try_wait(bar, parity)) return true;
+    for (uint32_t i = 1; i < kSpin; ++i) {
+        if (try_wait(bar, parity)) return true;
+        if (i > 256) __nanosleep(64);
+    }
+    return false;
+}
+__device__ __forceinline__ void copy_in(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+template <bool BF16>
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    if (BF16)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// 8x8 matrix of 16-bit values across the warp, transposed.
+__device__ __forceinline__ uint32_t transpose(uint32_t x) {
+    uint32_t y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
+// Four codes -> two pairs of fp16: (byte 0, byte 1) and (byte 2, byte 3).  Exact.
+template <bool E4M3>
+__device__ __forceinline__ void widen(uint32_t w, uint32_t &lo, uint32_t &hi) {
+    if (E4M3) {
+        asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %2;\ncvt.rn.f16x2.e4m3x2 %0, a;\ncvt.rn.f16x2.e4m3x2 %1, b;\n}\n" : "=r"(lo), "=r"(hi) : "r"(w));
+    } else {
+        // 0x6400 is 1024 in fp16, with a last place worth 1: 0x6400 + (code + 128) is 1152 + code
+        const uint32_t u = w ^ 0x80808080u;
+        const __half2 base = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));   // 1152
+        uint32_t a = __byte_perm(u, 0x64646464u, 0x4140), b = __byte_perm(u, 0x64646464u, 0x4342);
+        const __half2 x = __hsub2(*reinterpret_cast<__half2 *>(&a), base), y = __hsub2(*reinterpret_cast<__half2 *>(&b), base);
+        lo = *reinterpret_cast<const uint32_t *>(&x);
+        hi = *reinterpret_cast<const uint32_t *>(&y);
+    }
+}
+
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack2(float x, float y) {   // x in the low half
+    if (BF16) {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(x, y);
+        return *reinterpret_cast<const uint32_t *>(&v);
+    }
+    const __half2 v = __floats2half2_rn(x, y);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+template <bool BF16>
+__device__ __forceinline__ float2 unpack2(uint32_t w) {
+    return BF16 ? __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&w)) : __half22float2(*reinterpret_cast<const __half2 *>(&w));
+}
+// x, y and what 16 bits lose of them
+template <bool BF16>
+__device__ __forceinline__ uint32_t split2(float &x, float &y) {
+    const uint32_t w = pack2<BF16>(x, y);
+    const float2 f = unpack2<BF16>(w);
+    x -= f.x;
+    y -= f.y;
+    return w;
+}
+
+// ---- one warp's running state for the heads of a visit.  Lane 4 g + c holds, of each 16 x 8 score tile, tokens g and
+// g + 8 of heads 2 c and 2 c + 1; of the output dims g * D / 8 .. of the same heads.
+template <int D, int NT, bool BF16>
+struct State {
+    static constexpr int KS = D / 16, MT = D / 16;
+    float acc[NT][MT][4];
+    float m[NT][2], l[NT][2];
+    float vref, inv_vref;      // acc is in units of vref, a power of two near the scales of V seen last
+    uint32_t q[NT][KS][2];     // q as fp16 operand
+    float qf[NT][2];           // what its scores have to be multiplied by
+
+    // Raw q operand of k-steps 2 p, 2 p + 1 of head row `row` (16 bytes; the last 8 at head_dim 80).
+    __device__ __forceinline__ static uint4 q_words(const uint16_t *row, int p, int c, bool valid) {
+        uint4 w = make_uint4(0, 0, 0, 0);
+        if (!valid) return w;
+        if (p < D / 32) return *reinterpret_cast<const uint4 *>(row + 32 * p + 8 * c);
+        const uint2 h = *reinterpret_cast<const uint2 *>(row + 32 * p + 4 * c);
+        w.x = h.x; w.y = h.y;
+        return w;
+    }
+
+    __device__ __forceinline__ void start(const uint16_t *q0, int GT, float scale_log2, int lane) {
+        const int g = lane >> 2, c = lane & 3;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const bool valid = nt * 8 + g < GT;
+            const uint16_t *row = q0 + (size_t)(nt * 8 + g) * D;
+            uint4 w[(KS + 1) / 2];
+#pragma unroll
+            for (int p = 0; p < (KS + 1) / 2; ++p) w[p] = q_words(row, p, c, valid);
+            float f = scale_log2;
+            if (BF16) {   // by a power of two into the range of fp16
+                float top = 0.f;
+#pragma unroll
+                for (int p = 0; p < (KS + 1) / 2; ++p)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float2 v = unpack2<true>((&w[p].x)[i]);
+                        top = fmaxf(top, fmaxf(fabsf(v.x), fabsf(v.y)));
+                    }
+                top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
+                top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
+                int e = (int)(__float_as_uint(top) >> 23) - 127;
+                e = top > 0.f && e < 128 ? max(e, -126) : 0;
+                const float down = e == 127 ? 0x1p-127f : __uint_as_float((uint32_t)(127 - e) << 23);
+                f *= e == -126 ? 0x1p-126f : __uint_as_float((uint32_t)(127 + e) << 23);
+#pragma unroll
+                for (int p = 0; p < (KS + 1) / 2; ++p)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float2 v = unpack2<true>((&w[p].x)[i]);
+                        (&w[p].x)[i] = pack2<false>(v.x * down, v.y * down);
+                    }
+            }
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                q[nt][ks][0] = (&w[ks / 2].x)[2 * (ks % 2)];
+                q[nt][ks][1] = (&w[ks / 2].x)[2 * (ks % 2) + 1];
+            }
+            qf[nt][0] = __shfl_sync(~0u, f, 8 * c);        // head 2 c is row 2 c: lanes 8 c ..
+            qf[nt][1] = __shfl_sync(~0u, f, 8 * c + 4);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) { m[nt][i] = kNone; l[nt][i] = 0.f; }
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[nt][mt][i] = 0.f;
+        }
+        vref = 0.f;
+        inv_vref = 0.f;
+    }
+
+    // Brings acc into units that suit values of scale vs.
+    __device__ __forceinline__ void refer(float vs) {
+        const float r = vs * inv_vref;
+        if ((r >= 0x1p-7f && r <= 0x1p7f) || vs == 0.f) return;
+        const float now = fmaxf(__uint_as_float(__float_as_uint(vs) & 0x7f800000u), 0x1p-126f);
+        const float f = vref / now;
+        vref = now;
+        inv_vref = 1.f / now;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[nt][mt][i] *= f;
+    }
+
+    // Scores of a tile -> weights; moves the reference where a score exceeds it by more than kSlack.
+    __device__ __forceinline__ void weigh(float (&s)[NT][4]) {
+        bool over = false;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) over = over || s[nt][i] - m[nt][i & 1] > kSlack;
+        if (__any_sync(~0u, over)) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    float top = fmaxf(s[nt][i], s[nt][i + 2]);
+                    top = fmaxf(top, __shfl_xor_sync(~0u, top, 4));
+                    top = fmaxf(top, __shfl_xor_sync(~0u, top, 8));
+                    top = fmaxf(top, __shfl_xor_sync(~0u, top, 16));
+                    top = fmaxf(top, m[nt][i]);
+                    const float f = ex2(m[nt][i] - top);
+                    m[nt][i] = top;
+                    l[nt][i] *= f;
+#pragma unroll
+                    for (int mt = 0; mt < MT; ++mt) { acc[nt][mt][i] *= f; acc[nt][mt][i + 2] *= f; }
+                }
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[nt][i] = ex2(s[nt][i] - m[nt][i & 1]);
+            l[nt][0] += s[nt][0] + s[nt][2];
+            l[nt][1] += s[nt][1] + s[nt][3];
+        }
+    }
+
+    // One complete block; `unit` in shared memory.
+    template <bool E4M3>
+    __device__ __forceinline__ void visit(const uint8_t *unit, int lane) {
+        const float2 scale = *reinterpret_cast<const float2 *>(unit + 2 * kBT * D);
+        float s[NT][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[nt][i] = 0.f;
+#pragma unroll
+        for (int p = 0; p < (KS + 1) / 2; ++p) {
+            uint32_t w[4];
+            load4(unit, p, lane, w);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                if (2 * p + i >= KS) break;
+                uint32_t a0, a1, a2, a3;
+                widen<E4M3>(w[2 * i], a0, a2);
+                widen<E4M3>(w[2 * i + 1], a1, a3);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma<false>(s[nt], a0, a1, a2, a3, q[nt][2 * p + i][0], q[nt][2 * p + i][1]);
+            }
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[nt][i] *= qf[nt][i & 1] * scale.x;
+        weigh(s);
+        refer(scale.y);
+        const float vr = scale.y * inv_vref;
+        uint32_t hi[NT][2], lo[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                float x = s[nt][2 * i] * vr, y = s[nt][2 * i + 1] * vr;
+                hi[nt][i] = transpose(split2<false>(x, y));
+                lo[nt][i] = transpose(pack2<false>(x, y));
+            }
+#pragma unroll
+        for (int p = 0; p < (MT + 1) / 2; ++p) {
+            uint32_t w[4];
+            load4(unit + kBT * D, p, lane, w);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                if (2 * p + i >= MT) break;
+                uint32_t a0, a1, a2, a3;
+                widen<E4M3>(w[2 * i], a0, a2);
+                widen<E4M3>(w[2 * i + 1], a1, a3);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    mma<false>(acc[nt][2 * p + i], a0, a1, a2, a3, hi[nt][0], hi[nt][1]);
+                    mma<false>(acc[nt][2 * p + i], a0, a1, a2, a3, lo[nt][0], lo[nt][1]);
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ static void load4(const uint8_t *part, int p, int lane, uint32_t (&w)[4]) {
+        if (p < D / 32) {
+            const uint4 v = *reinterpret_cast<const uint4 *>(part + 512 * p + 16 * lane);
+            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+        } else {
+            const uint2 v = *reinterpret_cast<const uint2 *>(part + 512 * p + 8 * lane);
+            w[0] = v.x; w[1] = v.y; w[2] = w[3] = 0;
+        }
+    }
+
+    // The open block: n (1 .. 15) rows in 16 bits at k, v (global memory); later rows are not read.  Weights go in as
+    // as many 16-bit terms as fp32 has bits for.
+    __device__ __forceinline__ void open_block(const uint16_t *k, const uint16_t *v, int n, const uint16_t *q0, int GT,
+                                               float scale_log2, int lane) {
+        const int g = lane >> 2, c = lane & 3;
+        float s[NT][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[nt][i] = 0.f;
+#pragma unroll
+        for (int p = 0; p < (KS + 1) / 2; ++p) {
+            const uint4 a = q_words(k + (size_t)g * D, p, c, g < n), b = q_words(k + (size_t)(g + 8) * D, p, c, g + 8 < n);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const uint4 w = q_words(q0 + (size_t)(nt * 8 + g) * D, p, c, nt * 8 + g < GT);
+                mma<BF16>(s[nt], a.x, b.x, a.y, b.y, w.x, w.y);
+                if (2 * p + 1 < KS) mma<BF16>(s[nt], a.z, b.z, a.w, b.w, w.z, w.w);
+            }
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[nt][i] = g + 8 * (i >> 1) < n ? s[nt][i] * scale_log2 : -INFINITY;   // weight 0
+        weigh(s);
+        refer(1.f);
+        constexpr int TERMS = BF16 ? 3 : 2;
+        uint32_t t[TERMS][NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                float x = s[nt][2 * i] * inv_vref, y = s[nt][2 * i + 1] * inv_vref;
+#pragma unroll
+                for (int j = 0; j < TERMS; ++j) t[j][nt][i] = transpose(split2<BF16>(x, y));
+            }
+        uint32_t w[4][MT];     // dims g * D / 8 + 2 mt, + 1 of tokens 2 c, 2 c + 1, 2 c + 8, 2 c + 9
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int tok = 2 * c + (j & 1) + 8 * (j >> 1);
+            const uint32_t *row = reinterpret_cast<const uint32_t *>(v + (size_t)tok * D + g * (D / 8));
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) w[j][mt] = tok < n ? row[mt] : 0u;
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            const uint32_t a0 = __byte_perm(w[0][mt], w[1][mt], 0x5410), a1 = __byte_perm(w[0][mt], w[1][mt], 0x7632);
+            const uint32_t a2 = __byte_perm(w[2][mt], w[3][mt], 0x5410), a3 = __byte_perm(w[2][mt], w[3][mt], 0x7632);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < TERMS; ++j) mma<BF16>(acc[nt][mt], a0, a1, a2, a3, t[j][nt][0], t[j][nt][1]);
+        }
+    }
+
+    // Sums over the lanes that share a head.
+    __device__ __forceinline__ void finish() {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                l[nt][i] += __shfl_xor_sync(~0u, l[nt][i], 4);
+                l[nt][i] += __shfl_xor_sync(~0u, l[nt][i], 8);
+                l[nt][i] += __shfl_xor_sync(~0u, l[nt][i], 16);
+            }
+        if (vref == 0.f) vref = 1.f;
+    }
+};
+
+// Two neighbouring output values of one head.
+template <bool BF16>
+__device__ __forceinline__ void store2(const AttnParams &p, size_t at, float x, float y) {
+    if (p.out_f32) *reinterpret_cast<float2 *>(p.out_f32 + at) = make_float2(x, y);
+    if (p.out) *reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(p.out) + at) = pack2<BF16>(x, y);
+}
+
+// A visit as the producing lane writes it down for the whole warp.
+struct Visit {
+    int32_t seq, group;        // sequence, head group
+    int32_t flags;             // below; the tail's row count in the upper bits
+    int32_t pad;
+};
+enum { COPY = 1, OPEN = 2, FIRST = 4, LAST = 8, HEAD = 16, END = 32 };   // FIRST/LAST of the warp's part of an item; HEAD/END of the item itself
+
+template <int D, int NT>
+struct Shape {
+    static constexpr int NW = NT == 1 ? 16 : 8;
+    static constexpr int UNIT = unit_bytes(D);
+    static constexpr int ST = kRingBytes / (NW * UNIT);
+    static constexpr int HT = 8 * NT;
+    static_assert(ST >= 2 && ST <= 8, "ring depth");
+};
+
+template <int D, int NT, bool BF16, bool E4M3>
+__global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __grid_constant__ AttnParams p) {
+    using SH = Shape<D, NT>;
+    constexpr int NW = SH::NW, UNIT = SH::UNIT, ST = SH::ST, HT = SH::HT, THREADS = NW * 32;
+    extern __shared__ __align__(128) uint8_t smem[];
+    uint8_t *ring = smem;                                                       // [NW][ST] units
+    Visit *visits = reinterpret_cast<Visit *>(ring + (size_t)NW * ST * UNIT);   // [NW][ST]
+    uint64_t *bars = reinterpret_cast<uint64_t *>(visits + NW * ST);            // [NW][ST]
+    int *prefix = reinterpret_cast<int *>(bars + NW * ST);                      // [n_seqs + 1] blocks before a sequence
+    __shared__ int scan[NW];
+    __shared__ int rec_item[NW][2];            // items of which the warps left a partial result (flat: sequence, group)
+    __shared__ int run_item[NW + 1], run_first[NW + 2], n_runs;
+    __shared__ int list[2 * NW];               // slots of the records, in order
+    __shared__ int arrived;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int G = p.c.Hkv * p.P;               // head groups of a sequence
+
+    // ---- blocks before each sequence; sequences without any get their zeros
+    uint32_t bad = 0;
+    int carry = 0;
+    for (int s0 = 0; s0 < p.c.n_seqs; s0 += THREADS) {
+        const int s = s0 + tid;
+        int nb = 0;
+        if (s < p.c.n_seqs) {
+            bool b;
+            nb = (seq_len(p.c, s, b) + kBT - 1) / kBT;
+            if (b) bad |= ISV_STATUS_BAD_LENGTH;
+        }
+        int x = nb;
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const int y = __shfl_up_sync(~0u, x, o);
+            if (lane >= o) x += y;
+        }
+        if (lane == 31) scan[warp] = x;
+        __syncthreads();
+        int before = carry;
+        for (int w = 0; w < NW; ++w) {
+            if (w < warp) before += scan[w];
+            carry += scan[w];
+        }
+        if (s < p.c.n_seqs) prefix[s] = before + x - nb;
+        __syncthreads();
+    }
+    if (tid == 0) prefix[p.c.n_seqs] = carry;
+    if (lane < 2) rec_item[warp][lane] = -1;
+    if (lane < ST) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(s32(&bars[warp * ST + lane])) : "memory");
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncthreads();
+    for (int s = blockIdx.x; s < p.c.n_seqs; s += gridDim.x)
+        if (prefix[s] == prefix[s + 1])
+            for (int x = 2 * tid; x < p.Hq * D; x += 2 * THREADS) store2<BF16>(p, (size_t)s * p.Hq * D + x, 0.f, 0.f);
+
+    const long long total = (long long)carry * G;
+    const int ctas = (int)min((long long)gridDim.x, total);
+    if ((int)blockIdx.x >= ctas) {
+        if (bad && blockIdx.x == 0) atomicOr(p.c.status, bad);
+        return;
+    }
+    const int warps = (int)min((long long)NW, max(1ll, total / ((long long)ctas * kMinVisits)));
+    const long long shares = (long long)ctas * warps, me = (long long)blockIdx.x * warps + warp;
+    const int beg = warp < warps ? (int)(total * me / shares) : 0;
+    const int end = warp < warps ? (int)(total * (me + 1) / shares) : 0;
+
+    // ---- producer: 32 visits at a time are looked up, one per lane
+    uint64_t my_src = 0;
+    Visit my_visit{};
+    auto look_up = [&](int v) {
+        my_src = 0;
+        if (v >= end) return;
+        int lo = 0, hi = p.c.n_seqs;           // the last sequence whose visits begin at or before v
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if ((long long)prefix[mid] * G <= v) lo = mid; else hi = mid;
+        }
+        const int nb = prefix[lo + 1] - prefix[lo];
+        const int r = v - prefix[lo] * G, group = r / nb, blk = r - group * nb;
+        bool b;
+        const int len = seq_len(p.c, lo, b), full = len / kBT;
+        int flags = (v == beg || blk == 0 ? FIRST : 0) | (v == end - 1 || blk == nb - 1 ? LAST : 0) | (blk == 0 ? HEAD : 0) |
+                    (blk == nb - 1 ? END : 0);
+        if (blk < full) {
+            const int page = __ldg(p.c.table + (size_t)lo * p.c.table_stride + blk);
+            if (page >= 0 && page < p.c.n_pages) {
+                my_src = reinterpret_cast<uint64_t>(p.c.pool) + ((uint64_t)page * p.c.Hkv + group / p.P) * UNIT;
+                flags |= COPY;
+            } else if (page != ISV_BLOCK_NONE) {
+                bad |= ISV_STATUS_BAD_BLOCK_ID;
+            }
+        } else {
+            flags |= OPEN | (len % kBT) << 8;
+        }
+        my_visit = Visit{lo, group, flags, 0};
+    };
+    int next = beg;
+    auto produce = [&](int slot) {             // the next visit into this slot of the ring
+        if (next >= end) return;
+        const int i = (next - beg) & 31;
+        if (i == 0) look_up(next + lane);
+        const uint64_t src = __shfl_sync(~0u, my_src, i);
+        if (lane == i) visits[warp * ST + slot] = my_visit;
+        if (lane == 0 && src)
+            copy_in(s32(ring + (size_t)(warp * ST + slot) * UNIT), reinterpret_cast<const void *>(src), UNIT, s32(&bars[warp * ST + slot]));
+        ++next;
+    };
+    for (int i = 0; i < ST; ++i) produce(i);
+    __syncwarp();
+
+    // ---- consumer
+    State<D, NT, BF16> st;
+    const uint16_t *q0 = p.q;
+    uint32_t phases = 0;
+    bool lost = false;
+    int slot = 0;
+    bool whole = false;
+    for (int v = beg; v < end && !lost; ++v) {
+        const Visit t = visits[warp * ST + slot];
+        if (t.flags & FIRST) {
+            q0 = p.q + ((size_t)t.seq * p.Hq + (size_t)t.group * p.GT) * D;
+            st.start(q0, p.GT, p.scale_log2, lane);
+            whole = t.flags & HEAD;
+        }
+        if (t.flags & COPY) {
+            if (!wait(s32(&bars[warp * ST + slot]), (phases >> slot) & 1u)) lost = true;
+            else {
+                phases ^= 1u << slot;
+                st.template visit<E4M3>(ring + (size_t)(warp * ST + slot) * UNIT, lane);
+            }
+        } else if (t.flags & OPEN) {
+            const uint16_t *k = reinterpret_cast<const uint16_t *>(p.c.tails) + ((size_t)t.seq * 2 * p.c.Hkv + t.group / p.P) * kBT * D;
+            st.open_block(k, k + (size_t)p.c.Hkv * kBT * D, t.flags >> 8, q0, p.GT, p.scale_log2, lane);
+        }
+        __syncwarp();
+        if (!lost) produce(slot);
+        if (t.flags & LAST) {
+            st.finish();
+            const int g = lane >> 2, c = lane & 3;
+            if (whole && (t.flags & END)) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int h = nt * 8 + 2 * c + i;
+                        const float f = st.l[nt][i] == 0.f ? 0.f : st.vref / st.l[nt][i];
+                        if (h < p.GT) {
+                            const size_t at = ((size_t)t.seq * p.Hq + (size_t)t.group * p.GT + h) * D + g * (D / 8);
+#pragma unroll
+                            for (int mt = 0; mt < D / 16; ++mt) store2<BF16>(p, at + 2 * mt, st.acc[nt][mt][i] * f, st.acc[nt][mt][i + 2] * f);
+                        }
+                    }
+            } else {
+                // an item that begins before this warp's range leaves record 0, any other record 1
+                const int which = whole ? 1 : 0;
+                const size_t at = ((size_t)blockIdx.x * NW + warp) * 2 + which;
+                if (lane == 0) rec_item[warp][which] = t.seq * G + t.group;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int h = nt * 8 + 2 * c + i;
+                        if (h < p.GT) {
+                            float *o = p.part_o + (at * HT + h) * D + g * (D / 8);
+#pragma unroll
+                            for (int mt = 0; mt < D / 16; ++mt)
+                                *reinterpret_cast<float2 *>(o + 2 * mt) = make_float2(st.acc[nt][mt][i] * st.vref, st.acc[nt][mt][i + 2] * st.vref);
+                            if (g == 0) *reinterpret_cast<float2 *>(p.part_ml + (at * HT + h) * 2) = make_float2(st.m[nt][i], st.l[nt][i]);
+                        }
+                    }
+            }
+        }
+        slot = slot + 1 == ST ? 0 : slot + 1;
+        __syncwarp();
+    }
+    if (lost) {   // a copy did not arrive in time: give the others one more bounded chance and report
+        bad |= ISV_STATUS_WAIT_EXPIRED;
+        for (int i = 0; i < ST; ++i)
+            if (visits[warp * ST + i].flags & COPY) wait(s32(&bars[warp * ST + i]), (phases >> i) & 1u);
+    }
+    if (bad) atomicOr(p.c.status, bad);
+    __syncthreads();
+
+    // ---- partial results of this CTA: consecutive records of one item form a run
+    if (tid == 0) {
+        int n = 0, runs = 0, before = -1;
+        for (int w = 0; w < warps; ++w)
+            for (int i = 0; i < 2; ++i) {
+                const int item = rec_item[w][i];
+                if (item < 0) continue;
+                if (item != before) { run_item[runs] = item; run_first[runs++] = n; }
+                list[n++] = (blockIdx.x * NW + w) * 2 + i;
+                before = item;
+            }
+        run_first[runs] = n;
+        n_runs = runs;
+    }
+    __syncthreads();
+    const int cta_beg = (int)(total * blockIdx.x / ctas), cta_end = (int)(total * (blockIdx.x + 1) / ctas);
+    const int units = p.GT * (D / 4);
+    auto item_span = [&](int item, int &b, int &e) {
+        const int s = item / G, nb = prefix[s + 1] - prefix[s];
+        b = prefix[s] * G + (item - s * G) * nb;
+        e = b + nb;
+    };
+    // weighted sum of records [0, n) of one head, four dims
+    auto merge = [&](int n, auto slot_of, int h, int x, float &m, float &l) {
+        m = kNone;
+        for (int i = 0; i < n; ++i) m = fmaxf(m, __ldcg(p.part_ml + ((size_t)slot_of(i) * HT + h) * 2));
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        l = 0.f;
+#pragma unroll 4
+        for (int i = 0; i < n; ++i) {
+            const size_t at = (size_t)slot_of(i) * HT + h;
+            const float2 ml = __ldcg(reinterpret_cast<const float2 *>(p.part_ml + at * 2));
+            const float4 v = __ldcg(reinterpret_cast<const float4 *>(p.part_o + at * D + x));
+            const float w = ex2(ml.x - m);
+            l += w * ml.y;
+            o.x += w * v.x; o.y += w * v.y; o.z += w * v.z; o.w += w * v.w;
+        }
+        return o;
+    };
+    auto put = [&](int item, int h, int x, const float4 &o, float l) {
+        const float f = l == 0.f ? 0.f : 1.f / l;
+        const size_t at = ((size_t)item * p.GT + h) * D + x;      // item * GT is the flat query head
+        store2<BF16>(p, at, o.x * f, o.y * f);
+        store2<BF16>(p, at + 2, o.z * f, o.w * f);
+    };
+    const size_t cta_slots = (size_t)gridDim.x * NW * 2;
+    for (int u = tid; u < n_runs * units; u += THREADS) {
+        const int run = u / units, h = (u - run * units) / (D / 4), x = (u - run * units) % (D / 4) * 4;
+        const int r0 = run_first[run], item = run_item[run];
+        float m, l;
+        const float4 o = merge(run_first[run + 1] - r0, [&](int i) { return list[r0 + i]; }, h, x, m, l);
+        int b, e;
+        item_span(item, b, e);
+        if (b >= cta_beg && e <= cta_end) put(item, h, x, o, l);
+        else {
+            const size_t at = (cta_slots + blockIdx.x * 2 + (b > cta_beg ? 1 : 0)) * HT + h;
+            *reinterpret_cast<float4 *>(p.part_o + at * D + x) = o;
+            if (x == 0) *reinterpret_cast<float2 *>(p.part_ml + at * 2) = make_float2(m, l);
+        }
+    }
+    // ---- items that cross CTAs: the last CTA to arrive merges.  The ticket of an item is that of its first CTA, in
+    // which no other item continues into the next.
+    for (int k = 0; k < 2; ++k) {
+        if (k == 1 && n_runs < 2) break;
+        if (n_runs == 0) break;
+        const int item = run_item[k == 0 ? 0 : n_runs - 1];
+        int b, e;
+        item_span(item, b, e);
+        if (b >= cta_beg && e <= cta_end) continue;
+        auto owner = [&](int v) { return (int)((((long long)v + 1) * ctas - 1) / total); };   // CTA whose range holds visit v
+        const int c0 = owner(b), n = owner(e - 1) - c0 + 1;
+        __threadfence();
+        __syncthreads();
+        if (tid == 0) {
+            arrived = atomicAdd(p.tickets + c0, 1);
+            if (arrived == n - 1) p.tickets[c0] = 0;
+            __threadfence();
+        }
+        __syncthreads();
+        if (arrived != n - 1) continue;
+        const int first_slot = b == (int)(total * c0 / ctas) ? 0 : 1;
+        for (int u = tid; u < units; u += THREADS) {
+            const int h = u / (D / 4), x = u % (D / 4) * 4;
+            float m, l;
+            const float4 o = merge(n, [&](int i) { return (int)cta_slots + (c0 + i) * 2 + (i == 0 ? first_slot : 0); }, h, x, m, l);
+            put(item, h, x, o, l);
+        }
+    }
+}
+
+template <int D, int NT, bool BF16, bool E4M3>
+cudaError_t configure(size_t smem) {
+    return cudaFuncSetAttribute(attn_kernel<D, NT, BF16, E4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+}
+template <int D, int NT, bool BF16, bool E4M3>
+cudaError_t launch(const AttnParams &p, int grid, size_t smem, cudaStream_t st) {
+    attn_kernel<D, NT, BF16, E4M3><<<grid, Shape<D, NT>::NW * 32, smem, st>>>(p);
+    return cudaGetLastError();
+}
+
+// Calls f with the template arguments of a case.
+template <int D, int NT, typename F>
+cudaError_t pick_types(bool bf16, bool e4m3, F f) {
+    if (bf16) return e4m3 ? f.template operator()<D, NT, true, true>() : f.template operator()<D, NT, true, false>();
+    return e4m3 ? f.template operator()<D, NT, false, true>() : f.template operator()<D, NT, false, false>();
+}
+template <typename F>
+cudaError_t pick(int D, int GT, bool bf16, bool e4m3, F f) {
+    if (GT <= 8) {
+        if (D == 64) return pick_types<64, 1>(bf16, e4m3, f);
+        if (D == 80) return pick_types<80, 1>(bf16, e4m3, f);
+        return pick_types<128, 1>(bf16, e4m3, f);
+    }
+    if (D == 64) return pick_types<64, 2>(bf16, e4m3, f);
+    if (D == 80) return pick_types<80, 2>(bf16, e4m3, f);
+    return pick_types<128, 2>(bf16, e4m3, f);
+}
+struct Configure {
+    size_t smem;
+    template <int D, int NT, bool BF16, bool E4M3>
+    cudaError_t operator()() const { return configure<D, NT, BF16, E4M3>(smem); }
+};
+struct Launch {
+    const AttnParams &p;
+    int grid;
+    size_t smem;
+    cudaStream_t st;
+    template <int D, int NT, bool BF16, bool E4M3>
+    cudaError_t operator()() const { return launch<D, NT, BF16, E4M3>(p, grid, smem, st); }
+};
+
+}  // namespace
+
+int attn_warps(int GT) { return GT <= 8 ? Shape<128, 1>::NW : Shape<128, 2>::NW; }
+int attn_head_rows(int GT) { return GT <= 8 ? 8 : 16; }
+int attn_slots(int GT, int grid) { return grid * attn_warps(GT) * 2 + grid * 2; }
+
+size_t attn_smem(int D, int GT, int max_seqs) {
+    const size_t unit = unit_bytes(D), nw = attn_warps(GT), st = kRingBytes / (nw * unit);
+    return nw * st * (unit + sizeof(Visit) + 8) + 4 * ((size_t)max_seqs + 1);
+}
+cudaError_t attn_configure(int D, int GT, bool bf16, bool e4m3, size_t smem) { return pick(D, GT, bf16, e4m3, Configure{smem}); }
+cudaError_t launch_attn(const AttnParams &p, int D, bool bf16, bool e4m3, int grid, size_t smem, cudaStream_t st) {
+    return pick(D, p.GT, bf16, e4m3, Launch{p, grid, smem, st});
+}
+
+}  // namespace q8
+}  // namespace isv
