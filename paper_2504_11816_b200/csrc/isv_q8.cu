@@ -2,7 +2,6 @@
 // the treatment of open blocks are described in include/isv.h; the attention kernel is in isv_q8_attn.cu.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
-#include <cuda_fp8.h>
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -50,111 +49,217 @@ struct OnDevice {
     }
 };
 
+constexpr int kWriteThreads = 128;
+
 struct WriteParams {
     CacheParams c;
     const int32_t *new_lens;    // NULL = T
     const uint16_t *k, *v;
     int64_t seq_stride, token_stride;
     int32_t T, blocks;          // blocks: how many blocks T tokens can touch
-    int32_t bf16, e4m3;
 };
 
-__device__ __forceinline__ float to_f32(uint16_t b, int bf16) {
-    return bf16 ? __bfloat162float(__ushort_as_bfloat16(b)) : __half2float(__ushort_as_half(b));
-}
-
-// Byte of (token, dim) inside a unit's K part and inside its V part.
-__device__ __forceinline__ int k_byte(int t, int x, int d) {
-    const int whole = d / 32;
-    const int p = x / 32, h = t / 8, g = t % 8;
-    if (p < whole) {
-        const int c = (x % 32) / 8, i = (x % 8) / 4, j = x % 4;
-        return 512 * p + 16 * (4 * g + c) + 8 * i + 4 * h + j;
-    }
-    const int r = x - 32 * whole;
-    return 512 * whole + 8 * (4 * g + r / 4) + 4 * h + r % 4;
-}
-__device__ __forceinline__ int v_byte(int t, int x, int d) {
-    const int whole = d / 32;
-    const int g = x / (d / 8), r = x % (d / 8), tile = r / 2, h = r % 2;
-    const int c = (t % 8) / 2, j = t % 2 + 2 * (t / 8), lane = 4 * g + c;
-    if (tile < 2 * whole) return 512 * (tile / 2) + 16 * lane + 8 * (tile % 2) + 4 * h + j;
-    return 512 * whole + 8 * lane + 4 * h + j;
-}
+// ---- quantisation
+//
+// A code is the rounding of the exact quotient x / s.  The kernel multiplies by 1 / s: that product is off by at most
+// 2^-23 of its value, so its rounding is the right one unless it lies that close to a border between two codes.  Those
+// few elements are divided properly.
 
 // x / s rounded so that a later rounding to fewer bits gives what it gives for the exact quotient: the fp32
 // quotient, and where that is inexact and its last bit is 0 the neighbour on the side of the exact value ("round
 // to odd").  The residual is exact: x has at most 11 significant bits and the caller keeps s and x in the normal range.
 // Quotients below 2^-20 become the code 0 whatever their last bits.
-__device__ __forceinline__ float quotient_to_odd(float x, float s) {
+__device__ __noinline__ float quotient_to_odd(float x, float s) {
     const float q = __fdiv_rn(x, s);
     const float r = __fmaf_rn(-q, s, x);
     uint32_t b = __float_as_uint(q);
     if (fabsf(q) > 0x1p-20f && r != 0.f && !(b & 1u)) b += ((r > 0.f) == (q > 0.f)) ? 1u : ~0u;   // away from zero, or toward it
     return __uint_as_float(b);
 }
-__device__ __forceinline__ uint8_t encode(float q, int e4m3) {
-    if (e4m3) return (uint8_t)__nv_cvt_float_to_fp8(q, __NV_SATFINITE, __NV_E4M3);
-    return (uint8_t)(int8_t)max(-127, min(127, __float2int_rn(q)));
-}
 
-// One thread per (sequence, head) walks the blocks that the new tokens touch.
-__global__ void write_kernel(WriteParams p, int D) {
-    const int id = blockIdx.x * blockDim.x + threadIdx.x;
-    if (id >= p.c.n_seqs * p.c.Hkv) return;
-    const int s = id / p.c.Hkv, h = id % p.c.Hkv;
-    bool bad;
-    const int len = seq_len(p.c, s, bad);
-    const int asked = p.new_lens ? p.new_lens[s] : p.T;
-    const int n_new = min(max(asked, 0), min(p.T, len));
-    if (bad || n_new != asked) atomicOr(p.c.status, ISV_STATUS_BAD_LENGTH);
-    if (n_new == 0) return;
-    const int start = len - n_new;
-    for (int b = start / kBT; b <= (len - 1) / kBT; ++b) {
-        const bool complete = (b + 1) * kBT <= len;
-        uint8_t *unit = nullptr;
-        if (complete) {
-            const int page = p.c.table[(size_t)s * p.c.table_stride + b];
-            if (page < 0 || page >= p.c.n_pages) {
-                atomicOr(p.c.status, ISV_STATUS_BAD_BLOCK_ID);
-                continue;
-            }
-            unit = p.c.pool + ((size_t)page * p.c.Hkv + h) * unit_bytes(D);
-        }
-        for (int kv = 0; kv < 2; ++kv) {
-            uint16_t *tail = reinterpret_cast<uint16_t *>(p.c.tails) + (((size_t)s * 2 + kv) * p.c.Hkv + h) * kBT * D;
-            const uint16_t *src = (kv ? p.v : p.k) + s * p.seq_stride + (size_t)h * D;
-            auto row = [&](int t) {
-                const int pos = b * kBT + t;
-                return pos < start ? tail + t * D : src + (pos - start) * p.token_stride;
-            };
-            if (!complete) {
-                for (int t = 0; b * kBT + t < len; ++t)
-                    if (b * kBT + t >= start)
-                        for (int x = 0; x < D; ++x) tail[t * D + x] = row(t)[x];
-                continue;
-            }
-            float top = 0.f;
-            bool odd = false;
-            for (int t = 0; t < kBT; ++t)
-                for (int x = 0; x < D; ++x) {
-                    const float a = fabsf(to_f32(row(t)[x], p.bf16));
-                    odd = odd || !(a <= 3.4e38f);
-                    top = fmaxf(top, a);
-                }
-            // tiny blocks are scaled by a power of two so that the quotients' steps stay in the normal range
-            const float scale = odd ? __int_as_float(0x7fffffff) : __fdiv_rn(top, p.e4m3 ? 448.f : 127.f);
-            const float up = top < 0x1p-60f ? 0x1p64f : 1.f;
-            for (int t = 0; t < kBT; ++t)
-                for (int x = 0; x < D; ++x) {
-                    const float q = odd || top == 0.f ? 0.f : quotient_to_odd(to_f32(row(t)[x], p.bf16) * up, scale * up);
-                    unit[kv * kBT * D + (kv ? v_byte(t, x, D) : k_byte(t, x, D))] = encode(q, p.e4m3);
-                }
-            float *tags = reinterpret_cast<float *>(unit + 2 * kBT * D);
-            tags[kv] = scale;
-            tags[2 + kv] = 0.f;
+constexpr float kMagic = 12582912.f;   // 1.5 * 2^23: adding it rounds to an integer, which is then in the low bits
+
+// Four numbers -> four codes, in the bytes of a word.
+template <bool E4M3>
+__device__ __forceinline__ uint32_t encode_raw(const float (&q)[4]) {
+    uint32_t w;
+    if (E4M3) {
+        asm("{\n.reg .b16 a, b;\ncvt.rn.satfinite.e4m3x2.f32 a, %2, %1;\ncvt.rn.satfinite.e4m3x2.f32 b, %4, %3;\nmov.b32 %0, {a, b};\n}\n"
+            : "=r"(w) : "f"(q[0]), "f"(q[1]), "f"(q[2]), "f"(q[3]));
+    } else {
+        uint32_t r[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = __float_as_uint(q[i] + kMagic);
+        w = __byte_perm(__byte_perm(r[0], r[1], 0x0040), __byte_perm(r[2], r[3], 0x0040), 0x5410);
+    }
+    return w;
+}
+template <bool E4M3>
+__device__ __forceinline__ uint32_t encode(const float (&x)[4], float s, float inv) {
+    float q[4];
+    bool close = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        q[i] = x[i] * inv;
+        if (E4M3) {
+            // three bits behind the leading one are kept; below 2^-6 the steps stay as they are at 2^-6
+            const float a = fabsf(q[i]), n = a < 0x1p-6f ? a + 0x1p-6f : a;
+            close = close || ((__float_as_uint(n) - 0x7fffcu) & 0xfffffu) <= 8u;
+        } else {
+            close = close || fabsf(q[i] - ((q[i] + kMagic) - kMagic)) > 0.49998f;   // |q| <= 127: off by at most 1.6e-5
         }
     }
+    if (close)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = quotient_to_odd(x[i], s);
+    return encode_raw<E4M3>(q);
+}
+
+template <bool BF16>
+__device__ __forceinline__ float half_of(uint32_t w, int i) {   // the low (0) or high (1) 16-bit number of a word
+    if (BF16) return __uint_as_float(i ? w & 0xffff0000u : w << 16);
+    return __half2float(__ushort_as_half((unsigned short)(i ? w >> 16 : w & 0xffffu)));
+}
+
+// Scale of a part from the largest magnitude (as bits) that each lane has seen; `up` is the power of two by which numbers and
+// scale of a tiny block are multiplied so that the quotients' arithmetic stays in the normal range.
+template <bool BF16, bool E4M3>
+__device__ __forceinline__ float scale_of(uint32_t top2, float &up, float &inv) {
+#pragma unroll
+    for (int o = 16; o; o /= 2) top2 = __vmaxu2(top2, __shfl_xor_sync(~0u, top2, o));
+    const uint32_t bits = max(top2 & 0xffffu, top2 >> 16);       // magnitudes of 16-bit floats order like their bits
+    const float top = half_of<BF16>(bits, 0);
+    const bool odd = bits >= (BF16 ? 0x7f80u : 0x7c00u);
+    const float scale = odd ? __int_as_float(0x7fffffff) : __fdiv_rn(top, E4M3 ? 448.f : 127.f);
+    up = top < 0x1p-60f ? 0x1p64f : 1.f;
+    inv = odd || top == 0.f ? 0.f : __fdiv_rn(1.f, scale * up);
+    return scale;
+}
+
+// A warp per (sequence, block that its new tokens touch, KV head).  A lane's loads are the 16-bit rows in the order in which
+// the page wants its codes: lane 4 g + c takes tokens g, g + 8 of K, 8 dims at a time, and dims g * D / 8 .. of tokens
+// 2 c, 2 c + 1, 2 c + 8, 2 c + 9 of V; what it writes are 16-byte pieces, 512 contiguous bytes of the warp.
+template <int D, bool BF16, bool E4M3>
+__global__ void __launch_bounds__(kWriteThreads) write_kernel(const __grid_constant__ WriteParams p) {
+    constexpr int MT = D / 16, P = D / 32, REST = D % 32 ? 1 : 0;
+    const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+    const long long warps = (long long)gridDim.x * (kWriteThreads / 32), tasks = (long long)p.c.n_seqs * p.blocks * p.c.Hkv;
+    for (long long id = (long long)blockIdx.x * (kWriteThreads / 32) + threadIdx.x / 32; id < tasks; id += warps) {
+        const int h = (int)(id % p.c.Hkv), bi = (int)(id / p.c.Hkv % p.blocks), s = (int)(id / p.c.Hkv / p.blocks);
+        bool bad;
+        const int len = seq_len(p.c, s, bad);
+        const int asked = p.new_lens ? p.new_lens[s] : p.T;
+        const int n_new = min(max(asked, 0), min(p.T, len));
+        if ((bad || n_new != asked) && bi == 0 && h == 0 && lane == 0) atomicOr(p.c.status, ISV_STATUS_BAD_LENGTH);
+        const int start = len - n_new, b = start / kBT + bi, last = (len - 1) / kBT;
+        if (n_new == 0 || b > last) continue;
+        uint16_t *tail = reinterpret_cast<uint16_t *>(p.c.tails) + ((size_t)s * 2 * p.c.Hkv + h) * kBT * D;
+        const size_t tail_v = (size_t)p.c.Hkv * kBT * D;                     // from the K rows of a tail slot to its V rows
+        const uint16_t *k0 = p.k + s * p.seq_stride + (size_t)h * D, *v0 = p.v + s * p.seq_stride + (size_t)h * D;
+        if ((b + 1) * kBT <= len) {
+            const int page = p.c.table[(size_t)s * p.c.table_stride + b];
+            if (page < 0 || page >= p.c.n_pages) {
+                if (lane == 0) atomicOr(p.c.status, ISV_STATUS_BAD_BLOCK_ID);
+            } else {
+                auto row = [&](int kv, int t) {                              // rows before `start` wait in the tail slot
+                    const int pos = b * kBT + t;
+                    return pos < start ? tail + kv * tail_v + t * D : (kv ? v0 : k0) + (pos - start) * p.token_stride;
+                };
+                uint32_t k[2][2 * MT], v[4][MT];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint16_t *r = row(0, g + 8 * i);
+#pragma unroll
+                    for (int x = 0; x < P; ++x) {
+                        const uint4 w = *reinterpret_cast<const uint4 *>(r + 32 * x + 8 * c);
+                        k[i][4 * x] = w.x; k[i][4 * x + 1] = w.y; k[i][4 * x + 2] = w.z; k[i][4 * x + 3] = w.w;
+                    }
+                    if (REST) {
+                        const uint2 w = *reinterpret_cast<const uint2 *>(r + 32 * P + 4 * c);
+                        k[i][4 * P] = w.x; k[i][4 * P + 1] = w.y;
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint16_t *r = row(1, 2 * c + (j & 1) + 8 * (j >> 1)) + g * (D / 8);
+                    if (D % 64 == 0) {
+#pragma unroll
+                        for (int x = 0; x < MT / 4; ++x) {
+                            const uint4 w = *reinterpret_cast<const uint4 *>(r + 8 * x);
+                            v[j][4 * x] = w.x; v[j][4 * x + 1] = w.y; v[j][4 * x + 2] = w.z; v[j][4 * x + 3] = w.w;
+                        }
+                    } else {
+#pragma unroll
+                        for (int x = 0; x < MT; ++x) v[j][x] = *reinterpret_cast<const uint32_t *>(r + 2 * x);
+                    }
+                }
+                uint32_t tk = 0, tv = 0;
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int x = 0; x < 2 * MT; ++x) tk = __vmaxu2(tk, k[i][x] & 0x7fff7fffu);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int x = 0; x < MT; ++x) tv = __vmaxu2(tv, v[j][x] & 0x7fff7fffu);
+                uint8_t *unit = p.c.pool + ((size_t)page * p.c.Hkv + h) * unit_bytes(D);
+                float up, inv;
+                const float ks = scale_of<BF16, E4M3>(tk, up, inv);
+                // a block with an infinity or a NaN (inv = 0) gets codes of 0 and the scale NaN
+                auto code = [&](float a, float b2, float c2, float d2, float s_up) {
+                    const float x[4] = {a * up, b2 * up, c2 * up, d2 * up};
+                    return inv == 0.f ? 0u : encode<E4M3>(x, s_up, inv);
+                };
+#pragma unroll
+                for (int x = 0; x < P + REST; ++x) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {                            // k-steps 2 x, 2 x + 1; tokens g, g + 8
+                        const int ks2 = 2 * x + y / 2, i = y & 1;
+                        w[y] = ks2 < MT ? code(half_of<BF16>(k[i][2 * ks2], 0), half_of<BF16>(k[i][2 * ks2], 1),
+                                               half_of<BF16>(k[i][2 * ks2 + 1], 0), half_of<BF16>(k[i][2 * ks2 + 1], 1), ks * up) : 0u;
+                    }
+                    if (x < P) *reinterpret_cast<uint4 *>(unit + 512 * x + 16 * lane) = make_uint4(w[0], w[1], w[2], w[3]);
+                    else *reinterpret_cast<uint2 *>(unit + 512 * x + 8 * lane) = make_uint2(w[0], w[1]);
+                }
+                const float vs = scale_of<BF16, E4M3>(tv, up, inv);
+#pragma unroll
+                for (int x = 0; x < P + REST; ++x) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {                            // tiles 2 x, 2 x + 1; dims 2 tile, 2 tile + 1 of the lane's
+                        const int mt = 2 * x + y / 2, i = y & 1;
+                        w[y] = mt < MT ? code(half_of<BF16>(v[0][mt], i), half_of<BF16>(v[1][mt], i), half_of<BF16>(v[2][mt], i),
+                                              half_of<BF16>(v[3][mt], i), vs * up) : 0u;
+                    }
+                    if (x < P) *reinterpret_cast<uint4 *>(unit + kBT * D + 512 * x + 16 * lane) = make_uint4(w[0], w[1], w[2], w[3]);
+                    else *reinterpret_cast<uint2 *>(unit + kBT * D + 512 * x + 8 * lane) = make_uint2(w[0], w[1]);
+                }
+                if (lane == 0) *reinterpret_cast<float4 *>(unit + 2 * kBT * D) = make_float4(ks, vs, 0.f, 0.f);
+            }
+        }
+        // ---- the open block's new rows into the tail slot.  Where the first block completes with rows from the tail slot, its warp
+        // stores them, after it has read those.
+        if (len % kBT == 0) continue;
+        const bool mine = start % kBT == 0 ? b == last : bi == 0;
+        if (!mine) continue;
+        __syncwarp();
+        const int from = max(start, last * kBT);
+        for (int i = lane; i < (len - from) * (D / 8) * 2; i += 32) {
+            const int kv = i & 1, x = (i >> 1) % (D / 8), t = (i >> 1) / (D / 8) + from;
+            const uint4 w = *reinterpret_cast<const uint4 *>((kv ? v0 : k0) + (t - start) * p.token_stride + 8 * x);
+            *reinterpret_cast<uint4 *>(tail + kv * tail_v + (t - last * kBT) * D + 8 * x) = w;
+        }
+    }
+}
+
+template <int D>
+cudaError_t launch_write(const WriteParams &p, bool bf16, bool e4m3, int grid, cudaStream_t st) {
+    if (bf16 && e4m3) write_kernel<D, true, true><<<grid, kWriteThreads, 0, st>>>(p);
+    else if (bf16) write_kernel<D, true, false><<<grid, kWriteThreads, 0, st>>>(p);
+    else if (e4m3) write_kernel<D, false, true><<<grid, kWriteThreads, 0, st>>>(p);
+    else write_kernel<D, false, false><<<grid, kWriteThreads, 0, st>>>(p);
+    return cudaGetLastError();
 }
 
 }  // namespace
@@ -285,11 +390,16 @@ int isv_q8_write(isv_q8 *h, void *pool_dev, int32_t n_pages, void *tails_dev, co
     p.k = static_cast<const uint16_t *>(k_dev);
     p.v = static_cast<const uint16_t *>(v_dev);
     p.seq_stride = seq_stride; p.token_stride = token_stride; p.T = T;
-    p.bf16 = h->d.dtype == ISV_BF16; p.e4m3 = h->d.format == ISV_Q8_E4M3;
+    p.blocks = (T + kBT - 2) / kBT + 1;
+    const bool bf16 = h->d.dtype == ISV_BF16, e4m3 = h->d.format == ISV_Q8_E4M3;
+    const long long tasks = (long long)n_seqs * p.blocks * h->d.kv_heads, per = kWriteThreads / 32;
+    const int grid = (int)std::min<long long>((tasks + per - 1) / per, 1 << 24);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
     OnDevice on(h->device);
     if (on.e != cudaSuccess) return err(ISV_ECUDA, "isv_q8_write: %s", cudaGetErrorString(on.e));
-    write_kernel<<<(n_seqs * h->d.kv_heads + 63) / 64, 64, 0, static_cast<cudaStream_t>(stream)>>>(p, h->d.head_dim);
-    cudaError_t e = cudaGetLastError();
+    const cudaError_t e = h->d.head_dim == 64   ? launch_write<64>(p, bf16, e4m3, grid, st)
+                          : h->d.head_dim == 80 ? launch_write<80>(p, bf16, e4m3, grid, st)
+                                                : launch_write<128>(p, bf16, e4m3, grid, st);
     return e == cudaSuccess ? ISV_OK : err(ISV_ECUDA, "isv_q8_write: %s", cudaGetErrorString(e));
 }
 
