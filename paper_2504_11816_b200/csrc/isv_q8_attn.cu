@@ -475,7 +475,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
         int flags = (v == beg || blk == 0 ? FIRST : 0) | (v == end - 1 || blk == nb - 1 ? LAST : 0) | (blk == 0 ? HEAD : 0) |
                     (blk == nb - 1 ? END : 0);
         if (blk < full) {
-            const int page = __ldg(p.c.table + (size_t)lo * p.c.table_stride + blk);
+            const int page = p.c.table[(size_t)lo * p.c.table_stride + blk];
             if (page >= 0 && page < p.c.n_pages) {
                 my_src = reinterpret_cast<uint64_t>(p.c.pool) + ((uint64_t)page * p.c.Hkv + group / p.P) * UNIT;
                 flags |= COPY;
