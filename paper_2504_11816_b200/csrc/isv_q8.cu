@@ -94,10 +94,12 @@ __device__ __forceinline__ uint32_t encode_raw(const float (&q)[4]) {
     }
     return w;
 }
+// up: the power of two by which numbers and scale are multiplied, for blocks so small that the quotients' arithmetic would leave
+// the normal range (s has it already); those divide every element.
 template <bool E4M3>
-__device__ __forceinline__ uint32_t encode(const float (&x)[4], float s, float inv) {
+__device__ __forceinline__ uint32_t encode(const float (&x)[4], float s, float inv, float up) {
     float q[4];
-    bool close = false;
+    bool close = up != 1.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         q[i] = x[i] * inv;
@@ -111,7 +113,7 @@ __device__ __forceinline__ uint32_t encode(const float (&x)[4], float s, float i
     }
     if (close)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) q[i] = quotient_to_odd(x[i], s);
+        for (int i = 0; i < 4; ++i) q[i] = quotient_to_odd(x[i] * up, s);
     return encode_raw<E4M3>(q);
 }
 
@@ -121,140 +123,116 @@ __device__ __forceinline__ float half_of(uint32_t w, int i) {   // the low (0) o
     return __half2float(__ushort_as_half((unsigned short)(i ? w >> 16 : w & 0xffffu)));
 }
 
-// Scale of a part from the largest magnitude (as bits) that each lane has seen; `up` is the power of two by which numbers and
-// scale of a tiny block are multiplied so that the quotients' arithmetic stays in the normal range.
-template <bool BF16, bool E4M3>
-__device__ __forceinline__ float scale_of(uint32_t top2, float &up, float &inv) {
-#pragma unroll
-    for (int o = 16; o; o /= 2) top2 = __vmaxu2(top2, __shfl_xor_sync(~0u, top2, o));
-    const uint32_t bits = max(top2 & 0xffffu, top2 >> 16);       // magnitudes of 16-bit floats order like their bits
-    const float top = half_of<BF16>(bits, 0);
-    const bool odd = bits >= (BF16 ? 0x7f80u : 0x7c00u);
-    const float scale = odd ? __int_as_float(0x7fffffff) : __fdiv_rn(top, E4M3 ? 448.f : 127.f);
-    up = top < 0x1p-60f ? 0x1p64f : 1.f;
-    inv = odd || top == 0.f ? 0.f : __fdiv_rn(1.f, scale * up);
-    return scale;
-}
-
-// A warp per (sequence, block that its new tokens touch, KV head).  A lane's loads are the 16-bit rows in the order in which
-// the page wants its codes: lane 4 g + c takes tokens g, g + 8 of K, 8 dims at a time, and dims g * D / 8 .. of tokens
+// A warp per (sequence, block that its new tokens touch, KV head, K or V).  A lane's loads are the 16-bit rows in the order in
+// which the page wants its codes: lane 4 g + c takes tokens g, g + 8 of K, 8 dims at a time, and dims g * D / 8 .. of tokens
 // 2 c, 2 c + 1, 2 c + 8, 2 c + 9 of V; what it writes are 16-byte pieces, 512 contiguous bytes of the warp.
 template <int D, bool BF16, bool E4M3>
 __global__ void __launch_bounds__(kWriteThreads) write_kernel(const __grid_constant__ WriteParams p) {
     constexpr int MT = D / 16, P = D / 32, REST = D % 32 ? 1 : 0;
     const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
-    const long long warps = (long long)gridDim.x * (kWriteThreads / 32), tasks = (long long)p.c.n_seqs * p.blocks * p.c.Hkv;
-    for (long long id = (long long)blockIdx.x * (kWriteThreads / 32) + threadIdx.x / 32; id < tasks; id += warps) {
-        const int h = (int)(id % p.c.Hkv), bi = (int)(id / p.c.Hkv % p.blocks), s = (int)(id / p.c.Hkv / p.blocks);
-        bool bad;
-        const int len = seq_len(p.c, s, bad);
-        const int asked = p.new_lens ? p.new_lens[s] : p.T;
-        const int n_new = min(max(asked, 0), min(p.T, len));
-        if ((bad || n_new != asked) && bi == 0 && h == 0 && lane == 0) atomicOr(p.c.status, ISV_STATUS_BAD_LENGTH);
-        const int start = len - n_new, b = start / kBT + bi, last = (len - 1) / kBT;
-        if (n_new == 0 || b > last) continue;
-        uint16_t *tail = reinterpret_cast<uint16_t *>(p.c.tails) + ((size_t)s * 2 * p.c.Hkv + h) * kBT * D;
-        const size_t tail_v = (size_t)p.c.Hkv * kBT * D;                     // from the K rows of a tail slot to its V rows
-        const uint16_t *k0 = p.k + s * p.seq_stride + (size_t)h * D, *v0 = p.v + s * p.seq_stride + (size_t)h * D;
-        if ((b + 1) * kBT <= len) {
-            const int page = p.c.table[(size_t)s * p.c.table_stride + b];
-            if (page < 0 || page >= p.c.n_pages) {
-                if (lane == 0) atomicOr(p.c.status, ISV_STATUS_BAD_BLOCK_ID);
-            } else {
-                auto row = [&](int kv, int t) {                              // rows before `start` wait in the tail slot
-                    const int pos = b * kBT + t;
-                    return pos < start ? tail + kv * tail_v + t * D : (kv ? v0 : k0) + (pos - start) * p.token_stride;
-                };
-                uint32_t k[2][2 * MT], v[4][MT];
+    const int task = blockIdx.x * (kWriteThreads / 32) + threadIdx.x / 32, s = blockIdx.y;
+    const int kv = task & 1, bi = (task >> 1) / p.c.Hkv, h = (task >> 1) - bi * p.c.Hkv;
+    if (bi >= p.blocks) return;
+    bool bad;
+    const int len = seq_len(p.c, s, bad);
+    const int asked = p.new_lens ? p.new_lens[s] : p.T;
+    const int n_new = min(max(asked, 0), min(p.T, len));
+    if ((bad || n_new != asked) && task == 0 && lane == 0) atomicOr(p.c.status, ISV_STATUS_BAD_LENGTH);
+    const int start = len - n_new, b = start / kBT + bi, last = (len - 1) / kBT;
+    if (n_new == 0 || b > last) return;
+    uint16_t *tail = reinterpret_cast<uint16_t *>(p.c.tails) + (((size_t)s * 2 + kv) * p.c.Hkv + h) * kBT * D;
+    const uint16_t *src = (kv ? p.v : p.k) + s * p.seq_stride + (size_t)h * D;
+    const int page = (b + 1) * kBT <= len ? p.c.table[(size_t)s * p.c.table_stride + b] : 0;
+    if ((b + 1) * kBT <= len && (page < 0 || page >= p.c.n_pages)) {
+        if (lane == 0) atomicOr(p.c.status, ISV_STATUS_BAD_BLOCK_ID);
+    } else if ((b + 1) * kBT <= len) {
+        auto row = [&](int t) {                              // rows before `start` wait in the tail slot
+            const int pos = b * kBT + t;
+            return pos < start ? tail + t * D : src + (pos - start) * p.token_stride;
+        };
+        // r[2 * MT * i + ..]: K: the lane's words of token g + 8 i; V: r[MT * j + ..]: those of the lane's j-th token
+        uint32_t r[4 * MT];
+        if (kv == 0) {
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const uint16_t *r = row(0, g + 8 * i);
+            for (int i = 0; i < 2; ++i) {
+                const uint16_t *at = row(g + 8 * i);
 #pragma unroll
-                    for (int x = 0; x < P; ++x) {
-                        const uint4 w = *reinterpret_cast<const uint4 *>(r + 32 * x + 8 * c);
-                        k[i][4 * x] = w.x; k[i][4 * x + 1] = w.y; k[i][4 * x + 2] = w.z; k[i][4 * x + 3] = w.w;
-                    }
-                    if (REST) {
-                        const uint2 w = *reinterpret_cast<const uint2 *>(r + 32 * P + 4 * c);
-                        k[i][4 * P] = w.x; k[i][4 * P + 1] = w.y;
-                    }
+                for (int x = 0; x < P; ++x) {
+                    const uint4 w = *reinterpret_cast<const uint4 *>(at + 32 * x + 8 * c);
+                    r[2 * MT * i + 4 * x] = w.x; r[2 * MT * i + 4 * x + 1] = w.y; r[2 * MT * i + 4 * x + 2] = w.z; r[2 * MT * i + 4 * x + 3] = w.w;
                 }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint16_t *r = row(1, 2 * c + (j & 1) + 8 * (j >> 1)) + g * (D / 8);
-                    if (D % 64 == 0) {
-#pragma unroll
-                        for (int x = 0; x < MT / 4; ++x) {
-                            const uint4 w = *reinterpret_cast<const uint4 *>(r + 8 * x);
-                            v[j][4 * x] = w.x; v[j][4 * x + 1] = w.y; v[j][4 * x + 2] = w.z; v[j][4 * x + 3] = w.w;
-                        }
-                    } else {
-#pragma unroll
-                        for (int x = 0; x < MT; ++x) v[j][x] = *reinterpret_cast<const uint32_t *>(r + 2 * x);
-                    }
+                if (REST) {
+                    const uint2 w = *reinterpret_cast<const uint2 *>(at + 32 * P + 4 * c);
+                    r[2 * MT * i + 4 * P] = w.x; r[2 * MT * i + 4 * P + 1] = w.y;
                 }
-                uint32_t tk = 0, tv = 0;
+            }
+        } else {
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
+            for (int j = 0; j < 4; ++j) {
+                const uint16_t *at = row(2 * c + (j & 1) + 8 * (j >> 1)) + g * (D / 8);
+                if (D % 64 == 0) {
 #pragma unroll
-                    for (int x = 0; x < 2 * MT; ++x) tk = __vmaxu2(tk, k[i][x] & 0x7fff7fffu);
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int x = 0; x < MT; ++x) tv = __vmaxu2(tv, v[j][x] & 0x7fff7fffu);
-                uint8_t *unit = p.c.pool + ((size_t)page * p.c.Hkv + h) * unit_bytes(D);
-                float up, inv;
-                const float ks = scale_of<BF16, E4M3>(tk, up, inv);
-                // a block with an infinity or a NaN (inv = 0) gets codes of 0 and the scale NaN
-                auto code = [&](float a, float b2, float c2, float d2, float s_up) {
-                    const float x[4] = {a * up, b2 * up, c2 * up, d2 * up};
-                    return inv == 0.f ? 0u : encode<E4M3>(x, s_up, inv);
-                };
-#pragma unroll
-                for (int x = 0; x < P + REST; ++x) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) {                            // k-steps 2 x, 2 x + 1; tokens g, g + 8
-                        const int ks2 = 2 * x + y / 2, i = y & 1;
-                        w[y] = ks2 < MT ? code(half_of<BF16>(k[i][2 * ks2], 0), half_of<BF16>(k[i][2 * ks2], 1),
-                                               half_of<BF16>(k[i][2 * ks2 + 1], 0), half_of<BF16>(k[i][2 * ks2 + 1], 1), ks * up) : 0u;
+                    for (int x = 0; x < MT / 4; ++x) {
+                        const uint4 w = *reinterpret_cast<const uint4 *>(at + 8 * x);
+                        r[MT * j + 4 * x] = w.x; r[MT * j + 4 * x + 1] = w.y; r[MT * j + 4 * x + 2] = w.z; r[MT * j + 4 * x + 3] = w.w;
                     }
-                    if (x < P) *reinterpret_cast<uint4 *>(unit + 512 * x + 16 * lane) = make_uint4(w[0], w[1], w[2], w[3]);
-                    else *reinterpret_cast<uint2 *>(unit + 512 * x + 8 * lane) = make_uint2(w[0], w[1]);
-                }
-                const float vs = scale_of<BF16, E4M3>(tv, up, inv);
+                } else {
 #pragma unroll
-                for (int x = 0; x < P + REST; ++x) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) {                            // tiles 2 x, 2 x + 1; dims 2 tile, 2 tile + 1 of the lane's
-                        const int mt = 2 * x + y / 2, i = y & 1;
-                        w[y] = mt < MT ? code(half_of<BF16>(v[0][mt], i), half_of<BF16>(v[1][mt], i), half_of<BF16>(v[2][mt], i),
-                                              half_of<BF16>(v[3][mt], i), vs * up) : 0u;
-                    }
-                    if (x < P) *reinterpret_cast<uint4 *>(unit + kBT * D + 512 * x + 16 * lane) = make_uint4(w[0], w[1], w[2], w[3]);
-                    else *reinterpret_cast<uint2 *>(unit + kBT * D + 512 * x + 8 * lane) = make_uint2(w[0], w[1]);
+                    for (int x = 0; x < MT; ++x) r[MT * j + x] = *reinterpret_cast<const uint32_t *>(at + 2 * x);
                 }
-                if (lane == 0) *reinterpret_cast<float4 *>(unit + 2 * kBT * D) = make_float4(ks, vs, 0.f, 0.f);
             }
         }
-        // ---- the open block's new rows into the tail slot.  Where the first block completes with rows from the tail slot, its warp
-        // stores them, after it has read those.
-        if (len % kBT == 0) continue;
-        const bool mine = start % kBT == 0 ? b == last : bi == 0;
-        if (!mine) continue;
-        __syncwarp();
-        const int from = max(start, last * kBT);
-        for (int i = lane; i < (len - from) * (D / 8) * 2; i += 32) {
-            const int kv = i & 1, x = (i >> 1) % (D / 8), t = (i >> 1) / (D / 8) + from;
-            const uint4 w = *reinterpret_cast<const uint4 *>((kv ? v0 : k0) + (t - start) * p.token_stride + 8 * x);
-            *reinterpret_cast<uint4 *>(tail + kv * tail_v + (t - last * kBT) * D + 8 * x) = w;
+        uint32_t top2 = 0;                                   // magnitudes of 16-bit floats order like their bits
+#pragma unroll
+        for (int x = 0; x < 4 * MT; ++x) top2 = __vmaxu2(top2, r[x] & 0x7fff7fffu);
+#pragma unroll
+        for (int o = 16; o; o /= 2) top2 = __vmaxu2(top2, __shfl_xor_sync(~0u, top2, o));
+        const uint32_t bits = max(top2 & 0xffffu, top2 >> 16);
+        const float top = half_of<BF16>(bits, 0);
+        const bool odd = bits >= (BF16 ? 0x7f80u : 0x7c00u); // an infinity or a NaN: codes of 0 and the scale NaN
+        const float scale = odd ? __int_as_float(0x7fffffff) : __fdiv_rn(top, E4M3 ? 448.f : 127.f);
+        const float up = top < 0x1p-60f ? 0x1p64f : 1.f, s_up = scale * up;
+        const bool zeros = odd || top == 0.f;
+        const float inv = zeros ? 0.f : __fdiv_rn(1.f, s_up);
+        uint8_t *unit = p.c.pool + ((size_t)page * p.c.Hkv + h) * unit_bytes(D), *part = unit + kv * kBT * D;
+#pragma unroll
+        for (int x = 0; x < P + REST; ++x) {
+            uint32_t w[4] = {0, 0, 0, 0};
+            if (!zeros) {
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    const int t = 2 * x + y / 2, i = y & 1;  // K: k-step t, token g + 8 i; V: tile t, dim 2 t + i of the lane's
+                    if (t >= MT) continue;
+                    const float n[4] = {kv ? half_of<BF16>(r[t], i) : half_of<BF16>(r[2 * MT * i + 2 * t], 0),
+                                        kv ? half_of<BF16>(r[MT + t], i) : half_of<BF16>(r[2 * MT * i + 2 * t], 1),
+                                        kv ? half_of<BF16>(r[2 * MT + t], i) : half_of<BF16>(r[2 * MT * i + 2 * t + 1], 0),
+                                        kv ? half_of<BF16>(r[3 * MT + t], i) : half_of<BF16>(r[2 * MT * i + 2 * t + 1], 1)};
+                    w[y] = encode<E4M3>(n, s_up, inv, up);
+                }
+            }
+            if (x < P) *reinterpret_cast<uint4 *>(part + 512 * x + 16 * lane) = make_uint4(w[0], w[1], w[2], w[3]);
+            else *reinterpret_cast<uint2 *>(part + 512 * x + 8 * lane) = make_uint2(w[0], w[1]);
         }
+        if (lane == 0) {
+            float *tags = reinterpret_cast<float *>(unit + 2 * kBT * D);
+            tags[kv] = scale;
+            tags[2 + kv] = 0.f;
+        }
+    }
+    // ---- the open block's new rows into the tail slot.  Where the first block completes with rows from the tail slot, its warp
+    // stores them, after it has read those.
+    if (len % kBT == 0 || (start % kBT == 0 ? b != last : bi != 0)) return;
+    __syncwarp();
+    const int from = max(start, last * kBT);
+    for (int i = lane; i < (len - from) * (D / 8); i += 32) {
+        const int x = i % (D / 8), t = i / (D / 8) + from;
+        const uint4 w = *reinterpret_cast<const uint4 *>(src + (t - start) * p.token_stride + 8 * x);
+        *reinterpret_cast<uint4 *>(tail + (t - last * kBT) * D + 8 * x) = w;
     }
 }
 
 template <int D>
-cudaError_t launch_write(const WriteParams &p, bool bf16, bool e4m3, int grid, cudaStream_t st) {
+cudaError_t launch_write(const WriteParams &p, bool bf16, bool e4m3, dim3 grid, cudaStream_t st) {
     if (bf16 && e4m3) write_kernel<D, true, true><<<grid, kWriteThreads, 0, st>>>(p);
     else if (bf16) write_kernel<D, true, false><<<grid, kWriteThreads, 0, st>>>(p);
     else if (e4m3) write_kernel<D, false, true><<<grid, kWriteThreads, 0, st>>>(p);
@@ -392,8 +370,9 @@ int isv_q8_write(isv_q8 *h, void *pool_dev, int32_t n_pages, void *tails_dev, co
     p.seq_stride = seq_stride; p.token_stride = token_stride; p.T = T;
     p.blocks = (T + kBT - 2) / kBT + 1;
     const bool bf16 = h->d.dtype == ISV_BF16, e4m3 = h->d.format == ISV_Q8_E4M3;
-    const long long tasks = (long long)n_seqs * p.blocks * h->d.kv_heads, per = kWriteThreads / 32;
-    const int grid = (int)std::min<long long>((tasks + per - 1) / per, 1 << 24);
+    const long long tasks = 2ll * p.blocks * h->d.kv_heads, per = kWriteThreads / 32;
+    if (tasks >= (1ll << 31) - per) return err(ISV_EINVAL, "isv_q8_write: T * kv_heads too large");
+    const dim3 grid((unsigned)((tasks + per - 1) / per), (unsigned)n_seqs);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     OnDevice on(h->device);
     if (on.e != cudaSuccess) return err(ISV_ECUDA, "isv_q8_write: %s", cudaGetErrorString(on.e));
