@@ -50,6 +50,7 @@ struct OnDevice {
 };
 
 constexpr int kWriteThreads = 128;
+constexpr int kStaticSmem = 4096;   // room for what the attention kernel declares besides its dynamic shared memory
 
 struct WriteParams {
     CacheParams c;
@@ -327,12 +328,12 @@ int isv_q8_create(isv_q8 **out, const isv_q8_desc *desc) {
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, h->device);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&h->smem_optin, cudaDevAttrMaxSharedMemoryPerBlockOptin, h->device);
     h->grid = desc->max_ctas > 0 ? std::min(desc->max_ctas, sms) : sms;   // one CTA per SM
-    if (e == cudaSuccess && isv::q8::attn_smem(D, h->GT, desc->max_seqs) + 1024 > (size_t)h->smem_optin) {
+    if (e == cudaSuccess && isv::q8::attn_smem(D, h->GT, desc->max_seqs) + kStaticSmem > (size_t)h->smem_optin) {
         delete h;
         return err(ISV_EINVAL, "isv_q8_create: shared memory too small for this shape");
     }
-    const size_t rows = (size_t)isv::q8::attn_slots(h->GT, h->grid) * isv::q8::attn_head_rows(h->GT);
-    if (e == cudaSuccess) e = isv::q8::attn_configure(D, h->GT, desc->dtype == ISV_BF16, desc->format == ISV_Q8_E4M3, h->smem_optin - 1024);
+    const size_t rows = (size_t)isv::q8::attn_slots(h->grid) * isv::q8::attn_head_rows(h->GT);
+    if (e == cudaSuccess) e = isv::q8::attn_configure(D, h->GT, desc->dtype == ISV_BF16, desc->format == ISV_Q8_E4M3, h->smem_optin - kStaticSmem);
     if (e == cudaSuccess) e = cudaMalloc((void **)&h->status, 4);
     if (e == cudaSuccess) e = cudaMemset(h->status, 0, 4);
     if (e == cudaSuccess) e = cudaMalloc((void **)&h->part_o, rows * D * 4);

@@ -28,8 +28,8 @@ struct AttnParams {
     const uint16_t *q;          // [n_seqs][Hq][D]
     void *out;
     float *out_f32;
-    float *part_o;              // partial results: [slot][heads of a visit][D], [slot][heads of a visit][2]
-    float *part_ml;
+    float *part_o;              // partial results of items that cross CTAs: [slot][values of a visit's heads], two slots a CTA
+    float *part_ml;             // [slot][heads of a visit][m, l]
     int32_t *tickets;           // [grid], zero between launches
     int32_t Hq, P, GT;          // Hq = Hkv * P * GT; a visit serves GT query heads
     float scale_log2;           // log2(e) / sqrt(D)
@@ -45,7 +45,7 @@ __device__ __forceinline__ int seq_len(const CacheParams &c, int s, bool &bad) {
 // Shape of the attention kernel that serves GT query heads per visit at head_dim D.
 int attn_warps(int GT);
 int attn_head_rows(int GT);                                        // GT rounded up to whole tiles of 8
-int attn_slots(int GT, int grid);                                  // partial results of a launch
+int attn_slots(int grid);                                          // partial results of a launch
 size_t attn_smem(int D, int GT, int max_seqs);
 cudaError_t attn_configure(int D, int GT, bool bf16, bool e4m3, size_t smem);
 cudaError_t launch_attn(const AttnParams &p, int D, bool bf16, bool e4m3, int grid, size_t smem, cudaStream_t st);

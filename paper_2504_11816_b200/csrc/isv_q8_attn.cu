@@ -13,7 +13,7 @@
 // What bounds it is reading the cache.  All visits of all (sequence, KV head) pairs form one list that is cut into equal ranges,
 // one per warp, whatever the lengths.  A warp streams its visits through a ring of its own (one bulk copy of
 // a unit brings K, V and both scales).  A pair that several warps share leaves partial results that are merged in fixed
-// order, first within the CTA, then, for the pairs that cross CTAs, by the CTA that arrives last.
+// order, first within the CTA in shared memory, then, for the pairs that cross CTAs, by the CTA that arrives last.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -50,6 +50,7 @@ __device__ __forceinline__ void copy_in(uint32_t dst, const void *src, uint32_t 
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                  ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
+__device__ __forceinline__ void prefetch_l1(const void *p) { asm volatile("prefetch.global.L1 [%0];" ::"l"(p)); }
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -304,6 +305,10 @@ struct State {
     __device__ __forceinline__ void open_block(const uint16_t *k, const uint16_t *v, int n, const uint16_t *q0, int GT,
                                                float scale_log2, int lane) {
         const int g = lane >> 2, c = lane & 3;
+        if (128 * lane < n * D * 2) {      // the rows of V arrive while the scores are taken
+            prefetch_l1(reinterpret_cast<const uint8_t *>(k) + 128 * lane);
+            prefetch_l1(reinterpret_cast<const uint8_t *>(v) + 128 * lane);
+        }
         float s[NT][4];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -314,7 +319,9 @@ struct State {
             const uint4 a = q_words(k + (size_t)g * D, p, c, g < n), b = q_words(k + (size_t)(g + 8) * D, p, c, g + 8 < n);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                const uint4 w = q_words(q0 + (size_t)(nt * 8 + g) * D, p, c, nt * 8 + g < GT);
+                uint4 w;                   // q as it is (in fp16 the operand in use, in bf16 that one is scaled)
+                if (BF16) w = q_words(q0 + (size_t)(nt * 8 + g) * D, p, c, nt * 8 + g < GT);
+                else w = make_uint4(q[nt][2 * p][0], q[nt][2 * p][1], 2 * p + 1 < KS ? q[nt][(2 * p + 1) % KS][0] : 0, 2 * p + 1 < KS ? q[nt][(2 * p + 1) % KS][1] : 0);
                 mma<BF16>(s[nt], a.x, b.x, a.y, b.y, w.x, w.y);
                 if (2 * p + 1 < KS) mma<BF16>(s[nt], a.z, b.z, a.w, b.w, w.z, w.w);
             }
@@ -389,7 +396,9 @@ struct Shape {
     static constexpr int UNIT = unit_bytes(D);
     static constexpr int ST = kRingBytes / (NW * UNIT);
     static constexpr int HT = 8 * NT;
+    static constexpr int REC = HT * D / 2;     // pairs of output values in a record
     static_assert(ST >= 2 && ST <= 8, "ring depth");
+    static_assert(REC * 8 <= ST * UNIT, "a record fits a warp's part of the ring");
 };
 
 template <int D, int NT, bool BF16, bool E4M3>
@@ -398,14 +407,16 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
     constexpr int NW = SH::NW, UNIT = SH::UNIT, ST = SH::ST, HT = SH::HT, THREADS = NW * 32;
     extern __shared__ __align__(128) uint8_t smem[];
     uint8_t *ring = smem;                                                       // [NW][ST] units
-    Visit *visits = reinterpret_cast<Visit *>(ring + (size_t)NW * ST * UNIT);   // [NW][ST]
+    float2 *early = reinterpret_cast<float2 *>(ring + (size_t)NW * ST * UNIT);  // [NW][REC]: records left before a warp's end
+    Visit *visits = reinterpret_cast<Visit *>(early + NW * SH::REC);            // [NW][ST]
     uint64_t *bars = reinterpret_cast<uint64_t *>(visits + NW * ST);            // [NW][ST]
     int *prefix = reinterpret_cast<int *>(bars + NW * ST);                      // [n_seqs + 1] blocks before a sequence
     __shared__ int scan[NW];
     __shared__ int rec_item[NW][2];            // items of which the warps left a partial result (flat: sequence, group)
+    __shared__ float2 rec_ml[NW][2][HT];       // their m and l
     __shared__ int run_item[NW + 1], run_first[NW + 2], n_runs;
-    __shared__ int list[2 * NW];               // slots of the records, in order
-    __shared__ int arrived;
+    __shared__ int list[2 * NW];               // records in order: 2 * warp + which
+    __shared__ int last_of[2];                 // whether this CTA is the last of its first and its last item
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int G = p.c.Hkv * p.P;               // head groups of a sequence
 
@@ -488,13 +499,14 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
         my_visit = Visit{lo, group, flags, 0};
     };
     int next = beg;
+    bool lost = false;                         // a copy did not arrive in time: the range is walked to its end without its data
     auto produce = [&](int slot) {             // the next visit into this slot of the ring
         if (next >= end) return;
         const int i = (next - beg) & 31;
         if (i == 0) look_up(next + lane);
         const uint64_t src = __shfl_sync(~0u, my_src, i);
         if (lane == i) visits[warp * ST + slot] = my_visit;
-        if (lane == 0 && src)
+        if (lane == 0 && src && !lost)
             copy_in(s32(ring + (size_t)(warp * ST + slot) * UNIT), reinterpret_cast<const void *>(src), UNIT, s32(&bars[warp * ST + slot]));
         ++next;
     };
@@ -505,10 +517,9 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
     State<D, NT, BF16> st;
     const uint16_t *q0 = p.q;
     uint32_t phases = 0;
-    bool lost = false;
     int slot = 0;
     bool whole = false;
-    for (int v = beg; v < end && !lost; ++v) {
+    for (int v = beg; v < end; ++v) {
         const Visit t = visits[warp * ST + slot];
         if (t.flags & FIRST) {
             q0 = p.q + ((size_t)t.seq * p.Hq + (size_t)t.group * p.GT) * D;
@@ -516,8 +527,16 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
             whole = t.flags & HEAD;
         }
         if (t.flags & COPY) {
-            if (!wait(s32(&bars[warp * ST + slot]), (phases >> slot) & 1u)) lost = true;
-            else {
+            if (!lost && !wait(s32(&bars[warp * ST + slot]), (phases >> slot) & 1u)) {
+                // the copies in flight get one more bounded chance, so that none lands in memory used for something else
+                for (int i = 0; i < ST && i < end - v; ++i) {
+                    const int x = (slot + i) % ST;
+                    if (visits[warp * ST + x].flags & COPY) wait(s32(&bars[warp * ST + x]), (phases >> x) & 1u);
+                }
+                lost = true;
+                bad |= ISV_STATUS_WAIT_EXPIRED;
+            }
+            if (!lost) {
                 phases ^= 1u << slot;
                 st.template visit<E4M3>(ring + (size_t)(warp * ST + slot) * UNIT, lane);
             }
@@ -526,7 +545,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
             st.open_block(k, k + (size_t)p.c.Hkv * kBT * D, t.flags >> 8, q0, p.GT, p.scale_log2, lane);
         }
         __syncwarp();
-        if (!lost) produce(slot);
+        produce(slot);
         if (t.flags & LAST) {
             st.finish();
             const int g = lane >> 2, c = lane & 3;
@@ -546,121 +565,158 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
             } else {
                 // an item that begins before this warp's range leaves record 0, any other record 1
                 const int which = whole ? 1 : 0;
-                const size_t at = ((size_t)blockIdx.x * NW + warp) * 2 + which;
                 if (lane == 0) rec_item[warp][which] = t.seq * G + t.group;
+                // a later record is this warp's last: its part of the ring is no longer in use
+                float2 *o = which ? reinterpret_cast<float2 *>(ring + (size_t)warp * ST * UNIT) : early + warp * SH::REC;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const int h = nt * 8 + 2 * c + i;
-                        if (h < p.GT) {
-                            float *o = p.part_o + (at * HT + h) * D + g * (D / 8);
+                        if (g == 0) rec_ml[warp][which][nt * 8 + 2 * c + i] = make_float2(st.m[nt][i], st.l[nt][i]);
 #pragma unroll
-                            for (int mt = 0; mt < D / 16; ++mt)
-                                *reinterpret_cast<float2 *>(o + 2 * mt) = make_float2(st.acc[nt][mt][i] * st.vref, st.acc[nt][mt][i + 2] * st.vref);
-                            if (g == 0) *reinterpret_cast<float2 *>(p.part_ml + (at * HT + h) * 2) = make_float2(st.m[nt][i], st.l[nt][i]);
-                        }
+                        for (int mt = 0; mt < D / 16; ++mt)
+                            o[((nt * 2 + i) * (D / 16) + mt) * 32 + c * 8 + g] = make_float2(st.acc[nt][mt][i] * st.vref, st.acc[nt][mt][i + 2] * st.vref);
                     }
             }
         }
         slot = slot + 1 == ST ? 0 : slot + 1;
         __syncwarp();
     }
-    if (lost) {   // a copy did not arrive in time: give the others one more bounded chance and report
-        bad |= ISV_STATUS_WAIT_EXPIRED;
-        for (int i = 0; i < ST; ++i)
-            if (visits[warp * ST + i].flags & COPY) wait(s32(&bars[warp * ST + i]), (phases >> i) & 1u);
-    }
     if (bad) atomicOr(p.c.status, bad);
     __syncthreads();
 
     // ---- partial results of this CTA: consecutive records of one item form a run
-    if (tid == 0) {
-        int n = 0, runs = 0, before = -1;
-        for (int w = 0; w < warps; ++w)
-            for (int i = 0; i < 2; ++i) {
-                const int item = rec_item[w][i];
-                if (item < 0) continue;
-                if (item != before) { run_item[runs] = item; run_first[runs++] = n; }
-                list[n++] = (blockIdx.x * NW + w) * 2 + i;
-                before = item;
-            }
-        run_first[runs] = n;
-        n_runs = runs;
+    if (warp == 0) {
+        const int w = lane;                    // warps' records in order, two a lane
+        const int i0 = w < warps ? rec_item[w][0] : -1, i1 = w < warps ? rec_item[w][1] : -1;
+        const unsigned h0 = __ballot_sync(~0u, i0 >= 0), h1 = __ballot_sync(~0u, i1 >= 0), below = (1u << w) - 1u;
+        const int n0 = __popc(h0 & below) + __popc(h1 & below), n1 = n0 + (i0 >= 0);
+        if (i0 >= 0) list[n0] = 2 * w;
+        if (i1 >= 0) list[n1] = 2 * w + 1;
+        // an item begins a run where its own first record is: the records of an item are neighbours in the list
+        const int total_recs = __popc(h0) + __popc(h1);
+        __syncwarp();
+        const int r = lane < total_recs ? list[lane] : 0;
+        const int item = lane < total_recs ? rec_item[r >> 1][r & 1] : -1;
+        int before = __shfl_up_sync(~0u, item, 1);
+        if (lane == 0) before = -1;
+        const bool first = item >= 0 && item != before;
+        const unsigned f = __ballot_sync(~0u, first);
+        const int run = __popc(f & below);
+        if (first) { run_item[run] = item; run_first[run] = lane; }
+        if (lane == 0) { n_runs = __popc(f); run_first[__popc(f)] = total_recs; }
     }
     __syncthreads();
+    if (n_runs == 0) return;
     const int cta_beg = (int)(total * blockIdx.x / ctas), cta_end = (int)(total * (blockIdx.x + 1) / ctas);
-    const int units = p.GT * (D / 4);
+    constexpr int MT = D / 16, PAIRS = D / 2;
+    const int units = p.GT * PAIRS;            // unit (h, mt, g): output dims g * D / 8 + 2 mt, + 1 of head h
     auto item_span = [&](int item, int &b, int &e) {
         const int s = item / G, nb = prefix[s + 1] - prefix[s];
         b = prefix[s] * G + (item - s * G) * nb;
         e = b + nb;
     };
-    // weighted sum of records [0, n) of one head, four dims
-    auto merge = [&](int n, auto slot_of, int h, int x, float &m, float &l) {
-        m = kNone;
-        for (int i = 0; i < n; ++i) m = fmaxf(m, __ldcg(p.part_ml + ((size_t)slot_of(i) * HT + h) * 2));
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        l = 0.f;
-#pragma unroll 4
-        for (int i = 0; i < n; ++i) {
-            const size_t at = (size_t)slot_of(i) * HT + h;
-            const float2 ml = __ldcg(reinterpret_cast<const float2 *>(p.part_ml + at * 2));
-            const float4 v = __ldcg(reinterpret_cast<const float4 *>(p.part_o + at * D + x));
-            const float w = ex2(ml.x - m);
-            l += w * ml.y;
-            o.x += w * v.x; o.y += w * v.y; o.z += w * v.z; o.w += w * v.w;
-        }
-        return o;
-    };
-    auto put = [&](int item, int h, int x, const float4 &o, float l) {
+    auto put = [&](int item, int u, float2 o, float l) {
+        const int h = u / PAIRS, mt = u % PAIRS / 8, g = u % 8;
         const float f = l == 0.f ? 0.f : 1.f / l;
-        const size_t at = ((size_t)item * p.GT + h) * D + x;      // item * GT is the flat query head
-        store2<BF16>(p, at, o.x * f, o.y * f);
-        store2<BF16>(p, at + 2, o.z * f, o.w * f);
+        store2<BF16>(p, ((size_t)item * p.GT + h) * D + g * (D / 8) + 2 * mt, o.x * f, o.y * f);   // item * GT + h: the flat query head
     };
-    const size_t cta_slots = (size_t)gridDim.x * NW * 2;
-    for (int u = tid; u < n_runs * units; u += THREADS) {
-        const int run = u / units, h = (u - run * units) / (D / 4), x = (u - run * units) % (D / 4) * 4;
-        const int r0 = run_first[run], item = run_item[run];
-        float m, l;
-        const float4 o = merge(run_first[run + 1] - r0, [&](int i) { return list[r0 + i]; }, h, x, m, l);
+    for (int x = tid; x < n_runs * units; x += THREADS) {
+        const int run = x / units, u = x - run * units, h = u / PAIRS, mt = u % PAIRS / 8, g = u % 8;
+        const int r0 = run_first[run], r1 = run_first[run + 1], item = run_item[run];
+        const int place = (((h >> 3) * 2 + (h & 1)) * MT + mt) * 32 + ((h & 7) >> 1) * 8 + g;
+        float m = kNone, l = 0.f;
+        for (int r = r0; r < r1; ++r) m = fmaxf(m, rec_ml[list[r] >> 1][list[r] & 1][h].x);
+        float2 o = make_float2(0.f, 0.f);
+        for (int r = r0; r < r1; ++r) {
+            const int w = list[r] >> 1, which = list[r] & 1;
+            const float2 ml = rec_ml[w][which][h];
+            const float2 v = (which ? reinterpret_cast<const float2 *>(ring + (size_t)w * ST * UNIT) : early + w * SH::REC)[place];
+            const float f = ex2(ml.x - m);
+            l += f * ml.y;
+            o.x += f * v.x;
+            o.y += f * v.y;
+        }
         int b, e;
         item_span(item, b, e);
-        if (b >= cta_beg && e <= cta_end) put(item, h, x, o, l);
+        if (b >= cta_beg && e <= cta_end) put(item, u, o, l);
         else {
-            const size_t at = (cta_slots + blockIdx.x * 2 + (b > cta_beg ? 1 : 0)) * HT + h;
-            *reinterpret_cast<float4 *>(p.part_o + at * D + x) = o;
-            if (x == 0) *reinterpret_cast<float2 *>(p.part_ml + at * 2) = make_float2(m, l);
+            const int slot = blockIdx.x * 2 + (b > cta_beg ? 1 : 0);
+            __stcg(reinterpret_cast<float2 *>(p.part_o) + (size_t)slot * SH::REC + u, o);
+            if (u % PAIRS == 0) __stcg(reinterpret_cast<float2 *>(p.part_ml) + slot * HT + h, make_float2(m, l));
         }
     }
-    // ---- items that cross CTAs: the last CTA to arrive merges.  The ticket of an item is that of its first CTA, in
-    // which no other item continues into the next.
-    for (int k = 0; k < 2; ++k) {
-        if (k == 1 && n_runs < 2) break;
-        if (n_runs == 0) break;
-        const int item = run_item[k == 0 ? 0 : n_runs - 1];
-        int b, e;
+    // ---- items that cross CTAs (the first and the last of this one may): the last CTA to arrive merges.  The ticket of an
+    // item is that of its first CTA, in which no other item continues into the next.
+    auto owner = [&](int v) { return (int)((((long long)v + 1) * ctas - 1) / total); };   // CTA whose range holds visit v
+    auto crosses = [&](int k, int &item, int &c0, int &n, int &b) {
+        if (k == 1 && n_runs < 2) return false;
+        item = run_item[k == 0 ? 0 : n_runs - 1];
+        int e;
         item_span(item, b, e);
-        if (b >= cta_beg && e <= cta_end) continue;
-        auto owner = [&](int v) { return (int)((((long long)v + 1) * ctas - 1) / total); };   // CTA whose range holds visit v
-        const int c0 = owner(b), n = owner(e - 1) - c0 + 1;
-        __threadfence();
-        __syncthreads();
-        if (tid == 0) {
-            arrived = atomicAdd(p.tickets + c0, 1);
-            if (arrived == n - 1) p.tickets[c0] = 0;
+        if (b >= cta_beg && e <= cta_end) return false;
+        c0 = owner(b);
+        n = owner(e - 1) - c0 + 1;
+        return true;
+    };
+    __threadfence();
+    __syncthreads();
+    if (lane == 0 && warp < 2) {
+        int item, c0, n, b;
+        bool last = false;
+        if (crosses(warp, item, c0, n, b)) {
+            last = atomicAdd(p.tickets + c0, 1) == n - 1;
+            if (last) p.tickets[c0] = 0;
             __threadfence();
         }
-        __syncthreads();
-        if (arrived != n - 1) continue;
+        last_of[warp] = last;
+    }
+    __syncthreads();
+    float2 *ml = reinterpret_cast<float2 *>(ring);                 // [n][GT], then the sums of the parts of a unit's records
+    float2 *sums = ml + gridDim.x * HT;                            // [THREADS]
+    float *sums_l = reinterpret_cast<float *>(sums + THREADS);     // [THREADS]
+    const int split = max(1, THREADS / units);                     // threads that share a unit's records
+    for (int k = 0; k < 2; ++k) {
+        if (!last_of[k]) continue;
+        int item, c0, n, b;
+        crosses(k, item, c0, n, b);
         const int first_slot = b == (int)(total * c0 / ctas) ? 0 : 1;
-        for (int u = tid; u < units; u += THREADS) {
-            const int h = u / (D / 4), x = u % (D / 4) * 4;
-            float m, l;
-            const float4 o = merge(n, [&](int i) { return (int)cta_slots + (c0 + i) * 2 + (i == 0 ? first_slot : 0); }, h, x, m, l);
-            put(item, h, x, o, l);
+        auto slot_of = [&](int i) { return (c0 + i) * 2 + (i == 0 ? first_slot : 0); };
+        for (int i = tid; i < n * p.GT; i += THREADS)
+            ml[i] = __ldcg(reinterpret_cast<const float2 *>(p.part_ml) + slot_of(i / p.GT) * HT + i % p.GT);
+        __syncthreads();
+        for (int u0 = 0; u0 < units; u0 += THREADS) {
+            const int u = u0 + (split > 1 ? tid % units : tid), part = split > 1 ? tid / units : 0;
+            const bool active = u < units && part < split;
+            float m = kNone, l = 0.f;
+            float2 o = make_float2(0.f, 0.f);
+            if (active) {
+                const int h = u / PAIRS;
+                for (int i = 0; i < n; ++i) m = fmaxf(m, ml[i * p.GT + h].x);
+#pragma unroll 8
+                for (int i = part; i < n; i += split) {
+                    const float2 v = __ldcg(reinterpret_cast<const float2 *>(p.part_o) + (size_t)slot_of(i) * SH::REC + u);
+                    const float2 a = ml[i * p.GT + h];
+                    const float f = ex2(a.x - m);
+                    l += f * a.y;
+                    o.x += f * v.x;
+                    o.y += f * v.y;
+                }
+            }
+            if (split > 1) {
+                sums[tid] = o;
+                sums_l[tid] = l;
+                __syncthreads();
+                if (active && part == 0)
+                    for (int j = 1; j < split; ++j) {
+                        o.x += sums[j * units + u].x;
+                        o.y += sums[j * units + u].y;
+                        l += sums_l[j * units + u];
+                    }
+            }
+            if (active && part == 0) put(item, u, o, l);
         }
+        __syncthreads();
     }
 }
 
@@ -709,11 +765,12 @@ struct Launch {
 
 int attn_warps(int GT) { return GT <= 8 ? Shape<128, 1>::NW : Shape<128, 2>::NW; }
 int attn_head_rows(int GT) { return GT <= 8 ? 8 : 16; }
-int attn_slots(int GT, int grid) { return grid * attn_warps(GT) * 2 + grid * 2; }
+int attn_slots(int grid) { return 2 * grid; }
 
 size_t attn_smem(int D, int GT, int max_seqs) {
     const size_t unit = unit_bytes(D), nw = attn_warps(GT), st = kRingBytes / (nw * unit);
-    return nw * st * (unit + sizeof(Visit) + 8) + 4 * ((size_t)max_seqs + 1);
+    const size_t record = (size_t)attn_head_rows(GT) * D * 4;
+    return nw * (st * (unit + sizeof(Visit) + 8) + record) + 4 * ((size_t)max_seqs + 1);
 }
 cudaError_t attn_configure(int D, int GT, bool bf16, bool e4m3, size_t smem) { return pick(D, GT, bf16, e4m3, Configure{smem}); }
 cudaError_t launch_attn(const AttnParams &p, int D, bool bf16, bool e4m3, int grid, size_t smem, cudaStream_t st) {
