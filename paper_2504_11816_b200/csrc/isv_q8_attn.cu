@@ -89,6 +89,18 @@ __device__ __forceinline__ void widen(uint32_t w, uint32_t &lo, uint32_t &hi) {
     }
 }
 
+// The same for K, where the products can carry an offset: int8 codes + 128 as they are, in the last places of fp16 numbers of
+// exponent 0, i.e. (code + 128) * 2^-24, bytes 0 and 2 first, then 1 and 3.  Three instructions a word instead of five; a score
+// is then 2^24 * (sum - 128 * 2^-24 * sum of q).
+template <bool E4M3>
+__device__ __forceinline__ void widen_k(uint32_t w, uint32_t &lo, uint32_t &hi) {
+    if (E4M3) widen<true>(w, lo, hi);
+    else {
+        lo = (w ^ 0x00800080u) & 0x00ff00ffu;
+        hi = ((w >> 8) ^ 0x00800080u) & 0x00ff00ffu;
+    }
+}
+
 template <bool BF16>
 __device__ __forceinline__ uint32_t pack2(float x, float y) {   // x in the low half
     if (BF16) {
@@ -114,7 +126,7 @@ __device__ __forceinline__ uint32_t split2(float &x, float &y) {
 
 // ---- one warp's running state for the heads of a visit.  Lane 4 g + c holds, of each 16 x 8 score tile, tokens g and
 // g + 8 of heads 2 c and 2 c + 1; of the output dims g * D / 8 .. of the same heads.
-template <int D, int NT, bool BF16>
+template <int D, int NT, bool BF16, bool E4M3>
 struct State {
     static constexpr int KS = D / 16, MT = D / 16;
     float acc[NT][MT][4];
@@ -122,6 +134,7 @@ struct State {
     float vref, inv_vref;      // acc is in units of vref, a power of two near the scales of V seen last
     uint32_t q[NT][KS][2];     // q as fp16 operand
     float qf[NT][2];           // what its scores have to be multiplied by
+    float q128[NT][2];         // int8: 128 * the sum of the operand's values
 
     // Raw q operand of k-steps 2 p, 2 p + 1 of head row `row` (16 bytes; the last 8 at head_dim 80).
     __device__ __forceinline__ static uint4 q_words(const uint16_t *row, int p, int c, bool valid) {
@@ -166,13 +179,25 @@ struct State {
                         (&w[p].x)[i] = pack2<false>(v.x * down, v.y * down);
                     }
             }
+            float sum = 0.f;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
-                q[nt][ks][0] = (&w[ks / 2].x)[2 * (ks % 2)];
-                q[nt][ks][1] = (&w[ks / 2].x)[2 * (ks % 2) + 1];
+                const uint32_t x = (&w[ks / 2].x)[2 * (ks % 2)], y = (&w[ks / 2].x)[2 * (ks % 2) + 1];
+                q[nt][ks][0] = E4M3 ? x : __byte_perm(x, y, 0x5410);
+                q[nt][ks][1] = E4M3 ? y : __byte_perm(x, y, 0x7632);
+                if (!E4M3) {
+                    const float2 a = unpack2<false>(x), b = unpack2<false>(y);
+                    sum += (a.x + a.y) + (b.x + b.y);
+                }
             }
             qf[nt][0] = __shfl_sync(~0u, f, 8 * c);        // head 2 c is row 2 c: lanes 8 c ..
             qf[nt][1] = __shfl_sync(~0u, f, 8 * c + 4);
+            if (!E4M3) {
+                sum += __shfl_xor_sync(~0u, sum, 1);
+                sum += __shfl_xor_sync(~0u, sum, 2);
+                q128[nt][0] = 128.f * __shfl_sync(~0u, sum, 8 * c);
+                q128[nt][1] = 128.f * __shfl_sync(~0u, sum, 8 * c + 4);
+            }
 #pragma unroll
             for (int i = 0; i < 2; ++i) { m[nt][i] = kNone; l[nt][i] = 0.f; }
 #pragma unroll
@@ -234,14 +259,13 @@ struct State {
     }
 
     // One complete block; `unit` in shared memory.
-    template <bool E4M3>
     __device__ __forceinline__ void visit(const uint8_t *unit, int lane) {
         const float2 scale = *reinterpret_cast<const float2 *>(unit + 2 * kBT * D);
-        float s[NT][4];
+        float s[NT][4], odd[NT][4];        // two sums: half the length of the chain of dependent instructions
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[nt][i] = 0.f;
+            for (int i = 0; i < 4; ++i) s[nt][i] = odd[nt][i] = 0.f;
 #pragma unroll
         for (int p = 0; p < (KS + 1) / 2; ++p) {
             uint32_t w[4];
@@ -250,16 +274,19 @@ struct State {
             for (int i = 0; i < 2; ++i) {
                 if (2 * p + i >= KS) break;
                 uint32_t a0, a1, a2, a3;
-                widen<E4M3>(w[2 * i], a0, a2);
-                widen<E4M3>(w[2 * i + 1], a1, a3);
+                widen_k<E4M3>(w[2 * i], a0, a2);
+                widen_k<E4M3>(w[2 * i + 1], a1, a3);
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma<false>(s[nt], a0, a1, a2, a3, q[nt][2 * p + i][0], q[nt][2 * p + i][1]);
+                for (int nt = 0; nt < NT; ++nt) mma<false>(i ? odd[nt] : s[nt], a0, a1, a2, a3, q[nt][2 * p + i][0], q[nt][2 * p + i][1]);
             }
         }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[nt][i] *= qf[nt][i & 1] * scale.x;
+            for (int i = 0; i < 4; ++i) {
+                const float x = s[nt][i] + odd[nt][i];
+                s[nt][i] = (E4M3 ? x : fmaf(x, 0x1p24f, -q128[nt][i & 1])) * (qf[nt][i & 1] * scale.x);
+            }
         weigh(s);
         refer(scale.y);
         const float vr = scale.y * inv_vref;
@@ -321,7 +348,12 @@ struct State {
             for (int nt = 0; nt < NT; ++nt) {
                 uint4 w;                   // q as it is (in fp16 the operand in use, in bf16 that one is scaled)
                 if (BF16) w = q_words(q0 + (size_t)(nt * 8 + g) * D, p, c, nt * 8 + g < GT);
-                else w = make_uint4(q[nt][2 * p][0], q[nt][2 * p][1], 2 * p + 1 < KS ? q[nt][(2 * p + 1) % KS][0] : 0, 2 * p + 1 < KS ? q[nt][(2 * p + 1) % KS][1] : 0);
+                else {
+                    const uint32_t (&x)[2] = q[nt][2 * p], (&y)[2] = q[nt][(2 * p + 1) % KS];
+                    w = E4M3 ? make_uint4(x[0], x[1], y[0], y[1])
+                             : make_uint4(__byte_perm(x[0], x[1], 0x5410), __byte_perm(x[0], x[1], 0x7632),
+                                          __byte_perm(y[0], y[1], 0x5410), __byte_perm(y[0], y[1], 0x7632));
+                }
                 mma<BF16>(s[nt], a.x, b.x, a.y, b.y, w.x, w.y);
                 if (2 * p + 1 < KS) mma<BF16>(s[nt], a.z, b.z, a.w, b.w, w.z, w.w);
             }
@@ -410,7 +442,8 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
     float2 *early = reinterpret_cast<float2 *>(ring + (size_t)NW * ST * UNIT);  // [NW][REC]: records left before a warp's end
     Visit *visits = reinterpret_cast<Visit *>(early + NW * SH::REC);            // [NW][ST]
     uint64_t *bars = reinterpret_cast<uint64_t *>(visits + NW * ST);            // [NW][ST]
-    int *prefix = reinterpret_cast<int *>(bars + NW * ST);                      // [n_seqs + 1] blocks before a sequence
+    int *prefix = reinterpret_cast<int *>(bars + NW * ST);                      // [n_seqs + 1] visits of a head group before a sequence
+    uint8_t *open = reinterpret_cast<uint8_t *>(prefix + p.c.n_seqs + 1);       // [n_seqs] rows of the open block
     __shared__ int scan[NW];
     __shared__ int rec_item[NW][2];            // items of which the warps left a partial result (flat: sequence, group)
     __shared__ float2 rec_ml[NW][2][HT];       // their m and l
@@ -420,7 +453,11 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int G = p.c.Hkv * p.P;               // head groups of a sequence
 
-    // ---- blocks before each sequence; sequences without any get their zeros
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+    // ---- visits before each sequence: one per block and one, without data, at the front of each item, which is about
+    // what starting and finishing an item costs; sequences without any block get their zeros
     uint32_t bad = 0;
     int carry = 0;
     for (int s0 = 0; s0 < p.c.n_seqs; s0 += THREADS) {
@@ -428,7 +465,9 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
         int nb = 0;
         if (s < p.c.n_seqs) {
             bool b;
-            nb = (seq_len(p.c, s, b) + kBT - 1) / kBT;
+            const int len = seq_len(p.c, s, b);
+            nb = len ? (len + kBT - 1) / kBT + 1 : 0;
+            open[s] = (uint8_t)(len % kBT);
             if (b) bad |= ISV_STATUS_BAD_LENGTH;
         }
         int x = nb;
@@ -457,16 +496,20 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
         if (prefix[s] == prefix[s + 1])
             for (int x = 2 * tid; x < p.Hq * D; x += 2 * THREADS) store2<BF16>(p, (size_t)s * p.Hq * D + x, 0.f, 0.f);
 
-    const long long total = (long long)carry * G;
-    const int ctas = (int)min((long long)gridDim.x, total);
+    // range of part i of n: the first `rest` parts are one longer
+    const int total = carry * G;               // below 2^31: the host checks
+    const int ctas = min((int)gridDim.x, total);
     if ((int)blockIdx.x >= ctas) {
         if (bad && blockIdx.x == 0) atomicOr(p.c.status, bad);
         return;
     }
-    const int warps = (int)min((long long)NW, max(1ll, total / ((long long)ctas * kMinVisits)));
-    const long long shares = (long long)ctas * warps, me = (long long)blockIdx.x * warps + warp;
-    const int beg = warp < warps ? (int)(total * me / shares) : 0;
-    const int end = warp < warps ? (int)(total * (me + 1) / shares) : 0;
+    const int share = total / ctas, rest = total - share * ctas;
+    auto cta_at = [&](int c) { return share * c + min(c, rest); };
+    const int cta_beg = cta_at(blockIdx.x), cta_end = cta_at(blockIdx.x + 1), cta_n = cta_end - cta_beg;
+    const int warps = min(NW, max(1, cta_n / kMinVisits));
+    const int mine = cta_n / warps, more = cta_n - mine * warps;
+    const int beg = warp < warps ? cta_beg + mine * warp + min(warp, more) : 0;
+    const int end = warp < warps ? beg + mine + (warp < more ? 1 : 0) : 0;
 
     // ---- producer: 32 visits at a time are looked up, one per lane
     uint64_t my_src = 0;
@@ -477,15 +520,14 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
         int lo = 0, hi = p.c.n_seqs;           // the last sequence whose visits begin at or before v
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
-            if ((long long)prefix[mid] * G <= v) lo = mid; else hi = mid;
+            if (prefix[mid] * G <= v) lo = mid; else hi = mid;
         }
         const int nb = prefix[lo + 1] - prefix[lo];
-        const int r = v - prefix[lo] * G, group = r / nb, blk = r - group * nb;
-        bool b;
-        const int len = seq_len(p.c, lo, b), full = len / kBT;
-        int flags = (v == beg || blk == 0 ? FIRST : 0) | (v == end - 1 || blk == nb - 1 ? LAST : 0) | (blk == 0 ? HEAD : 0) |
-                    (blk == nb - 1 ? END : 0);
-        if (blk < full) {
+        const int r = v - prefix[lo] * G, group = r / nb, at = r - group * nb, blk = at - 1;
+        int flags = (v == beg || at == 0 ? FIRST : 0) | (v == end - 1 || at == nb - 1 ? LAST : 0) | (at == 0 ? HEAD : 0) |
+                    (at == nb - 1 ? END : 0);
+        if (blk < 0) {
+        } else if (blk < nb - 1 - (open[lo] != 0)) {
             const int page = p.c.table[(size_t)lo * p.c.table_stride + blk];
             if (page >= 0 && page < p.c.n_pages) {
                 my_src = reinterpret_cast<uint64_t>(p.c.pool) + ((uint64_t)page * p.c.Hkv + group / p.P) * UNIT;
@@ -494,7 +536,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
                 bad |= ISV_STATUS_BAD_BLOCK_ID;
             }
         } else {
-            flags |= OPEN | (len % kBT) << 8;
+            flags |= OPEN | open[lo] << 8;
         }
         my_visit = Visit{lo, group, flags, 0};
     };
@@ -514,7 +556,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
     __syncwarp();
 
     // ---- consumer
-    State<D, NT, BF16> st;
+    State<D, NT, BF16, E4M3> st;
     const uint16_t *q0 = p.q;
     uint32_t phases = 0;
     int slot = 0;
@@ -538,7 +580,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
             }
             if (!lost) {
                 phases ^= 1u << slot;
-                st.template visit<E4M3>(ring + (size_t)(warp * ST + slot) * UNIT, lane);
+                st.visit(ring + (size_t)(warp * ST + slot) * UNIT, lane);
             }
         } else if (t.flags & OPEN) {
             const uint16_t *k = reinterpret_cast<const uint16_t *>(p.c.tails) + ((size_t)t.seq * 2 * p.c.Hkv + t.group / p.P) * kBT * D;
@@ -608,7 +650,6 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
     }
     __syncthreads();
     if (n_runs == 0) return;
-    const int cta_beg = (int)(total * blockIdx.x / ctas), cta_end = (int)(total * (blockIdx.x + 1) / ctas);
     constexpr int MT = D / 16, PAIRS = D / 2;
     const int units = p.GT * PAIRS;            // unit (h, mt, g): output dims g * D / 8 + 2 mt, + 1 of head h
     auto item_span = [&](int item, int &b, int &e) {
@@ -626,8 +667,10 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
         const int r0 = run_first[run], r1 = run_first[run + 1], item = run_item[run];
         const int place = (((h >> 3) * 2 + (h & 1)) * MT + mt) * 32 + ((h & 7) >> 1) * 8 + g;
         float m = kNone, l = 0.f;
+#pragma unroll 4
         for (int r = r0; r < r1; ++r) m = fmaxf(m, rec_ml[list[r] >> 1][list[r] & 1][h].x);
         float2 o = make_float2(0.f, 0.f);
+#pragma unroll 4
         for (int r = r0; r < r1; ++r) {
             const int w = list[r] >> 1, which = list[r] & 1;
             const float2 ml = rec_ml[w][which][h];
@@ -648,7 +691,10 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
     }
     // ---- items that cross CTAs (the first and the last of this one may): the last CTA to arrive merges.  The ticket of an
     // item is that of its first CTA, in which no other item continues into the next.
-    auto owner = [&](int v) { return (int)((((long long)v + 1) * ctas - 1) / total); };   // CTA whose range holds visit v
+    auto owner = [&](int v) {                  // CTA whose range holds visit v
+        const int longer = rest * (share + 1);
+        return v < longer ? v / (share + 1) : rest + (v - longer) / share;
+    };
     auto crosses = [&](int k, int &item, int &c0, int &n, int &b) {
         if (k == 1 && n_runs < 2) return false;
         item = run_item[k == 0 ? 0 : n_runs - 1];
@@ -680,7 +726,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
         if (!last_of[k]) continue;
         int item, c0, n, b;
         crosses(k, item, c0, n, b);
-        const int first_slot = b == (int)(total * c0 / ctas) ? 0 : 1;
+        const int first_slot = b == cta_at(c0) ? 0 : 1;
         auto slot_of = [&](int i) { return (c0 + i) * 2 + (i == 0 ? first_slot : 0); };
         for (int i = tid; i < n * p.GT; i += THREADS)
             ml[i] = __ldcg(reinterpret_cast<const float2 *>(p.part_ml) + slot_of(i / p.GT) * HT + i % p.GT);
@@ -693,7 +739,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
             if (active) {
                 const int h = u / PAIRS;
                 for (int i = 0; i < n; ++i) m = fmaxf(m, ml[i * p.GT + h].x);
-#pragma unroll 8
+#pragma unroll 4
                 for (int i = part; i < n; i += split) {
                     const float2 v = __ldcg(reinterpret_cast<const float2 *>(p.part_o) + (size_t)slot_of(i) * SH::REC + u);
                     const float2 a = ml[i * p.GT + h];
@@ -726,8 +772,17 @@ cudaError_t configure(size_t smem) {
 }
 template <int D, int NT, bool BF16, bool E4M3>
 cudaError_t launch(const AttnParams &p, int grid, size_t smem, cudaStream_t st) {
-    attn_kernel<D, NT, BF16, E4M3><<<grid, Shape<D, NT>::NW * 32, smem, st>>>(p);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(Shape<D, NT>::NW * 32);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;   // see the kernel's griddepcontrol pair
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, attn_kernel<D, NT, BF16, E4M3>, p);
 }
 
 // Calls f with the template arguments of a case.
@@ -770,7 +825,7 @@ int attn_slots(int grid) { return 2 * grid; }
 size_t attn_smem(int D, int GT, int max_seqs) {
     const size_t unit = unit_bytes(D), nw = attn_warps(GT), st = kRingBytes / (nw * unit);
     const size_t record = (size_t)attn_head_rows(GT) * D * 4;
-    return nw * (st * (unit + sizeof(Visit) + 8) + record) + 4 * ((size_t)max_seqs + 1);
+    return nw * (st * (unit + sizeof(Visit) + 8) + record) + 4 * ((size_t)max_seqs + 1) + max_seqs;
 }
 cudaError_t attn_configure(int D, int GT, bool bf16, bool e4m3, size_t smem) { return pick(D, GT, bf16, e4m3, Configure{smem}); }
 cudaError_t launch_attn(const AttnParams &p, int D, bool bf16, bool e4m3, int grid, size_t smem, cudaStream_t st) {
