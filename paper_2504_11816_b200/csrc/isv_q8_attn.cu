@@ -57,6 +57,13 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
+// (x & mask) ^ flip in one instruction (two immediate operands would make it two)
+__device__ __forceinline__ uint32_t mask_flip(uint32_t x, uint32_t mask, uint32_t flip) {
+    uint32_t y;
+    asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(y) : "r"(x), "r"(mask), "r"(flip));
+    return y;
+}
+
 template <bool BF16>
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     if (BF16)
@@ -96,8 +103,8 @@ template <bool E4M3>
 __device__ __forceinline__ void widen_k(uint32_t w, uint32_t &lo, uint32_t &hi) {
     if (E4M3) widen<true>(w, lo, hi);
     else {
-        lo = (w ^ 0x00800080u) & 0x00ff00ffu;
-        hi = ((w >> 8) ^ 0x00800080u) & 0x00ff00ffu;
+        lo = mask_flip(w, 0x00ff00ffu, 0x00800080u);
+        hi = mask_flip(w >> 8, 0x00ff00ffu, 0x00800080u);
     }
 }
 
@@ -414,6 +421,27 @@ __device__ __forceinline__ void store2(const AttnParams &p, size_t at, float x, 
     if (p.out) *reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(p.out) + at) = pack2<BF16>(x, y);
 }
 
+// The first n (at most 4) of some records, each (m, l) and two output values, into a running result.
+__device__ __forceinline__ void merge4(const float2 (&ml)[4], const float2 (&v)[4], int n, float &m, float &l, float2 &o) {
+    float top = m;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = i < n ? fmaxf(top, ml[i].x) : top;
+    const float f = ex2(m - top);
+    l *= f;
+    o.x *= f;
+    o.y *= f;
+    m = top;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float w = ex2(ml[i].x - top);
+        if (i < n) {   // and not where w is 0: a NaN stays one
+            l += w * ml[i].y;
+            o.x += w * v[i].x;
+            o.y += w * v[i].y;
+        }
+    }
+}
+
 // A visit as the producing lane writes it down for the whole warp.
 struct Visit {
     int32_t seq, group;        // sequence, head group
@@ -552,8 +580,6 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
             copy_in(s32(ring + (size_t)(warp * ST + slot) * UNIT), reinterpret_cast<const void *>(src), UNIT, s32(&bars[warp * ST + slot]));
         ++next;
     };
-    for (int i = 0; i < ST; ++i) produce(i);
-    __syncwarp();
 
     // ---- consumer
     State<D, NT, BF16, E4M3> st;
@@ -561,8 +587,11 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
     uint32_t phases = 0;
     int slot = 0;
     bool whole = false;
-    for (int v = beg; v < end; ++v) {
-        const Visit t = visits[warp * ST + slot];
+    // the first ST turns only fill the ring
+#pragma unroll 1
+    for (int v = beg - ST; v < end; ++v) {
+        Visit t{};
+        if (v >= beg) t = visits[warp * ST + slot];
         if (t.flags & FIRST) {
             q0 = p.q + ((size_t)t.seq * p.Hq + (size_t)t.group * p.GT) * D;
             st.start(q0, p.GT, p.scale_log2, lane);
@@ -667,18 +696,16 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
         const int r0 = run_first[run], r1 = run_first[run + 1], item = run_item[run];
         const int place = (((h >> 3) * 2 + (h & 1)) * MT + mt) * 32 + ((h & 7) >> 1) * 8 + g;
         float m = kNone, l = 0.f;
-#pragma unroll 4
-        for (int r = r0; r < r1; ++r) m = fmaxf(m, rec_ml[list[r] >> 1][list[r] & 1][h].x);
         float2 o = make_float2(0.f, 0.f);
-#pragma unroll 4
-        for (int r = r0; r < r1; ++r) {
-            const int w = list[r] >> 1, which = list[r] & 1;
-            const float2 ml = rec_ml[w][which][h];
-            const float2 v = (which ? reinterpret_cast<const float2 *>(ring + (size_t)w * ST * UNIT) : early + w * SH::REC)[place];
-            const float f = ex2(ml.x - m);
-            l += f * ml.y;
-            o.x += f * v.x;
-            o.y += f * v.y;
+        for (int r = r0; r < r1; r += 4) {
+            float2 ml[4], v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int rec = list[min(r + i, r1 - 1)], w = rec >> 1;
+                ml[i] = rec_ml[w][rec & 1][h];
+                v[i] = (rec & 1 ? reinterpret_cast<const float2 *>(ring + (size_t)w * ST * UNIT) : early + w * SH::REC)[place];
+            }
+            merge4(ml, v, r1 - r, m, l, o);
         }
         int b, e;
         item_span(item, b, e);
@@ -718,47 +745,42 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
         last_of[warp] = last;
     }
     __syncthreads();
-    float2 *ml = reinterpret_cast<float2 *>(ring);                 // [n][GT], then the sums of the parts of a unit's records
-    float2 *sums = ml + gridDim.x * HT;                            // [THREADS]
-    float *sums_l = reinterpret_cast<float *>(sums + THREADS);     // [THREADS]
+    float4 *sums = reinterpret_cast<float4 *>(ring);               // [THREADS]: m, l, o of a thread's share of a unit's records
     const int split = max(1, THREADS / units);                     // threads that share a unit's records
     for (int k = 0; k < 2; ++k) {
         if (!last_of[k]) continue;
         int item, c0, n, b;
         crosses(k, item, c0, n, b);
         const int first_slot = b == cta_at(c0) ? 0 : 1;
-        auto slot_of = [&](int i) { return (c0 + i) * 2 + (i == 0 ? first_slot : 0); };
-        for (int i = tid; i < n * p.GT; i += THREADS)
-            ml[i] = __ldcg(reinterpret_cast<const float2 *>(p.part_ml) + slot_of(i / p.GT) * HT + i % p.GT);
-        __syncthreads();
         for (int u0 = 0; u0 < units; u0 += THREADS) {
-            const int u = u0 + (split > 1 ? tid % units : tid), part = split > 1 ? tid / units : 0;
+            const int part = split > 1 ? tid / units : 0, u = split > 1 ? tid - part * units : u0 + tid;
             const bool active = u < units && part < split;
             float m = kNone, l = 0.f;
             float2 o = make_float2(0.f, 0.f);
-            if (active) {
-                const int h = u / PAIRS;
-                for (int i = 0; i < n; ++i) m = fmaxf(m, ml[i * p.GT + h].x);
-#pragma unroll 4
-                for (int i = part; i < n; i += split) {
-                    const float2 v = __ldcg(reinterpret_cast<const float2 *>(p.part_o) + (size_t)slot_of(i) * SH::REC + u);
-                    const float2 a = ml[i * p.GT + h];
-                    const float f = ex2(a.x - m);
-                    l += f * a.y;
-                    o.x += f * v.x;
-                    o.y += f * v.y;
-                }
-            }
-            if (split > 1) {
-                sums[tid] = o;
-                sums_l[tid] = l;
-                __syncthreads();
-                if (active && part == 0)
-                    for (int j = 1; j < split; ++j) {
-                        o.x += sums[j * units + u].x;
-                        o.y += sums[j * units + u].y;
-                        l += sums_l[j * units + u];
+            if (active)
+                for (int i = part; i < n; i += 4 * split) {
+                    float2 ml[4], v[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int x = min(i + j * split, n - 1), at = (c0 + x) * 2 + (x == 0 ? first_slot : 0);
+                        ml[j] = __ldcg(reinterpret_cast<const float2 *>(p.part_ml) + at * HT + u / PAIRS);
+                        v[j] = __ldcg(reinterpret_cast<const float2 *>(p.part_o) + (size_t)at * SH::REC + u);
                     }
+                    merge4(ml, v, (n - 1 - i) / split + 1, m, l, o);
+                }
+            if (split > 1) {
+                sums[tid] = make_float4(m, l, o.x, o.y);
+                __syncthreads();
+                if (active && part == 0) {
+                    for (int j = 1; j < split; ++j) {
+                        const float4 x = sums[j * units + u];
+                        const float top = fmaxf(m, x.x), f = ex2(m - top), f2 = ex2(x.x - top);
+                        m = top;
+                        l = l * f + x.y * f2;
+                        o.x = o.x * f + x.z * f2;
+                        o.y = o.y * f + x.w * f2;
+                    }
+                }
             }
             if (active && part == 0) put(item, u, o, l);
         }
