@@ -43,7 +43,6 @@ __device__ __forceinline__ int seq_len(const CacheParams &c, int s, bool &bad) {
 }
 
 // Shape of the attention kernel that serves GT query heads per visit at head_dim D.
-int attn_warps(int GT);
 int attn_head_rows(int GT);                                        // GT rounded up to whole tiles of 8
 int attn_slots(int grid);                                          // partial results of a launch
 size_t attn_smem(int D, int GT, int max_seqs);

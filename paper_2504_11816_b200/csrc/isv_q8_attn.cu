@@ -27,7 +27,6 @@ namespace {
 constexpr float kNone = -1.0e30f;            // reference of a head that has no score yet: differences stay finite
 constexpr uint32_t kSpin = 1u << 22;
 constexpr float kSlack = 8.f;                // scores may exceed the reference by this much (log2) before it moves
-constexpr int kRingBytes = 132 << 10;        // per SM
 constexpr int kMinVisits = 2;                // visits of a warp below which fewer warps of a CTA take part
 
 __device__ __forceinline__ uint32_t s32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -421,23 +420,24 @@ __device__ __forceinline__ void store2(const AttnParams &p, size_t at, float x, 
     if (p.out) *reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(p.out) + at) = pack2<BF16>(x, y);
 }
 
-// The first n (at most 4) of some records, each (m, l) and two output values, into a running result.
-__device__ __forceinline__ void merge4(const float2 (&ml)[4], const float2 (&v)[4], int n, float &m, float &l, float2 &o) {
+// The first n (at most N) of some records, each (m, l) and J pairs of output values, into a running result.
+template <int N, int J>
+__device__ __forceinline__ void merge(const float2 (&ml)[N], const float2 (&v)[N][J], int n, float &m, float &l, float2 (&o)[J]) {
     float top = m;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) top = i < n ? fmaxf(top, ml[i].x) : top;
+    for (int i = 0; i < N; ++i) top = i < n ? fmaxf(top, ml[i].x) : top;
     const float f = ex2(m - top);
-    l *= f;
-    o.x *= f;
-    o.y *= f;
     m = top;
+    l *= f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int j = 0; j < J; ++j) { o[j].x *= f; o[j].y *= f; }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
         const float w = ex2(ml[i].x - top);
         if (i < n) {   // and not where w is 0: a NaN stays one
             l += w * ml[i].y;
-            o.x += w * v[i].x;
-            o.y += w * v[i].y;
+#pragma unroll
+            for (int j = 0; j < J; ++j) { o[j].x += w * v[i][j].x; o[j].y += w * v[i][j].y; }
         }
     }
 }
@@ -450,11 +450,13 @@ struct Visit {
 };
 enum { COPY = 1, OPEN = 2, FIRST = 4, LAST = 8, HEAD = 16, END = 32 };   // FIRST/LAST of the warp's part of an item; HEAD/END of the item itself
 
+// Warps of a CTA: as many as the registers allow without spills (16 x 128 registers at head_dim 128 spilled up to 90 bytes in the
+// loop: 66.9 us instead of 57.4 at 32 sequences x 1088 tokens x 32 heads); ring: 130 to 150 KB in flight per SM.
 template <int D, int NT>
 struct Shape {
-    static constexpr int NW = NT == 1 ? 16 : 8;
+    static constexpr int NW = NT == 2 ? 8 : D == 128 ? 12 : 16;
     static constexpr int UNIT = unit_bytes(D);
-    static constexpr int ST = kRingBytes / (NW * UNIT);
+    static constexpr int ST = (D == 128 && NT == 1 ? 149 << 10 : 132 << 10) / (NW * UNIT);
     static constexpr int HT = 8 * NT;
     static constexpr int REC = HT * D / 2;     // pairs of output values in a record
     static_assert(ST >= 2 && ST <= 8, "ring depth");
@@ -679,41 +681,54 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
     }
     __syncthreads();
     if (n_runs == 0) return;
-    constexpr int MT = D / 16, PAIRS = D / 2;
-    const int units = p.GT * PAIRS;            // unit (h, mt, g): output dims g * D / 8 + 2 mt, + 1 of head h
+    // A warp merges one head of one run: lane i holds the pairs i, i + 32 of the head, in the order (tile, g): output dims
+    // g * D / 8 + 2 tile, + 1.
+    constexpr int MT = D / 16, PAIRS = D / 2, J = (PAIRS + 31) / 32;
     auto item_span = [&](int item, int &b, int &e) {
         const int s = item / G, nb = prefix[s + 1] - prefix[s];
         b = prefix[s] * G + (item - s * G) * nb;
         e = b + nb;
     };
-    auto put = [&](int item, int u, float2 o, float l) {
-        const int h = u / PAIRS, mt = u % PAIRS / 8, g = u % 8;
+    auto put = [&](int item, int h, const float2 (&o)[J], float l) {
         const float f = l == 0.f ? 0.f : 1.f / l;
-        store2<BF16>(p, ((size_t)item * p.GT + h) * D + g * (D / 8) + 2 * mt, o.x * f, o.y * f);   // item * GT + h: the flat query head
+        const size_t at = ((size_t)item * p.GT + h) * D;   // item * GT + h: the flat query head
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int u = lane + 32 * j;
+            if (u < PAIRS) store2<BF16>(p, at + (u % 8) * (D / 8) + 2 * (u / 8), o[j].x * f, o[j].y * f);
+        }
     };
-    for (int x = tid; x < n_runs * units; x += THREADS) {
-        const int run = x / units, u = x - run * units, h = u / PAIRS, mt = u % PAIRS / 8, g = u % 8;
+#pragma unroll 1
+    for (int x = warp; x < n_runs * p.GT; x += NW) {
+        const int run = x / p.GT, h = x - run * p.GT;
         const int r0 = run_first[run], r1 = run_first[run + 1], item = run_item[run];
-        const int place = (((h >> 3) * 2 + (h & 1)) * MT + mt) * 32 + ((h & 7) >> 1) * 8 + g;
+        const int place = ((h >> 3) * 2 + (h & 1)) * MT * 32 + ((h & 7) >> 1) * 8 + lane % 8 + lane / 8 * 32;
         float m = kNone, l = 0.f;
-        float2 o = make_float2(0.f, 0.f);
+        float2 o[J];
+#pragma unroll
+        for (int j = 0; j < J; ++j) o[j] = make_float2(0.f, 0.f);
+#pragma unroll 1
         for (int r = r0; r < r1; r += 4) {
-            float2 ml[4], v[4];
+            float2 ml[4], v[4][J];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int rec = list[min(r + i, r1 - 1)], w = rec >> 1;
+                const float2 *from = rec & 1 ? reinterpret_cast<const float2 *>(ring + (size_t)w * ST * UNIT) : early + w * SH::REC;
                 ml[i] = rec_ml[w][rec & 1][h];
-                v[i] = (rec & 1 ? reinterpret_cast<const float2 *>(ring + (size_t)w * ST * UNIT) : early + w * SH::REC)[place];
+#pragma unroll
+                for (int j = 0; j < J; ++j) v[i][j] = lane + 32 * j < PAIRS ? from[place + 128 * j] : make_float2(0.f, 0.f);
             }
-            merge4(ml, v, r1 - r, m, l, o);
+            merge(ml, v, r1 - r, m, l, o);
         }
         int b, e;
         item_span(item, b, e);
-        if (b >= cta_beg && e <= cta_end) put(item, u, o, l);
+        if (b >= cta_beg && e <= cta_end) put(item, h, o, l);
         else {
             const int slot = blockIdx.x * 2 + (b > cta_beg ? 1 : 0);
-            __stcg(reinterpret_cast<float2 *>(p.part_o) + (size_t)slot * SH::REC + u, o);
-            if (u % PAIRS == 0) __stcg(reinterpret_cast<float2 *>(p.part_ml) + slot * HT + h, make_float2(m, l));
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+                if (lane + 32 * j < PAIRS) __stcg(reinterpret_cast<float2 *>(p.part_o) + (size_t)slot * SH::REC + h * PAIRS + lane + 32 * j, o[j]);
+            if (lane == 0) __stcg(reinterpret_cast<float2 *>(p.part_ml) + slot * HT + h, make_float2(m, l));
         }
     }
     // ---- items that cross CTAs (the first and the last of this one may): the last CTA to arrive merges.  The ticket of an
@@ -745,44 +760,52 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
         last_of[warp] = last;
     }
     __syncthreads();
-    float4 *sums = reinterpret_cast<float4 *>(ring);               // [THREADS]: m, l, o of a thread's share of a unit's records
-    const int split = max(1, THREADS / units);                     // threads that share a unit's records
+    // the warps share a head's records, then the first of them adds up what they found
+    const int parts = max(1, NW / p.GT), part = warp / p.GT;       // GT <= NW, or every warp takes whole heads
+    float2 *sums = reinterpret_cast<float2 *>(ring);               // [NW][J][32], then [NW] (m, l)
+    float2 *sums_ml = sums + NW * J * 32;
     for (int k = 0; k < 2; ++k) {
         if (!last_of[k]) continue;
         int item, c0, n, b;
         crosses(k, item, c0, n, b);
         const int first_slot = b == cta_at(c0) ? 0 : 1;
-        for (int u0 = 0; u0 < units; u0 += THREADS) {
-            const int part = split > 1 ? tid / units : 0, u = split > 1 ? tid - part * units : u0 + tid;
-            const bool active = u < units && part < split;
+#pragma unroll 1
+        for (int h = warp % p.GT; h < p.GT; h += NW) {
             float m = kNone, l = 0.f;
-            float2 o = make_float2(0.f, 0.f);
-            if (active)
-                for (int i = part; i < n; i += 4 * split) {
-                    float2 ml[4], v[4];
+            float2 o[J];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int x = min(i + j * split, n - 1), at = (c0 + x) * 2 + (x == 0 ? first_slot : 0);
-                        ml[j] = __ldcg(reinterpret_cast<const float2 *>(p.part_ml) + at * HT + u / PAIRS);
-                        v[j] = __ldcg(reinterpret_cast<const float2 *>(p.part_o) + (size_t)at * SH::REC + u);
-                    }
-                    merge4(ml, v, (n - 1 - i) / split + 1, m, l, o);
+            for (int j = 0; j < J; ++j) o[j] = make_float2(0.f, 0.f);
+#pragma unroll 1
+            for (int i = part; i < n && part < parts; i += 6 * parts) {
+                float2 ml[6], v[6][J];
+#pragma unroll
+                for (int x = 0; x < 6; ++x) {
+                    const int r = min(i + x * parts, n - 1), at = (c0 + r) * 2 + (r == 0 ? first_slot : 0);
+                    ml[x] = __ldcg(reinterpret_cast<const float2 *>(p.part_ml) + at * HT + h);
+#pragma unroll
+                    for (int j = 0; j < J; ++j)
+                        v[x][j] = lane + 32 * j < PAIRS ? __ldcg(reinterpret_cast<const float2 *>(p.part_o) + (size_t)at * SH::REC + h * PAIRS + lane + 32 * j)
+                                                        : make_float2(0.f, 0.f);
                 }
-            if (split > 1) {
-                sums[tid] = make_float4(m, l, o.x, o.y);
+                merge(ml, v, (n - 1 - i) / parts + 1, m, l, o);
+            }
+            if (parts > 1) {
+#pragma unroll
+                for (int j = 0; j < J; ++j) sums[(warp * J + j) * 32 + lane] = o[j];
+                if (lane == 0) sums_ml[warp] = make_float2(m, l);
                 __syncthreads();
-                if (active && part == 0) {
-                    for (int j = 1; j < split; ++j) {
-                        const float4 x = sums[j * units + u];
-                        const float top = fmaxf(m, x.x), f = ex2(m - top), f2 = ex2(x.x - top);
-                        m = top;
-                        l = l * f + x.y * f2;
-                        o.x = o.x * f + x.z * f2;
-                        o.y = o.y * f + x.w * f2;
-                    }
+                if (part > 0) break;
+#pragma unroll 1
+                for (int y = 1; y < parts; ++y) {
+                    const int w = y * p.GT + h;
+                    float2 ml[1] = {sums_ml[w]}, v[1][J];
+#pragma unroll
+                    for (int j = 0; j < J; ++j) v[0][j] = sums[(w * J + j) * 32 + lane];
+                    merge(ml, v, 1, m, l, o);
                 }
             }
-            if (active && part == 0) put(item, u, o, l);
+            put(item, h, o, l);
+            if (parts > 1) break;
         }
         __syncthreads();
     }
@@ -840,14 +863,17 @@ struct Launch {
 
 }  // namespace
 
-int attn_warps(int GT) { return GT <= 8 ? Shape<128, 1>::NW : Shape<128, 2>::NW; }
 int attn_head_rows(int GT) { return GT <= 8 ? 8 : 16; }
 int attn_slots(int grid) { return 2 * grid; }
 
+template <int D, int NT>
+size_t smem_of(int max_seqs) {
+    using SH = Shape<D, NT>;
+    return SH::NW * (SH::ST * (SH::UNIT + sizeof(Visit) + 8) + SH::REC * 8) + 4 * ((size_t)max_seqs + 1) + max_seqs;
+}
 size_t attn_smem(int D, int GT, int max_seqs) {
-    const size_t unit = unit_bytes(D), nw = attn_warps(GT), st = kRingBytes / (nw * unit);
-    const size_t record = (size_t)attn_head_rows(GT) * D * 4;
-    return nw * (st * (unit + sizeof(Visit) + 8) + record) + 4 * ((size_t)max_seqs + 1) + max_seqs;
+    if (GT <= 8) return D == 64 ? smem_of<64, 1>(max_seqs) : D == 80 ? smem_of<80, 1>(max_seqs) : smem_of<128, 1>(max_seqs);
+    return D == 64 ? smem_of<64, 2>(max_seqs) : D == 80 ? smem_of<80, 2>(max_seqs) : smem_of<128, 2>(max_seqs);
 }
 cudaError_t attn_configure(int D, int GT, bool bf16, bool e4m3, size_t smem) { return pick(D, GT, bf16, e4m3, Configure{smem}); }
 cudaError_t launch_attn(const AttnParams &p, int D, bool bf16, bool e4m3, int grid, size_t smem, cudaStream_t st) {
