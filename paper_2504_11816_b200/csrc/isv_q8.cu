@@ -338,8 +338,9 @@ int isv_q8_create(isv_q8 **out, const isv_q8_desc *desc) {
     if (e == cudaSuccess) e = cudaMemset(h->status, 0, 4);
     if (e == cudaSuccess) e = cudaMalloc((void **)&h->part_o, rows * D * 4);
     if (e == cudaSuccess) e = cudaMalloc((void **)&h->part_ml, rows * 2 * 4);
-    if (e == cudaSuccess) e = cudaMalloc((void **)&h->tickets, (size_t)h->grid * 4);
-    if (e == cudaSuccess) e = cudaMemset(h->tickets, 0, (size_t)h->grid * 4);
+    const size_t tickets = (size_t)h->grid * isv::q8::attn_head_rows(h->GT) * 4;
+    if (e == cudaSuccess) e = cudaMalloc((void **)&h->tickets, tickets);
+    if (e == cudaSuccess) e = cudaMemset(h->tickets, 0, tickets);
     if (e == cudaSuccess) e = cudaDeviceSynchronize();   // the zeros are there before any stream's first call
     if (e != cudaSuccess) {
         cudaGetLastError();

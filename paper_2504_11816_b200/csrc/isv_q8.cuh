@@ -30,7 +30,7 @@ struct AttnParams {
     float *out_f32;
     float *part_o;              // partial results of items that cross CTAs: [slot][values of a visit's heads], two slots a CTA
     float *part_ml;             // [slot][heads of a visit][m, l]
-    int32_t *tickets;           // [grid], zero between launches
+    int32_t *tickets;           // [grid][heads of a visit], zero between launches
     int32_t Hq, P, GT;          // Hq = Hkv * P * GT; a visit serves GT query heads
     float scale_log2;           // log2(e) / sqrt(D)
 };

@@ -13,7 +13,7 @@
 // What bounds it is reading the cache.  All visits of all (sequence, KV head) pairs form one list that is cut into equal ranges,
 // one per warp, whatever the lengths.  A warp streams its visits through a ring of its own (one bulk copy of
 // a unit brings K, V and both scales).  A pair that several warps share leaves partial results that are merged in fixed
-// order, first within the CTA in shared memory, then, for the pairs that cross CTAs, by the CTA that arrives last.
+// order, first within the CTA in shared memory, then, for the pairs that cross CTAs, by the warp that arrives last.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -27,6 +27,7 @@ namespace {
 constexpr float kNone = -1.0e30f;            // reference of a head that has no score yet: differences stay finite
 constexpr uint32_t kSpin = 1u << 22;
 constexpr float kSlack = 8.f;                // scores may exceed the reference by this much (log2) before it moves
+constexpr int kFly = 8;                      // partial results that the last merge has in flight
 constexpr int kMinVisits = 2;                // visits of a warp below which fewer warps of a CTA take part
 
 __device__ __forceinline__ uint32_t s32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -479,7 +480,6 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
     __shared__ float2 rec_ml[NW][2][HT];       // their m and l
     __shared__ int run_item[NW + 1], run_first[NW + 2], n_runs;
     __shared__ int list[2 * NW];               // records in order: 2 * warp + which
-    __shared__ int last_of[2];                 // whether this CTA is the last of its first and its last item
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int G = p.c.Hkv * p.P;               // head groups of a sequence
 
@@ -684,19 +684,9 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
     // A warp merges one head of one run: lane i holds the pairs i, i + 32 of the head, in the order (tile, g): output dims
     // g * D / 8 + 2 tile, + 1.
     constexpr int MT = D / 16, PAIRS = D / 2, J = (PAIRS + 31) / 32;
-    auto item_span = [&](int item, int &b, int &e) {
-        const int s = item / G, nb = prefix[s + 1] - prefix[s];
-        b = prefix[s] * G + (item - s * G) * nb;
-        e = b + nb;
-    };
-    auto put = [&](int item, int h, const float2 (&o)[J], float l) {
-        const float f = l == 0.f ? 0.f : 1.f / l;
-        const size_t at = ((size_t)item * p.GT + h) * D;   // item * GT + h: the flat query head
-#pragma unroll
-        for (int j = 0; j < J; ++j) {
-            const int u = lane + 32 * j;
-            if (u < PAIRS) store2<BF16>(p, at + (u % 8) * (D / 8) + 2 * (u / 8), o[j].x * f, o[j].y * f);
-        }
+    auto cta_of = [&](int v) {                 // CTA whose range holds visit v
+        const int longer = rest * (share + 1);
+        return v < longer ? v / (share + 1) : rest + (v - longer) / share;
     };
 #pragma unroll 1
     for (int x = warp; x < n_runs * p.GT; x += NW) {
@@ -720,94 +710,54 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
             }
             merge(ml, v, r1 - r, m, l, o);
         }
-        int b, e;
-        item_span(item, b, e);
-        if (b >= cta_beg && e <= cta_end) put(item, h, o, l);
-        else {
+        const int s = item / G, nb = prefix[s + 1] - prefix[s], b = prefix[s] * G + (item - s * G) * nb, e = b + nb;
+        // An item that crosses CTAs (the first and the last of a CTA may): its CTAs' results meet in memory, and the warp that
+        // brings a head's last one merges them.  The ticket is that of the item's first CTA, in which no other item
+        // continues into the next.
+        if (b < cta_beg || e > cta_end) {
             const int slot = blockIdx.x * 2 + (b > cta_beg ? 1 : 0);
 #pragma unroll
             for (int j = 0; j < J; ++j)
                 if (lane + 32 * j < PAIRS) __stcg(reinterpret_cast<float2 *>(p.part_o) + (size_t)slot * SH::REC + h * PAIRS + lane + 32 * j, o[j]);
             if (lane == 0) __stcg(reinterpret_cast<float2 *>(p.part_ml) + slot * HT + h, make_float2(m, l));
-        }
-    }
-    // ---- items that cross CTAs (the first and the last of this one may): the last CTA to arrive merges.  The ticket of an
-    // item is that of its first CTA, in which no other item continues into the next.
-    auto owner = [&](int v) {                  // CTA whose range holds visit v
-        const int longer = rest * (share + 1);
-        return v < longer ? v / (share + 1) : rest + (v - longer) / share;
-    };
-    auto crosses = [&](int k, int &item, int &c0, int &n, int &b) {
-        if (k == 1 && n_runs < 2) return false;
-        item = run_item[k == 0 ? 0 : n_runs - 1];
-        int e;
-        item_span(item, b, e);
-        if (b >= cta_beg && e <= cta_end) return false;
-        c0 = owner(b);
-        n = owner(e - 1) - c0 + 1;
-        return true;
-    };
-    __threadfence();
-    __syncthreads();
-    if (lane == 0 && warp < 2) {
-        int item, c0, n, b;
-        bool last = false;
-        if (crosses(warp, item, c0, n, b)) {
-            last = atomicAdd(p.tickets + c0, 1) == n - 1;
-            if (last) p.tickets[c0] = 0;
             __threadfence();
-        }
-        last_of[warp] = last;
-    }
-    __syncthreads();
-    // the warps share a head's records, then the first of them adds up what they found
-    const int parts = max(1, NW / p.GT), part = warp / p.GT;       // GT <= NW, or every warp takes whole heads
-    float2 *sums = reinterpret_cast<float2 *>(ring);               // [NW][J][32], then [NW] (m, l)
-    float2 *sums_ml = sums + NW * J * 32;
-    for (int k = 0; k < 2; ++k) {
-        if (!last_of[k]) continue;
-        int item, c0, n, b;
-        crosses(k, item, c0, n, b);
-        const int first_slot = b == cta_at(c0) ? 0 : 1;
-#pragma unroll 1
-        for (int h = warp % p.GT; h < p.GT; h += NW) {
-            float m = kNone, l = 0.f;
-            float2 o[J];
+            __syncwarp();
+            const int c0 = cta_of(b), n = cta_of(e - 1) - c0 + 1;
+            int *ticket = p.tickets + c0 * HT + h;
+            int last = 0;
+            if (lane == 0) {
+                last = atomicAdd(ticket, 1) == n - 1;
+                if (last) *ticket = 0;
+                __threadfence();
+            }
+            if (!__shfl_sync(~0u, last, 0)) continue;
+            const int first_slot = b == cta_at(c0) ? 0 : 1;
+            m = kNone;
+            l = 0.f;
 #pragma unroll
             for (int j = 0; j < J; ++j) o[j] = make_float2(0.f, 0.f);
 #pragma unroll 1
-            for (int i = part; i < n && part < parts; i += 6 * parts) {
-                float2 ml[6], v[6][J];
+            for (int i = 0; i < n; i += kFly) {
+                float2 ml[kFly], v[kFly][J];
 #pragma unroll
-                for (int x = 0; x < 6; ++x) {
-                    const int r = min(i + x * parts, n - 1), at = (c0 + r) * 2 + (r == 0 ? first_slot : 0);
-                    ml[x] = __ldcg(reinterpret_cast<const float2 *>(p.part_ml) + at * HT + h);
+                for (int y = 0; y < kFly; ++y) {
+                    const int z = min(i + y, n - 1), at = (c0 + z) * 2 + (z == 0 ? first_slot : 0);
+                    ml[y] = __ldcg(reinterpret_cast<const float2 *>(p.part_ml) + at * HT + h);
 #pragma unroll
                     for (int j = 0; j < J; ++j)
-                        v[x][j] = lane + 32 * j < PAIRS ? __ldcg(reinterpret_cast<const float2 *>(p.part_o) + (size_t)at * SH::REC + h * PAIRS + lane + 32 * j)
+                        v[y][j] = lane + 32 * j < PAIRS ? __ldcg(reinterpret_cast<const float2 *>(p.part_o) + (size_t)at * SH::REC + h * PAIRS + lane + 32 * j)
                                                         : make_float2(0.f, 0.f);
                 }
-                merge(ml, v, (n - 1 - i) / parts + 1, m, l, o);
+                merge(ml, v, n - i, m, l, o);
             }
-            if (parts > 1) {
-#pragma unroll
-                for (int j = 0; j < J; ++j) sums[(warp * J + j) * 32 + lane] = o[j];
-                if (lane == 0) sums_ml[warp] = make_float2(m, l);
-                __syncthreads();
-                if (part > 0) break;
-#pragma unroll 1
-                for (int y = 1; y < parts; ++y) {
-                    const int w = y * p.GT + h;
-                    float2 ml[1] = {sums_ml[w]}, v[1][J];
-#pragma unroll
-                    for (int j = 0; j < J; ++j) v[0][j] = sums[(w * J + j) * 32 + lane];
-                    merge(ml, v, 1, m, l, o);
-                }
-            }
-            put(item, h, o, l);
-            if (parts > 1) break;
         }
-        __syncthreads();
+        const float f = l == 0.f ? 0.f : 1.f / l;
+        const size_t at = ((size_t)item * p.GT + h) * D;       // item * GT + h: the flat query head
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int u = lane + 32 * j;
+            if (u < PAIRS) store2<BF16>(p, at + (u % 8) * (D / 8) + 2 * (u / 8), o[j].x * f, o[j].y * f);
+        }
     }
 }
 
