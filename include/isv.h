@@ -558,6 +558,9 @@ typedef struct isv_linear4 isv_linear4;
 int isv_linear4_create(isv_linear4 **out, const void *w4_dev, const void *scales_dev, int32_t N, int32_t K,
                        int32_t group, int32_t dtype, int32_t max_M, void *stream);
 int isv_linear4_forward(isv_linear4 *l, const void *x_dev, void *y_dev, float *y_f32_dev, int32_t M, void *stream);
+/* Waits for `stream` and returns ISV_EDEVICE_STATUS (and clears the status) if a bounded wait inside a kernel
+ * of this handle expired since the last query. */
+int isv_linear4_status(isv_linear4 *l, void *stream, uint32_t *status_out);
 int isv_linear4_free(isv_linear4 *l);
 
 /* Text of the calling thread's last error; valid until its next call. */

@@ -48,7 +48,8 @@ EXPORTS = [
     "isv_attn_decode_static", "isv_linear_create", "isv_linear_forward", "isv_linear_status", "isv_linear_free",
     "isv_q8_sizes", "isv_q8_create", "isv_q8_free", "isv_q8_write", "isv_q8_attn", "isv_q8_status",
     "isv_pages_copy", "isv_pages_fork", "isv_pages_resize", "isv_pages_compact",
-    "isv_linear4_create", "isv_linear4_forward", "isv_linear4_free",
+    "isv_linear4_create", "isv_linear4_forward", "isv_linear4_status",
+    "isv_linear4_free",
     "isv_last_error",
 ]
 
@@ -174,6 +175,7 @@ def lib():
     L.isv_pages_compact.argtypes = [vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, i32, vp, vp, vp]
     L.isv_linear4_create.argtypes = [P(vp), vp, vp, i32, i32, i32, i32, i32, vp]
     L.isv_linear4_forward.argtypes = [vp, vp, vp, vp, i32, vp]
+    L.isv_linear4_status.argtypes = [vp, vp, P(ctypes.c_uint32)]
     L.isv_linear4_free.argtypes = [vp]
     L.isv_last_error.argtypes = []
     L.isv_last_error.restype = ctypes.c_char_p
@@ -464,6 +466,12 @@ def isv_linear4_create(w4, scales, N: int, K: int, group: int, dtype: int, max_M
 
 def isv_linear4_forward(l: int, x, y, y_f32, M: int, stream: int = 0):
     _check(lib().isv_linear4_forward(l, _ptr(x), _ptr(y), _ptr(y_f32), M, stream or None))
+
+
+def isv_linear4_status(l: int, stream: int = 0) -> int:
+    st = ctypes.c_uint32(0)
+    _check(lib().isv_linear4_status(l, stream or None, ctypes.byref(st)))
+    return st.value
 
 
 def isv_linear4_free(l: int):

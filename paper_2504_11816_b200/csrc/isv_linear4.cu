@@ -6,10 +6,11 @@
 // in shared memory, i.e. a store and a load more per weight).  Nibbles become numbers by placing them in the mantissa of
 // 1024 (fp16) or 128 (bf16) and subtracting: exact, as are the products; sums are fp32 and a group's sum is scaled once.
 //
-// isv_linear4_create lays the weights out in operand order: blocks of 32 rows, per block all of K in chunks of 32, per
-// chunk 16 bytes for each lane of a warp, so a warp's loads are 512 contiguous bytes and need no shared memory.  A CTA
-// takes one block of rows and its warps share K in steps of 128; where there are few blocks a cluster of CTAs shares a block's K
-// and adds up through distributed shared memory.  The order of all sums is fixed.
+// isv_linear4_create lays the weights out in operand order: blocks of 32 rows, per block all of K in steps of 128 (padded with
+// zeros), per step 64 bytes for each lane of a warp and behind them the step's scales: one bulk copy of contiguous memory.
+// A warp streams its steps through a ring of its own in shared memory, so that the bytes in flight do not cost
+// registers.  The warps of a CTA share a row block's K; where there are few blocks a cluster of CTAs does, and adds
+// up through distributed shared memory.  The order of all sums is fixed.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -58,53 +59,73 @@ constexpr int kChunk = 32;     // k of a chunk: two steps of the matrix instruct
 constexpr int kStep = 128;     // k of a warp's step: four chunks
 constexpr int kWarps = 8;
 constexpr int kMaxCluster = 8;
+constexpr uint32_t kSpin = 1u << 22;
+
+__host__ __device__ constexpr int step_bytes(int group) { return kRows * kStep / 2 + kRows * (kStep / group) * 2; }
 
 struct Linear4Params {
-    const uint4 *w;            // [blocks][chunks][32 lanes]
-    const uint2 *scales;       // [blocks][K / group][8]: rows g, g + 8, g + 16, g + 24
+    const uint8_t *w;          // [blocks][steps][step_bytes]: weights [4 chunks][32 lanes][16], scales [groups][8][4] (rows g, g + 8, ..)
     const uint16_t *x;
     uint16_t *y;
     float *y_f32;
-    int32_t M, N, K;
+    uint32_t *status;
+    int32_t M, N, K, blocks;
 };
 
 struct PackParams {
     const uint8_t *w;          // [N][K / 2]
     const uint16_t *s;         // [N][K / group]
-    uint32_t *w_out;
-    uint16_t *s_out;
-    int32_t N, K, group, blocks;
+    uint8_t *out;
+    int32_t N, K, group, blocks, steps;
 };
 
 // Word i of a lane (4 g + c) in a chunk: row tile i / 2, k-step i % 2.  Its nibble 4 e + r belongs to operand register r:
-// row g + 8 * (r % 2) of the tile, k = 8 c + 4 (i % 2) + 2 (r / 2) + e of the chunk.  Rows from N on are zeros.
+// row g + 8 * (r % 2) of the tile, k = 8 c + 4 (i % 2) + 2 (r / 2) + e of the chunk.  Rows from N and k from K on are zeros.
 __global__ void pack_kernel(PackParams p) {
-    const long long words = (long long)p.blocks * (p.K / kChunk) * 128, scales = (long long)p.blocks * kRows * (p.K / p.group);
-    const long long stride = (long long)gridDim.x * blockDim.x, at = (long long)blockIdx.x * blockDim.x + threadIdx.x;
-    for (long long id = at; id < words; id += stride) {
-        const int i = (int)(id & 3), lane = (int)(id >> 2) & 31, g = lane >> 2, c = lane & 3;
-        const int chunk = (int)((id >> 7) % (p.K / kChunk));
-        const int block = (int)((id >> 7) / (p.K / kChunk));
-        uint32_t w = 0;
-        for (int n = 0; n < 8; ++n) {
-            const int r = n & 3, e = n >> 2;
-            const long long row = (long long)block * kRows + (i >> 1) * 16 + g + 8 * (r & 1);
-            const int k = chunk * kChunk + 8 * c + 4 * (i & 1) + 2 * (r >> 1) + e;
-            uint32_t u = 8;
-            if (row < p.N) {
-                const uint8_t b = p.w[row * (p.K / 2) + k / 2];
-                u = k & 1 ? b >> 4 : b & 15;
+    const int words = kRows * kStep / 8, halves = kRows * (kStep / p.group), bytes = step_bytes(p.group);
+    for (long long id = blockIdx.x; id < (long long)p.blocks * p.steps; id += gridDim.x) {
+        const int step = (int)(id % p.steps);
+        const long long row0 = id / p.steps * kRows;
+        uint8_t *out = p.out + (size_t)id * bytes;
+        for (int t = threadIdx.x; t < words; t += blockDim.x) {
+            const int i = t & 3, lane = (t >> 2) & 31, g = lane >> 2, c = lane & 3, chunk = t >> 7;
+            uint32_t w = 0;
+            for (int n = 0; n < 8; ++n) {
+                const int r = n & 3, e = n >> 2;
+                const long long row = row0 + (i >> 1) * 16 + g + 8 * (r & 1);
+                const int k = step * kStep + chunk * kChunk + 8 * c + 4 * (i & 1) + 2 * (r >> 1) + e;
+                uint32_t u = 8;
+                if (row < p.N && k < p.K) {
+                    const uint8_t b = p.w[row * (p.K / 2) + k / 2];
+                    u = k & 1 ? b >> 4 : b & 15;
+                }
+                w |= u << (4 * n);
             }
-            w |= u << (4 * n);
+            reinterpret_cast<uint32_t *>(out)[t] = w;
         }
-        p.w_out[id] = w;
+        for (int t = threadIdx.x; t < halves; t += blockDim.x) {
+            const int i = t & 3, g = (t >> 2) & 7, group = step * (kStep / p.group) + (t >> 5);
+            const long long row = row0 + g + 8 * i;
+            reinterpret_cast<uint16_t *>(out + kRows * kStep / 2)[t] = row < p.N && group < p.K / p.group ? p.s[row * (p.K / p.group) + group] : 0;
+        }
     }
-    for (long long id = at; id < scales; id += stride) {   // [block][group][g][4]
-        const int i = (int)(id & 3), g = (int)(id >> 2) & 7;
-        const int group = (int)((id >> 5) % (p.K / p.group));
-        const long long row = (id >> 5) / (p.K / p.group) * kRows + g + 8 * i;
-        p.s_out[id] = row < p.N ? p.s[row * (p.K / p.group) + group] : 0;
+}
+
+__device__ __forceinline__ uint32_t s32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) {
+    for (uint32_t i = 0; i < kSpin; ++i) {
+        uint32_t ok;
+        asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}\n"
+                     : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+        if (ok) return true;
+        if (i > 256) __nanosleep(64);
     }
+    return false;
+}
+__device__ __forceinline__ void copy_in(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
 template <bool BF16>
@@ -122,6 +143,13 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
             : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// (x & mask) | bits in one instruction (two immediate operands would make it two)
+__device__ __forceinline__ uint32_t mask_or(uint32_t x, uint32_t mask, uint32_t bits) {
+    uint32_t y;
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(y) : "r"(x), "r"(mask), "r"(bits));
+    return y;
+}
+
 // Eight nibbles u -> four pairs of u - 8.
 template <bool BF16>
 __device__ __forceinline__ void widen(uint32_t w, uint32_t (&a)[4]) {
@@ -129,7 +157,7 @@ __device__ __forceinline__ void widen(uint32_t w, uint32_t (&a)[4]) {
         const __nv_bfloat162 base = __floats2bfloat162_rn(136.f, 136.f);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            uint32_t v = ((w >> (4 * r)) & 0x000f000fu) | 0x43004300u;          // 128 + u
+            uint32_t v = mask_or(w >> (4 * r), 0x000f000fu, 0x43004300u);       // 128 + u
             const __nv_bfloat162 d = __hsub2(*reinterpret_cast<__nv_bfloat162 *>(&v), base);
             a[r] = *reinterpret_cast<const uint32_t *>(&d);
         }
@@ -139,7 +167,7 @@ __device__ __forceinline__ void widen(uint32_t w, uint32_t (&a)[4]) {
 #pragma unroll
         for (int r = 0; r < 4; r += 2) {
             const uint32_t v = w >> (4 * r);
-            uint32_t even = (v & 0x000f000fu) | 0x64006400u, odd = (v & 0x00f000f0u) | 0x64006400u;   // 1024 + u, 1024 + 16 u
+            uint32_t even = mask_or(v, 0x000f000fu, 0x64006400u), odd = mask_or(v, 0x00f000f0u, 0x64006400u);   // 1024 + u, 1024 + 16 u
             const __half2 x = __hsub2(*reinterpret_cast<__half2 *>(&even), base);
             const __half2 y = __hfma2(*reinterpret_cast<__half2 *>(&odd), part, base16);
             a[r] = *reinterpret_cast<const uint32_t *>(&x);
@@ -148,137 +176,193 @@ __device__ __forceinline__ void widen(uint32_t w, uint32_t (&a)[4]) {
     }
 }
 
-// NT tiles of 8 tokens; blockIdx.y counts passes of 8 * NT tokens.
-template <int NT, int GROUP, bool BF16>
-__global__ void __launch_bounds__(kWarps * 32) linear4_kernel(const __grid_constant__ Linear4Params p) {
-    constexpr int CHUNKS = kStep / kChunk, PER = GROUP / kChunk;       // chunks of a step, of a group
-    constexpr int COLS = 8 * NT, PITCH = kRows + 1;
-    __shared__ float sums[kWarps][COLS][PITCH];
+template <int NT, int RW>
+struct Shape {
+    static constexpr int COLS = 8 * NT, KW = kWarps / RW, TILE = kRows * RW, PITCH = TILE + 1;
+    static constexpr int BUF = NT == 4 ? 1 : 2;                        // two buffers of sums: one barrier a tile
+    static constexpr int SUMS = KW * COLS * PITCH;
+    // what registers and shared memory allow: CTAs of an SM, and steps that a warp has in flight (about 150 KB an SM)
+    static constexpr int RESIDENT = NT == 1 ? 3 : NT == 2 ? 2 : 1, RING = NT == 1 ? 3 : NT == 2 ? 4 : 8;
+    static constexpr size_t smem(int group) { return (size_t)kWarps * RING * (step_bytes(group) + 8) + (size_t)BUF * SUMS * 4; }
+};
+
+// NT tiles of 8 tokens, RW blocks of rows side by side in a CTA (its other warps share K); blockIdx.y counts passes of 8 * NT
+// tokens.  CTAs (clusters) walk the row tiles, and a warp's ring goes on across the border between two of them.
+template <int NT, int RW, int GROUP, bool BF16>
+__global__ void __launch_bounds__(kWarps * 32, Shape<NT, RW>::RESIDENT) linear4_kernel(const __grid_constant__ Linear4Params p) {
+    using SH = Shape<NT, RW>;
+    constexpr int CHUNKS = kStep / kChunk, GROUPS = kStep / GROUP, PER = GROUP / kChunk;
+    constexpr int COLS = SH::COLS, KW = SH::KW, TILE = SH::TILE, PITCH = SH::PITCH, BUF = SH::BUF, BYTES = step_bytes(GROUP);
+    constexpr bool AHEAD = NT < 4;                                     // x of the next step in registers
+    extern __shared__ __align__(128) uint8_t smem[];
+    uint8_t *ring = smem;                                              // [kWarps][RING][BYTES]
+    uint64_t *bars = reinterpret_cast<uint64_t *>(ring + kWarps * SH::RING * BYTES);
+    float *sums = reinterpret_cast<float *>(bars + kWarps * SH::RING);    // [BUF][KW][COLS][PITCH]
     cg::cluster_group cluster = cg::this_cluster();
     const int cs = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
-    const int block = blockIdx.x / cs, m0 = blockIdx.y * COLS;
-    const int chunks = p.K / kChunk, groups = p.K / GROUP;
-    const int steps = (p.K + kStep - 1) / kStep;
-    const int end = (int)((long long)steps * (rank + 1) / cs);
-    const uint4 *w = p.w + (size_t)block * chunks * 32 + lane;
-    const uint2 *scales = p.scales + (size_t)block * groups * 8 + g;
+    const int rw = warp % RW, kw = warp / RW, m0 = blockIdx.y * COLS;
+    const int steps = (p.K + kStep - 1) / kStep, tiles = (p.blocks + RW - 1) / RW, stride = gridDim.x / cs;
+    const int first = steps * rank / cs + kw, end = steps * (rank + 1) / cs;
 
-    uint4 next[CHUNKS];
-    auto fetch = [&](int step) {
-#pragma unroll
-        for (int i = 0; i < CHUNKS; ++i) {
-            const int chunk = step * CHUNKS + i;
-            next[i] = step < end && chunk < chunks ? __ldg(w + (size_t)chunk * 32) : make_uint4(0x88888888u, 0x88888888u, 0x88888888u, 0x88888888u);
-        }
+    uint8_t *mine = ring + warp * SH::RING * BYTES;
+    const uint32_t bar0 = s32(bars + warp * SH::RING);
+    if (lane < SH::RING) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar0 + 8 * lane) : "memory");
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    int next_tile = blockIdx.x / cs, next_step = first;
+    auto fetch = [&](int slot) {
+        if (first >= end || next_tile * RW + rw >= p.blocks) return;
+        if (lane == 0) copy_in(s32(mine + slot * BYTES), p.w + ((size_t)(next_tile * RW + rw) * steps + next_step) * BYTES, BYTES, bar0 + 8 * slot);
+        next_step += KW;
+        if (next_step >= end) { next_step = first; next_tile += stride; }
     };
-    int step = (int)((long long)steps * rank / cs) + warp;
-    fetch(step);               // the weights do not change: they are on their way before the predecessor has ended
+#pragma unroll 1
+    for (int i = 0; i < SH::RING; ++i) fetch(i);   // the weights do not change: they are on their way before the predecessor has ended
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    float total[2][NT][4];
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) total[t][nt][i] = 0.f;
-    for (; step < end; step += kWarps) {
-        uint4 now[CHUNKS];
-#pragma unroll
-        for (int i = 0; i < CHUNKS; ++i) now[i] = next[i];
-        uint4 x[CHUNKS][NT];
+    uint4 x[CHUNKS][NT];
+    auto load_x = [&](int step) {
 #pragma unroll
         for (int i = 0; i < CHUNKS; ++i)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                const int m = m0 + nt * 8 + g, chunk = step * CHUNKS + i;
-                x[i][nt] = m < p.M && chunk < chunks ? *reinterpret_cast<const uint4 *>(p.x + (size_t)m * p.K + chunk * kChunk + 8 * c)
-                                                     : make_uint4(0, 0, 0, 0);
+                const int m = m0 + nt * 8 + g, k = step * kStep + i * kChunk;
+                x[i][nt] = m < p.M && k < p.K ? *reinterpret_cast<const uint4 *>(p.x + (size_t)m * p.K + k + 8 * c) : make_uint4(0, 0, 0, 0);
             }
-        uint2 sc[CHUNKS / PER];
+    };
+    if (AHEAD) load_x(first);
+    int slot = 0;
+    uint32_t phase = 0;
+    bool lost = false;
+    int turn = 0;
+    for (int tile = blockIdx.x / cs; tile < tiles; tile += stride, turn ^= BUF - 1) {
+        float total[2][NT][4];
 #pragma unroll
-        for (int i = 0; i < CHUNKS / PER; ++i) {
-            const int group = step * (CHUNKS / PER) + i;
-            sc[i] = group < groups ? __ldg(scales + (size_t)group * 8) : make_uint2(0, 0);
-        }
-        fetch(step + kWarps);
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int i0 = 0; i0 < CHUNKS / PER; ++i0) {
-            float part[2][NT][4];
+            for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+                for (int i = 0; i < 4; ++i) total[t][nt][i] = 0.f;
+#pragma unroll 1
+        for (int step = first; step < end && tile * RW + rw < p.blocks; step += KW) {
+            uint4 now[CHUNKS][NT];
+            if (!AHEAD) load_x(step);
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+            for (int i = 0; i < CHUNKS; ++i)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) part[t][nt][i] = 0.f;
+                for (int nt = 0; nt < NT; ++nt) now[i][nt] = x[i][nt];
+            if (AHEAD) load_x(step + KW < end ? step + KW : first);
+            if (!wait(bar0 + 8 * slot, phase)) lost = true;
+            const uint8_t *in = mine + slot * BYTES;
 #pragma unroll
-            for (int i = i0 * PER; i < (i0 + 1) * PER; ++i) {
-                const uint32_t words[4] = {now[i].x, now[i].y, now[i].z, now[i].w};
+            for (int i0 = 0; i0 < GROUPS; ++i0) {
+                float part[2][NT][4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    uint32_t a[4];
-                    widen<BF16>(words[j], a);
+                for (int t = 0; t < 2; ++t)
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
-                        mma<BF16>(part[j >> 1][nt], a, j & 1 ? x[i][nt].z : x[i][nt].x, j & 1 ? x[i][nt].w : x[i][nt].y);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) part[t][nt][i] = 0.f;
+#pragma unroll
+                for (int i = i0 * PER; i < (i0 + 1) * PER; ++i) {
+                    const uint4 w = *reinterpret_cast<const uint4 *>(in + 512 * i + 16 * lane);
+                    const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint32_t a[4];
+                        widen<BF16>(words[j], a);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+                            mma<BF16>(part[j >> 1][nt], a, j & 1 ? now[i][nt].z : now[i][nt].x, j & 1 ? now[i][nt].w : now[i][nt].y);
+                    }
                 }
+                const uint2 sc = *reinterpret_cast<const uint2 *>(in + kRows * kStep / 2 + 64 * i0 + 8 * g);
+                const float s[4] = {to_f32<BF16>(sc.x & 0xffffu), to_f32<BF16>(sc.x >> 16), to_f32<BF16>(sc.y & 0xffffu), to_f32<BF16>(sc.y >> 16)};
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) total[t][nt][i] += part[t][nt][i] * s[2 * t + (i >> 1)];
             }
-            const float s[4] = {to_f32<BF16>(sc[i0].x & 0xffffu), to_f32<BF16>(sc[i0].x >> 16), to_f32<BF16>(sc[i0].y & 0xffffu),
-                                to_f32<BF16>(sc[i0].y >> 16)};
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) total[t][nt][i] += part[t][nt][i] * s[2 * t + (i >> 1)];
+            __syncwarp();
+            fetch(slot);
+            if (++slot == SH::RING) { slot = 0; phase ^= 1u; }
         }
+        float *mine_sums = sums + turn * SH::SUMS;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    mine_sums[(kw * COLS + nt * 8 + 2 * c + (i & 1)) * PITCH + rw * kRows + t * 16 + g + 8 * (i >> 1)] = total[t][nt][i];
+        if (cs > 1) cluster.sync(); else __syncthreads();
+        const int cols = min(COLS, p.M - m0);
+        // the CTAs of a cluster share the outputs; each adds the warps of all of them in order
+        for (int o = rank * kWarps * 32 + threadIdx.x; o < cols * TILE; o += cs * kWarps * 32) {
+            const int m = o / TILE, r = o % TILE, n = tile * TILE + r;
+            float v = 0.f;
+            for (int k = 0; k < cs; ++k) {
+                const float *other = mine_sums;
+                if (cs > 1) other = cluster.map_shared_rank(other, k);
+#pragma unroll
+                for (int i = 0; i < KW; ++i) v += other[(i * COLS + m) * PITCH + r];
+            }
+            if (n < p.N) {
+                const size_t at = (size_t)(m0 + m) * p.N + n;
+                if (p.y_f32) p.y_f32[at] = v;
+                if (p.y) p.y[at] = BF16 ? __bfloat16_as_ushort(__float2bfloat16(v)) : __half_as_ushort(__float2half(v));
+            }
+        }
+        if (BUF == 1) { if (cs > 1) cluster.sync(); else __syncthreads(); }
     }
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sums[warp][nt * 8 + 2 * c + (i & 1)][t * 16 + g + 8 * (i >> 1)] = total[t][nt][i];
-    if (cs > 1) cluster.sync(); else __syncthreads();
-    const int cols = min(COLS, p.M - m0);
-    // the CTAs of a cluster share the outputs; each adds the warps of all of them in order
-    for (int o = rank * kWarps * 32 + threadIdx.x; o < cols * kRows; o += cs * kWarps * 32) {
-        const int m = o / kRows, r = o % kRows, n = block * kRows + r;
-        float v = 0.f;
-        for (int k = 0; k < cs; ++k) {
-            const float *other = cs > 1 ? cluster.map_shared_rank(&sums[0][0][0], k) : &sums[0][0][0];
-#pragma unroll
-            for (int i = 0; i < kWarps; ++i) v += other[(i * COLS + m) * PITCH + r];
-        }
-        if (n < p.N) {
-            const size_t at = (size_t)(m0 + m) * p.N + n;
-            if (p.y_f32) p.y_f32[at] = v;
-            if (p.y) p.y[at] = BF16 ? __bfloat16_as_ushort(__float2bfloat16(v)) : __half_as_ushort(__float2half(v));
-        }
-    }
+    if (lost && lane == 0) atomicOr(p.status, ISV_STATUS_WAIT_EXPIRED);
     if (cs > 1) cluster.sync();   // nobody leaves while its sums may be read
 }
 
-template <int NT, int GROUP>
-cudaError_t launch(const Linear4Params &p, bool bf16, const cudaLaunchConfig_t &cfg) {
-    return bf16 ? cudaLaunchKernelEx(&cfg, linear4_kernel<NT, GROUP, true>, p) : cudaLaunchKernelEx(&cfg, linear4_kernel<NT, GROUP, false>, p);
+template <int NT, int RW, int GROUP>
+cudaError_t launch(const Linear4Params &p, bool bf16, cudaLaunchConfig_t cfg) {
+    cfg.dynamicSmemBytes = Shape<NT, RW>::smem(GROUP);
+    return bf16 ? cudaLaunchKernelEx(&cfg, linear4_kernel<NT, RW, GROUP, true>, p)
+                : cudaLaunchKernelEx(&cfg, linear4_kernel<NT, RW, GROUP, false>, p);
 }
-template <int NT>
+template <int NT, int RW, int GROUP>
+cudaError_t configure(bool bf16) {
+    const int smem = (int)Shape<NT, RW>::smem(GROUP);
+    return bf16 ? cudaFuncSetAttribute(linear4_kernel<NT, RW, GROUP, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)
+                : cudaFuncSetAttribute(linear4_kernel<NT, RW, GROUP, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+}
+template <int NT, int RW>
+cudaError_t configure(int group, bool bf16) {
+    return group == 32 ? configure<NT, RW, 32>(bf16) : group == 64 ? configure<NT, RW, 64>(bf16) : configure<NT, RW, 128>(bf16);
+}
+cudaError_t configure(int group, bool bf16) {
+    cudaError_t e = configure<1, 1>(group, bf16);
+    if (e == cudaSuccess) e = configure<2, 1>(group, bf16);
+    if (e == cudaSuccess) e = configure<4, 1>(group, bf16);
+    if (e == cudaSuccess) e = configure<1, 4>(group, bf16);
+    if (e == cudaSuccess) e = configure<2, 4>(group, bf16);
+    if (e == cudaSuccess) e = configure<4, 4>(group, bf16);
+    return e;
+}
+template <int NT, int RW>
 cudaError_t launch(const Linear4Params &p, int group, bool bf16, const cudaLaunchConfig_t &cfg) {
-    if (group == 32) return launch<NT, 32>(p, bf16, cfg);
-    if (group == 64) return launch<NT, 64>(p, bf16, cfg);
-    return launch<NT, 128>(p, bf16, cfg);
+    if (group == 32) return launch<NT, RW, 32>(p, bf16, cfg);
+    if (group == 64) return launch<NT, RW, 64>(p, bf16, cfg);
+    return launch<NT, RW, 128>(p, bf16, cfg);
 }
 
 }  // namespace
 
 struct isv_linear4 {
-    int N = 0, K = 0, group = 0, max_M = 0, device = 0, blocks = 0, cluster = 1;
+    int N = 0, K = 0, group = 0, max_M = 0, device = 0, blocks = 0, sms = 0;
     bool bf16 = false;
-    uint32_t *w = nullptr;
-    uint16_t *scales = nullptr;
+    uint8_t *w = nullptr;
+    uint32_t *status = nullptr;
 };
 
 extern "C" {
@@ -288,7 +372,7 @@ int isv_linear4_free(isv_linear4 *l) {
     OnDevice on(l->device);
     cudaDeviceSynchronize();   // calls may have been made on any stream
     cudaFree(l->w);
-    cudaFree(l->scales);
+    cudaFree(l->status);
     delete l;
     return ISV_OK;
 }
@@ -312,12 +396,14 @@ int isv_linear4_create(isv_linear4 **out, const void *w4_dev, const void *scales
     int sms = 0;
     cudaError_t e = cudaGetDevice(&l->device);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, l->device);
-    // few blocks of rows: several CTAs share the K of one, while each of their warps keeps two steps
-    while (l->cluster < kMaxCluster && l->blocks * l->cluster < 2 * sms && K >= 2 * l->cluster * 2 * kWarps * kStep) l->cluster *= 2;
-    if (e == cudaSuccess) e = cudaMalloc((void **)&l->w, (size_t)l->blocks * kRows * (K / 2));
-    if (e == cudaSuccess) e = cudaMalloc((void **)&l->scales, (size_t)l->blocks * kRows * (K / group) * 2);
+    l->sms = sms;
+    const int steps = (K + kStep - 1) / kStep;
+    if (e == cudaSuccess) e = configure(group, l->bf16);
+    if (e == cudaSuccess) e = cudaMalloc((void **)&l->w, (size_t)l->blocks * steps * step_bytes(group));
+    if (e == cudaSuccess) e = cudaMalloc((void **)&l->status, 4);
+    if (e == cudaSuccess) e = cudaMemsetAsync(l->status, 0, 4, st);
     if (e == cudaSuccess) {
-        const PackParams p = {static_cast<const uint8_t *>(w4_dev), static_cast<const uint16_t *>(scales_dev), l->w, l->scales, N, K, group, l->blocks};
+        const PackParams p = {static_cast<const uint8_t *>(w4_dev), static_cast<const uint16_t *>(scales_dev), l->w, N, K, group, l->blocks, steps};
         pack_kernel<<<8 * sms, 256, 0, st>>>(p);
         e = cudaGetLastError();
     }
@@ -339,28 +425,51 @@ int isv_linear4_forward(isv_linear4 *l, const void *x_dev, void *y_dev, float *y
     if ((reinterpret_cast<uintptr_t>(y_dev) & 1u) || (reinterpret_cast<uintptr_t>(y_f32_dev) & 3u))
         return err(ISV_EINVAL, "outputs must be aligned to their elements");
     Linear4Params p{};
-    p.w = reinterpret_cast<const uint4 *>(l->w); p.scales = reinterpret_cast<const uint2 *>(l->scales); p.x = static_cast<const uint16_t *>(x_dev);
+    p.w = l->w; p.status = l->status; p.x = static_cast<const uint16_t *>(x_dev);
     p.y = static_cast<uint16_t *>(y_dev); p.y_f32 = y_f32_dev;
-    p.M = M; p.N = l->N; p.K = l->K;
+    p.M = M; p.N = l->N; p.K = l->K; p.blocks = l->blocks;
     OnDevice on(l->device);
     if (on.e != cudaSuccess) return err(ISV_ECUDA, "isv_linear4_forward: %s", cudaGetErrorString(on.e));
     const int nt = M <= 8 ? 1 : M <= 16 ? 2 : 4;
+    // From four tokens on x is as much traffic as a block's weights: four blocks then share what a CTA reads of it,
+    // if enough CTAs are left.
+    const int rw = M > 4 && l->blocks >= l->sms / 8 ? 4 : 1;
+    const int tiles = (l->blocks + rw - 1) / rw, steps = (l->K + kStep - 1) / kStep;
+    // few tiles: several CTAs share the K of one, while each of their warps keeps two steps
+    int cluster = 1;
+    while (cluster < kMaxCluster && tiles * cluster < 2 * l->sms && steps >= 2 * cluster * 2 * (kWarps / rw)) cluster *= 2;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(l->blocks * l->cluster), (unsigned)((M + 8 * nt - 1) / (8 * nt)));
+    cfg.gridDim = dim3((unsigned)(std::min(tiles, std::max(1, (nt == 1 ? Shape<1, 1>::RESIDENT : nt == 2 ? Shape<2, 1>::RESIDENT : Shape<4, 1>::RESIDENT) * l->sms / cluster)) * cluster), (unsigned)((M + 8 * nt - 1) / (8 * nt)));
     cfg.blockDim = dim3(kWarps * 32);
     cfg.stream = static_cast<cudaStream_t>(stream);
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;   // see the kernel's griddepcontrol pair
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)l->cluster;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    const cudaError_t e = nt == 1   ? launch<1>(p, l->group, l->bf16, cfg)
-                          : nt == 2 ? launch<2>(p, l->group, l->bf16, cfg)
-                                    : launch<4>(p, l->group, l->bf16, cfg);
+    cudaError_t e;
+    if (rw == 1) e = nt == 1 ? launch<1, 1>(p, l->group, l->bf16, cfg) : nt == 2 ? launch<2, 1>(p, l->group, l->bf16, cfg) : launch<4, 1>(p, l->group, l->bf16, cfg);
+    else e = nt == 1 ? launch<1, 4>(p, l->group, l->bf16, cfg) : nt == 2 ? launch<2, 4>(p, l->group, l->bf16, cfg) : launch<4, 4>(p, l->group, l->bf16, cfg);
     return e == cudaSuccess ? ISV_OK : err(ISV_ECUDA, "isv_linear4_forward: %s", cudaGetErrorString(e));
+}
+
+int isv_linear4_status(isv_linear4 *l, void *stream, uint32_t *status_out) {
+    if (!l || !status_out) return err(ISV_EINVAL, "null argument");
+    OnDevice on(l->device);
+    if (on.e != cudaSuccess) return err(ISV_ECUDA, "isv_linear4_status: %s", cudaGetErrorString(on.e));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    cudaError_t e = cudaMemcpyAsync(status_out, l->status, 4, cudaMemcpyDeviceToHost, st);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    if (e == cudaSuccess && *status_out) {
+        e = cudaMemsetAsync(l->status, 0, 4, st);
+        if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+    }
+    if (e != cudaSuccess) return err(ISV_ECUDA, "isv_linear4_status: %s", cudaGetErrorString(e));
+    if (*status_out) return err(ISV_EDEVICE_STATUS, "the 4-bit linear kernel reported status 0x%x", *status_out);
+    return ISV_OK;
 }
 
 }  // extern "C"

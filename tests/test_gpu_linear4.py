@@ -49,6 +49,7 @@ def test_matches_the_reference(N, K, group, dtype):
             only = torch.zeros_like(y16)
             B.isv_linear4_forward(l, xd, only, None, M)
             assert torch.equal(only, y16)
+            assert B.isv_linear4_status(l) == 0
         finally:
             B.isv_linear4_free(l)
 

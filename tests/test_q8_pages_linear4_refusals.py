@@ -111,4 +111,5 @@ def test_linear4_create(kw, text):
 
 def test_linear4_calls_need_a_handle():
     _refused(B.ISV_EINVAL, "null handle", B.isv_linear4_forward, None, A, A, None, 1)
+    _refused(B.ISV_EINVAL, "null", B.isv_linear4_status, None)
     _refused(B.ISV_EINVAL, "null handle", B.isv_linear4_free, None)
