@@ -30,7 +30,7 @@ constexpr int kCtas = 8;           // CTAs of the cluster (the portable maximum)
 constexpr int kThreads = 1024;
 constexpr int kMaxRows = 4096;
 constexpr int kMaxDevices = 64;
-constexpr int kCopyThreads = 256;
+constexpr int kCopyThreads = 256, kCopyUnroll = 4;
 
 int err(int code, const char *fmt, ...) {
     char buf[512];
@@ -61,10 +61,10 @@ __device__ __forceinline__ int blocks_of(const TableParams &p, int len, uint32_t
     return b;
 }
 
-// What an operation does with row r: `from` is the table row it reads (-1 = none), the first `keep` blocks stay,
-// blocks [lo, hi) get fresh pages, blocks from hi on become ISV_BLOCK_NONE.
+// What an operation does with a row: blocks [0, min(lo, hi)) stay, blocks [lo, hi) get fresh pages, blocks from hi on
+// become ISV_BLOCK_NONE.
 struct Row {
-    int from, keep, lo, hi;
+    int lo, hi;
 };
 
 // Exclusive prefix sums of one value per thread over the CTA; returns the thread's prefix, `total` the sum.
@@ -102,81 +102,82 @@ __global__ void __launch_bounds__(kThreads, 1) table_kernel(TableParams p) {
     uint32_t *fin = bits + p.words;                                     // [slice]: all marks of this CTA's slice
     int *before = reinterpret_cast<int *>(fin + p.slice);               // [slice]: live pages of the slice before the word
     int *need = before + p.slice;                                       // [n_rows + 1]: fresh pages before row r
-    int *first = need + p.n_rows + 1;                                   // FORK [n_in]: first row that continues a parent
+    int *rows_hi = need + p.n_rows + 1;                                 // [n_rows]: Row::hi; FORK: 2 * hi + (hi - lo)
+    int *rows_lo = rows_hi + p.n_rows;                                  // RESIZE [n_rows]: Row::lo
+    int *first = rows_lo;                                               // FORK [n_in]: first row that continues a parent
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = (int)cluster.block_rank(), tid = threadIdx.x;
     uint32_t bad = 0;
 
     for (int i = tid; i < p.words; i += kThreads) bits[i] = 0;
-    if (OP == FORK) {
+    if (OP == FORK)
         for (int i = tid; i < p.n_in; i += kThreads) first[i] = p.n_rows;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    auto parent_of = [&](int r) {
+        const int q = p.other[r];
+        if (q >= 0 && q < p.n_in) return q;
+        if (q != ISV_BLOCK_NONE) bad |= ISV_STATUS_BAD_BLOCK_ID;
+        return -1;
+    };
+    if (OP == FORK) {
         __syncthreads();
         for (int r = tid; r < p.n_rows; r += kThreads) {
-            const int q = p.other[r];
-            if (q >= 0 && q < p.n_in) atomicMin(&first[q], r);
+            const int q = parent_of(r);
+            if (q >= 0) atomicMin(&first[q], r);
+        }
+        __syncthreads();
+    }
+    // every CTA has the whole list of rows
+    for (int r = tid; r < p.n_rows; r += kThreads) {
+        if (OP == FORK) {
+            const int from = parent_of(r), len = from < 0 ? 0 : p.lens[from], hi = blocks_of(p, len, bad);
+            int own = 0;             // 1: the row gets a page of its own for its open block
+            if (hi > 0 && p.open_in_pool && len % kBT && len / kBT < p.max_blocks && first[from] < r) {
+                const int page = p.table[(size_t)from * p.stride + hi - 1];
+                own = page >= 0 && page < p.n_pages;
+            }
+            rows_hi[r] = 2 * hi + own;
+        } else {
+            rows_hi[r] = blocks_of(p, OP == RESIZE ? p.other[r] : p.lens[r], bad);
+            if (OP == RESIZE) rows_lo[r] = blocks_of(p, p.lens[r], bad);
         }
     }
     __syncthreads();
-
-    auto row_of = [&](int r, uint32_t &flags) {
-        Row w;
-        if (OP == FORK) {
-            const int q = p.other[r];
-            w.from = q >= 0 && q < p.n_in ? q : -1;
-            if (w.from < 0 && q != ISV_BLOCK_NONE) flags |= ISV_STATUS_BAD_BLOCK_ID;
-            const int len = w.from < 0 ? 0 : p.lens[w.from];
-            w.hi = blocks_of(p, len, flags);
-            w.lo = w.hi;
-            if (w.hi > 0 && p.open_in_pool && len % kBT && len / kBT < p.max_blocks && first[w.from] < r) {
-                const int page = p.table[(size_t)w.from * p.stride + w.hi - 1];
-                if (page >= 0 && page < p.n_pages) w.lo = w.hi - 1;
-            }
-            w.keep = w.lo;
-        } else {
-            w.from = r;
-            w.lo = blocks_of(p, p.lens[r], flags);
-            w.hi = OP == RESIZE ? blocks_of(p, p.other[r], flags) : w.lo;
-            w.keep = min(w.lo, w.hi);
-        }
-        return w;
+    auto row_of = [&](int r) {
+        const int x = rows_hi[r];
+        return OP == FORK ? Row{x / 2 - (x & 1), x / 2} : OP == RESIZE ? Row{rows_lo[r], x} : Row{x, x};
     };
 
     // ---- marks; FORK also copies the kept entries to the new table
     const int per = kCtas * kThreads / p.row_threads;
     const int at = rank * kThreads + tid;
     for (int r = at / p.row_threads; r < p.n_rows; r += per) {
-        uint32_t flags = 0;
-        const Row w = row_of(r, flags);
-        bad |= flags;
-        for (int j = at % p.row_threads; j < w.keep; j += p.row_threads) {
-            const int id = p.table[(size_t)w.from * p.stride + j];
+        const Row w = row_of(r);
+        const int keep = min(w.lo, w.hi);
+        const int32_t *from = p.table + (size_t)(OP == FORK ? (keep ? p.other[r] : 0) : r) * p.stride;
+#pragma unroll 4
+        for (int j = at % p.row_threads; j < keep; j += p.row_threads) {
+            const int id = from[j];
             if (OP == FORK) p.table_out[(size_t)r * p.stride + j] = id;
             if (id >= 0 && id < p.n_pages) atomicOr(&bits[id >> 5], 1u << (id & 31));
             else if (id != ISV_BLOCK_NONE) bad |= ISV_STATUS_BAD_BLOCK_ID;
         }
     }
-    // ---- fresh pages before each row (every CTA has the whole list)
+    // ---- fresh pages before each row
     int wanted = 0;
     if (OP != COMPACT) {
         const int each = (p.n_rows + kThreads - 1) / kThreads;
         int sum = 0;
-        for (int i = 0; i < each; ++i) {
-            const int r = tid * each + i;
-            if (r < p.n_rows) {
-                uint32_t flags = 0;
-                const Row w = row_of(r, flags);
-                sum += max(0, w.hi - w.lo);
-            }
+        for (int r = tid * each; r < min(tid * each + each, p.n_rows); ++r) {
+            const Row w = row_of(r);
+            sum += max(0, w.hi - w.lo);
         }
         int x = block_scan(sum, warp_sums, wanted);
-        for (int i = 0; i < each; ++i) {
-            const int r = tid * each + i;
-            if (r < p.n_rows) {
-                uint32_t flags = 0;
-                const Row w = row_of(r, flags);
-                need[r] = x;
-                x += max(0, w.hi - w.lo);
-            }
+        for (int r = tid * each; r < min(tid * each + each, p.n_rows); ++r) {
+            const Row w = row_of(r);
+            need[r] = x;
+            x += max(0, w.hi - w.lo);
         }
         if (tid == 0) need[p.n_rows] = wanted;
     }
@@ -226,19 +227,17 @@ __global__ void __launch_bounds__(kThreads, 1) table_kernel(TableParams p) {
                 const int m = (lo + hi) / 2;
                 if (need[m] <= r) lo = m; else hi = m;
             }
-            uint32_t flags = 0;
-            const Row w = row_of(lo, flags);
+            const Row w = row_of(lo);
             p.table_out[(size_t)lo * p.stride + w.lo + (r - need[lo])] = id;
             if (OP == FORK) {
-                p.src[lo] = p.table[(size_t)w.from * p.stride + w.lo];
+                p.src[lo] = p.table[(size_t)p.other[lo] * p.stride + w.lo];
                 p.dst[lo] = id;
             }
         }
         // ---- the rest of the rows
         if (wanted > free_pages) bad |= ISV_STATUS_NO_PAGES;
         for (int r = at / p.row_threads; r < p.n_rows; r += per) {
-            uint32_t flags = 0;
-            const Row w = row_of(r, flags);
+            const Row w = row_of(r);
             const int lacking = w.lo + max(0, free_pages - need[r]);    // first block of the row without a page
             for (int j = w.lo + at % p.row_threads; j < p.max_blocks; j += p.row_threads)
                 if (j >= w.hi || j >= lacking) p.table_out[(size_t)r * p.stride + j] = ISV_BLOCK_NONE;
@@ -246,7 +245,8 @@ __global__ void __launch_bounds__(kThreads, 1) table_kernel(TableParams p) {
                 for (int j = w.hi + at % p.row_threads; j < w.lo; j += p.row_threads)
                     p.table_out[(size_t)r * p.stride + j] = ISV_BLOCK_NONE;
             if (OP == FORK && at % p.row_threads == 0) {
-                p.lens_out[r] = w.from < 0 ? 0 : p.lens[w.from];
+                const int from = parent_of(r);
+                p.lens_out[r] = from < 0 ? 0 : p.lens[from];
                 if (w.hi == w.lo || lacking <= w.lo) p.src[r] = p.dst[r] = ISV_BLOCK_NONE;
             }
         }
@@ -272,11 +272,10 @@ __global__ void __launch_bounds__(kThreads, 1) table_kernel(TableParams p) {
         if (rank == 0 && tid == 0) { p.counts[0] = live; p.counts[1] = moves; }
         cluster.sync();                    // all moves are in place
         for (int r = at / p.row_threads; r < p.n_rows; r += per) {
-            uint32_t flags = 0;
-            const Row w = row_of(r, flags);
+            const int keep = row_of(r).hi;
             for (int j = at % p.row_threads; j < p.max_blocks; j += p.row_threads) {
                 int id = ISV_BLOCK_NONE;
-                if (j < w.keep) {
+                if (j < keep) {
                     id = p.table[(size_t)r * p.stride + j];
                     if (id >= live && id < p.n_pages) id = __ldcg(&p.dst[live_before(id) - below]);
                 }
@@ -295,27 +294,42 @@ struct CopyParams {
     uint32_t *status;
     uint64_t dst_stride, src_stride;       // 16-byte units
     int32_t page;                          // 16-byte units of a page
+    int32_t pieces;                        // of a page
     int32_t n, n_dst, n_src, layers;
 };
 
-__global__ void __launch_bounds__(kCopyThreads) copy_kernel(CopyParams p) {
+// Each CTA takes pieces of pages: 16 KB, so that a thread has four loads in flight (128 KB an SM), and a few pages fill the
+// machine.  Bound by HBM.
+__global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constant__ CopyParams p) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int n = p.n_dev ? min(p.n, max(0, *p.n_dev)) : p.n;
-    for (long long item = blockIdx.x; item < (long long)n * p.layers; item += gridDim.x) {
-        const int i = (int)(item % n), layer = (int)(item / n);
-        const int s = p.src_ids[i], d = p.dst_ids ? p.dst_ids[i] : i;
-        if (s < 0 || s >= p.n_src || d < 0 || d >= p.n_dst) {
-            if (s != ISV_BLOCK_NONE && d != ISV_BLOCK_NONE && threadIdx.x == 0 && p.status)
-                atomicOr(p.status, ISV_STATUS_BAD_BLOCK_ID);
-            continue;
+    const uint32_t items = (uint32_t)n * (uint32_t)p.pieces;               // the host checks that they fit
+    for (int layer = blockIdx.y; layer < p.layers; layer += gridDim.y)
+        for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
+            const int i = (int)(item / (uint32_t)p.pieces), piece = (int)(item - (uint32_t)i * (uint32_t)p.pieces);
+            const int s = p.src_ids[i], d = p.dst_ids ? p.dst_ids[i] : i;
+            if (s < 0 || s >= p.n_src || d < 0 || d >= p.n_dst) {
+                if (s != ISV_BLOCK_NONE && d != ISV_BLOCK_NONE && threadIdx.x == 0 && p.status)
+                    atomicOr(p.status, ISV_STATUS_BAD_BLOCK_ID);
+                continue;
+            }
+            const uint4 *from = p.src + layer * p.src_stride + (size_t)s * p.page;
+            uint4 *to = p.dst + layer * p.dst_stride + (size_t)d * p.page;
+            uint4 v[kCopyUnroll];
+            const int x = piece * kCopyThreads * kCopyUnroll + threadIdx.x;
+#pragma unroll
+            for (int k = 0; k < kCopyUnroll; ++k)
+                if (x + k * kCopyThreads < p.page) v[k] = from[x + k * kCopyThreads];
+#pragma unroll
+            for (int k = 0; k < kCopyUnroll; ++k)
+                if (x + k * kCopyThreads < p.page) to[x + k * kCopyThreads] = v[k];
         }
-        const uint4 *from = p.src + layer * p.src_stride + (size_t)s * p.page;
-        uint4 *to = p.dst + layer * p.dst_stride + (size_t)d * p.page;
-        for (int x = threadIdx.x; x < p.page; x += kCopyThreads) to[x] = from[x];
-    }
 }
 
-size_t table_smem(const TableParams &p, bool fork) {
-    return 4ull * ((size_t)p.words + 2 * (size_t)p.slice + p.n_rows + 1 + (fork ? p.n_in : 0));
+size_t table_smem(const TableParams &p, int op) {
+    const size_t last = op == FORK ? p.n_in : op == RESIZE ? p.n_rows : 0;
+    return 4ull * ((size_t)p.words + 2 * (size_t)p.slice + 2 * (size_t)p.n_rows + 1 + last);
 }
 
 template <int OP>
@@ -324,7 +338,7 @@ int launch_table(const char *who, TableParams &p, void *stream) {
     p.slice = (p.words + kCtas - 1) / kCtas;
     int rows = 1;
     while (rows < p.n_rows) rows *= 2;
-    p.row_threads = std::max(32, kCtas * kThreads / rows);
+    p.row_threads = std::max(8, kCtas * kThreads / rows);
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return err(ISV_ECUDA, "%s: %s", who, cudaGetErrorString(e));
@@ -334,21 +348,23 @@ int launch_table(const char *who, TableParams &p, void *stream) {
         most.words = ISV_PAGES_MAX / 32;
         most.slice = most.words / kCtas;
         most.n_rows = most.n_in = kMaxRows;
-        e = cudaFuncSetAttribute(table_kernel<OP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)table_smem(most, OP == FORK));
+        e = cudaFuncSetAttribute(table_kernel<OP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)table_smem(most, OP));
         if (e != cudaSuccess) return err(ISV_ECUDA, "%s: %s", who, cudaGetErrorString(e));
         if (dev < kMaxDevices) ready[dev].store(true);
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(kCtas);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = table_smem(p, OP == FORK);
+    cfg.dynamicSmemBytes = table_smem(p, OP);
     cfg.stream = static_cast<cudaStream_t>(stream);
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;   // see the kernel's griddepcontrol pair
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = kCtas;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     e = cudaLaunchKernelEx(&cfg, table_kernel<OP>, p);
     return e == cudaSuccess ? ISV_OK : err(ISV_ECUDA, "%s: %s", who, cudaGetErrorString(e));
 }
@@ -394,9 +410,19 @@ int isv_pages_copy(void *dst_pool_dev, int32_t n_dst_pages, const void *src_pool
     p.src_ids = src_ids_dev; p.dst_ids = dst_ids_dev; p.n_dev = n_dev; p.status = status_dev;
     p.dst_stride = dst_layer_stride / 16; p.src_stride = src_layer_stride / 16; p.page = (int32_t)(page_bytes / 16);
     p.n = n; p.n_dst = n_dst_pages; p.n_src = n_src_pages; p.layers = layers;
-    const long long items = (long long)n * layers;
-    copy_kernel<<<(unsigned)std::min<long long>(items, 148 * 8), kCopyThreads, 0, static_cast<cudaStream_t>(stream)>>>(p);
-    cudaError_t e = cudaGetLastError();
+    p.pieces = (p.page + kCopyThreads * kCopyUnroll - 1) / (kCopyThreads * kCopyUnroll);
+    if ((unsigned long long)n * (unsigned)p.pieces >= (1ull << 32)) return err(ISV_EINVAL, "isv_pages_copy: n * page_bytes too large");
+    const unsigned items = (unsigned)n * (unsigned)p.pieces, rows = (unsigned)std::min(layers, 65535);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(std::max(1u, std::min(items, 148u * 8u / std::min(rows, 148u * 8u))), rows);   // about 8 CTAs an SM
+    cfg.blockDim = dim3(kCopyThreads);
+    cfg.stream = static_cast<cudaStream_t>(stream);
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;   // see the kernel's griddepcontrol pair
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, copy_kernel, p);
     return e == cudaSuccess ? ISV_OK : err(ISV_ECUDA, "isv_pages_copy: %s", cudaGetErrorString(e));
 }
 
