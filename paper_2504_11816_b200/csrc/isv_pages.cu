@@ -97,7 +97,7 @@ template <int OP>
 __global__ void __launch_bounds__(kThreads, 1) table_kernel(TableParams p) {
     extern __shared__ uint32_t smem[];
     __shared__ int warp_sums[32];
-    __shared__ int slice_live;
+    __shared__ int slice_live[kCtas];          // live pages of every slice: each CTA tells all
     uint32_t *bits = smem;                                              // [words]: this CTA's marks
     uint32_t *fin = bits + p.words;                                     // [slice]: all marks of this CTA's slice
     int *before = reinterpret_cast<int *>(fin + p.slice);               // [slice]: live pages of the slice before the word
@@ -156,12 +156,16 @@ __global__ void __launch_bounds__(kThreads, 1) table_kernel(TableParams p) {
         const Row w = row_of(r);
         const int keep = min(w.lo, w.hi);
         const int32_t *from = p.table + (size_t)(OP == FORK ? (keep ? p.other[r] : 0) : r) * p.stride;
-#pragma unroll 4
-        for (int j = at % p.row_threads; j < keep; j += p.row_threads) {
-            const int id = from[j];
-            if (OP == FORK) p.table_out[(size_t)r * p.stride + j] = id;
-            if (id >= 0 && id < p.n_pages) atomicOr(&bits[id >> 5], 1u << (id & 31));
-            else if (id != ISV_BLOCK_NONE) bad |= ISV_STATUS_BAD_BLOCK_ID;
+        for (int j = at % p.row_threads; j < keep; j += 4 * p.row_threads) {
+            int id[4];                 // four loads in flight
+#pragma unroll
+            for (int i = 0; i < 4; ++i) id[i] = j + i * p.row_threads < keep ? from[j + i * p.row_threads] : ISV_BLOCK_NONE;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (OP == FORK && j + i * p.row_threads < keep) p.table_out[(size_t)r * p.stride + j + i * p.row_threads] = id[i];
+                if (id[i] >= 0 && id[i] < p.n_pages) atomicOr(&bits[id[i] >> 5], 1u << (id[i] & 31));
+                else if (id[i] != ISV_BLOCK_NONE) bad |= ISV_STATUS_BAD_BLOCK_ID;
+            }
         }
     }
     // ---- fresh pages before each row
@@ -203,13 +207,12 @@ __global__ void __launch_bounds__(kThreads, 1) table_kernel(TableParams p) {
         before[k] = x;
         x += __popc(fin[k]);
     }
-    if (tid == 0) slice_live = total;
+    if (tid < kCtas) cluster.map_shared_rank(slice_live, tid)[rank] = total;
     cluster.sync();
     int base = 0, live = 0;                // live pages before this slice, and in all
     for (int c = 0; c < kCtas; ++c) {
-        const int n = *cluster.map_shared_rank(&slice_live, c);
-        if (c < rank) base += n;
-        live += n;
+        if (c < rank) base += slice_live[c];
+        live += slice_live[c];
     }
     const int first_id = rank * p.slice * 32;
     const int ids = max(0, min(p.slice * 32, p.n_pages - first_id));
@@ -254,7 +257,7 @@ __global__ void __launch_bounds__(kThreads, 1) table_kernel(TableParams p) {
         auto live_before = [&](int id) {   // over the whole pool
             const int c = (id >> 5) / p.slice, k = (id >> 5) % p.slice;
             int n = 0;
-            for (int i = 0; i < c; ++i) n += *cluster.map_shared_rank(&slice_live, i);
+            for (int i = 0; i < c; ++i) n += slice_live[i];
             if (c < kCtas)
                 n += cluster.map_shared_rank(before, c)[k] + __popc(cluster.map_shared_rank(fin, c)[k] & ((1u << (id & 31)) - 1u));
             return n;
@@ -284,7 +287,7 @@ __global__ void __launch_bounds__(kThreads, 1) table_kernel(TableParams p) {
         }
     }
     if (bad && p.status) atomicOr(p.status, bad);
-    cluster.sync();                        // nobody leaves while its shared memory may be read
+    if (OP == COMPACT) cluster.sync();     // nobody leaves while its shared memory may be read
 }
 
 struct CopyParams {
