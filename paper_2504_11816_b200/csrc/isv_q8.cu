@@ -63,59 +63,118 @@ struct WriteParams {
 // ---- quantisation
 //
 // A code is the rounding of the exact quotient x / s.  The kernel multiplies by 1 / s: that product is off by at most
-// 2^-23 of its value, so its rounding is the right one unless it lies that close to a border between two codes.  Those
-// few elements are divided properly.
-
-// x / s rounded so that a later rounding to fewer bits gives what it gives for the exact quotient: the fp32
-// quotient, and where that is inexact and its last bit is 0 the neighbour on the side of the exact value ("round
-// to odd").  The residual is exact: x has at most 11 significant bits and the caller keeps s and x in the normal range.
-// Quotients below 2^-20 become the code 0 whatever their last bits.
-__device__ __noinline__ float quotient_to_odd(float x, float s) {
-    const float q = __fdiv_rn(x, s);
-    const float r = __fmaf_rn(-q, s, x);
-    uint32_t b = __float_as_uint(q);
-    if (fabsf(q) > 0x1p-20f && r != 0.f && !(b & 1u)) b += ((r > 0.f) == (q > 0.f)) ? 1u : ~0u;   // away from zero, or toward it
-    return __uint_as_float(b);
-}
+// 2^-23 of its value, so its rounding is the right one unless it lies that close to the border m between two codes.  There the
+// sign of x - m * s decides, which one fused multiply-add gives exactly (m has at most eight bits; the caller keeps x
+// and s in the normal range): 0 is a tie.  Ties are common, x = absmax / 2 is one for int8, and with eight bits of bf16 so
+// are others: nearly every word of a block has one.
 
 constexpr float kMagic = 12582912.f;   // 1.5 * 2^23: adding it rounds to an integer, which is then in the low bits
 
+// Two fp32 numbers in one register pair: the multiplications and additions below take one instruction for both.
+__device__ __forceinline__ uint64_t pair(float x, float y) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ float2 unpair(uint64_t v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// a * b + c
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// e4m3 keeps three bits behind the leading one, and below 2^-6 the steps that it has at 2^-6: |q|, below 2^-6 raised by 2^-6,
+// has its borders where the last 20 bits are 0x80000.
+__device__ __forceinline__ float raised(float q) {
+    const float a = fabsf(q);
+    return a < 0x1p-6f ? a + 0x1p-6f : a;
+}
+template <bool E4M3>
+__device__ __forceinline__ bool near_border(float q) {
+    if (E4M3) return ((__float_as_uint(raised(q)) - 0x7fffcu) & 0xfffffu) <= 8u;
+    return fabsf(q - ((q + kMagic) - kMagic)) > 0.49998f;             // |q| <= 127: off by at most 1.6e-5
+}
+// A number that rounds as x / s does, where q = x * (1 / s) lies near a border.
+template <bool E4M3>
+__device__ __forceinline__ float settle(float q, float x, float s) {
+    if (!near_border<E4M3>(q)) return q;
+    if (E4M3) {
+        const float low = fabsf(q) < 0x1p-6f ? 0x1p-6f : 0.f;
+        const uint32_t border = (__float_as_uint(raised(q)) & 0xfff00000u) | 0x80000u;
+        const float e = __fmaf_rn(-(__uint_as_float(border) - low), s, fabsf(x));
+        const float y = __uint_as_float(border + (e > 0.f ? 0x1000u : e < 0.f ? ~0xfffu : 0u)) - low;
+        return copysignf(y, q);
+    }
+    const float m = ((q - 0.5f) + kMagic) - kMagic + 0.5f, e = __fmaf_rn(-m, s, x);
+    return e > 0.f ? m + 0.25f : e < 0.f ? m - 0.25f : m;
+}
+
+__device__ __forceinline__ uint32_t low_bytes(const float2 (&r)[2]) {
+    return __byte_perm(__byte_perm(__float_as_uint(r[0].x), __float_as_uint(r[0].y), 0x0040),
+                       __byte_perm(__float_as_uint(r[1].x), __float_as_uint(r[1].y), 0x0040), 0x5410);
+}
 // Four numbers -> four codes, in the bytes of a word.
 template <bool E4M3>
-__device__ __forceinline__ uint32_t encode_raw(const float (&q)[4]) {
+__device__ __forceinline__ uint32_t codes_of(const float2 (&q)[2]) {
     uint32_t w;
     if (E4M3) {
         asm("{\n.reg .b16 a, b;\ncvt.rn.satfinite.e4m3x2.f32 a, %2, %1;\ncvt.rn.satfinite.e4m3x2.f32 b, %4, %3;\nmov.b32 %0, {a, b};\n}\n"
-            : "=r"(w) : "f"(q[0]), "f"(q[1]), "f"(q[2]), "f"(q[3]));
+            : "=r"(w) : "f"(q[0].x), "f"(q[0].y), "f"(q[1].x), "f"(q[1].y));
     } else {
-        uint32_t r[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) r[i] = __float_as_uint(q[i] + kMagic);
-        w = __byte_perm(__byte_perm(r[0], r[1], 0x0040), __byte_perm(r[2], r[3], 0x0040), 0x5410);
+        const float2 r[2] = {make_float2(q[0].x + kMagic, q[0].y + kMagic), make_float2(q[1].x + kMagic, q[1].y + kMagic)};
+        w = low_bytes(r);
     }
     return w;
 }
-// up: the power of two by which numbers and scale are multiplied, for blocks so small that the quotients' arithmetic would leave
-// the normal range (s has it already); those divide every element.
+// The four int8 codes of numbers some of which may lie next to a border.  A call of its own: inlined sixteen times it made the
+// kernel's code so long that a prompt of 16 x 1024 tokens x 32 heads took 109 us instead of 86.  With e4m3 it is inlined:
+// nearly every word needs it, and an append of one token to 256 sequences takes 8.6 us instead of 10.4.
+__device__ __noinline__ uint32_t int8_settled(float a, float b, float c, float d, float s, float inv) {
+    const float2 q[2] = {make_float2(settle<false>(a * inv, a, s), settle<false>(b * inv, b, s)),
+                         make_float2(settle<false>(c * inv, c, s), settle<false>(d * inv, d, s))};
+    return codes_of<false>(q);
+}
+// up: the power of two by which numbers and scale are multiplied, for blocks so small that the arithmetic would leave the
+// normal range (s and inv have it already).
 template <bool E4M3>
-__device__ __forceinline__ uint32_t encode(const float (&x)[4], float s, float inv, float up) {
-    float q[4];
+__device__ __forceinline__ uint32_t encode(const float2 (&x)[2], float s, float inv, float up) {
+    const uint64_t inv2 = pair(inv, inv);
     bool close = up != 1.f;
+    float2 q[2], r[2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        q[i] = x[i] * inv;
+    for (int i = 0; i < 2; ++i) {
+        const uint64_t v = pair(x[i].x, x[i].y);
         if (E4M3) {
-            // three bits behind the leading one are kept; below 2^-6 the steps stay as they are at 2^-6
-            const float a = fabsf(q[i]), n = a < 0x1p-6f ? a + 0x1p-6f : a;
-            close = close || ((__float_as_uint(n) - 0x7fffcu) & 0xfffffu) <= 8u;
-        } else {
-            close = close || fabsf(q[i] - ((q[i] + kMagic) - kMagic)) > 0.49998f;   // |q| <= 127: off by at most 1.6e-5
+            q[i] = unpair(mul2(v, inv2));
+            close = close || near_border<true>(q[i].x) || near_border<true>(q[i].y);
+        } else {   // t: rounded to the integer n, which is in its low bits; d: how far the quotient is from n
+            const uint64_t t = fma2(v, inv2, pair(kMagic, kMagic)), n = add2(t, pair(-kMagic, -kMagic));
+            const float2 d = unpair(fma2(v, inv2, mul2(n, pair(-1.f, -1.f))));
+            r[i] = unpair(t);
+            close = close || fabsf(d.x) > 0.49998f || fabsf(d.y) > 0.49998f;
         }
     }
+    if (!E4M3) return close ? int8_settled(x[0].x * up, x[0].y * up, x[1].x * up, x[1].y * up, s, inv) : low_bytes(r);
     if (close)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) q[i] = quotient_to_odd(x[i] * up, s);
-    return encode_raw<E4M3>(q);
+        for (int i = 0; i < 2; ++i)
+            q[i] = make_float2(settle<true>(x[i].x * up * inv, x[i].x * up, s), settle<true>(x[i].y * up * inv, x[i].y * up, s));
+    return codes_of<true>(q);
 }
 
 template <bool BF16>
@@ -124,13 +183,95 @@ __device__ __forceinline__ float half_of(uint32_t w, int i) {   // the low (0) o
     return __half2float(__ushort_as_half((unsigned short)(i ? w >> 16 : w & 0xffffu)));
 }
 
-// A warp per (sequence, block that its new tokens touch, KV head, K or V).  A lane's loads are the 16-bit rows in the order in
-// which the page wants its codes: lane 4 g + c takes tokens g, g + 8 of K, 8 dims at a time, and dims g * D / 8 .. of tokens
-// 2 c, 2 c + 1, 2 c + 8, 2 c + 9 of V; what it writes are 16-byte pieces, 512 contiguous bytes of the warp.
+// Quantises a complete block's K (V = false) or V part: `row(t)` is the address of token t's row, `unit` the block's place.
+// A lane's loads are the 16-bit rows in the order in which the page wants its codes: lane 4 g + c takes tokens g, g + 8 of K,
+// 8 dims at a time, and dims g * D / 8 .. of tokens 2 c, 2 c + 1, 2 c + 8, 2 c + 9 of V; what it writes are 16-byte pieces, 512
+// contiguous bytes of the warp.
+template <int D, bool BF16, bool E4M3, bool V, typename Rows>
+__device__ __forceinline__ void quantise(Rows row, uint8_t *unit, int lane) {
+    constexpr int MT = D / 16, P = D / 32, REST = D % 32 ? 1 : 0;
+    const int g = lane >> 2, c = lane & 3;
+    // r[2 * MT * i + ..]: K: the lane's words of token g + 8 i; V: r[MT * j + ..]: those of the lane's j-th token
+    uint32_t r[4 * MT];
+    if (!V) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint16_t *at = row(g + 8 * i);
+#pragma unroll
+            for (int x = 0; x < P; ++x) {
+                const uint4 w = *reinterpret_cast<const uint4 *>(at + 32 * x + 8 * c);
+                r[2 * MT * i + 4 * x] = w.x; r[2 * MT * i + 4 * x + 1] = w.y; r[2 * MT * i + 4 * x + 2] = w.z; r[2 * MT * i + 4 * x + 3] = w.w;
+            }
+            if (REST) {
+                const uint2 w = *reinterpret_cast<const uint2 *>(at + 32 * P + 4 * c);
+                r[2 * MT * i + 4 * P] = w.x; r[2 * MT * i + 4 * P + 1] = w.y;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint16_t *at = row(2 * c + (j & 1) + 8 * (j >> 1)) + g * (D / 8);
+            if (D % 64 == 0) {
+#pragma unroll
+                for (int x = 0; x < MT / 4; ++x) {
+                    const uint4 w = *reinterpret_cast<const uint4 *>(at + 8 * x);
+                    r[MT * j + 4 * x] = w.x; r[MT * j + 4 * x + 1] = w.y; r[MT * j + 4 * x + 2] = w.z; r[MT * j + 4 * x + 3] = w.w;
+                }
+            } else {
+#pragma unroll
+                for (int x = 0; x < MT; ++x) r[MT * j + x] = *reinterpret_cast<const uint32_t *>(at + 2 * x);
+            }
+        }
+    }
+    uint32_t top2 = 0;                                   // magnitudes of 16-bit floats order like their bits
+#pragma unroll
+    for (int x = 0; x < 4 * MT; ++x) top2 = __vmaxu2(top2, r[x] & 0x7fff7fffu);
+#pragma unroll
+    for (int o = 16; o; o /= 2) top2 = __vmaxu2(top2, __shfl_xor_sync(~0u, top2, o));
+    const uint32_t bits = max(top2 & 0xffffu, top2 >> 16);
+    const float top = half_of<BF16>(bits, 0);
+    const bool odd = bits >= (BF16 ? 0x7f80u : 0x7c00u); // an infinity or a NaN: codes of 0 and the scale NaN
+    const float scale = odd ? __int_as_float(0x7fffffff) : __fdiv_rn(top, E4M3 ? 448.f : 127.f);
+    const float up = top < 0x1p-60f ? 0x1p64f : 1.f, s_up = scale * up;
+    const bool zeros = odd || top == 0.f;
+    const float inv = zeros ? 0.f : __fdiv_rn(1.f, s_up);
+    uint8_t *part = unit + (V ? kBT * D : 0);
+#pragma unroll
+    for (int x = 0; x < P + REST; ++x) {
+        uint32_t w[4] = {0, 0, 0, 0};
+        if (!zeros) {
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const int t = 2 * x + y / 2, i = y & 1;  // K: k-step t, token g + 8 i; V: tile t, dim 2 t + i of the lane's
+                if (t >= MT) continue;
+                float2 n[2];
+                if (V) {
+                    n[0] = make_float2(half_of<BF16>(r[t], i), half_of<BF16>(r[MT + t], i));
+                    n[1] = make_float2(half_of<BF16>(r[2 * MT + t], i), half_of<BF16>(r[3 * MT + t], i));
+                } else {
+                    const uint32_t a = r[2 * MT * i + 2 * t], b = r[2 * MT * i + 2 * t + 1];
+                    n[0] = make_float2(half_of<BF16>(a, 0), half_of<BF16>(a, 1));
+                    n[1] = make_float2(half_of<BF16>(b, 0), half_of<BF16>(b, 1));
+                }
+                w[y] = encode<E4M3>(n, s_up, inv, up);
+            }
+        }
+        if (x < P) *reinterpret_cast<uint4 *>(part + 512 * x + 16 * lane) = make_uint4(w[0], w[1], w[2], w[3]);
+        else *reinterpret_cast<uint2 *>(part + 512 * x + 8 * lane) = make_uint2(w[0], w[1]);
+    }
+    if (lane == 0) {
+        float *tags = reinterpret_cast<float *>(unit + 2 * kBT * D);
+        tags[V] = scale;
+        tags[2 + V] = 0.f;
+    }
+}
+
+// A warp per (sequence, block that its new tokens touch, KV head, K or V).
 template <int D, bool BF16, bool E4M3>
 __global__ void __launch_bounds__(kWriteThreads) write_kernel(const __grid_constant__ WriteParams p) {
-    constexpr int MT = D / 16, P = D / 32, REST = D % 32 ? 1 : 0;
-    const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int lane = threadIdx.x & 31;
     const int task = blockIdx.x * (kWriteThreads / 32) + threadIdx.x / 32, s = blockIdx.y;
     const int kv = task & 1, bi = (task >> 1) / p.c.Hkv, h = (task >> 1) - bi * p.c.Hkv;
     if (bi >= p.blocks) return;
@@ -143,81 +284,18 @@ __global__ void __launch_bounds__(kWriteThreads) write_kernel(const __grid_const
     if (n_new == 0 || b > last) return;
     uint16_t *tail = reinterpret_cast<uint16_t *>(p.c.tails) + (((size_t)s * 2 + kv) * p.c.Hkv + h) * kBT * D;
     const uint16_t *src = (kv ? p.v : p.k) + s * p.seq_stride + (size_t)h * D;
-    const int page = (b + 1) * kBT <= len ? p.c.table[(size_t)s * p.c.table_stride + b] : 0;
-    if ((b + 1) * kBT <= len && (page < 0 || page >= p.c.n_pages)) {
-        if (lane == 0) atomicOr(p.c.status, ISV_STATUS_BAD_BLOCK_ID);
-    } else if ((b + 1) * kBT <= len) {
-        auto row = [&](int t) {                              // rows before `start` wait in the tail slot
-            const int pos = b * kBT + t;
-            return pos < start ? tail + t * D : src + (pos - start) * p.token_stride;
-        };
-        // r[2 * MT * i + ..]: K: the lane's words of token g + 8 i; V: r[MT * j + ..]: those of the lane's j-th token
-        uint32_t r[4 * MT];
-        if (kv == 0) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint16_t *at = row(g + 8 * i);
-#pragma unroll
-                for (int x = 0; x < P; ++x) {
-                    const uint4 w = *reinterpret_cast<const uint4 *>(at + 32 * x + 8 * c);
-                    r[2 * MT * i + 4 * x] = w.x; r[2 * MT * i + 4 * x + 1] = w.y; r[2 * MT * i + 4 * x + 2] = w.z; r[2 * MT * i + 4 * x + 3] = w.w;
-                }
-                if (REST) {
-                    const uint2 w = *reinterpret_cast<const uint2 *>(at + 32 * P + 4 * c);
-                    r[2 * MT * i + 4 * P] = w.x; r[2 * MT * i + 4 * P + 1] = w.y;
-                }
-            }
+    if ((b + 1) * kBT <= len) {
+        const int page = p.c.table[(size_t)s * p.c.table_stride + b];
+        if (page < 0 || page >= p.c.n_pages) {
+            if (lane == 0) atomicOr(p.c.status, ISV_STATUS_BAD_BLOCK_ID);
         } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint16_t *at = row(2 * c + (j & 1) + 8 * (j >> 1)) + g * (D / 8);
-                if (D % 64 == 0) {
-#pragma unroll
-                    for (int x = 0; x < MT / 4; ++x) {
-                        const uint4 w = *reinterpret_cast<const uint4 *>(at + 8 * x);
-                        r[MT * j + 4 * x] = w.x; r[MT * j + 4 * x + 1] = w.y; r[MT * j + 4 * x + 2] = w.z; r[MT * j + 4 * x + 3] = w.w;
-                    }
-                } else {
-#pragma unroll
-                    for (int x = 0; x < MT; ++x) r[MT * j + x] = *reinterpret_cast<const uint32_t *>(at + 2 * x);
-                }
-            }
-        }
-        uint32_t top2 = 0;                                   // magnitudes of 16-bit floats order like their bits
-#pragma unroll
-        for (int x = 0; x < 4 * MT; ++x) top2 = __vmaxu2(top2, r[x] & 0x7fff7fffu);
-#pragma unroll
-        for (int o = 16; o; o /= 2) top2 = __vmaxu2(top2, __shfl_xor_sync(~0u, top2, o));
-        const uint32_t bits = max(top2 & 0xffffu, top2 >> 16);
-        const float top = half_of<BF16>(bits, 0);
-        const bool odd = bits >= (BF16 ? 0x7f80u : 0x7c00u); // an infinity or a NaN: codes of 0 and the scale NaN
-        const float scale = odd ? __int_as_float(0x7fffffff) : __fdiv_rn(top, E4M3 ? 448.f : 127.f);
-        const float up = top < 0x1p-60f ? 0x1p64f : 1.f, s_up = scale * up;
-        const bool zeros = odd || top == 0.f;
-        const float inv = zeros ? 0.f : __fdiv_rn(1.f, s_up);
-        uint8_t *unit = p.c.pool + ((size_t)page * p.c.Hkv + h) * unit_bytes(D), *part = unit + kv * kBT * D;
-#pragma unroll
-        for (int x = 0; x < P + REST; ++x) {
-            uint32_t w[4] = {0, 0, 0, 0};
-            if (!zeros) {
-#pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    const int t = 2 * x + y / 2, i = y & 1;  // K: k-step t, token g + 8 i; V: tile t, dim 2 t + i of the lane's
-                    if (t >= MT) continue;
-                    const float n[4] = {kv ? half_of<BF16>(r[t], i) : half_of<BF16>(r[2 * MT * i + 2 * t], 0),
-                                        kv ? half_of<BF16>(r[MT + t], i) : half_of<BF16>(r[2 * MT * i + 2 * t], 1),
-                                        kv ? half_of<BF16>(r[2 * MT + t], i) : half_of<BF16>(r[2 * MT * i + 2 * t + 1], 0),
-                                        kv ? half_of<BF16>(r[3 * MT + t], i) : half_of<BF16>(r[2 * MT * i + 2 * t + 1], 1)};
-                    w[y] = encode<E4M3>(n, s_up, inv, up);
-                }
-            }
-            if (x < P) *reinterpret_cast<uint4 *>(part + 512 * x + 16 * lane) = make_uint4(w[0], w[1], w[2], w[3]);
-            else *reinterpret_cast<uint2 *>(part + 512 * x + 8 * lane) = make_uint2(w[0], w[1]);
-        }
-        if (lane == 0) {
-            float *tags = reinterpret_cast<float *>(unit + 2 * kBT * D);
-            tags[kv] = scale;
-            tags[2 + kv] = 0.f;
+            auto row = [&](int t) {                      // rows before `start` wait in the tail slot
+                const int pos = b * kBT + t;
+                return pos < start ? tail + t * D : src + (pos - start) * p.token_stride;
+            };
+            uint8_t *unit = p.c.pool + ((size_t)page * p.c.Hkv + h) * unit_bytes(D);
+            if (kv) quantise<D, BF16, E4M3, true>(row, unit, lane);
+            else quantise<D, BF16, E4M3, false>(row, unit, lane);
         }
     }
     // ---- the open block's new rows into the tail slot.  Where the first block completes with rows from the tail slot, its warp
@@ -234,11 +312,17 @@ __global__ void __launch_bounds__(kWriteThreads) write_kernel(const __grid_const
 
 template <int D>
 cudaError_t launch_write(const WriteParams &p, bool bf16, bool e4m3, dim3 grid, cudaStream_t st) {
-    if (bf16 && e4m3) write_kernel<D, true, true><<<grid, kWriteThreads, 0, st>>>(p);
-    else if (bf16) write_kernel<D, true, false><<<grid, kWriteThreads, 0, st>>>(p);
-    else if (e4m3) write_kernel<D, false, true><<<grid, kWriteThreads, 0, st>>>(p);
-    else write_kernel<D, false, false><<<grid, kWriteThreads, 0, st>>>(p);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(kWriteThreads);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;   // see the kernel's griddepcontrol pair
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (bf16) return e4m3 ? cudaLaunchKernelEx(&cfg, write_kernel<D, true, true>, p) : cudaLaunchKernelEx(&cfg, write_kernel<D, true, false>, p);
+    return e4m3 ? cudaLaunchKernelEx(&cfg, write_kernel<D, false, true>, p) : cudaLaunchKernelEx(&cfg, write_kernel<D, false, false>, p);
 }
 
 }  // namespace
