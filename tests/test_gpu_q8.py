@@ -400,3 +400,44 @@ def test_two_handles_on_two_streams_at_once():
         torch.cuda.synchronize()
         for c, o in zip((a, b), outs):
             c.check(o.to(c.dt), o)
+
+
+def test_as_many_sequences_as_a_handle_takes():
+    lens = [int(x) for x in np.random.default_rng(3).integers(0, 40, 4096)]
+    lens[5], lens[4095] = 300, 33
+    with Cache(lens, 4, 2, 64, "f16", seed=18) as c:
+        c.fill()
+        out, out32 = c.attend()
+        c.check(out, out32, rows=[0, 1, 5, 6, 1023, 1024, 2000, 4094, 4095])
+        empty = [s for s, n in enumerate(lens) if n == 0]
+        assert (out32[empty] == 0).all() and (out[empty] == 0).all()
+
+
+def test_a_handle_serves_calls_of_fewer_sequences_and_other_pools():
+    with Cache([33, 100, 7], 8, 2, 128, "bf16", B.ISV_Q8_E4M3, seed=19) as a, Cache([260], 8, 2, 128, "bf16", B.ISV_Q8_E4M3, seed=20) as b:
+        a.fill()
+        own, b.h = b.h, a.h                     # the second cache through the first one's handle
+        b.fill().check_bytes()
+        b.check(*b.attend())
+        a.check(*a.attend())
+        b.h = own
+
+
+def test_queries_far_from_one_and_not_finite():
+    """Rows of q of any size keep fp32 accuracy; an infinity or NaN in one head reaches that head only."""
+    with Cache([64, 21], 8, 2, 128, "bf16", B.ISV_Q8_INT8, seed=21) as c:
+        c.fill()
+        c.q[0, 0] *= 1e-30
+        c.q[0, 1] *= 1e-4
+        c.q[0, 2] *= 20
+        c.q[1, 3] = 0
+        clean = c.attend()
+        c.check(*clean)
+        c.q[0, 5, 17] = float("nan")
+        c.q[1, 7, 3] = float("inf")
+        out, out32 = c.attend()
+        assert torch.isnan(out32[0, 5]).all() and torch.isnan(out32[1, 7]).all()
+        fine = torch.ones(2, 8, dtype=torch.bool)
+        fine[0, 5] = fine[1, 7] = False
+        assert torch.isfinite(out32[fine.cuda()]).all()
+        assert torch.allclose(out32[fine.cuda()], clean[1][fine.cuda()], rtol=0, atol=1e-4)
