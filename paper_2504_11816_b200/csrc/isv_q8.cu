@@ -479,7 +479,7 @@ int isv_q8_attn(isv_q8 *h, const void *pool_dev, int32_t n_pages, const void *ta
         return err(ISV_EINVAL, "isv_q8_attn: q and outputs must be 16-byte aligned");
     if (n_seqs == 0) return ISV_OK;
     const long long groups = (long long)h->d.kv_heads * h->P;
-    if (((long long)max_blocks_per_seq + 2) * n_seqs * groups >= (1ll << 31))
+    if (((long long)max_blocks_per_seq + 3) * n_seqs * groups >= (1ll << 31))
         return err(ISV_EINVAL, "isv_q8_attn: n_seqs * blocks * heads too large");
     AttnParams p{};
     p.c = cache_params(h, pool_dev, n_pages, tails_dev, block_table_dev, table_stride, max_blocks_per_seq, seq_lens_dev, n_seqs);
