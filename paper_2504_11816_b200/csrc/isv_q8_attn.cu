@@ -689,6 +689,25 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
         const int longer = rest * (share + 1);
         return v < longer ? v / (share + 1) : rest + (v - longer) / share;
     };
+    auto span = [&](int item, int &b, int &e) {
+        const int s = item / G, nb = prefix[s + 1] - prefix[s];
+        b = prefix[s] * G + (item - s * G) * nb;
+        e = b + nb;
+    };
+    auto put = [&](int item, int h, const float2 (&o)[J], float l) {
+        const float f = l == 0.f ? 0.f : 1.f / l;
+        const size_t at = ((size_t)item * p.GT + h) * D;       // item * GT + h: the flat query head
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int u = lane + 32 * j;
+            if (u < PAIRS) store2<BF16>(p, at + (u % 8) * (D / 8) + 2 * (u / 8), o[j].x * f, o[j].y * f);
+        }
+    };
+    // An item that crosses CTAs (only the first and the last of a CTA may): its CTAs' results meet in memory, and the warp
+    // that brings a head's last one merges them.  The ticket is that of the item's first CTA, in which no other item
+    // continues into the next.  A warp has at most 2 * 16 / 8 + 1 such heads; lane i keeps the i-th, and all their tickets
+    // are drawn at once.
+    int mine_x = 0, crossing = 0;
 #pragma unroll 1
     for (int x = warp; x < n_runs * p.GT; x += NW) {
         const int run = x / p.GT, h = x - run * p.GT;
@@ -711,54 +730,60 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
             }
             merge(ml, v, r1 - r, m, l, o);
         }
-        const int s = item / G, nb = prefix[s + 1] - prefix[s], b = prefix[s] * G + (item - s * G) * nb, e = b + nb;
-        // An item that crosses CTAs (the first and the last of a CTA may): its CTAs' results meet in memory, and the warp that
-        // brings a head's last one merges them.  The ticket is that of the item's first CTA, in which no other item
-        // continues into the next.
-        if (b < cta_beg || e > cta_end) {
-            const int slot = blockIdx.x * 2 + (b > cta_beg ? 1 : 0);
+        int b, e;
+        span(item, b, e);
+        if (b >= cta_beg && e <= cta_end) {
+            put(item, h, o, l);
+            continue;
+        }
+        const int slot = blockIdx.x * 2 + (b > cta_beg ? 1 : 0);
 #pragma unroll
-            for (int j = 0; j < J; ++j)
-                if (lane + 32 * j < PAIRS) __stcg(reinterpret_cast<float2 *>(p.part_o) + (size_t)slot * SH::REC + h * PAIRS + lane + 32 * j, o[j]);
-            if (lane == 0) __stcg(reinterpret_cast<float2 *>(p.part_ml) + slot * HT + h, make_float2(m, l));
-            __threadfence();
-            __syncwarp();
-            const int c0 = cta_of(b), n = cta_of(e - 1) - c0 + 1;
-            int *ticket = p.tickets + c0 * HT + h;
-            int last = 0;
-            if (lane == 0) {
-                last = atomicAdd(ticket, 1) == n - 1;
-                if (last) *ticket = 0;
-                __threadfence();
-            }
-            if (!__shfl_sync(~0u, last, 0)) continue;
-            const int first_slot = b == cta_at(c0) ? 0 : 1;
-            m = kNone;
-            l = 0.f;
-#pragma unroll
-            for (int j = 0; j < J; ++j) o[j] = make_float2(0.f, 0.f);
+        for (int j = 0; j < J; ++j)
+            if (lane + 32 * j < PAIRS) __stcg(reinterpret_cast<float2 *>(p.part_o) + (size_t)slot * SH::REC + h * PAIRS + lane + 32 * j, o[j]);
+        if (lane == 0) __stcg(reinterpret_cast<float2 *>(p.part_ml) + slot * HT + h, make_float2(m, l));
+        if (lane == crossing) mine_x = x;
+        ++crossing;
+    }
+    if (crossing == 0) return;
+    __threadfence();
+    __syncwarp();
+    bool last = false;
+    if (lane < crossing) {
+        const int run = mine_x / p.GT, h = mine_x - run * p.GT;
+        int b, e;
+        span(run_item[run], b, e);
+        const int c0 = cta_of(b);
+        int *ticket = p.tickets + c0 * HT + h;
+        last = atomicAdd(ticket, 1) == cta_of(e - 1) - c0;
+        if (last) *ticket = 0;
+        __threadfence();
+    }
+    unsigned todo = __ballot_sync(~0u, last);
 #pragma unroll 1
-            for (int i = 0; i < n; i += kFly) {
-                float2 ml[kFly], v[kFly][J];
+    for (; todo; todo &= todo - 1) {
+        const int x = __shfl_sync(~0u, mine_x, __ffs(todo) - 1), run = x / p.GT, h = x - run * p.GT, item = run_item[run];
+        int b, e;
+        span(item, b, e);
+        const int c0 = cta_of(b), n = cta_of(e - 1) - c0 + 1, first_slot = b == cta_at(c0) ? 0 : 1;
+        float m = kNone, l = 0.f;
+        float2 o[J];
 #pragma unroll
-                for (int y = 0; y < kFly; ++y) {
-                    const int z = min(i + y, n - 1), at = (c0 + z) * 2 + (z == 0 ? first_slot : 0);
-                    ml[y] = __ldcg(reinterpret_cast<const float2 *>(p.part_ml) + at * HT + h);
+        for (int j = 0; j < J; ++j) o[j] = make_float2(0.f, 0.f);
+#pragma unroll 1
+        for (int i = 0; i < n; i += kFly) {
+            float2 ml[kFly], v[kFly][J];
 #pragma unroll
-                    for (int j = 0; j < J; ++j)
-                        v[y][j] = lane + 32 * j < PAIRS ? __ldcg(reinterpret_cast<const float2 *>(p.part_o) + (size_t)at * SH::REC + h * PAIRS + lane + 32 * j)
-                                                        : make_float2(0.f, 0.f);
-                }
-                merge(ml, v, n - i, m, l, o);
+            for (int y = 0; y < kFly; ++y) {
+                const int z = min(i + y, n - 1), at = (c0 + z) * 2 + (z == 0 ? first_slot : 0);
+                ml[y] = __ldcg(reinterpret_cast<const float2 *>(p.part_ml) + at * HT + h);
+#pragma unroll
+                for (int j = 0; j < J; ++j)
+                    v[y][j] = lane + 32 * j < PAIRS ? __ldcg(reinterpret_cast<const float2 *>(p.part_o) + (size_t)at * SH::REC + h * PAIRS + lane + 32 * j)
+                                                    : make_float2(0.f, 0.f);
             }
+            merge(ml, v, n - i, m, l, o);
         }
-        const float f = l == 0.f ? 0.f : 1.f / l;
-        const size_t at = ((size_t)item * p.GT + h) * D;       // item * GT + h: the flat query head
-#pragma unroll
-        for (int j = 0; j < J; ++j) {
-            const int u = lane + 32 * j;
-            if (u < PAIRS) store2<BF16>(p, at + (u % 8) * (D / 8) + 2 * (u / 8), o[j].x * f, o[j].y * f);
-        }
+        put(item, h, o, l);
     }
 }
 
