@@ -28,7 +28,9 @@ constexpr float kNone = -1.0e30f;            // reference of a head that has no 
 constexpr uint32_t kSpin = 1u << 22;
 constexpr float kSlack = 8.f;                // scores may exceed the reference by this much (log2) before it moves
 constexpr int kFly = 10;                     // partial results that the last merge has in flight
-constexpr int kMinVisits = 2;                // visits of a warp below which fewer warps of a CTA take part
+// Visits below which fewer CTAs, and fewer warps of a CTA, take part: every CTA more is one more partial result to merge (one
+// sequence of 4096 tokens, 8 heads on one KV head: 18.5 us on 148 CTAs, 11.4 on 32).
+constexpr int kMinCtaVisits = 8, kMinVisits = 2;
 
 __device__ __forceinline__ uint32_t s32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
@@ -529,7 +531,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
 
     // range of part i of n: the first `rest` parts are one longer
     const int total = carry * G;               // below 2^31: the host checks
-    const int ctas = min((int)gridDim.x, total);
+    const int ctas = total ? min((int)gridDim.x, max(1, total / kMinCtaVisits)) : 0;
     if ((int)blockIdx.x >= ctas) {
         if (bad && blockIdx.x == 0) atomicOr(p.c.status, bad);
         return;
