@@ -182,7 +182,7 @@ struct Shape {
     static constexpr int BUF = NT == 4 ? 1 : 2;                        // two buffers of sums: one barrier a tile
     static constexpr int SUMS = KW * COLS * PITCH;
     // what registers and shared memory allow: CTAs of an SM, and steps that a warp has in flight (about 150 KB an SM)
-    static constexpr int RESIDENT = NT == 1 ? 3 : NT == 2 ? 2 : 1, RING = NT == 1 ? 3 : NT == 2 ? 4 : 8;
+    static constexpr int RESIDENT = NT == 1 ? 3 : 2, RING = NT == 1 ? 3 : 4;
     static constexpr size_t smem(int group) { return (size_t)kWarps * RING * (step_bytes(group) + 8) + (size_t)BUF * SUMS * 4; }
 };
 
@@ -229,26 +229,15 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<NT, RW>::RESIDENT) linear4_
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    uint4 x[CHUNKS][NT];
+    // x of one chunk, loaded one chunk ahead (a whole step of it would cost 32 tokens the second CTA of an SM)
+    uint4 x[NT];
     const uint16_t *xs = p.x + (size_t)(m0 + g) * p.K + 8 * c;
-    auto load_x = [&](int step) {
-        const bool cut = (step + 1) * kStep > p.K;       // the last step where K is no multiple of one
+    auto load_x = [&](uint4 (&to)[NT], int k) {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const uint4 *at = reinterpret_cast<const uint4 *>(xs + (size_t)nt * 8 * p.K + step * kStep);
-#pragma unroll
-            for (int i = 0; i < CHUNKS; ++i) x[i][nt] = make_uint4(0, 0, 0, 0);
-            if (m0 + nt * 8 + g >= p.M) continue;
-            if (!cut) {
-#pragma unroll
-                for (int i = 0; i < CHUNKS; ++i) x[i][nt] = at[i * kChunk / 8];
-            } else {
-#pragma unroll
-                for (int i = 0; i < CHUNKS; ++i)
-                    if (step * kStep + i * kChunk < p.K) x[i][nt] = at[i * kChunk / 8];
-            }
-        }
+        for (int nt = 0; nt < NT; ++nt)
+            to[nt] = m0 + nt * 8 + g < p.M && k < p.K ? *reinterpret_cast<const uint4 *>(xs + (size_t)nt * 8 * p.K + k) : make_uint4(0, 0, 0, 0);
     };
+    load_x(x, first * kStep);
     int slot = 0;
     uint32_t phase = 0;
     bool lost = false;
@@ -263,7 +252,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<NT, RW>::RESIDENT) linear4_
                 for (int i = 0; i < 4; ++i) total[t][nt][i] = 0.f;
 #pragma unroll 1
         for (int step = first; step < end && tile * RW + rw < p.blocks; step += KW) {
-            load_x(step);      // from L1 or L2, while the wait and the first conversions go on
+            const int after = (step + KW < end ? step + KW : first) * kStep;
             if (!wait(bar0 + 8 * slot, phase)) lost = true;
             const uint8_t *in = mine + slot * BYTES;
 #pragma unroll
@@ -277,6 +266,8 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<NT, RW>::RESIDENT) linear4_
                         for (int i = 0; i < 4; ++i) part[t][nt][i] = 0.f;
 #pragma unroll
                 for (int i = i0 * PER; i < (i0 + 1) * PER; ++i) {
+                    uint4 next_x[NT];
+                    load_x(next_x, i + 1 < CHUNKS ? step * kStep + (i + 1) * kChunk : after);
                     const uint4 w = *reinterpret_cast<const uint4 *>(in + 512 * i + 16 * lane);
                     const uint32_t words[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
@@ -285,8 +276,10 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<NT, RW>::RESIDENT) linear4_
                         widen<BF16>(words[j], a);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt)
-                            mma<BF16>(part[j >> 1][nt], a, j & 1 ? x[i][nt].z : x[i][nt].x, j & 1 ? x[i][nt].w : x[i][nt].y);
+                            mma<BF16>(part[j >> 1][nt], a, j & 1 ? x[nt].z : x[nt].x, j & 1 ? x[nt].w : x[nt].y);
                     }
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) x[nt] = next_x[nt];
                 }
                 const uint2 sc = *reinterpret_cast<const uint2 *>(in + kRows * kStep / 2 + 64 * i0 + 8 * g);
                 const float s[4] = {to_f32<BF16>(sc.x & 0xffffu), to_f32<BF16>(sc.x >> 16), to_f32<BF16>(sc.y & 0xffffu), to_f32<BF16>(sc.y >> 16)};
@@ -445,7 +438,7 @@ int isv_linear4_forward(isv_linear4 *l, const void *x_dev, void *y_dev, float *y
     const int rw = M > 4 && l->blocks >= l->sms / 8 ? 4 : 1;
     const int tiles = (l->blocks + rw - 1) / rw, steps = (l->K + kStep - 1) / kStep;
     // Clusters of any size up to 8 share a tile's K.  A round of tiles takes the steps of a warp and about one and a half
-    // steps' time for its start and its sums (eight with 32 columns of sums); the size with the shortest sum of rounds is
+    // steps' time for its start and its sums (with 32 columns of sums eight, and one more for each CTA); the size with the shortest sum of rounds is
     // taken.  Against a cluster of 1 throughout: 4096 x 11008 at one token 12.2 -> 9.1 us, 2560 x 10240 8.0 -> 6.2; against
     // as many CTAs as are resident: 22016 x 4096 at 16 tokens 25.8 -> 23.7.
     const int room = (nt == 1 ? Shape<1, 1>::RESIDENT : nt == 2 ? Shape<2, 1>::RESIDENT : Shape<4, 1>::RESIDENT) * l->sms;
@@ -453,7 +446,7 @@ int isv_linear4_forward(isv_linear4 *l, const void *x_dev, void *y_dev, float *y
     int cluster = 1;
     long long best = 0;
     for (int cs = 1; cs <= kMaxCluster && cs <= std::min(steps, room); ++cs) {
-        const long long rounds = (tiles + room / cs - 1) / (room / cs), cost = rounds * (2 * ((steps + cs * kw - 1) / (cs * kw)) + (nt == 4 ? 16 : 3));
+        const long long rounds = (tiles + room / cs - 1) / (room / cs), cost = rounds * (2 * ((steps + cs * kw - 1) / (cs * kw)) + (nt == 4 ? 16 + 2 * cs : 3));
         if (cs == 1 || cost < best) { best = cost; cluster = cs; }
     }
     cudaLaunchConfig_t cfg = {};
