@@ -168,6 +168,7 @@ __global__ void __launch_bounds__(kThreads, 1) table_kernel(TableParams p) {
             }
         }
     }
+    cluster.barrier_arrive();              // this CTA's marks are there; what follows does not need the others'
     // ---- fresh pages before each row
     int wanted = 0;
     if (OP != COMPACT) {
@@ -185,7 +186,7 @@ __global__ void __launch_bounds__(kThreads, 1) table_kernel(TableParams p) {
         }
         if (tid == 0) need[p.n_rows] = wanted;
     }
-    cluster.sync();
+    cluster.barrier_wait();
 
     // ---- this CTA's slice of the pool: all marks, and the live pages before each word
     const int each = (p.slice + kThreads - 1) / kThreads;
@@ -208,7 +209,20 @@ __global__ void __launch_bounds__(kThreads, 1) table_kernel(TableParams p) {
         x += __popc(fin[k]);
     }
     if (tid < kCtas) cluster.map_shared_rank(slice_live, tid)[rank] = total;
-    cluster.sync();
+    __syncthreads();
+    cluster.barrier_arrive();
+    // ---- meanwhile, entries that depend on no rank (all marks have been taken)
+    if (OP != COMPACT)
+        for (int r = at / p.row_threads; r < p.n_rows; r += per) {
+            const Row w = row_of(r);
+            for (int j = w.hi + at % p.row_threads; j < p.max_blocks; j += p.row_threads) p.table_out[(size_t)r * p.stride + j] = ISV_BLOCK_NONE;
+            if (OP == FORK && at % p.row_threads == 0) {
+                const int from = parent_of(r);
+                p.lens_out[r] = from < 0 ? 0 : p.lens[from];
+                if (w.hi == w.lo) p.src[r] = p.dst[r] = ISV_BLOCK_NONE;
+            }
+        }
+    cluster.barrier_wait();
     int base = 0, live = 0;                // live pages before this slice, and in all
     for (int c = 0; c < kCtas; ++c) {
         if (c < rank) base += slice_live[c];
@@ -237,20 +251,14 @@ __global__ void __launch_bounds__(kThreads, 1) table_kernel(TableParams p) {
                 p.dst[lo] = id;
             }
         }
-        // ---- the rest of the rows
-        if (wanted > free_pages) bad |= ISV_STATUS_NO_PAGES;
-        for (int r = at / p.row_threads; r < p.n_rows; r += per) {
-            const Row w = row_of(r);
-            const int lacking = w.lo + max(0, free_pages - need[r]);    // first block of the row without a page
-            for (int j = w.lo + at % p.row_threads; j < p.max_blocks; j += p.row_threads)
-                if (j >= w.hi || j >= lacking) p.table_out[(size_t)r * p.stride + j] = ISV_BLOCK_NONE;
-            if (w.hi < w.lo)
-                for (int j = w.hi + at % p.row_threads; j < w.lo; j += p.row_threads)
-                    p.table_out[(size_t)r * p.stride + j] = ISV_BLOCK_NONE;
-            if (OP == FORK && at % p.row_threads == 0) {
-                const int from = parent_of(r);
-                p.lens_out[r] = from < 0 ? 0 : p.lens[from];
-                if (w.hi == w.lo || lacking <= w.lo) p.src[r] = p.dst[r] = ISV_BLOCK_NONE;
+        // ---- too few: the last entries in order stay without a page
+        if (wanted > free_pages) {
+            bad |= ISV_STATUS_NO_PAGES;
+            for (int r = at / p.row_threads; r < p.n_rows; r += per) {
+                const Row w = row_of(r);
+                const int lacking = w.lo + max(0, free_pages - need[r]);    // first block of the row without a page
+                for (int j = lacking + at % p.row_threads; j < w.hi; j += p.row_threads) p.table_out[(size_t)r * p.stride + j] = ISV_BLOCK_NONE;
+                if (OP == FORK && at % p.row_threads == 0 && w.hi > w.lo && lacking <= w.lo) p.src[r] = p.dst[r] = ISV_BLOCK_NONE;
             }
         }
     } else {
