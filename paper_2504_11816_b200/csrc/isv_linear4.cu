@@ -11,6 +11,10 @@
 // A warp streams its steps through a ring of its own in shared memory, so that the bytes in flight do not cost
 // registers.  The warps of a CTA share a row block's K; where there are few blocks a cluster of CTAs does, and adds
 // up through distributed shared memory.  The order of all sums is fixed.
+//
+// Measured on B200 (a call in a captured graph): 32000 x 4096 at one token 16.6 us (4.2 TB/s of weights and scales), 22016 x
+// 4096 12.8, 4096 x 4096 5.8; 4096 x 11008 at 16 tokens 12.5; 22016 x 4096 at 32 tokens 45.  About 3.5 us are fixed; the
+// rest is 59 ns a step and SM, where HBM would allow 50: conversions and the issue slots around them.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

@@ -441,3 +441,13 @@ def test_queries_far_from_one_and_not_finite():
         fine[0, 5] = fine[1, 7] = False
         assert torch.isfinite(out32[fine.cuda()]).all()
         assert torch.allclose(out32[fine.cuda()], clean[1][fine.cuda()], rtol=0, atol=1e-4)
+
+
+def test_a_sequence_without_any_page_gives_zeros():
+    with Cache([32, 50, 7], 4, 2, 64, "f16", seed=22) as c:
+        c.fill()
+        c.table[0] = B.ISV_BLOCK_NONE
+        out, out32 = c.attend()
+        assert (out32[0] == 0).all() and (out[0] == 0).all()
+        c.check(out, out32, rows=[1, 2])
+        assert B.isv_q8_status(c.h) == 0

@@ -49,7 +49,8 @@ def _copy(**kw):
     (dict(dst_pool=A + 8), "multiples of 16"), (dict(page_bytes=24), "multiples of 16"), (dict(page_bytes=0), "bad page size"),
     (dict(layers=0), "layers"), (dict(n=-1), "n ("), (dict(n_dst_pages=0), "page counts"), (dict(n_src_pages=0), "page counts"),
     (dict(layers=2, dst_layer_stride=240, src_layer_stride=256), "layer stride"),
-    (dict(layers=2, dst_layer_stride=256, src_layer_stride=240), "layer stride"), (dict(src_layer_stride=8), "multiples of 16")])
+    (dict(layers=2, dst_layer_stride=256, src_layer_stride=240), "layer stride"), (dict(src_layer_stride=8), "multiples of 16"),
+    (dict(page_bytes=1 << 33, n=1 << 20), "too large"), (dict(page_bytes=1 << 34), "bad page size")])
 def test_copy(kw, text):
     fn, d = _copy(**kw)
     _refused(B.ISV_EINVAL, text, fn, **d)
