@@ -458,10 +458,12 @@ struct Visit {
 enum { COPY = 1, OPEN = 2, FIRST = 4, LAST = 8, HEAD = 16, END = 32 };   // FIRST/LAST of the warp's part of an item; HEAD/END of the item itself
 
 // Warps of a CTA: as many as the registers allow without spills (16 x 128 registers at head_dim 128 spilled up to 90 bytes in the
-// loop: 66.9 us instead of 57.4 at 32 sequences x 1088 tokens x 32 heads); ring: 130 to 150 KB in flight per SM.
+// loop: 66.9 us instead of 57.4 at 32 sequences x 1088 tokens x 32 heads; with two tiles 12 instead of 8 at head_dim 80 are
+// worth up to 24 bytes of them: 2 sequences of 7000 to 15287 tokens, 384 / 32 heads, 49.6 -> 42.3); ring: 130 to 150 KB in
+// flight per SM.
 template <int D, int NT>
 struct Shape {
-    static constexpr int NW = NT == 2 ? 8 : D == 128 ? 12 : 16;
+    static constexpr int NW = NT == 2 ? (D == 128 ? 8 : 12) : D == 128 ? 12 : 16;
     static constexpr int UNIT = unit_bytes(D);
     static constexpr int ST = (D == 128 && NT == 1 ? 149 << 10 : 132 << 10) / (NW * UNIT);
     static constexpr int HT = 8 * NT;
