@@ -33,6 +33,7 @@ constexpr int kThreads = 1024;
 constexpr int kMaxRows = 4096;
 constexpr int kMaxDevices = 64;
 constexpr int kCopyThreads = 256, kCopyUnroll = 4;
+constexpr unsigned kCopyMaxGrid = 1u << 20;   // CTAs of a copy along x: the kernel's 32-bit counter of items takes that many past the last
 
 int err(int code, const char *fmt, ...) {
     char buf[512];
@@ -317,7 +318,7 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constan
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int n = p.n_dev ? min(p.n, max(0, *p.n_dev)) : p.n;
-    const uint32_t items = (uint32_t)n * (uint32_t)p.pieces;               // the host checks that they fit
+    const uint32_t items = (uint32_t)n * (uint32_t)p.pieces;               // the host checks that they, and a grid more, fit
     for (int layer = blockIdx.y; layer < p.layers; layer += gridDim.y)
         for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
             const int i = (int)(item / (uint32_t)p.pieces), piece = (int)(item - (uint32_t)i * (uint32_t)p.pieces);
@@ -424,7 +425,7 @@ int isv_pages_copy(void *dst_pool_dev, int32_t n_dst_pages, const void *src_pool
     p.dst_stride = dst_layer_stride / 16; p.src_stride = src_layer_stride / 16; p.page = (int32_t)(page_bytes / 16);
     p.n = n; p.n_dst = n_dst_pages; p.n_src = n_src_pages; p.layers = layers;
     p.pieces = (p.page + kCopyThreads * kCopyUnroll - 1) / (kCopyThreads * kCopyUnroll);
-    if ((unsigned long long)n * (unsigned)p.pieces >= (1ull << 32)) return err(ISV_EINVAL, "isv_pages_copy: n * page_bytes too large");
+    if ((unsigned long long)n * (unsigned)p.pieces >= (1ull << 32) - kCopyMaxGrid) return err(ISV_EINVAL, "isv_pages_copy: n * page_bytes too large");
     const unsigned items = (unsigned)n * (unsigned)p.pieces, rows = (unsigned)std::min(layers, 65535);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(std::max(1u, std::min(items, 148u * 8u / std::min(rows, 148u * 8u))), rows);   // about 8 CTAs an SM
