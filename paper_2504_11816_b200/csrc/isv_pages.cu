@@ -181,7 +181,9 @@ __global__ void __launch_bounds__(kThreads, 1) table_kernel(TableParams p) {
             const Row w = row_of(r);
             sum += max(0, w.hi - w.lo);
         }
-        int x = block_scan(sum, warp_sums, wanted);
+        // A pool has at most ISV_PAGES_MAX pages, so a demand beyond that is counted as that: the scan stays below 2^30, where
+        // long tables could ask for more than 2^31 entries.  Prefixes below n_pages, the only ones that matter, are exact.
+        int x = block_scan(min(sum, ISV_PAGES_MAX), warp_sums, wanted);
         for (int r = tid * each; r < min(tid * each + each, p.n_rows); ++r) {
             const Row w = row_of(r);
             need[r] = x;
