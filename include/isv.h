@@ -458,7 +458,7 @@ int isv_q8_free(isv_q8 *h);
  *     k_dev, v_dev + s * seq_stride + t * token_stride, each [kv_heads][head_dim] 16-bit
  * (strides in elements, multiples of 8).  new_lens_dev NULL = T new tokens for every sequence.  Blocks that
  * are complete afterwards are quantised into the page that block_table_dev ([n_seqs][table_stride],
- * max_blocks_per_seq <= table_stride entries of a row are used) names; the rest goes to the tail slot
+ * max_blocks_per_seq <= table_stride entries of a row are used, at most 2^27 - 2) names; the rest goes to the tail slot
  * tails_dev[s].  A sequence with no new token keeps everything.  Page ids outside [0, n_pages) are skipped
  * and flagged (ISV_STATUS_BAD_BLOCK_ID), also ISV_BLOCK_NONE; lengths are clamped to what the table row
  * and the tail slot hold, 16 * max_blocks_per_seq + 15, and new lengths to [0, min(T, length)], and flagged

@@ -352,7 +352,8 @@ int check_cache(const char *who, const isv_q8 *h, const void *pool, int32_t n_pa
     if (!pool || !tails || !table || !lens) return err(ISV_EINVAL, "%s: pool, tails, table and lengths are required", who);
     if (misaligned(pool) || misaligned(tails)) return err(ISV_EINVAL, "%s: pool and tails must be 16-byte aligned", who);
     if (n_seqs < 0 || n_seqs > h->d.max_seqs) return err(ISV_EINVAL, "%s: n_seqs (%d) must be in [0, %d]", who, n_seqs, h->d.max_seqs);
-    if (n_pages < 1 || max_blocks < 1 || stride < max_blocks || max_blocks >= (1 << 27))
+    // the longest length that a row of max_blocks allows, 16 * max_blocks + 15, is rounded up to whole blocks in 32 bits
+    if (n_pages < 1 || max_blocks < 1 || stride < max_blocks || max_blocks >= (1 << 27) - 1)
         return err(ISV_EINVAL, "%s: bad page count (%d) or table row (%d entries, stride %d)", who, n_pages, max_blocks, stride);
     return ISV_OK;
 }
