@@ -561,6 +561,12 @@ int isv_linear4_forward(isv_linear4 *l, const void *x_dev, void *y_dev, float *y
 /* Waits for `stream` and returns ISV_EDEVICE_STATUS (and clears the status) if a bounded wait inside a kernel
  * of this handle expired since the last query. */
 int isv_linear4_status(isv_linear4 *l, void *stream, uint32_t *status_out);
+/* As isv_set_wait_limit and isv_inject_lost_copy, for the copies of weights of this handle: `polls` of a barrier before
+ * a wait gives up (0 = the built-in default), and launches in which one warp arms a barrier without issuing its copy.  A
+ * warp whose wait runs out issues no more copies, gives those in flight one more bounded chance to land, and leaves
+ * its sums incomplete; the launch ends, isv_linear4_status reports it once, and the handle stays usable. */
+int isv_linear4_set_wait_limit(isv_linear4 *l, uint32_t polls);
+int isv_linear4_inject_lost_copy(isv_linear4 *l, int32_t launches);
 int isv_linear4_free(isv_linear4 *l);
 
 /* Text of the calling thread's last error; valid until its next call. */

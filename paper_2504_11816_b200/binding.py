@@ -49,7 +49,7 @@ EXPORTS = [
     "isv_q8_sizes", "isv_q8_create", "isv_q8_free", "isv_q8_write", "isv_q8_attn", "isv_q8_status",
     "isv_pages_copy", "isv_pages_fork", "isv_pages_resize", "isv_pages_compact",
     "isv_linear4_create", "isv_linear4_forward", "isv_linear4_status",
-    "isv_linear4_free",
+    "isv_linear4_set_wait_limit", "isv_linear4_inject_lost_copy", "isv_linear4_free",
     "isv_last_error",
 ]
 
@@ -176,6 +176,8 @@ def lib():
     L.isv_linear4_create.argtypes = [P(vp), vp, vp, i32, i32, i32, i32, i32, vp]
     L.isv_linear4_forward.argtypes = [vp, vp, vp, vp, i32, vp]
     L.isv_linear4_status.argtypes = [vp, vp, P(ctypes.c_uint32)]
+    L.isv_linear4_set_wait_limit.argtypes = [vp, ctypes.c_uint32]
+    L.isv_linear4_inject_lost_copy.argtypes = [vp, i32]
     L.isv_linear4_free.argtypes = [vp]
     L.isv_last_error.argtypes = []
     L.isv_last_error.restype = ctypes.c_char_p
@@ -472,6 +474,14 @@ def isv_linear4_status(l: int, stream: int = 0) -> int:
     st = ctypes.c_uint32(0)
     _check(lib().isv_linear4_status(l, stream or None, ctypes.byref(st)))
     return st.value
+
+
+def isv_linear4_set_wait_limit(l: int, polls: int):
+    _check(lib().isv_linear4_set_wait_limit(l, polls))
+
+
+def isv_linear4_inject_lost_copy(l: int, launches: int):
+    _check(lib().isv_linear4_inject_lost_copy(l, launches))
 
 
 def isv_linear4_free(l: int):

@@ -21,6 +21,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cstdarg>
 #include <cstdio>
 #include <new>
@@ -63,7 +64,8 @@ constexpr int kChunk = 32;     // k of a chunk: two steps of the matrix instruct
 constexpr int kStep = 128;     // k of a warp's step: four chunks
 constexpr int kWarps = 8;
 constexpr int kMaxCluster = 8;
-constexpr uint32_t kSpin = 1u << 22;
+constexpr uint32_t kSpinLimit = 1u << 22;    // polls before a wait gives up (Linear4Params::spin_limit overrides it)
+constexpr uint32_t kDrainLimit = 1u << 18;   // for each copy that may be in flight behind a lost one: 16 ms and more
 
 __host__ __device__ constexpr int step_bytes(int group) { return kRows * kStep / 2 + kRows * (kStep / group) * 2; }
 
@@ -74,6 +76,8 @@ struct Linear4Params {
     float *y_f32;
     uint32_t *status;
     int32_t M, N, K, blocks;
+    uint32_t spin_limit;       // polls of a barrier before a wait gives up
+    int32_t drop_first_copy;   // failure injection: warp 0 of CTA 0 arms its first slot without issuing the copy
 };
 
 struct PackParams {
@@ -116,8 +120,8 @@ __global__ void pack_kernel(PackParams p) {
 }
 
 __device__ __forceinline__ uint32_t s32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) {
-    for (uint32_t i = 0; i < kSpin; ++i) {
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, uint32_t limit) {
+    for (uint32_t i = 0; i < limit; ++i) {
         uint32_t ok;
         asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}\n"
                      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
@@ -126,8 +130,10 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) {
     }
     return false;
 }
-__device__ __forceinline__ void copy_in(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
+__device__ __forceinline__ void arm(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy_in(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                  ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
@@ -206,7 +212,8 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<NT, RW>::RESIDENT) linear4_
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
     const int rw = warp % RW, kw = warp / RW, m0 = blockIdx.y * COLS;
     const int steps = (p.K + kStep - 1) / kStep, tiles = (p.blocks + RW - 1) / RW, stride = gridDim.x / cs;
-    const int first = steps * rank / cs + kw, end = steps * (rank + 1) / cs;
+    const int first = steps * rank / cs + kw;
+    int end = steps * (rank + 1) / cs;
 
     uint8_t *mine = ring + warp * SH::RING * BYTES;
     const uint32_t bar0 = s32(bars + warp * SH::RING);
@@ -216,9 +223,12 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<NT, RW>::RESIDENT) linear4_
     int next_tile = blockIdx.x / cs, next_step = first;
     const uint8_t *next = p.w + ((size_t)(next_tile * RW + rw) * steps + first) * BYTES;
     bool fetching = first < end && next_tile * RW + rw < p.blocks;
-    auto fetch = [&](int slot) {
+    auto fetch = [&](int slot, bool drop) {
         if (!fetching) return;
-        if (lane == 0) copy_in(s32(mine + slot * BYTES), next, BYTES, bar0 + 8 * slot);
+        if (lane == 0) {
+            arm(bar0 + 8 * slot, BYTES);
+            if (!drop) copy_in(s32(mine + slot * BYTES), next, BYTES, bar0 + 8 * slot);
+        }
         next_step += KW;
         next += KW * BYTES;
         if (next_step >= end) {
@@ -229,7 +239,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<NT, RW>::RESIDENT) linear4_
         }
     };
 #pragma unroll 1
-    for (int i = 0; i < SH::RING; ++i) fetch(i);   // the weights do not change: they are on their way before the predecessor has ended
+    for (int i = 0; i < SH::RING; ++i) fetch(i, p.drop_first_copy && i + warp + blockIdx.x + blockIdx.y == 0);   // the weights do not change: they are on their way before the predecessor has ended
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
@@ -244,7 +254,6 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<NT, RW>::RESIDENT) linear4_
     load_x(x, first * kStep);
     int slot = 0;
     uint32_t phase = 0;
-    bool lost = false;
     int turn = 0;
     for (int tile = blockIdx.x / cs; tile < tiles; tile += stride, turn ^= BUF - 1) {
         float total[2][NT][4];
@@ -257,7 +266,20 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<NT, RW>::RESIDENT) linear4_
 #pragma unroll 1
         for (int step = first; step < end && tile * RW + rw < p.blocks; step += KW) {
             const int after = (step + KW < end ? step + KW : first) * kStep;
-            if (!wait(bar0 + 8 * slot, phase)) lost = true;
+            if (!__all_sync(~0u, wait(bar0 + 8 * slot, phase, p.spin_limit))) {
+                // A copy did not arrive in time: the warp issues no more of them, gives those in flight one more bounded
+                // chance, so that none lands in memory that is somebody else's by then (a slot without one takes the whole
+                // limit too), and goes on to the barriers ahead with sums that are incomplete.
+#pragma unroll 1
+                for (int i = 0; i < SH::RING; ++i) {
+                    wait(bar0 + 8 * slot, phase, kDrainLimit);
+                    if (++slot == SH::RING) { slot = 0; phase ^= 1u; }
+                }
+                if (lane == 0) atomicOr(p.status, ISV_STATUS_WAIT_EXPIRED);
+                fetching = false;
+                end = 0;           // no further step, in this tile or another
+                break;
+            }
             const uint8_t *in = mine + slot * BYTES;
 #pragma unroll
             for (int i0 = 0; i0 < GROUPS; ++i0) {
@@ -295,7 +317,7 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<NT, RW>::RESIDENT) linear4_
                         for (int i = 0; i < 4; ++i) total[t][nt][i] += part[t][nt][i] * s[2 * t + (i >> 1)];
             }
             __syncwarp();
-            fetch(slot);
+            fetch(slot, false);
             if (++slot == SH::RING) { slot = 0; phase ^= 1u; }
         }
         float *mine_sums = sums + turn * SH::SUMS;
@@ -326,7 +348,6 @@ __global__ void __launch_bounds__(kWarps * 32, Shape<NT, RW>::RESIDENT) linear4_
         }
         if (BUF == 1) { if (cs > 1) cluster.sync(); else __syncthreads(); }
     }
-    if (lost && lane == 0) atomicOr(p.status, ISV_STATUS_WAIT_EXPIRED);
     if (cs > 1) cluster.sync();   // nobody leaves while its sums may be read
 }
 
@@ -367,6 +388,8 @@ cudaError_t launch(const Linear4Params &p, int group, bool bf16, const cudaLaunc
 struct isv_linear4 {
     int N = 0, K = 0, group = 0, max_M = 0, device = 0, blocks = 0, sms = 0;
     bool bf16 = false;
+    std::atomic<uint32_t> wait_polls{kSpinLimit};
+    std::atomic<int32_t> lost_copies{0};      // failure injection: launches still to lose a copy
     uint8_t *w = nullptr;
     uint32_t *status = nullptr;
 };
@@ -434,6 +457,8 @@ int isv_linear4_forward(isv_linear4 *l, const void *x_dev, void *y_dev, float *y
     p.w = l->w; p.status = l->status; p.x = static_cast<const uint16_t *>(x_dev);
     p.y = static_cast<uint16_t *>(y_dev); p.y_f32 = y_f32_dev;
     p.M = M; p.N = l->N; p.K = l->K; p.blocks = l->blocks;
+    p.spin_limit = l->wait_polls.load();
+    if (l->lost_copies.load() > 0) p.drop_first_copy = l->lost_copies.fetch_sub(1) > 0;
     OnDevice on(l->device);
     if (on.e != cudaSuccess) return err(ISV_ECUDA, "isv_linear4_forward: %s", cudaGetErrorString(on.e));
     const int nt = M <= 8 ? 1 : M <= 16 ? 2 : 4;
@@ -484,6 +509,19 @@ int isv_linear4_status(isv_linear4 *l, void *stream, uint32_t *status_out) {
     }
     if (e != cudaSuccess) return err(ISV_ECUDA, "isv_linear4_status: %s", cudaGetErrorString(e));
     if (*status_out) return err(ISV_EDEVICE_STATUS, "the 4-bit linear kernel reported status 0x%x", *status_out);
+    return ISV_OK;
+}
+
+int isv_linear4_set_wait_limit(isv_linear4 *l, uint32_t polls) {
+    if (!l) return err(ISV_EINVAL, "null handle");
+    l->wait_polls = polls ? polls : kSpinLimit;
+    return ISV_OK;
+}
+
+int isv_linear4_inject_lost_copy(isv_linear4 *l, int32_t launches) {
+    if (!l) return err(ISV_EINVAL, "null handle");
+    if (launches < 0) return err(ISV_EINVAL, "launches must not be negative");
+    l->lost_copies = launches;
     return ISV_OK;
 }
 
