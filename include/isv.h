@@ -482,6 +482,13 @@ int isv_q8_attn(isv_q8 *h, const void *pool_dev, int32_t n_pages, const void *ta
 /* Waits for `stream` and returns ISV_EDEVICE_STATUS (and clears the status) if a call on this handle
  * flagged a problem since the last query. */
 int isv_q8_status(isv_q8 *h, void *stream, uint32_t *status_out);
+/* As isv_set_wait_limit and isv_inject_lost_copy, for the attention's copies: `polls` of a barrier before a wait gives up
+ * (0 = the built-in default), and launches in which the first block of the first sequence (if that has 16 tokens or more)
+ * is armed without issuing its copy.  A warp whose wait runs out issues no more copies, gives those in flight one more
+ * bounded chance to land and goes on without data; the launch ends with incomplete outputs, isv_q8_status reports it
+ * once, and the handle stays usable. */
+int isv_q8_set_wait_limit(isv_q8 *h, uint32_t polls);
+int isv_q8_inject_lost_copy(isv_q8 *h, int32_t launches);
 
 /* ---- pages of a paged cache ------------------------------------------------ */
 

@@ -47,6 +47,7 @@ EXPORTS = [
     "isv_set_host_timeout", "isv_set_wait_limit", "isv_inject_lost_copy",
     "isv_attn_decode_static", "isv_linear_create", "isv_linear_forward", "isv_linear_status", "isv_linear_free",
     "isv_q8_sizes", "isv_q8_create", "isv_q8_free", "isv_q8_write", "isv_q8_attn", "isv_q8_status",
+    "isv_q8_set_wait_limit", "isv_q8_inject_lost_copy",
     "isv_pages_copy", "isv_pages_fork", "isv_pages_resize", "isv_pages_compact",
     "isv_linear4_create", "isv_linear4_forward", "isv_linear4_status",
     "isv_linear4_set_wait_limit", "isv_linear4_inject_lost_copy", "isv_linear4_free",
@@ -169,6 +170,8 @@ def lib():
     L.isv_q8_write.argtypes = [vp, vp, i32, vp, vp, i32, i32, vp, vp, vp, vp, i64, i64, i32, i32, vp]
     L.isv_q8_attn.argtypes = [vp, vp, i32, vp, vp, i32, i32, vp, vp, vp, vp, i32, vp]
     L.isv_q8_status.argtypes = [vp, vp, P(ctypes.c_uint32)]
+    L.isv_q8_set_wait_limit.argtypes = [vp, ctypes.c_uint32]
+    L.isv_q8_inject_lost_copy.argtypes = [vp, i32]
     L.isv_pages_copy.argtypes = [vp, i32, vp, i32, u64, i32, u64, u64, vp, vp, i32, vp, vp, vp]
     L.isv_pages_fork.argtypes = [vp, vp, i32, vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp]
     L.isv_pages_resize.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, vp, vp]
@@ -425,6 +428,14 @@ def isv_q8_status(h: int, stream: int = 0) -> int:
     st = ctypes.c_uint32(0)
     _check(lib().isv_q8_status(h, stream or None, ctypes.byref(st)))
     return st.value
+
+
+def isv_q8_set_wait_limit(h: int, polls: int):
+    _check(lib().isv_q8_set_wait_limit(h, polls))
+
+
+def isv_q8_inject_lost_copy(h: int, launches: int):
+    _check(lib().isv_q8_inject_lost_copy(h, launches))
 
 
 def isv_pages_copy(dst_pool, n_dst_pages: int, src_pool, n_src_pages: int, page_bytes: int, layers: int,

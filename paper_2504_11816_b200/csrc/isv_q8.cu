@@ -5,6 +5,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -49,6 +50,7 @@ struct OnDevice {
     }
 };
 
+constexpr uint32_t kSpinLimit = 1u << 22;   // polls before a wait of the attention kernel gives up, unless isv_q8_set_wait_limit says otherwise
 constexpr int kWriteThreads = 128;
 constexpr int kStaticSmem = 4096;   // room for what the attention kernel declares besides its dynamic shared memory
 
@@ -339,6 +341,8 @@ struct isv_q8 {
     uint32_t *status = nullptr;
     float *part_o = nullptr, *part_ml = nullptr;   // the attention's partial results
     int32_t *tickets = nullptr;
+    std::atomic<uint32_t> wait_polls{kSpinLimit};
+    std::atomic<int32_t> lost_copies{0};           // failure injection: attention launches still to lose a copy
 };
 
 namespace {
@@ -492,6 +496,8 @@ int isv_q8_attn(isv_q8 *h, const void *pool_dev, int32_t n_pages, const void *ta
     p.part_o = h->part_o; p.part_ml = h->part_ml; p.tickets = h->tickets;
     p.Hq = h->d.q_heads; p.P = h->P; p.GT = h->GT;
     p.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)h->d.head_dim));
+    p.spin_limit = h->wait_polls.load();
+    if (h->lost_copies.load() > 0) p.drop_first_copy = h->lost_copies.fetch_sub(1) > 0;
     OnDevice on(h->device);
     if (on.e != cudaSuccess) return err(ISV_ECUDA, "isv_q8_attn: %s", cudaGetErrorString(on.e));
     cudaError_t e = isv::q8::launch_attn(p, h->d.head_dim, h->d.dtype == ISV_BF16, h->d.format == ISV_Q8_E4M3, h->grid,
@@ -512,6 +518,19 @@ int isv_q8_status(isv_q8 *h, void *stream, uint32_t *status_out) {
     }
     if (e != cudaSuccess) return err(ISV_ECUDA, "isv_q8_status: %s", cudaGetErrorString(e));
     if (*status_out) return err(ISV_EDEVICE_STATUS, "a call on the 8-bit cache reported status 0x%x", *status_out);
+    return ISV_OK;
+}
+
+int isv_q8_set_wait_limit(isv_q8 *h, uint32_t polls) {
+    if (!h) return err(ISV_EINVAL, "null handle");
+    h->wait_polls = polls ? polls : kSpinLimit;
+    return ISV_OK;
+}
+
+int isv_q8_inject_lost_copy(isv_q8 *h, int32_t launches) {
+    if (!h) return err(ISV_EINVAL, "null handle");
+    if (launches < 0) return err(ISV_EINVAL, "launches must not be negative");
+    h->lost_copies = launches;
     return ISV_OK;
 }
 

@@ -33,6 +33,8 @@ struct AttnParams {
     int32_t *tickets;           // [grid][heads of a visit], zero between launches
     int32_t Hq, P, GT;          // Hq = Hkv * P * GT; a visit serves GT query heads
     float scale_log2;           // log2(e) / sqrt(D)
+    uint32_t spin_limit;        // polls of a barrier before a wait gives up
+    int32_t drop_first_copy;    // failure injection: the second visit of all, the first block's, is armed without issuing its copy
 };
 
 // Tokens of sequence s, clamped to what its table row and its tail slot hold.

@@ -29,7 +29,7 @@ namespace q8 {
 namespace {
 
 constexpr float kNone = -1.0e30f;            // reference of a head that has no score yet: differences stay finite
-constexpr uint32_t kSpin = 1u << 22;
+constexpr uint32_t kDrainLimit = 1u << 18;   // polls for each copy that may be in flight behind a lost one: 16 ms and more
 constexpr float kSlack = 8.f;                // scores may exceed the reference by this much (log2) before it moves
 constexpr int kFly = 10;                     // partial results that the last merge has in flight
 // Visits below which fewer CTAs, and fewer warps of a CTA, take part: every CTA more is one more partial result to merge (one
@@ -43,16 +43,18 @@ __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
                  : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
-__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity) {
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, uint32_t limit) {
     if (try_wait(bar, parity)) return true;
-    for (uint32_t i = 1; i < kSpin; ++i) {
+    for (uint32_t i = 1; i < limit; ++i) {
         if (try_wait(bar, parity)) return true;
         if (i > 256) __nanosleep(64);
     }
     return false;
 }
-__device__ __forceinline__ void copy_in(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
+__device__ __forceinline__ void arm(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy_in(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                  ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
@@ -592,8 +594,11 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
         if (i == 0) look_up(next + lane);
         const uint64_t src = __shfl_sync(~0u, my_src, i);
         if (lane == i) visits[warp * ST + slot] = my_visit;
-        if (lane == 0 && src && !lost)
-            copy_in(s32(ring + (size_t)(warp * ST + slot) * UNIT), reinterpret_cast<const void *>(src), UNIT, s32(&bars[warp * ST + slot]));
+        if (lane == 0 && src && !lost) {
+            const uint32_t bar = s32(&bars[warp * ST + slot]);
+            arm(bar, UNIT);
+            if (!(p.drop_first_copy && next == 1)) copy_in(s32(ring + (size_t)(warp * ST + slot) * UNIT), reinterpret_cast<const void *>(src), UNIT, bar);
+        }
         ++next;
     };
 
@@ -614,12 +619,15 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
             whole = t.flags & HEAD;
         }
         if (t.flags & COPY) {
-            if (!lost && !wait(s32(&bars[warp * ST + slot]), (phases >> slot) & 1u)) {
+            // all lanes have to agree: what a lane alone had seen arrive would split the warp at the next vote
+            if (!lost && !__all_sync(~0u, wait(s32(&bars[warp * ST + slot]), (phases >> slot) & 1u, p.spin_limit))) {
                 // the copies in flight get one more bounded chance, so that none lands in memory used for something else
+#pragma unroll 1
                 for (int i = 0; i < ST && i < end - v; ++i) {
                     const int x = (slot + i) % ST;
-                    if (visits[warp * ST + x].flags & COPY) wait(s32(&bars[warp * ST + x]), (phases >> x) & 1u);
+                    if (visits[warp * ST + x].flags & COPY) wait(s32(&bars[warp * ST + x]), (phases >> x) & 1u, kDrainLimit);
                 }
+                __syncwarp();
                 lost = true;
                 bad |= ISV_STATUS_WAIT_EXPIRED;
             }
