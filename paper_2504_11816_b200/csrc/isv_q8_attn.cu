@@ -28,7 +28,7 @@ namespace isv {
 namespace q8 {
 namespace {
 
-constexpr float kNone = -1.0e30f;            // reference of a head that has no score yet: differences stay finite
+constexpr float kNone = -3.402823466e38f;    // reference of a head that has no score yet: the lowest number, so that no score lies below it
 constexpr uint32_t kDrainLimit = 1u << 18;   // polls for each copy that may be in flight behind a lost one: 16 ms and more
 constexpr float kSlack = 8.f;                // scores may exceed the reference by this much (log2) before it moves
 constexpr int kFly = 10;                     // partial results that the last merge has in flight

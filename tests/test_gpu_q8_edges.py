@@ -27,3 +27,32 @@ def test_rows_longer_than_32_bit_lengths_are_refused():
         torch.cuda.synchronize()
         c.check(out, None)
         c.check_bytes()
+
+
+def _aligned(c, factor):
+    """Makes every query a multiple of its KV head's first key, so that the scores have that factor's sign, all of them."""
+    g = c.Hq // c.H
+    for s in range(len(c.lens)):
+        for h in range(c.Hq):
+            k = c.k[s][0, h // g].double()
+            c.q[s, h] = (k / k.norm() ** 2 * factor).to(c.dt).cuda()
+
+
+@pytest.mark.parametrize("fmt", [B.ISV_Q8_INT8, B.ISV_Q8_E4M3])
+@pytest.mark.parametrize("factor", [-1e20, -1e31, -1e34, -1e37, 1e34])
+def test_scores_of_any_size(factor, fmt):
+    """One token: whatever its score, the result is its V.  Equal keys: whatever the score, the mean of the V."""
+    for lens in ([1, 15], [16, 47], [3000]):
+        def make(x):
+            x[:] = x[:1]                                                # the same row throughout
+            return x
+        with Cache(lens, 4, 2, 64, "bf16", fmt, seed=31, make=make) as c:
+            c.fill()
+            _aligned(c, factor)
+            out, out32 = c.attend()
+            for s, n in enumerate(lens):
+                _, _, V = c.units(s)
+                want = V.mean(1).repeat(2, 0)
+                # rows of complete blocks and of the open one differ by roundings of their codes; any mean of them lies in between
+                room = 2 * abs(V - V[:, :1]).max() + 1e-5 * abs(V).max()
+                assert abs(out32[s].double().cpu().numpy() - want).max() <= room, (n, factor)
