@@ -65,7 +65,7 @@ constexpr int kStep = 128;     // k of a warp's step: four chunks
 constexpr int kWarps = 8;
 constexpr int kMaxCluster = 8;
 constexpr uint32_t kSpinLimit = 1u << 22;    // polls before a wait gives up (Linear4Params::spin_limit overrides it)
-constexpr uint32_t kDrainLimit = 1u << 18;   // for each copy that may be in flight behind a lost one: 16 ms and more
+constexpr uint32_t kDrainLimit = 1u << 14;   // for each copy that may be in flight behind a lost one: tens of ms
 
 __host__ __device__ constexpr int step_bytes(int group) { return kRows * kStep / 2 + kRows * (kStep / group) * 2; }
 

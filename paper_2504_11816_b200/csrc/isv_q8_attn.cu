@@ -29,7 +29,7 @@ namespace q8 {
 namespace {
 
 constexpr float kNone = -3.402823466e38f;    // reference of a head that has no score yet: the lowest number, so that no score lies below it
-constexpr uint32_t kDrainLimit = 1u << 18;   // polls for each copy that may be in flight behind a lost one: 16 ms and more
+constexpr uint32_t kDrainLimit = 1u << 14;   // polls for each copy that may be in flight behind a lost one: tens of ms
 constexpr float kSlack = 8.f;                // scores may exceed the reference by this much (log2) before it moves
 constexpr int kFly = 10;                     // partial results that the last merge has in flight
 // Visits below which fewer CTAs, and fewer warps of a CTA, take part: every CTA more is one more partial result to merge (one
