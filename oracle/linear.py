@@ -46,3 +46,22 @@ def linear4_error(x, w4: np.ndarray, scales, group: int) -> np.ndarray:
     K = u.shape[1]
     w = np.abs(u - 8.0) * np.repeat(np.abs(to_f64(scales)), group, axis=1)
     return (K + K // group + 64) * 2.0 ** -23 * np.matmul(np.abs(to_f64(x)), w.T)
+
+
+def linear4_typical(x, w4: np.ndarray, scales, group: int) -> np.ndarray:
+    """How far sums in fp32 may be from :func:`linear4`, output by output, when their roundings are independent (what
+    :func:`linear4_error` bounds is the worst case).  A running sum stays near r = root of the sum of the squared terms, or near the
+    largest partial sum where that is more; each of the K / 16 steps rounds by at most 2^-23 of it, and independent
+    roundings add like the root of their number: 4 * sqrt(K / 16) * 2^-23 of it, and 8 more for the last sums."""
+    u = np.empty((w4.shape[0], 2 * w4.shape[1]), np.float64)
+    u[:, 0::2] = w4 & 15
+    u[:, 1::2] = w4 >> 4
+    K = u.shape[1]
+    w = (u - 8.0) * np.repeat(to_f64(scales), group, axis=1)
+    x = to_f64(x)
+    size = np.sqrt(np.matmul(np.square(x), np.square(w).T))
+    part = np.zeros_like(size)
+    for k in range(0, K, group):
+        part += np.matmul(x[:, k:k + group], w[:, k:k + group].T)
+        size = np.maximum(size, np.abs(part))
+    return (8 + 4 * np.sqrt(K / 16)) * 2.0 ** -23 * size

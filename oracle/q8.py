@@ -114,3 +114,30 @@ def attend_error(q: np.ndarray, K: np.ndarray, V: np.ndarray) -> float:
     mag = max(np.max(np.abs(K[h // g]) @ np.abs(q[h])) for h in range(q.shape[0])) / np.sqrt(d)
     e = (d + 3) * 2.0 ** -23 * mag
     return float(2 * np.max(np.abs(V)) * (2 * e + 2.0 ** -20 + 2 * (K.shape[1] + 600) * 2.0 ** -23))
+
+
+def attend_typical(q: np.ndarray, K: np.ndarray, V: np.ndarray) -> np.ndarray:
+    """How far the results [Hq, d] of an evaluation in fp32 may be from :func:`attend`, output by output: several times
+    what independent roundings add up to, where :func:`attend_error` is what they could at worst, for the largest output.
+
+    With weights w, results o and A = sum |q K| / sqrt d of a token: its score is off by a few of the 2^-23 A that its sums
+    and factors round by (4 of them are counted), its weight by 2^-20 of its own on top (2^x, splits into 16-bit parts,
+    units).  An error e of a score moves the result by w e (v - o), and independent ones add like the
+    root of their squares; 4 times that is allowed.  Each of the n / 16 blocks, and each partial result, is one
+    rounded addition to sums that stay below a = sum w |v|: sqrt(n / 16) of 2^-23 a, and 8 more for the
+    products within a block and the last factors."""
+    out = np.zeros(q.shape)
+    n = K.shape[1]
+    if n == 0:
+        return out
+    g, d = q.shape[0] // K.shape[0], q.shape[1]
+    o = attend(q, K, V)
+    for h in range(q.shape[0]):
+        k, v = K[h // g], V[h // g]
+        s = k @ q[h] / np.sqrt(d)
+        w = np.exp(s - s.max())
+        w /= w.sum()
+        e = w * (4 * 2.0 ** -23 * (np.abs(k) @ np.abs(q[h])) / np.sqrt(d) + 2.0 ** -20)
+        spread = np.sqrt(np.square(e) @ np.square(v - o[h]))
+        out[h] = 4 * spread + (8 + np.sqrt(n / BT)) * 2.0 ** -23 * (w @ np.abs(v))
+    return out
