@@ -21,11 +21,16 @@ int set_error(int code, const char *msg);
 
 namespace {
 
+using isv::q8::add2;
 using isv::q8::AttnParams;
 using isv::q8::CacheParams;
+using isv::q8::fma2;
 using isv::q8::kBT;
+using isv::q8::mul2;
+using isv::q8::pair;
 using isv::q8::seq_len;
 using isv::q8::unit_bytes;
+using isv::q8::unpair;
 
 int err(int code, const char *fmt, ...) {
     char buf[512];
@@ -71,34 +76,6 @@ struct WriteParams {
 // are others: nearly every word of a block has one.
 
 constexpr float kMagic = 12582912.f;   // 1.5 * 2^23: adding it rounds to an integer, which is then in the low bits
-
-// Two fp32 numbers in one register pair: the multiplications and additions below take one instruction for both.
-__device__ __forceinline__ uint64_t pair(float x, float y) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
-    return r;
-}
-__device__ __forceinline__ float2 unpair(uint64_t v) {
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-    return r;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-// a * b + c
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
 
 // e4m3 keeps three bits behind the leading one, and below 2^-6 the steps that it has at 2^-6: |q|, below 2^-6 raised by 2^-6,
 // has its borders where the last 20 bits are 0x80000.

@@ -1,13 +1,15 @@
 // Decode attention over the 8-bit cache (isv_q8_attn; layout and formats: include/isv.h).
 //
 // Per (sequence, KV head) and block of 16 tokens, with q of the GT query heads that share the KV head:
-//     S[token][head] = K q^T * (scale_K * log2(e) / sqrt(D)),  p = 2^(S - m),  l += p,  O[dim][head] += V^T (p * scale_V)
+//     S[token][head] = K q^T * (scale_K * log2(e) / sqrt(D)),  p = 2^(S - m),  l += p,  O[dim][head] += (V^T p) * scale_V
 // with a running reference m per head, everything accumulated in fp32.  Both products run on the tensor cores
 // (mma.m16n8k16, fp16 operands) with the cache as the 16-row operand and the query heads as the 8 columns: a
 // visit of one block costs D / 16 instructions for the scores and D / 8 for the output however many of the 8
 // columns are in use, half of what heads as rows would take.  8-bit codes are exact in fp16; q is brought into fp16
-// by a power of two per head (exact but for elements 2^-14 below the largest); p * scale_V goes in as an fp16 value and its
-// fp16 remainder, so its rounding (2^-22) does not show.  The codes lie in memory in the order of the operand
+// by a power of two per head (exact but for elements 2^-14 below the largest).  p goes in as an fp16 value and its fp16
+// remainder, scaled per block and head so that the block's largest weight lies near the top of fp16's range: a weight is then
+// off by 2^-22 of itself, or by 2^-40 of the block's largest, however small the block's weights are next to another one's.  The
+// block's product is scaled back, by scale_V too, as it is added to the output in fp32.  The codes lie in memory in the order of the operand
 // registers, so a lane's operands are 16-byte shared-memory loads without conflicts and nothing is transposed.
 //
 // What bounds it is reading the cache.  All visits of all (sequence, KV head) pairs form one list that is cut into equal ranges,
@@ -31,6 +33,7 @@ namespace {
 constexpr float kNone = -3.402823466e38f;    // reference of a head that has no score yet: the lowest number, so that no score lies below it
 constexpr uint32_t kDrainLimit = 1u << 14;   // polls for each copy that may be in flight behind a lost one: tens of ms
 constexpr float kSlack = 8.f;                // scores may exceed the reference by this much (log2) before it moves
+constexpr float kLeast = -100.f;             // log2 of the smallest unit of a block's weights
 constexpr int kFly = 10;                     // partial results that the last merge has in flight
 // Visits below which fewer CTAs, and fewer warps of a CTA, take part: every CTA more is one more partial result to merge (one
 // sequence of 4096 tokens, 8 heads on one KV head: 18.5 us on 148 CTAs, 11.4 on 32).
@@ -81,6 +84,21 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
         asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
             : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// The same product alone.
+template <bool BF16>
+__device__ __forceinline__ void mma_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    if (BF16)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+            : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+            : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+// acc += t * (f.x, f.y, f.x, f.y)
+__device__ __forceinline__ void add_scaled(float (&acc)[4], const float (&t)[4], uint64_t f) {
+    const float2 a = unpair(fma2(pair(t[0], t[1]), f, pair(acc[0], acc[1]))), b = unpair(fma2(pair(t[2], t[3]), f, pair(acc[2], acc[3])));
+    acc[0] = a.x; acc[1] = a.y; acc[2] = b.x; acc[3] = b.y;
+}
 // 8x8 matrix of 16-bit values across the warp, transposed.
 __device__ __forceinline__ uint32_t transpose(uint32_t x) {
     uint32_t y;
@@ -125,6 +143,10 @@ __device__ __forceinline__ uint32_t pack2(float x, float y) {   // x in the low 
     const __half2 v = __floats2half2_rn(x, y);
     return *reinterpret_cast<const uint32_t *>(&v);
 }
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t x, uint32_t y) {
+    const __nv_bfloat162 m = __hmax2(*reinterpret_cast<const __nv_bfloat162 *>(&x), *reinterpret_cast<const __nv_bfloat162 *>(&y));
+    return *reinterpret_cast<const uint32_t *>(&m);
+}
 template <bool BF16>
 __device__ __forceinline__ float2 unpack2(uint32_t w) {
     return BF16 ? __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(&w)) : __half22float2(*reinterpret_cast<const __half2 *>(&w));
@@ -144,6 +166,9 @@ __device__ __forceinline__ uint32_t split2(float &x, float &y) {
 template <int D, int NT, bool BF16, bool E4M3>
 struct State {
     static constexpr int KS = D / 16, MT = D / 16;
+    // Weights of at most 2^0.25 are multiplied by this as they become fp16: the top of its range.  In an open block with bf16
+    // rows they stay bf16, whose range needs nothing; there it is the sums over 16 large values of V that need room.
+    static constexpr float kUp = 0x1p15f, kUpOpen = BF16 ? 0x1p-8f : kUp;
     float acc[NT][MT][4];
     float m[NT][2], l[NT][2];
     float vref, inv_vref;      // acc is in units of vref, a power of two near the scales of V seen last
@@ -224,10 +249,10 @@ struct State {
         inv_vref = 0.f;
     }
 
-    // Brings acc into units that suit values of scale vs.
+    // Brings acc into units in which values of scale vs stay far inside fp32's range.
     __device__ __forceinline__ void refer(float vs) {
         const float r = vs * inv_vref;
-        if ((r >= 0x1p-7f && r <= 0x1p7f) || vs == 0.f) return;
+        if ((r >= 0x1p-40f && r <= 0x1p40f) || vs == 0.f) return;
         const float now = fmaxf(__uint_as_float(__float_as_uint(vs) & 0x7f800000u), 0x1p-126f);
         const float f = vref / now;
         vref = now;
@@ -240,8 +265,9 @@ struct State {
                 for (int i = 0; i < 4; ++i) acc[nt][mt][i] *= f;
     }
 
-    // Scores of a tile -> weights; moves the reference where a score exceeds it by more than kSlack.
-    __device__ __forceinline__ void weigh(float (&s)[NT][4]) {
+    // Scores of a tile -> weights p, as p = s * unit with a unit of the block per head in which its largest weight is between
+    // 2^-0.25 and 2^0.25 (unless that is below 2^-100); moves the reference where a score exceeds it by more than kSlack.
+    __device__ __forceinline__ void weigh(float (&s)[NT][4], float (&unit)[NT][2]) {
         bool over = false;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -267,9 +293,19 @@ struct State {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[nt][i] = ex2(s[nt][i] - m[nt][i & 1]);
-            l[nt][0] += s[nt][0] + s[nt][2];
-            l[nt][1] += s[nt][1] + s[nt][3];
+            for (int i = 0; i < 4; ++i) s[nt][i] -= m[nt][i & 1];
+            // the unit's exponent needs no more than bf16's bits: two heads in one register; a NaN is left to the weights
+            uint32_t top2 = pack2<true>(fmaxf(fmaxf(s[nt][0], s[nt][2]), kLeast), fmaxf(fmaxf(s[nt][1], s[nt][3]), kLeast));
+#pragma unroll
+            for (int o = 4; o < 32; o *= 2) top2 = max_bf16x2(top2, __shfl_xor_sync(~0u, top2, o));
+            const float top[2] = {__uint_as_float(top2 << 16), __uint_as_float(top2 & 0xffff0000u)};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[nt][i] = ex2(s[nt][i] - top[i & 1]);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                unit[nt][i] = ex2(top[i]);
+                l[nt][i] = fmaf(s[nt][i] + s[nt][i + 2], unit[nt][i], l[nt][i]);
+            }
         }
     }
 
@@ -302,18 +338,22 @@ struct State {
                 const float x = s[nt][i] + odd[nt][i];
                 s[nt][i] = (E4M3 ? x : fmaf(x, 0x1p24f, -q128[nt][i & 1])) * (qf[nt][i & 1] * scale.x);
             }
-        weigh(s);
+        float unit_p[NT][2];
+        weigh(s, unit_p);
         refer(scale.y);
-        const float vr = scale.y * inv_vref;
+        const float vr = scale.y * inv_vref * (1.f / kUp);
         uint32_t hi[NT][2], lo[NT][2];
+        uint64_t back[NT];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                float x = s[nt][2 * i] * vr, y = s[nt][2 * i + 1] * vr;
+                float x = s[nt][2 * i] * kUp, y = s[nt][2 * i + 1] * kUp;
                 hi[nt][i] = transpose(split2<false>(x, y));
                 lo[nt][i] = transpose(pack2<false>(x, y));
             }
+            back[nt] = pair(unit_p[nt][0] * vr, unit_p[nt][1] * vr);
+        }
 #pragma unroll
         for (int p = 0; p < (MT + 1) / 2; ++p) {
             uint32_t w[4];
@@ -326,8 +366,10 @@ struct State {
                 widen<E4M3>(w[2 * i + 1], a1, a3);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
-                    mma<false>(acc[nt][2 * p + i], a0, a1, a2, a3, hi[nt][0], hi[nt][1]);
-                    mma<false>(acc[nt][2 * p + i], a0, a1, a2, a3, lo[nt][0], lo[nt][1]);
+                    float t[4];
+                    mma_first<false>(t, a0, a1, a2, a3, hi[nt][0], hi[nt][1]);
+                    mma<false>(t, a0, a1, a2, a3, lo[nt][0], lo[nt][1]);
+                    add_scaled(acc[nt][2 * p + i], t, back[nt]);
                 }
             }
         }
@@ -377,18 +419,23 @@ struct State {
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int i = 0; i < 4; ++i) s[nt][i] = g + 8 * (i >> 1) < n ? s[nt][i] * scale_log2 : -INFINITY;   // weight 0
-        weigh(s);
+        float unit_p[NT][2];
+        weigh(s, unit_p);
         refer(1.f);
         constexpr int TERMS = BF16 ? 3 : 2;
         uint32_t t[TERMS][NT][2];
+        uint64_t back[NT];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                float x = s[nt][2 * i] * inv_vref, y = s[nt][2 * i + 1] * inv_vref;
+                float x = s[nt][2 * i] * kUpOpen, y = s[nt][2 * i + 1] * kUpOpen;
 #pragma unroll
                 for (int j = 0; j < TERMS; ++j) t[j][nt][i] = transpose(split2<BF16>(x, y));
             }
+            const float f = inv_vref * (1.f / kUpOpen);
+            back[nt] = pair(unit_p[nt][0] * f, unit_p[nt][1] * f);
+        }
         uint32_t w[4][MT];     // dims g * D / 8 + 2 mt, + 1 of tokens 2 c, 2 c + 1, 2 c + 8, 2 c + 9
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -402,9 +449,13 @@ struct State {
             const uint32_t a0 = __byte_perm(w[0][mt], w[1][mt], 0x5410), a1 = __byte_perm(w[0][mt], w[1][mt], 0x7632);
             const uint32_t a2 = __byte_perm(w[2][mt], w[3][mt], 0x5410), a3 = __byte_perm(w[2][mt], w[3][mt], 0x7632);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int nt = 0; nt < NT; ++nt) {
+                float sum[4];
+                mma_first<BF16>(sum, a0, a1, a2, a3, t[0][nt][0], t[0][nt][1]);
 #pragma unroll
-                for (int j = 0; j < TERMS; ++j) mma<BF16>(acc[nt][mt], a0, a1, a2, a3, t[j][nt][0], t[j][nt][1]);
+                for (int j = 1; j < TERMS; ++j) mma<BF16>(sum, a0, a1, a2, a3, t[j][nt][0], t[j][nt][1]);
+                add_scaled(acc[nt][mt], sum, back[nt]);
+            }
         }
     }
 
