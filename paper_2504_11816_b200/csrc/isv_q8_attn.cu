@@ -68,13 +68,6 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
-// (x & mask) ^ flip in one instruction (two immediate operands would make it two)
-__device__ __forceinline__ uint32_t mask_flip(uint32_t x, uint32_t mask, uint32_t flip) {
-    uint32_t y;
-    asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(y) : "r"(x), "r"(mask), "r"(flip));
-    return y;
-}
-
 template <bool BF16>
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     if (BF16)
@@ -122,18 +115,6 @@ __device__ __forceinline__ void widen(uint32_t w, uint32_t &lo, uint32_t &hi) {
     }
 }
 
-// The same for K, where the products can carry an offset: int8 codes + 128 as they are, in the last places of fp16 numbers of
-// exponent 0, i.e. (code + 128) * 2^-24, bytes 0 and 2 first, then 1 and 3.  Three instructions a word instead of five; a score
-// is then 2^24 * (sum - 128 * 2^-24 * sum of q).
-template <bool E4M3>
-__device__ __forceinline__ void widen_k(uint32_t w, uint32_t &lo, uint32_t &hi) {
-    if (E4M3) widen<true>(w, lo, hi);
-    else {
-        lo = mask_flip(w, 0x00ff00ffu, 0x00800080u);
-        hi = mask_flip(w >> 8, 0x00ff00ffu, 0x00800080u);
-    }
-}
-
 template <bool BF16>
 __device__ __forceinline__ uint32_t pack2(float x, float y) {   // x in the low half
     if (BF16) {
@@ -174,7 +155,6 @@ struct State {
     float vref, inv_vref;      // acc is in units of vref, a power of two near the scales of V seen last
     uint32_t q[NT][KS][2];     // q as fp16 operand
     float qf[NT][2];           // what its scores have to be multiplied by
-    float q128[NT][2];         // int8: 128 * the sum of the operand's values
 
     // Raw q operand of k-steps 2 p, 2 p + 1 of head row `row` (16 bytes; the last 8 at head_dim 80).
     __device__ __forceinline__ static uint4 q_words(const uint16_t *row, int p, int c, bool valid) {
@@ -219,25 +199,13 @@ struct State {
                         (&w[p].x)[i] = pack2<false>(v.x * down, v.y * down);
                     }
             }
-            float sum = 0.f;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
-                const uint32_t x = (&w[ks / 2].x)[2 * (ks % 2)], y = (&w[ks / 2].x)[2 * (ks % 2) + 1];
-                q[nt][ks][0] = E4M3 ? x : __byte_perm(x, y, 0x5410);
-                q[nt][ks][1] = E4M3 ? y : __byte_perm(x, y, 0x7632);
-                if (!E4M3) {
-                    const float2 a = unpack2<false>(x), b = unpack2<false>(y);
-                    sum += (a.x + a.y) + (b.x + b.y);
-                }
+                q[nt][ks][0] = (&w[ks / 2].x)[2 * (ks % 2)];
+                q[nt][ks][1] = (&w[ks / 2].x)[2 * (ks % 2) + 1];
             }
             qf[nt][0] = __shfl_sync(~0u, f, 8 * c);        // head 2 c is row 2 c: lanes 8 c ..
             qf[nt][1] = __shfl_sync(~0u, f, 8 * c + 4);
-            if (!E4M3) {
-                sum += __shfl_xor_sync(~0u, sum, 1);
-                sum += __shfl_xor_sync(~0u, sum, 2);
-                q128[nt][0] = 128.f * __shfl_sync(~0u, sum, 8 * c);
-                q128[nt][1] = 128.f * __shfl_sync(~0u, sum, 8 * c + 4);
-            }
 #pragma unroll
             for (int i = 0; i < 2; ++i) { m[nt][i] = kNone; l[nt][i] = 0.f; }
 #pragma unroll
@@ -325,8 +293,8 @@ struct State {
             for (int i = 0; i < 2; ++i) {
                 if (2 * p + i >= KS) break;
                 uint32_t a0, a1, a2, a3;
-                widen_k<E4M3>(w[2 * i], a0, a2);
-                widen_k<E4M3>(w[2 * i + 1], a1, a3);
+                widen<E4M3>(w[2 * i], a0, a2);
+                widen<E4M3>(w[2 * i + 1], a1, a3);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) mma<false>(i ? odd[nt] : s[nt], a0, a1, a2, a3, q[nt][2 * p + i][0], q[nt][2 * p + i][1]);
             }
@@ -335,8 +303,7 @@ struct State {
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float x = s[nt][i] + odd[nt][i];
-                s[nt][i] = (E4M3 ? x : fmaf(x, 0x1p24f, -q128[nt][i & 1])) * (qf[nt][i & 1] * scale.x);
+                s[nt][i] = (s[nt][i] + odd[nt][i]) * (qf[nt][i & 1] * scale.x);
             }
         float unit_p[NT][2];
         weigh(s, unit_p);
@@ -407,9 +374,7 @@ struct State {
                 if (BF16) w = q_words(q0 + (size_t)(nt * 8 + g) * D, p, c, nt * 8 + g < GT);
                 else {
                     const uint32_t (&x)[2] = q[nt][2 * p], (&y)[2] = q[nt][(2 * p + 1) % KS];
-                    w = E4M3 ? make_uint4(x[0], x[1], y[0], y[1])
-                             : make_uint4(__byte_perm(x[0], x[1], 0x5410), __byte_perm(x[0], x[1], 0x7632),
-                                          __byte_perm(y[0], y[1], 0x5410), __byte_perm(y[0], y[1], 0x7632));
+                    w = make_uint4(x[0], x[1], y[0], y[1]);
                 }
                 mma<BF16>(s[nt], a.x, b.x, a.y, b.y, w.x, w.y);
                 if (2 * p + 1 < KS) mma<BF16>(s[nt], a.z, b.z, a.w, b.w, w.z, w.w);

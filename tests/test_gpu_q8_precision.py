@@ -81,3 +81,23 @@ def test_small_weights_on_blocks_of_smaller_values(order, fmt):
             c.fill()
             scores_of_the_first(c, nats)
             near(c)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("mean", [0, 2])
+@pytest.mark.parametrize("d,dtype", [(128, "f16"), (80, "bf16"), (64, "f16")])
+def test_large_channels_of_k(d, dtype, mean, fmt):
+    """Four channels of K are far from zero, q has a mean: the scores are small sums of codes that are small next to 128."""
+    made = [0]
+
+    def make(x):
+        made[0] += 1
+        if made[0] % 2:
+            x[..., 3] += 200
+            x[..., 17] -= 200
+            x[..., 40] += 50
+            x[..., 41] -= 50
+        return x
+    with Cache([4096, 1003], 4, 2, d, dtype, fmt, seed=44, make=make) as c:
+        c.q += mean
+        near(c.fill())
