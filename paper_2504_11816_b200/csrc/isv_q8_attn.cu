@@ -6,7 +6,7 @@
 // (mma.m16n8k16, fp16 operands) with the cache as the 16-row operand and the query heads as the 8 columns: a
 // visit of one block costs D / 16 instructions for the scores and D / 8 for the output however many of the 8
 // columns are in use, half of what heads as rows would take.  8-bit codes are exact in fp16; q is brought into fp16
-// by a power of two per head (exact but for elements 2^-14 below the largest).  p goes in as an fp16 value and its fp16
+// by a power of two per head (exact but for elements 2^-32 below the largest).  p goes in as an fp16 value and its fp16
 // remainder, scaled per block and head so that the block's largest weight lies near the top of fp16's range: a weight is then
 // off by 2^-22 of itself, or by 2^-40 of the block's largest, however small the block's weights are next to another one's.  The
 // block's product is scaled back, by scale_V too, as it is added to the output in fp32.  The codes lie in memory in the order of the operand
@@ -30,7 +30,8 @@ namespace isv {
 namespace q8 {
 namespace {
 
-constexpr float kNone = -3.402823466e38f;    // reference of a head that has no score yet: the lowest number, so that no score lies below it
+constexpr float kMost = 3.402823466e38f;     // the largest number
+constexpr float kNone = -kMost;              // reference of a head that has no score yet: the lowest number, so that no score lies below it
 constexpr uint32_t kDrainLimit = 1u << 14;   // polls for each copy that may be in flight behind a lost one: tens of ms
 constexpr float kSlack = 8.f;                // scores may exceed the reference by this much (log2) before it moves
 constexpr float kLeast = -100.f;             // log2 of the smallest unit of a block's weights
@@ -176,7 +177,7 @@ struct State {
 #pragma unroll
             for (int p = 0; p < (KS + 1) / 2; ++p) w[p] = q_words(row, p, c, valid);
             float f = scale_log2;
-            if (BF16) {   // by a power of two into the range of fp16
+            if (BF16) {   // by a power of two to the top of fp16's range: eight bits of bf16 are exact from 2^-32 of the largest on
                 float top = 0.f;
 #pragma unroll
                 for (int p = 0; p < (KS + 1) / 2; ++p)
@@ -188,15 +189,15 @@ struct State {
                 top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
                 top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
                 int e = (int)(__float_as_uint(top) >> 23) - 127;
-                e = top > 0.f && e < 128 ? max(e, -126) : 0;
-                const float down = e == 127 ? 0x1p-127f : __uint_as_float((uint32_t)(127 - e) << 23);
-                f *= e == -126 ? 0x1p-126f : __uint_as_float((uint32_t)(127 + e) << 23);
+                e = e == 128 ? 0 : max(e, -100);   // not finite, or so small that f would leave the normal range
+                const float up = __uint_as_float((uint32_t)(127 + 15 - e) << 23);
+                f *= __uint_as_float((uint32_t)(127 - 15 + e) << 23);
 #pragma unroll
                 for (int p = 0; p < (KS + 1) / 2; ++p)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const float2 v = unpack2<true>((&w[p].x)[i]);
-                        (&w[p].x)[i] = pack2<false>(v.x * down, v.y * down);
+                        (&w[p].x)[i] = pack2<false>(v.x * up, v.y * up);
                     }
             }
 #pragma unroll
@@ -303,7 +304,9 @@ struct State {
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                s[nt][i] = (s[nt][i] + odd[nt][i]) * (qf[nt][i & 1] * scale.x);
+                // the factor may overflow where no product does
+                const float f = qf[nt][i & 1] * scale.x;
+                s[nt][i] = (s[nt][i] + odd[nt][i]) * (f > kMost ? kMost : f);
             }
         float unit_p[NT][2];
         weigh(s, unit_p);

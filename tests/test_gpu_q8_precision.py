@@ -101,3 +101,31 @@ def test_large_channels_of_k(d, dtype, mean, fmt):
     with Cache([4096, 1003], 4, 2, d, dtype, fmt, seed=44, make=make) as c:
         c.q += mean
         near(c.fill())
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("d", [64, 80, 128])
+def test_queries_whose_elements_lie_far_apart(d, fmt):
+    """One element of each query is 2^10 to 2^30 times the others, on a channel where K is zero: the others make the scores.
+    And rows of q from 2^-120 to 2^100 on keys that bring the scores back to ordinary size."""
+    made = [0]
+
+    def make(x):
+        made[0] += 1
+        if made[0] % 2:
+            x[..., 9] = 0
+        return x
+    with Cache([300, 47, 900], 8, 2, d, "bf16", fmt, seed=45, make=make) as c:
+        c.fill()
+        for h in range(8):
+            c.q[:, h, 9] = 2.0 ** (10 + 3 * h) * (-1) ** h
+        near(c)
+    for e in (-120, -60, 60, 100):
+        made[0] = 0
+
+        def keys(x):
+            made[0] += 1
+            return x * 2.0 ** -e if made[0] % 2 else x
+        with Cache([300, 47], 4, 2, d, "bf16", fmt, seed=46, make=keys) as c:
+            c.q.mul_(2.0 ** e)
+            near(c.fill())
