@@ -153,7 +153,7 @@ struct State {
     static constexpr float kUp = 0x1p15f, kUpOpen = BF16 ? 0x1p-8f : kUp;
     float acc[NT][MT][4];
     float m[NT][2], l[NT][2];
-    float vref, inv_vref;      // acc is in units of vref, a power of two near the scales of V seen last
+    float vref, inv_vref;      // acc is in units of vref, a power of two not far below the largest scale of V seen
     uint32_t q[NT][KS][2];     // q as fp16 operand
     float qf[NT][2];           // what its scores have to be multiplied by
 
@@ -218,10 +218,10 @@ struct State {
         inv_vref = 0.f;
     }
 
-    // Brings acc into units in which values of scale vs stay far inside fp32's range.
+    // Brings acc into units in which values of scale vs do not come near the end of fp32's range.  Units only grow: smaller
+    // values have all of fp32's exponents below, where larger ones, enlarged by a smaller unit, could overflow.
     __device__ __forceinline__ void refer(float vs) {
-        const float r = vs * inv_vref;
-        if ((r >= 0x1p-40f && r <= 0x1p40f) || vs == 0.f) return;
+        if (!(vs > vref * 0x1p40f)) return;
         const float now = fmaxf(__uint_as_float(__float_as_uint(vs) & 0x7f800000u), 0x1p-126f);
         const float f = vref / now;
         vref = now;
@@ -389,7 +389,24 @@ struct State {
             for (int i = 0; i < 4; ++i) s[nt][i] = g + 8 * (i >> 1) < n ? s[nt][i] * scale_log2 : -INFINITY;   // weight 0
         float unit_p[NT][2];
         weigh(s, unit_p);
-        refer(1.f);
+        uint32_t w[4][MT];     // dims g * D / 8 + 2 mt, + 1 of tokens 2 c, 2 c + 1, 2 c + 8, 2 c + 9
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int tok = 2 * c + (j & 1) + 8 * (j >> 1);
+            const uint32_t *row = reinterpret_cast<const uint32_t *>(v + (size_t)tok * D + g * (D / 8));
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) w[j][mt] = tok < n ? row[mt] : 0u;
+        }
+        if (BF16) {            // their largest; an infinity or a NaN counts as the largest number
+            uint32_t top2 = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt) top2 = __vmaxu2(top2, w[j][mt] & 0x7fff7fffu);
+            refer(__uint_as_float(min(__reduce_max_sync(~0u, max(top2 & 0xffffu, top2 >> 16)), 0x7f7fu) << 16));
+        } else {
+            refer(1.f);
+        }
         constexpr int TERMS = BF16 ? 3 : 2;
         uint32_t t[TERMS][NT][2];
         uint64_t back[NT];
@@ -403,14 +420,6 @@ struct State {
             }
             const float f = inv_vref * (1.f / kUpOpen);
             back[nt] = pair(unit_p[nt][0] * f, unit_p[nt][1] * f);
-        }
-        uint32_t w[4][MT];     // dims g * D / 8 + 2 mt, + 1 of tokens 2 c, 2 c + 1, 2 c + 8, 2 c + 9
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int tok = 2 * c + (j & 1) + 8 * (j >> 1);
-            const uint32_t *row = reinterpret_cast<const uint32_t *>(v + (size_t)tok * D + g * (D / 8));
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) w[j][mt] = tok < n ? row[mt] : 0u;
         }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {

@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+from oracle import q8 as oq
 from paper_2504_11816_b200 import binding as B
 from test_gpu_q8 import Cache
 
@@ -56,3 +57,29 @@ def test_scores_of_any_size(factor, fmt):
                 # rows of complete blocks and of the open one differ by roundings of their codes; any mean of them lies in between
                 room = 2 * abs(V - V[:, :1]).max() + 1e-5 * abs(V).max()
                 assert abs(out32[s].double().cpu().numpy() - want).max() <= room, (n, factor)
+
+
+@pytest.mark.parametrize("fmt", [B.ISV_Q8_INT8, B.ISV_Q8_E4M3])
+@pytest.mark.parametrize("sizes", [(1, 1e-37, 2.0 ** -133, 1), (2.0 ** -133, 1e-37, 1, 1e-37), (2.0 ** -133,), (1e-37, 1), (1e30, 1e-37, 1e30)])
+def test_values_whose_blocks_lie_at_the_ends_of_bf16(sizes, fmt):
+    """Ordinary blocks of V before and behind blocks of the smallest and of very large numbers: finite results, as exact as
+    the largest block asks for.  The sizes go round block by block; the open block has the next one."""
+    made = [0]
+
+    def make(x):
+        made[0] += 1
+        if made[0] % 2 == 0:
+            for b in range((x.shape[0] + 15) // 16):
+                y = x[16 * b:16 * b + 16]
+                y.clamp_(-3, 3).div_(3).mul_(sizes[b % len(sizes)])
+        return x
+    lens = [len(sizes) * 16 * 30, 16 * len(sizes) * 2 + 5, 16 * len(sizes), 37, 4]
+    with Cache(lens, 4, 2, 64, "bf16", fmt, seed=33, make=make) as c:
+        c.fill()
+        _, out32 = c.attend()
+        for s in range(len(lens)):
+            _, K, V = c.units(s)
+            q = c.q[s].double().cpu().numpy()
+            off = abs(out32[s].double().cpu().numpy() - oq.attend(q, K, V))
+            # half a step of fp32's smallest numbers, each block's and the products' own
+            assert (off <= oq.attend_typical(q, K, V) + lens[s] * 2.0 ** -148).all(), s
