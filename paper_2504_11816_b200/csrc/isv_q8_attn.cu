@@ -457,26 +457,30 @@ __device__ __forceinline__ void store2(const AttnParams &p, size_t at, float x, 
     if (p.out) *reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(p.out) + at) = pack2<BF16>(x, y);
 }
 
-// The first n (at most N) of some records, each (m, l) and J pairs of output values, into a running result.
+// The first n (at most N) of some records into a running result.  A record is (m, l) and J pairs of output values, which are
+// those of its own tokens alone, divided by its l: their means stay inside the range of V, where a sum over a long history
+// could pass the largest number.
 template <int N, int J>
 __device__ __forceinline__ void merge(const float2 (&ml)[N], const float2 (&v)[N][J], int n, float &m, float &l, float2 (&o)[J]) {
-    float top = m;
+    float top = m, w[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) top = i < n ? fmaxf(top, ml[i].x) : top;
-    const float f = ex2(m - top);
+    const float f = l * ex2(m - top);
     m = top;
-    l *= f;
-#pragma unroll
-    for (int j = 0; j < J; ++j) { o[j].x *= f; o[j].y *= f; }
+    l = f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const float w = ex2(ml[i].x - top);
-        if (i < n) {   // and not where w is 0: a NaN stays one
-            l += w * ml[i].y;
-#pragma unroll
-            for (int j = 0; j < J; ++j) { o[j].x += w * v[i][j].x; o[j].y += w * v[i][j].y; }
-        }
+        w[i] = i < n ? ex2(ml[i].x - top) * ml[i].y : 0.f;
+        l += w[i];
     }
+    const float part = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int j = 0; j < J; ++j) { o[j].x *= f * part; o[j].y *= f * part; }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (i < n)   // and not where w is 0: a NaN stays one
+#pragma unroll
+            for (int j = 0; j < J; ++j) { o[j].x += w[i] * part * v[i][j].x; o[j].y += w[i] * part * v[i][j].y; }
 }
 
 // A visit as the producing lane writes it down for the whole warp.
@@ -696,9 +700,10 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         if (g == 0) rec_ml[warp][which][nt * 8 + 2 * c + i] = make_float2(st.m[nt][i], st.l[nt][i]);
+                        const float f = st.l[nt][i] == 0.f ? 0.f : st.vref / st.l[nt][i];
 #pragma unroll
                         for (int mt = 0; mt < D / 16; ++mt)
-                            o[((nt * 2 + i) * (D / 16) + mt) * 32 + c * 8 + g] = make_float2(st.acc[nt][mt][i] * st.vref, st.acc[nt][mt][i + 2] * st.vref);
+                            o[((nt * 2 + i) * (D / 16) + mt) * 32 + c * 8 + g] = make_float2(st.acc[nt][mt][i] * f, st.acc[nt][mt][i + 2] * f);
                     }
             }
         }
@@ -743,13 +748,12 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
         b = prefix[s] * G + (item - s * G) * nb;
         e = b + nb;
     };
-    auto put = [&](int item, int h, const float2 (&o)[J], float l) {
-        const float f = l == 0.f ? 0.f : 1.f / l;
+    auto put = [&](int item, int h, const float2 (&o)[J]) {
         const size_t at = ((size_t)item * p.GT + h) * D;       // item * GT + h: the flat query head
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const int u = lane + 32 * j;
-            if (u < PAIRS) store2<BF16>(p, at + (u % 8) * (D / 8) + 2 * (u / 8), o[j].x * f, o[j].y * f);
+            if (u < PAIRS) store2<BF16>(p, at + (u % 8) * (D / 8) + 2 * (u / 8), o[j].x, o[j].y);
         }
     };
     // An item that crosses CTAs (only the first and the last of a CTA may): its CTAs' results meet in memory, and the warp
@@ -782,7 +786,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
         int b, e;
         span(item, b, e);
         if (b >= cta_beg && e <= cta_end) {
-            put(item, h, o, l);
+            put(item, h, o);
             continue;
         }
         const int slot = blockIdx.x * 2 + (b > cta_beg ? 1 : 0);
@@ -832,7 +836,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
             }
             merge(ml, v, n - i, m, l, o);
         }
-        put(item, h, o, l);
+        put(item, h, o);
     }
 }
 

@@ -83,3 +83,28 @@ def test_values_whose_blocks_lie_at_the_ends_of_bf16(sizes, fmt):
             off = abs(out32[s].double().cpu().numpy() - oq.attend(q, K, V))
             # half a step of fp32's smallest numbers, each block's and the products' own
             assert (off <= oq.attend_typical(q, K, V) + lens[s] * 2.0 ** -148).all(), s
+
+
+@pytest.mark.parametrize("fmt", [B.ISV_Q8_INT8, B.ISV_Q8_E4M3])
+@pytest.mark.parametrize("sizes", [(3.3e38,), (1, 1e38, 2.0 ** -133), (3e38, 1)])
+@pytest.mark.parametrize("max_ctas", [0, 3])
+def test_sums_of_values_beyond_the_largest_number(max_ctas, sizes, fmt):
+    """The weighted mean of V is finite where the weighted sum over many tokens is not, in one warp and in partial results."""
+    made = [0]
+
+    def make(x):
+        made[0] += 1
+        if made[0] % 2 == 0:
+            for b in range((x.shape[0] + 15) // 16):
+                y = x[16 * b:16 * b + 16]
+                y.clamp_(-3, 3).div_(3).mul_(sizes[b % len(sizes)])
+        return x
+    lens = [5003, 16, 300, 9]
+    with Cache(lens, 8, 2, 128, "bf16", fmt, seed=34, make=make, max_ctas=max_ctas) as c:
+        c.fill()
+        _, out32 = c.attend()
+        for s in range(len(lens)):
+            _, K, V = c.units(s)
+            q = c.q[s].double().cpu().numpy()
+            off = abs(out32[s].double().cpu().numpy() - oq.attend(q, K, V))
+            assert (off <= oq.attend_typical(q, K, V)).all(), s
