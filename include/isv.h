@@ -472,8 +472,9 @@ int isv_q8_write(isv_q8 *h, void *pool_dev, int32_t n_pages, void *tails_dev, co
  * as isv_attn_decode: complete blocks from their pages, the open block from its tail slot.  A sequence of
  * length 0 yields zeros.  q_dev [n_seqs][q_heads][head_dim] 16-bit; out_dev (16-bit) and out_f32_dev (fp32),
  * same shape, may each be NULL, not both.  A block without a page (ISV_BLOCK_NONE) is left out and not
- * flagged; other ids outside [0, n_pages) are left out and flagged.  fp32 arithmetic; the same inputs give
- * the same bits.  Asynchronous on `stream`; may be captured. */
+ * flagged; other ids outside [0, n_pages) are left out and flagged.  fp32 arithmetic, except that over complete
+ * blocks bf16 rows of q are exact from 2^-32 of their largest element on and smaller elements are rounded to
+ * 2^-39 of the power of two below it; the same inputs give the same bits.  Asynchronous on `stream`; may be captured. */
 int isv_q8_attn(isv_q8 *h, const void *pool_dev, int32_t n_pages, const void *tails_dev,
                 const int32_t *block_table_dev, int32_t table_stride, int32_t max_blocks_per_seq,
                 const int32_t *seq_lens_dev, const void *q_dev, void *out_dev, float *out_f32_dev,

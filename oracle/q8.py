@@ -116,7 +116,7 @@ def attend_error(q: np.ndarray, K: np.ndarray, V: np.ndarray) -> float:
     return float(2 * np.max(np.abs(V)) * (2 * e + 2.0 ** -20 + 2 * (K.shape[1] + 600) * 2.0 ** -23))
 
 
-def attend_typical(q: np.ndarray, K: np.ndarray, V: np.ndarray) -> np.ndarray:
+def attend_typical(q: np.ndarray, K: np.ndarray, V: np.ndarray, q_step=None) -> np.ndarray:
     """How far the results [Hq, d] of an evaluation in fp32 may be from :func:`attend`, output by output: several times
     what independent roundings add up to, where :func:`attend_error` is what they could at worst, for the largest output.
 
@@ -125,7 +125,11 @@ def attend_typical(q: np.ndarray, K: np.ndarray, V: np.ndarray) -> np.ndarray:
     units).  An error e of a score moves the result by w e (v - o), and independent ones add like the
     root of their squares; 4 times that is allowed.  Each of the n / 16 blocks, and each partial result, is one
     rounded addition to sums that stay below a = sum w |v|: sqrt(n / 16) of 2^-23 a, and 8 more for the
-    products within a block and the last factors."""
+    products within a block and the last factors.
+
+    q_step [Hq]: where the elements of q are held in a fixed step (rows of bf16 as fp16 numbers whose largest lies in [2^15, 2^16):
+    steps of 2^-24, i.e. 2^-39 of the power of two below the row's largest), half a step of each
+    element is off at most, and a score by that times sum |K| / sqrt d."""
     out = np.zeros(q.shape)
     n = K.shape[1]
     if n == 0:
@@ -138,6 +142,8 @@ def attend_typical(q: np.ndarray, K: np.ndarray, V: np.ndarray) -> np.ndarray:
         w = np.exp(s - s.max())
         w /= w.sum()
         e = w * (4 * 2.0 ** -23 * (np.abs(k) @ np.abs(q[h])) / np.sqrt(d) + 2.0 ** -20)
+        if q_step is not None:
+            e = e + w * q_step[h] / 2 * np.abs(k).sum(1) / np.sqrt(d)
         spread = np.sqrt(np.square(e) @ np.square(v - o[h]))
         out[h] = 4 * spread + (8 + np.sqrt(n / BT)) * 2.0 ** -23 * (w @ np.abs(v))
     return out

@@ -148,9 +148,7 @@ __device__ __forceinline__ uint32_t split2(float &x, float &y) {
 template <int D, int NT, bool BF16, bool E4M3>
 struct State {
     static constexpr int KS = D / 16, MT = D / 16;
-    // Weights of at most 2^0.25 are multiplied by this as they become fp16: the top of its range.  In an open block with bf16
-    // rows they stay bf16, whose range needs nothing; there it is the sums over 16 large values of V that need room.
-    static constexpr float kUp = 0x1p15f, kUpOpen = BF16 ? 0x1p-8f : kUp;
+    static constexpr float kUp = 0x1p15f;   // weights of at most 2^0.25 become fp16 numbers at the top of its range
     float acc[NT][MT][4];
     float m[NT][2], l[NT][2];
     float vref, inv_vref;      // acc is in units of vref, a power of two not far below the largest scale of V seen
@@ -397,13 +395,17 @@ struct State {
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) w[j][mt] = tok < n ? row[mt] : 0u;
         }
-        if (BF16) {            // their largest; an infinity or a NaN counts as the largest number
+        // bf16 needs nothing for the weights; where the values are near an end of its range, their products stay off it
+        float up = kUp;
+        if (BF16) {            // the largest value; an infinity or a NaN counts as the largest number
             uint32_t top2 = 0;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) top2 = __vmaxu2(top2, w[j][mt] & 0x7fff7fffu);
-            refer(__uint_as_float(min(__reduce_max_sync(~0u, max(top2 & 0xffffu, top2 >> 16)), 0x7f7fu) << 16));
+            const float top = __uint_as_float(min(__reduce_max_sync(~0u, max(top2 & 0xffffu, top2 >> 16)), 0x7f7fu) << 16);
+            up = top > 0x1p100f ? 0x1p-8f : top < 0x1p-60f ? 0x1p60f : 1.f;
+            refer(top);
         } else {
             refer(1.f);
         }
@@ -414,11 +416,11 @@ struct State {
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                float x = s[nt][2 * i] * kUpOpen, y = s[nt][2 * i + 1] * kUpOpen;
+                float x = s[nt][2 * i] * up, y = s[nt][2 * i + 1] * up;
 #pragma unroll
                 for (int j = 0; j < TERMS; ++j) t[j][nt][i] = transpose(split2<BF16>(x, y));
             }
-            const float f = inv_vref * (1.f / kUpOpen);
+            const float f = inv_vref / up;
             back[nt] = pair(unit_p[nt][0] * f, unit_p[nt][1] * f);
         }
 #pragma unroll
