@@ -284,7 +284,7 @@ __global__ void __launch_bounds__(kThreads, 1) table_kernel(TableParams p) {
             if (!is_live && id < live) p.dst[id - lb] = id;
             if (is_live && id >= live) p.src[lb - below] = id;
         }
-        for (int i = moves + rank * kThreads + tid; i < p.max_moves; i += kCtas * kThreads) p.src[i] = p.dst[i] = ISV_BLOCK_NONE;
+        for (uint32_t i = moves + rank * kThreads + tid; i < (uint32_t)p.max_moves; i += kCtas * kThreads) p.src[i] = p.dst[i] = ISV_BLOCK_NONE;
         if (rank == 0 && tid == 0) { p.counts[0] = live; p.counts[1] = moves; }
         cluster.sync();                    // all moves are in place
         for (int r = at / p.row_threads; r < p.n_rows; r += per) {
@@ -321,7 +321,7 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constan
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int n = p.n_dev ? min(p.n, max(0, *p.n_dev)) : p.n;
     const uint32_t items = (uint32_t)n * (uint32_t)p.pieces;               // the host checks that they, and a grid more, fit
-    for (int layer = blockIdx.y; layer < p.layers; layer += gridDim.y)
+    for (uint32_t layer = blockIdx.y; layer < (uint32_t)p.layers; layer += gridDim.y)   // unsigned: the last step may pass 2^31
         for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
             const int i = (int)(item / (uint32_t)p.pieces), piece = (int)(item - (uint32_t)i * (uint32_t)p.pieces);
             const int s = p.src_ids[i], d = p.dst_ids ? p.dst_ids[i] : i;
