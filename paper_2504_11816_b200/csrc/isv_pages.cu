@@ -429,8 +429,13 @@ int isv_pages_copy(void *dst_pool_dev, int32_t n_dst_pages, const void *src_pool
     p.pieces = (p.page + kCopyThreads * kCopyUnroll - 1) / (kCopyThreads * kCopyUnroll);
     if ((unsigned long long)n * (unsigned)p.pieces >= (1ull << 32) - kCopyMaxGrid) return err(ISV_EINVAL, "isv_pages_copy: n * page_bytes too large");
     const unsigned items = (unsigned)n * (unsigned)p.pieces, rows = (unsigned)std::min(layers, 65535);
+    int dev = 0, sms = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return err(ISV_ECUDA, "isv_pages_copy: %s", cudaGetErrorString(e));
+    const unsigned room = std::min(8u * (unsigned)sms, kCopyMaxGrid);   // about 8 CTAs an SM
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(std::max(1u, std::min(items, 148u * 8u / std::min(rows, 148u * 8u))), rows);   // about 8 CTAs an SM
+    cfg.gridDim = dim3(std::max(1u, std::min(items, room / std::min(rows, room))), rows);
     cfg.blockDim = dim3(kCopyThreads);
     cfg.stream = static_cast<cudaStream_t>(stream);
     cudaLaunchAttribute attr[1];
@@ -438,7 +443,7 @@ int isv_pages_copy(void *dst_pool_dev, int32_t n_dst_pages, const void *src_pool
     attr[0].val.programmaticStreamSerializationAllowed = 1;   // see the kernel's griddepcontrol pair
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, copy_kernel, p);
+    e = cudaLaunchKernelEx(&cfg, copy_kernel, p);
     return e == cudaSuccess ? ISV_OK : err(ISV_ECUDA, "isv_pages_copy: %s", cudaGetErrorString(e));
 }
 
