@@ -352,6 +352,11 @@ struct State {
         }
     }
 
+    // A pair of 16-bit numbers with zeros for infinities and NaN.
+    __device__ __forceinline__ static uint32_t numbers(uint32_t w) {
+        return w & ~__vcmpgeu2(w & 0x7fff7fffu, BF16 ? 0x7f807f80u : 0x7c007c00u);
+    }
+
     // The open block: n (1 .. 15) rows in 16 bits at k, v (global memory); later rows are not read.  Weights go in as
     // as many 16-bit terms as fp32 has bits for.
     __device__ __forceinline__ void open_block(const uint16_t *k, const uint16_t *v, int n, const uint16_t *q0, int GT,
@@ -397,13 +402,16 @@ struct State {
         }
         // bf16 needs nothing for the weights; where the values are near an end of its range, their products stay off it
         float up = kUp;
-        if (BF16) {            // the largest value; an infinity or a NaN counts as the largest number
-            uint32_t top2 = 0;
+        constexpr uint32_t kInf = BF16 ? 0x7f80u : 0x7c00u;
+        uint32_t top2 = 0;     // the largest magnitude
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int mt = 0; mt < MT; ++mt) top2 = __vmaxu2(top2, w[j][mt] & 0x7fff7fffu);
-            const float top = __uint_as_float(min(__reduce_max_sync(~0u, max(top2 & 0xffffu, top2 >> 16)), 0x7f7fu) << 16);
+            for (int mt = 0; mt < MT; ++mt) top2 = __vmaxu2(top2, w[j][mt] & 0x7fff7fffu);
+        top2 = __reduce_max_sync(~0u, max(top2 & 0xffffu, top2 >> 16));
+        const bool finite = top2 < kInf;
+        if (BF16) {
+            const float top = __uint_as_float(min(top2, kInf - 1) << 16);
             up = top > 0x1p100f ? 0x1p-8f : top < 0x1p-60f ? 0x1p60f : 1.f;
             refer(top);
         } else {
@@ -432,7 +440,11 @@ struct State {
                 float sum[4];
                 mma_first<BF16>(sum, a0, a1, a2, a3, t[0][nt][0], t[0][nt][1]);
 #pragma unroll
-                for (int j = 1; j < TERMS; ++j) mma<BF16>(sum, a0, a1, a2, a3, t[j][nt][0], t[j][nt][1]);
+                for (int j = 1; j < TERMS; ++j) {
+                    if (finite) mma<BF16>(sum, a0, a1, a2, a3, t[j][nt][0], t[j][nt][1]);
+                    // an infinity has met the weight's first term and meets no remainder: that may be 0 or negative
+                    else mma<BF16>(sum, numbers(a0), numbers(a1), numbers(a2), numbers(a3), t[j][nt][0], t[j][nt][1]);
+                }
                 add_scaled(acc[nt][mt], sum, back[nt]);
             }
         }

@@ -7,6 +7,12 @@ from paper_2504_11816_b200 import binding as B
 pytestmark = pytest.mark.gpu
 
 
+@pytest.fixture(autouse=True)
+def _return_the_memory():
+    yield
+    torch.cuda.empty_cache()
+
+
 def _dev(x):
     return torch.tensor(x, dtype=torch.int32, device="cuda")
 

@@ -108,3 +108,44 @@ def test_sums_of_values_beyond_the_largest_number(max_ctas, sizes, fmt):
             q = c.q[s].double().cpu().numpy()
             off = abs(out32[s].double().cpu().numpy() - oq.attend(q, K, V))
             assert (off <= oq.attend_typical(q, K, V)).all(), s
+
+
+@pytest.mark.parametrize("fmt", [B.ISV_Q8_INT8, B.ISV_Q8_E4M3])
+@pytest.mark.parametrize("dtype,hq,hkv,d", [("f16", 4, 2, 64), ("bf16", 8, 1, 128), ("f16", 12, 1, 80), ("bf16", 2, 2, 80)])
+def test_infinities_in_the_open_block(dtype, hq, hkv, d, fmt):
+    """V of a token that is still held in 16 bits: an infinity of either sign gives one in its dim, two of both signs or a NaN
+    give NaN, every other dim is as exact as ever.  K: an infinite score leaves the token out or makes the head NaN."""
+    with Cache([37, 613, 5], hq, hkv, d, dtype, fmt, seed=35) as c:
+        c.fill()
+        inf = float("inf")
+        for s in range(3):
+            for t, x, value in ((0, 3, inf), (2, 5, -inf), (1, 7, inf), (3, 7, -inf), (4, 9, float("nan")), (1, d - 1, inf)):
+                c.tails[s, 1, 0, t, x] = value
+                c.v[s][c.lens[s] // 16 * 16 + t, 0, x] = value
+        _, out32 = c.attend()
+        assert B.isv_q8_status(c.h) == 0
+        g = hq // hkv
+        for s in range(3):
+            _, K, V = c.units(s)
+            q, got = c.q[s].double().cpu().numpy(), out32[s].double().cpu().numpy()
+            assert (got[:g, [3, d - 1]] == inf).all() and (got[:g, 5] == -inf).all()
+            assert (got[:g, [7, 9]] != got[:g, [7, 9]]).all()
+            V = V.copy()
+            V[0][:, [3, 5, 7, 9, d - 1]] = 0
+            got[:g, [3, 5, 7, 9, d - 1]] = 0
+            assert (abs(got - oq.attend(q, K, V)) <= oq.attend_typical(q, K, V)).all(), s
+    with Cache([20, 300], hq, hkv, d, dtype, fmt, seed=36) as c:
+        c.fill()
+        c.q[:, :, 11] = abs(c.q[:, :, 11]) + 0.5
+        for s in range(2):
+            c.tails[s, 0, 0, 1, 11] = -inf                  # the score is -inf: the weight is 0
+        _, out32 = c.attend()
+        for s in range(2):
+            _, K, V = c.units(s)
+            q, got = c.q[s].double().cpu().numpy(), out32[s].double().cpu().numpy()
+            keep = [t for t in range(c.lens[s]) if t != c.lens[s] // 16 * 16 + 1]
+            want, room = oq.attend(q, K[:, keep], V[:, keep]), oq.attend_typical(q, K[:, keep], V[:, keep])
+            assert (abs(got - want) <= room)[:hq // hkv].all(), s
+            c.tails[s, 0, 0, 1, 11] = inf                   # the score is inf
+        _, out32 = c.attend()
+        assert torch.isnan(out32[:, :hq // hkv]).all() and torch.isfinite(out32[:, hq // hkv:]).all()
