@@ -474,7 +474,10 @@ int isv_q8_write(isv_q8 *h, void *pool_dev, int32_t n_pages, void *tails_dev, co
  * same shape, may each be NULL, not both.  A block without a page (ISV_BLOCK_NONE) is left out and not
  * flagged; other ids outside [0, n_pages) are left out and flagged.  fp32 arithmetic, except that over complete
  * blocks bf16 rows of q are exact from 2^-32 of their largest element on and smaller elements are rounded to
- * 2^-39 of the power of two below it; the same inputs give the same bits.  Asynchronous on `stream`; may be captured. */
+ * 2^-39 of the power of two below it; the same inputs give the same bits.  pool, tails, q and outputs are
+ * 16-byte aligned.  With g query heads per KV head and t the largest divisor of g up to 16, the cache is read
+ * g / t times (17 times for g = 17); n_seqs * (max_blocks_per_seq + 3) * kv_heads * g / t must be below 2^31.
+ * Asynchronous on `stream`; may be captured. */
 int isv_q8_attn(isv_q8 *h, const void *pool_dev, int32_t n_pages, const void *tails_dev,
                 const int32_t *block_table_dev, int32_t table_stride, int32_t max_blocks_per_seq,
                 const int32_t *seq_lens_dev, const void *q_dev, void *out_dev, float *out_f32_dev,
@@ -503,6 +506,9 @@ int isv_q8_inject_lost_copy(isv_q8 *h, int32_t launches);
  *   n_pages          pages of the pool, at most ISV_PAGES_MAX; ids outside [0, n_pages) are kept as they are,
  *                    and flagged with ISV_STATUS_BAD_BLOCK_ID unless ISV_BLOCK_NONE
  *   status_dev       optional uint32 into which ISV_STATUS_* bits are ORed
+ * A row that is shortened (isv_pages_resize) to end inside a complete block: where it shares that page, the
+ * caller gives it one of its own, or its next tokens go into the shared one; with open_in_pool = 0 the tokens
+ * that it keeps of the block are stored again, since its tail slot does not hold them.
  * Free pages are handed out lowest id first.  Lengths that are negative or not covered by max_blocks_per_seq
  * are clamped and flagged (ISV_STATUS_BAD_LENGTH).  n_rows <= 4096.  All calls are asynchronous on `stream`,
  * use no memory but what they are given, run on the current device, and may be captured into a CUDA graph.
@@ -522,7 +528,8 @@ int isv_pages_copy(void *dst_pool_dev, int32_t n_dst_pages, const void *src_pool
 /* Row s of the new table (table_out_dev, lens_out_dev; n_rows_out rows, same stride) continues old row
  * parent_dev[s]: the same row again (keep), another one (reorder), one that several rows name (fork), or
  * ISV_BLOCK_NONE for an empty row.  Old rows that nobody continues are freed.  Entries behind a row's blocks
- * become ISV_BLOCK_NONE.  Where rows continue the same parent and its last block is open (open_in_pool = 1
+ * become ISV_BLOCK_NONE; lens_out_dev[s] is the parent's length as it was, also where that had to be clamped.
+ * Where rows continue the same parent and its last block is open (open_in_pool = 1
  * and length mod 16 not 0), the first of them keeps that page and every other one gets a fresh page, in row
  * order; copy_src_dev[s], copy_dst_dev[s] is then the pair for isv_pages_copy, else ISV_BLOCK_NONE twice.
  * Fresh pages may be pages of freed rows.  Without enough free pages the last rows' entries become
@@ -557,7 +564,7 @@ int isv_pages_compact(const int32_t *block_table_dev, const int32_t *lens_dev, i
  * <= 64 tokens: a quarter of the weight bytes that bound a decode step's linear layers at small batches.
  *   w4_dev      uint8 [N][K / 2]: u[n][2 i] in the low and u[n][2 i + 1] in the high four bits of byte i
  *   scales_dev  [N][K / group] 16-bit of `dtype`; group 32, 64 or 128, K a multiple of it; N >= 1
- *   x_dev [M][K] 16-bit;  y_dev [M][N] 16-bit and / or y_f32_dev [M][N] fp32 (one may be NULL)
+ *   x_dev [M][K] 16-bit, 16-byte aligned;  y_dev [M][N] 16-bit and / or y_f32_dev [M][N] fp32 (one may be NULL)
  * isv_linear4_create lays the weights out anew in memory of its own (on `stream`, then waits for it): w4_dev and
  * scales_dev may be freed afterwards.  isv_linear4_forward is asynchronous on the stream it is given, keeps no
  * state between calls (calls may overlap) and may be captured; it runs on the handle's device.  Products are
