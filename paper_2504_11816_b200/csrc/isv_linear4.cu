@@ -1,7 +1,7 @@
 // Decode linear layers with 4-bit weights and a 16-bit scale per (row, group of k): y = x . w^T for a few tokens.
 //
 // The product is bound by reading the weights, half a byte each, and what the SMs have to do per byte is large: turning
-// eight nibbles into 16-bit numbers takes about ten instructions, so the multiplications must not cost any.  They run on
+// eight nibbles into 16-bit numbers takes nine instructions (fp16) or eleven (bf16), so the multiplications must not cost any.  They run on
 // mma.m16n8k16 with 16 weight rows as the rows and 8 tokens as the columns (one token takes as long as eight; tcgen05 would want the widened weights
 // in shared memory, i.e. a store and a load more per weight).  Nibbles become numbers by placing them in the mantissa of
 // 1024 (fp16) or 128 (bf16) and subtracting: exact, as are the products; sums are fp32 and a group's sum is scaled once.
@@ -12,9 +12,10 @@
 // registers.  The warps of a CTA share a row block's K; where there are few blocks a cluster of CTAs does, and adds
 // up through distributed shared memory.  The order of all sums is fixed.
 //
-// Measured on B200 (a call in a captured graph): 32000 x 4096 at one token 16.6 us (4.2 TB/s of weights and scales), 22016 x
-// 4096 12.8, 4096 x 4096 5.8; 4096 x 11008 at 16 tokens 12.5; 22016 x 4096 at 32 tokens 45.  About 3.5 us are fixed; the
-// rest is 59 ns a step and SM, where HBM would allow 50: conversions and the issue slots around them.
+// Measured on B200 (a call in a captured graph): 32000 x 4096 at one token 16.9 us (4.1 TB/s of weights and scales), 22016 x
+// 4096 13.0, 4096 x 4096 5.8; 4096 x 11008 at 16 tokens 12.7; 22016 x 4096 at 32 tokens 45.5.  About 3.5 us are fixed; the
+// rest is 59 ns a step and SM, where HBM would allow 50.  Issue slots are busy to 60 %, HBM to 35 % of its peak: what is
+// left is latency, a warp's chain of wait, conversions and products.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -462,7 +463,7 @@ int isv_linear4_forward(isv_linear4 *l, const void *x_dev, void *y_dev, float *y
     OnDevice on(l->device);
     if (on.e != cudaSuccess) return err(ISV_ECUDA, "isv_linear4_forward: %s", cudaGetErrorString(on.e));
     const int nt = M <= 8 ? 1 : M <= 16 ? 2 : 4;
-    // From four tokens on x is as much traffic as a block's weights: four blocks then share what a CTA reads of it,
+    // From five tokens on x is as much traffic as a block's weights: four blocks then share what a CTA reads of it,
     // if enough CTAs are left.
     const int rw = M > 4 && l->blocks >= l->sms / 8 ? 4 : 1;
     const int tiles = (l->blocks + rw - 1) / rw, steps = (l->K + kStep - 1) / kStep;

@@ -8,7 +8,7 @@
 // memory and counts; the exclusive prefix of those counts gives every page its rank among the free (or live)
 // pages, and a rank says which table entry a free page goes to.  There are no atomics whose order matters.
 // Bound by the latency of five phases that depend on one another (rows, marks, union, ranks, assignment), 1 to 2 us each:
-// resize of 512 rows x 256 blocks in a pool of 65536 pages 8.6 us on B200; eight CTAs of 1024 threads (of 512: 10.7).
+// resize of 512 rows x 256 blocks in a pool of 65536 pages 8.7 us on B200; eight CTAs of 1024 threads (of 512: 10.7).
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 

@@ -246,8 +246,8 @@ __device__ __forceinline__ void quantise(Rows row, uint8_t *unit, int lane) {
 }
 
 // A warp per (sequence, block that its new tokens touch, KV head, K or V).  Measured on B200: 16 prompts of 1024 tokens on
-// average, 32 heads x 128, fp16 to int8: 85.8 us, 4.7 TB/s of rows read and codes written, with 56 % of the issue slots
-// busy; one token for each of 256 sequences, 8 heads x 128, bf16 to e4m3: 9.1 us, the latency of the blocks it completes (2.4
+// average, 32 heads x 128, fp16 to int8: 86.7 us, 4.6 TB/s of rows read and codes written, with 57 % of the issue slots and
+// 50 % of HBM busy, so bound by latency (a warp has nothing in flight while it encodes); one token for each of 256 sequences, 8 heads x 128, bf16 to e4m3: 9.1 us, the latency of the blocks it completes (2.4
 // where none is).
 template <int D, bool BF16, bool E4M3>
 __global__ void __launch_bounds__(kWriteThreads) write_kernel(const __grid_constant__ WriteParams p) {

@@ -17,9 +17,12 @@
 // a unit brings K, V and both scales).  A pair that several warps share leaves partial results that are merged in fixed
 // order, first within the CTA in shared memory, then, for the pairs that cross CTAs, by the warp that arrives last.
 //
-// Measured on B200 (times of a call in a captured graph): 256 sequences x 4111 tokens, 32 query / 8 KV heads x 128, bf16, e4m3:
-// 356 us, 6.1 TB/s; 32 x 1088 tokens, 32 heads x 128, fp16, int8: 54.8 us, 5.2 TB/s; one sequence of 8191 tokens, 32 / 8 heads:
-// 12.7 us, of which the reading would take 2.6.  What is not reading is about 9 us: look-up and first data 4, merges 4.
+// Measured on B200, a call in a captured graph (and among others through the Python binding): 256 sequences x 4111 tokens, 32
+// query / 8 KV heads x 128, bf16, e4m3: 338 to 350 us, 6.4 to 6.2 TB/s (369 us); 32 x 1088 tokens, 32 heads x 128, fp16, int8:
+// 61.5 us, 4.7 TB/s (62.1); one sequence of 8191 tokens, 32 / 8 heads: 13.6 us (13.6), of which the reading would take 2.6.
+// In short calls about 10 us are look-up and first data, and merges.  What keeps fp32's precision (a block's own unit, products
+// added in fp32, K's codes without an offset) takes 7 us of the 32 x 1088 tokens: 54.4 us without it.  There neither HBM (55 %)
+// nor the issue slots (49 %) are full: with three warps a scheduler, a visit's chain of dependent steps is what is left.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -37,7 +40,7 @@ constexpr float kSlack = 8.f;                // scores may exceed the reference 
 constexpr float kLeast = -100.f;             // log2 of the smallest unit of a block's weights
 constexpr int kFly = 10;                     // partial results that the last merge has in flight
 // Visits below which fewer CTAs, and fewer warps of a CTA, take part: every CTA more is one more partial result to merge (one
-// sequence of 4096 tokens, 8 heads on one KV head: 18.5 us on 148 CTAs, 11.4 on 32).
+// sequence of 4096 tokens, 8 heads on one KV head: 18.5 us on 148 CTAs, 11.4 on 32 when this was chosen, 11.8 now).
 constexpr int kMinCtaVisits = 8, kMinVisits = 2;
 
 __device__ __forceinline__ uint32_t s32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -505,10 +508,10 @@ struct Visit {
 };
 enum { COPY = 1, OPEN = 2, FIRST = 4, LAST = 8, HEAD = 16, END = 32 };   // FIRST/LAST of the warp's part of an item; HEAD/END of the item itself
 
-// Warps of a CTA: as many as the registers allow without spills (16 x 128 registers at head_dim 128 spilled up to 90 bytes in the
-// loop: 66.9 us instead of 57.4 at 32 sequences x 1088 tokens x 32 heads; with two tiles 12 instead of 8 at head_dim 80 are
-// worth up to 24 bytes of them: 2 sequences of 7000 to 15287 tokens, 384 / 32 heads, 49.6 -> 42.3); ring: 130 to 150 KB in
-// flight per SM.
+// Warps of a CTA: as many as the registers allow without spills that cost more than the warps bring (32 sequences x 1088
+// tokens x 32 heads x 128: 61.4 us with 12, 65.3 with 11, and 16 spilled up to 90 bytes in the loop; with two tiles 12 instead of
+// 8 at head_dim 64 and 80: 2 sequences of 7000 to 15287 tokens, 384 / 32 heads x 80, 57.7 -> 47.8); ring: 130 to 150 KB in flight
+// per SM.
 template <int D, int NT>
 struct Shape {
     static constexpr int NW = NT == 2 ? (D == 128 ? 8 : 12) : D == 128 ? 12 : 16;
@@ -544,7 +547,7 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
 
     // ---- visits before each sequence: one per block, one without data at the front of each item, which is about what starting
     // and finishing an item costs, and one behind an open block, which costs two (32 ragged rows of 0 to 1152 tokens, 32
-    // heads of 80: 42 us without, 36.8 with the first, 31.3 with both); sequences without any block get their zeros
+    // heads of 80: 42 us without, 36.8 with the first, 31.3 with both when chosen, 31.4 now); sequences without any block get their zeros
     uint32_t bad = 0;
     int carry = 0;
     for (int s0 = 0; s0 < p.c.n_seqs; s0 += THREADS) {
@@ -586,7 +589,8 @@ __global__ void __launch_bounds__(Shape<D, NT>::NW * 32, 1) attn_kernel(const __
     // range of part i of n: the first `rest` parts are one longer
     const int total = carry * G;               // below 2^31: the host checks
     // An item of V visits over C CTAs takes about V / C * 0.1 us of reading and C * 0.07 us of merging: C = 1.2 sqrt(V) has
-    // the shortest sum (one sequence on one KV head: 65536 tokens 21.1 -> 18.1 us, 21041 tokens x 80 17.0 -> 12.6).
+    // the shortest sum (one sequence on one KV head: 65536 tokens 21.1 -> 18.1 us, 21041 tokens x 80 17.0 -> 12.6 when chosen;
+    // 19.1 and 13.4 now).
     int cap = (int)gridDim.x;
     const long long reach = (long long)total * p.c.n_seqs * G;
     if (reach < (long long)gridDim.x * gridDim.x) cap = min(cap, p.c.n_seqs * G + (int)(1.2f * sqrtf((float)reach)));   // items * (1 + 1.2 sqrt(V))
