@@ -1,8 +1,8 @@
 // Decode linear layers with 4-bit weights and a 16-bit scale per (row, group of k): y = x . w^T for a few tokens.
 //
 // The product is bound by reading the weights, half a byte each, and what the SMs have to do per byte is large: turning
-// eight nibbles into 16-bit numbers takes nine instructions (fp16) or eleven (bf16), so the multiplications must not cost any.  They run on
-// mma.m16n8k16 with 16 weight rows as the rows and 8 tokens as the columns (one token takes as long as eight; tcgen05 would want the widened weights
+// eight nibbles into 16-bit numbers takes nine instructions (fp16) or eleven (bf16), so the multiplications must not cost
+// any.  They run on mma.m16n8k16 with 16 weight rows as the rows and 8 tokens as the columns (one token takes as long as eight; tcgen05 would want the widened weights
 // in shared memory, i.e. a store and a load more per weight).  Nibbles become numbers by placing them in the mantissa of
 // 1024 (fp16) or 128 (bf16) and subtracting: exact, as are the products; sums are fp32 and a group's sum is scaled once.
 //

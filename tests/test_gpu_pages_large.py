@@ -13,6 +13,12 @@ def _return_the_memory():
     torch.cuda.empty_cache()
 
 
+def _needs(gb):
+    free, _ = torch.cuda.mem_get_info()
+    if free < gb << 30:
+        pytest.skip(f"{gb} GB of device memory are not free")
+
+
 def _dev(x):
     return torch.tensor(x, dtype=torch.int32, device="cuda")
 
@@ -20,6 +26,7 @@ def _dev(x):
 def test_rows_that_ask_for_more_than_two_to_the_31_pages():
     """17 rows grow by 2^27 - 1 blocks each: 2.28e9 entries are wanted, and a few hundred pages are free.  The first row gets
     them, in order; every other entry becomes ISV_BLOCK_NONE."""
+    _needs(12)
     rows, most, n_pages = 17, 2 ** 27 - 1, 1000
     table = torch.zeros((rows, most), dtype=torch.int32, device="cuda")
     table[16, :7] = torch.arange(100, 107, dtype=torch.int32, device="cuda")
@@ -36,6 +43,7 @@ def test_rows_that_ask_for_more_than_two_to_the_31_pages():
 
 def test_as_many_layers_as_an_int_holds():
     """2^31 - 1 layers of two 16-byte pages: the step from layer to layer passes 2^31 at the end."""
+    _needs(76)
     layers = 2 ** 31 - 1
     pool = torch.zeros((layers, 2, 2), dtype=torch.int64, device="cuda")
     for at in range(0, layers, 1 << 28):
@@ -52,6 +60,7 @@ def test_as_many_layers_as_an_int_holds():
 
 def test_as_many_moves_as_an_int_holds():
     """Lists of 2^31 - 1 moves: the step that fills them up passes 2^31 at the end."""
+    _needs(24)
     m = 2 ** 31 - 1
     table, out = _dev([[5, 0]]), _dev([[9, 9]])
     src, dst = (torch.full((m,), 77, dtype=torch.int32, device="cuda") for _ in range(2))
