@@ -59,6 +59,7 @@ extern "C" {
 
 #define ISV_F16   0
 #define ISV_BF16  1
+#define ISV_F32   2    /* isv_draft_verify only */
 
 #define ISV_BLOCK_NONE      (-1)
 #define ISV_BLOCK_HOST_BIT  (1 << 30)
@@ -69,6 +70,7 @@ extern "C" {
 #define ISV_STATUS_BAD_LENGTH    4u   /* a device-side sequence length was negative or exceeded */
                                       /* the table row; it was clamped to what the row covers  */
 #define ISV_STATUS_NO_PAGES      8u   /* isv_pages_*: fewer free pages than were needed        */
+#define ISV_STATUS_BAD_TOKEN     16u  /* isv_draft_verify: a drafted token outside the vocabulary, or no probability */
 
 typedef struct isv_kv isv_kv;   /* opaque; created by isv_kv_alloc, destroyed by isv_kv_free */
 
@@ -583,6 +585,118 @@ int isv_linear4_status(isv_linear4 *l, void *stream, uint32_t *status_out);
 int isv_linear4_set_wait_limit(isv_linear4 *l, uint32_t polls);
 int isv_linear4_inject_lost_copy(isv_linear4 *l, int32_t launches);
 int isv_linear4_free(isv_linear4 *l);
+
+/* ---- chunks of new tokens over a caller-owned paged cache --------------------- */
+
+/* (The paper has no counterpart: its prefill stage stores keys and values that are given, and its decode stage attends
+ * with one query per sequence.)  For callers that own their pool and block table (isv_attn_decode_static, isv_pages_*):
+ * a chunk of a prompt, drafted tokens that the model is to check, or one token per sequence is stored with the position
+ * rotation applied on the way (isv_chunk_write), its queries attend to the cache and to one another (isv_chunk_attn), and
+ * what of a draft holds is decided (isv_draft_verify), whose lengths isv_pages_resize takes.
+ *
+ * The pool is [n_pages][K|V][kv_heads][16 tokens][head_dim] 16-bit in the order described under "KV pool layout" above,
+ * one layer of it.  Sequence s has seq_lens_dev[s] tokens, the new ones included; its last new_lens_dev[s] <= T of them
+ * (NULL = T of every sequence) are the chunk, at positions seq_lens_dev[s] - new_lens_dev[s] and on.  Their q, k, v and
+ * outputs are rows row_starts_dev[s] and on (NULL = s * T) of arrays of n_rows rows; rows of no sequence are neither read
+ * nor written.  Row strides are in elements, multiples of 8, and hold at least a token's heads: q, k and v may be parts
+ * of one array.
+ * Lengths are clamped to what the table row holds (16 * max_blocks_per_seq), new lengths to [0, min(T, length)] and to the
+ * rows there are, and flagged (ISV_STATUS_BAD_LENGTH).  All pointers but block tables, lengths, starts, prefixes, slopes,
+ * frequencies and positions (aligned to their elements) are 16-byte aligned. */
+#define ISV_ROTARY_HALVES    0   /* element i turns with element i + rotary_dim / 2 */
+#define ISV_ROTARY_ADJACENT  1   /* element 2 i turns with element 2 i + 1          */
+
+typedef struct {
+    int32_t q_heads;             /* query heads; multiple of kv_heads                           */
+    int32_t kv_heads;
+    int32_t head_dim;            /* 64, 80 or 128                                               */
+    int32_t dtype;               /* ISV_F16 or ISV_BF16                                         */
+    int32_t max_seqs;            /* sequences per call, <= 4096                                 */
+    int32_t max_ctas;            /* cap on the attention kernel's grid; 0 = one CTA per SM      */
+    int32_t rotary_dim;          /* leading elements of a head that are turned: a multiple of   */
+                                 /* 16 up to head_dim, 0 = none                                 */
+    int32_t rotary_pairs;        /* ISV_ROTARY_HALVES or ISV_ROTARY_ADJACENT                    */
+    int32_t rotary_axes;         /* position axes, 1 to 4                                       */
+    float   scale;               /* of the scores; 0 = 1 / sqrt(head_dim)                       */
+    float   softcap;             /* cap of the scores; 0 = none                                 */
+} isv_chunk_desc;
+
+typedef struct isv_chunk isv_chunk;
+
+/* Allocates the attention's scratch and a status word on the current device (synchronous).  The handle holds no cache:
+ * any number of layers and pools may be used with it.  isv_chunk_attn calls on one handle share its scratch: order them
+ * on one stream or with events (one handle per stream or captured graph that may overlap another).  Calls run on the
+ * handle's device, whichever is current. */
+int isv_chunk_create(isv_chunk **out, const isv_chunk_desc *desc);
+int isv_chunk_free(isv_chunk *h);
+
+/* Stores the chunk's keys and values of one layer and turns its keys and queries:
+ *     angle_i = position * inv_freq_dev[i],  i < rotary_dim / 2
+ *     (a, b)  ->  (a cos - b sin, b cos + a sin) * magnitude    for the i-th pair of each head of k and q
+ * computed in fp32 (the angle in 64 bits) and rounded once.  V is stored as it is.
+ *   k_dev, v_dev     rows of kv_stride elements, [kv_heads][head_dim] each
+ *   q_dev            rows of q_stride elements, [q_heads][head_dim] each; NULL = there are no queries to turn
+ *   q_out_dev        [n_rows][q_heads][head_dim]; NULL = q_dev is turned in place
+ *   inv_freq_dev     fp32 [rotary_dim / 2], radians per position
+ *   positions_dev    int32 [rotary_axes][n_rows]: positions to turn by; NULL = the token's position in its sequence
+ *   pair_axis_dev    uint8 [rotary_dim / 2]: which axis pair i goes by (images and video: time, height, width; values
+ *                    beyond the last axis mean the last); NULL = axis 0
+ *   magnitude        factor on the turned elements, 1 for none
+ * A token whose block has no page (ISV_BLOCK_NONE or an id outside [0, n_pages)) is not stored, and flagged
+ * (ISV_STATUS_BAD_BLOCK_ID); its query is turned all the same.  The inputs and the pool must not overlap.
+ * Asynchronous on `stream`; may be captured into a CUDA graph; calls may overlap. */
+int isv_chunk_write(isv_chunk *h, void *pool_dev, int32_t n_pages, const int32_t *block_table_dev, int32_t table_stride,
+                    int32_t max_blocks_per_seq, const int32_t *seq_lens_dev, const int32_t *new_lens_dev,
+                    const int32_t *row_starts_dev, int32_t n_rows, const void *k_dev, const void *v_dev, int64_t kv_stride,
+                    const void *q_dev, int64_t q_stride, void *q_out_dev, const float *inv_freq_dev,
+                    const int32_t *positions_dev, const uint8_t *pair_axis_dev, float magnitude, int32_t n_seqs, int32_t T,
+                    void *stream);
+
+/* out[row][h] = softmax over the visible j of score(j), times V:
+ *     x = (q . K_j) * scale;  if softcap > 0: x = softcap * tanh(x / softcap);  score(j) = x - slopes_dev[h] * |p - j|
+ * for the query at position p of its sequence, p the chunk's first position and on.  Visible are the tokens with
+ *     j <= p and (window = 0 or p - j < window), and those with j < prefix_lens_dev[s]
+ * (a prefix that all queries see, later ones too), as far as they exist.  slopes_dev: fp32 [q_heads], or NULL;
+ * prefix_lens_dev: int32 [n_seqs], or NULL.  Query head h reads KV head h / (q_heads / kv_heads).  out_dev (16-bit) and
+ * out_f32_dev (fp32) are [n_rows][q_heads][head_dim] and may each be NULL, not both.  A block without a page
+ * (ISV_BLOCK_NONE) is left out and not flagged; other ids outside [0, n_pages) are left out and flagged.  A query that
+ * sees nothing yields zeros.  What stands in invisible tokens, infinities and NaN too, changes nothing.
+ * Asynchronous on `stream`; may be captured. */
+int isv_chunk_attn(isv_chunk *h, const void *pool_dev, int32_t n_pages, const int32_t *block_table_dev, int32_t table_stride,
+                   int32_t max_blocks_per_seq, const int32_t *seq_lens_dev, const int32_t *new_lens_dev,
+                   const int32_t *row_starts_dev, int32_t n_rows, const void *q_dev, int64_t q_stride, const float *slopes_dev,
+                   const int32_t *prefix_lens_dev, int32_t window, void *out_dev, float *out_f32_dev, int32_t n_seqs, int32_t T,
+                   void *stream);
+
+/* Waits for `stream` and returns ISV_EDEVICE_STATUS (and clears the status) if a call on this handle flagged a problem
+ * since the last query. */
+int isv_chunk_status(isv_chunk *h, void *stream, uint32_t *status_out);
+
+/* Which drafted tokens the target model's probabilities let stand, and the token behind them, so that the result is
+ * distributed as the target's own tokens (given uniforms in [0, 1) that are independent of everything else).  With
+ * n = n_draft_dev[s] <= max_draft drafts x_0 .. x_(n-1), target rows p_0 .. p_n and draft rows q_0 .. q_(n-1):
+ *     a = the first i < n for which u_i * q_i(x_i) < p_i(x_i) does not hold, or n
+ *     next token: drawn from max(p_a - q_a, 0) where a < n (from p_a if that is 0 everywhere), from p_n where a = n
+ * A draw takes the lowest index whose running sum exceeds u * total, with u = uniforms[s][max_draft].  Sums are taken in
+ * 64 bits; probabilities that are negative or NaN count as 0, and need not sum to 1.
+ *   target_dev     rows of vocab probabilities: rows row_starts_dev[s] .. + n (NULL = from s * (max_draft + 1) on) of n_rows
+ *   draft_dev      [n_seqs][max_draft][vocab]; NULL = the drafts were certain (looked up, or the draft's best token):
+ *                  q_i is 1 at x_i and 0 elsewhere.  dtype of both: ISV_F32, ISV_F16 or ISV_BF16
+ *   drafted_dev    int32 [n_seqs][max_draft];  n_draft_dev int32 [n_seqs];  uniforms_dev fp32 [n_seqs][max_draft + 1]
+ *   tokens_dev     int32 [n_seqs][max_draft + 1]: the a drafts that stand, the next token, then -1
+ *   accepted_dev   int32 [n_seqs]: a
+ *   lens_out_dev   int32 [n_seqs] or NULL: seq_lens_dev[s] - n + a, the length to keep (isv_pages_resize) of a cache in
+ *                  which all n drafts stand
+ *   status_dev     optional uint32 into which ISV_STATUS_* bits are ORed
+ * A drafted token outside [0, vocab) does not stand (ISV_STATUS_BAD_TOKEN).  Where all of a row's probabilities are 0 the
+ * next token is -1 (ISV_STATUS_BAD_TOKEN).  Counts outside [0, max_draft] and rows that are not there are clamped and
+ * flagged (ISV_STATUS_BAD_LENGTH); a sequence without any row gets no token.  max_draft <= 1024.  Probabilities are aligned
+ * to their elements.  Uses no memory but what it is given and runs on the current device; asynchronous on `stream`; may be
+ * captured; results do not depend on scheduling. */
+int isv_draft_verify(const void *target_dev, const int32_t *row_starts_dev, int32_t n_rows, const void *draft_dev,
+                     int32_t vocab, int32_t dtype, const int32_t *drafted_dev, const int32_t *n_draft_dev,
+                     const float *uniforms_dev, const int32_t *seq_lens_dev, int32_t n_seqs, int32_t max_draft,
+                     int32_t *tokens_dev, int32_t *accepted_dev, int32_t *lens_out_dev, uint32_t *status_dev, void *stream);
 
 /* Text of the calling thread's last error; valid until its next call. */
 const char *isv_last_error(void);

@@ -28,15 +28,19 @@ ISV_EDEVICE_STATUS = -7
 ISV_ENODEVICE = -8
 ISV_F16 = 0
 ISV_BF16 = 1
+ISV_F32 = 2
 ISV_BLOCK_NONE = -1
 ISV_BLOCK_HOST_BIT = 1 << 30
 ISV_STATUS_BAD_BLOCK_ID = 1
 ISV_STATUS_WAIT_EXPIRED = 2
 ISV_STATUS_BAD_LENGTH = 4
 ISV_STATUS_NO_PAGES = 8
+ISV_STATUS_BAD_TOKEN = 16
 ISV_Q8_INT8 = 0
 ISV_Q8_E4M3 = 1
 ISV_PAGES_MAX = 1 << 20
+ISV_ROTARY_HALVES = 0
+ISV_ROTARY_ADJACENT = 1
 
 EXPORTS = [
     "isv_kv_alloc", "isv_kv_free", "isv_kv_reset", "isv_kv_info", "isv_kv_fill", "isv_kv_fill_async",
@@ -51,6 +55,7 @@ EXPORTS = [
     "isv_pages_copy", "isv_pages_fork", "isv_pages_resize", "isv_pages_compact",
     "isv_linear4_create", "isv_linear4_forward", "isv_linear4_status",
     "isv_linear4_set_wait_limit", "isv_linear4_inject_lost_copy", "isv_linear4_free",
+    "isv_chunk_create", "isv_chunk_free", "isv_chunk_write", "isv_chunk_attn", "isv_chunk_status", "isv_draft_verify",
     "isv_last_error",
 ]
 
@@ -112,6 +117,12 @@ class FillTimes(ctypes.Structure):
 class Q8Desc(ctypes.Structure):
     _fields_ = [(name, ctypes.c_int32) for name in
                 ("q_heads", "kv_heads", "head_dim", "dtype", "format", "max_seqs", "max_ctas")]
+
+
+class ChunkDesc(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in
+                ("q_heads", "kv_heads", "head_dim", "dtype", "max_seqs", "max_ctas", "rotary_dim", "rotary_pairs", "rotary_axes")]
+    _fields_ += [("scale", ctypes.c_float), ("softcap", ctypes.c_float)]
 
 
 _lib = None
@@ -182,6 +193,13 @@ def lib():
     L.isv_linear4_set_wait_limit.argtypes = [vp, ctypes.c_uint32]
     L.isv_linear4_inject_lost_copy.argtypes = [vp, i32]
     L.isv_linear4_free.argtypes = [vp]
+    f32 = ctypes.c_float
+    L.isv_chunk_create.argtypes = [P(vp), P(ChunkDesc)]
+    L.isv_chunk_free.argtypes = [vp]
+    L.isv_chunk_write.argtypes = [vp, vp, i32, vp, i32, i32, vp, vp, vp, i32, vp, vp, i64, vp, i64, vp, vp, vp, vp, f32, i32, i32, vp]
+    L.isv_chunk_attn.argtypes = [vp, vp, i32, vp, i32, i32, vp, vp, vp, i32, vp, i64, vp, vp, i32, vp, vp, i32, i32, vp]
+    L.isv_chunk_status.argtypes = [vp, vp, P(ctypes.c_uint32)]
+    L.isv_draft_verify.argtypes = [vp, vp, i32, vp, i32, i32, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp]
     L.isv_last_error.argtypes = []
     L.isv_last_error.restype = ctypes.c_char_p
     for name in EXPORTS:
@@ -497,6 +515,48 @@ def isv_linear4_inject_lost_copy(l: int, launches: int):
 
 def isv_linear4_free(l: int):
     _check(lib().isv_linear4_free(l))
+
+
+def isv_chunk_create(**kw) -> int:
+    """Fields of ``isv_chunk_desc`` as keyword arguments (``rotary_axes`` is 1 if not given); returns the handle."""
+    h = ctypes.c_void_p()
+    _check(lib().isv_chunk_create(ctypes.byref(h), ctypes.byref(ChunkDesc(**{"rotary_axes": 1, **kw}))))
+    return h.value
+
+
+def isv_chunk_free(h: int):
+    _check(lib().isv_chunk_free(h))
+
+
+def isv_chunk_write(h: int, pool, n_pages: int, block_table, table_stride: int, max_blocks_per_seq: int, seq_lens, new_lens, row_starts,
+                    n_rows: int, k, v, kv_stride: int, q, q_stride: int, q_out, inv_freq, positions, pair_axis, magnitude: float,
+                    n_seqs: int, T: int, stream: int = 0):
+    """Stores a chunk of new tokens per sequence, keys and queries turned by their positions (see ``include/isv.h``)."""
+    _check(lib().isv_chunk_write(h, _ptr(pool), n_pages, _ptr(block_table), table_stride, max_blocks_per_seq, _ptr(seq_lens),
+                                 _ptr(new_lens), _ptr(row_starts), n_rows, _ptr(k), _ptr(v), kv_stride, _ptr(q), q_stride,
+                                 _ptr(q_out), _ptr(inv_freq), _ptr(positions), _ptr(pair_axis), magnitude, n_seqs, T, stream or None))
+
+
+def isv_chunk_attn(h: int, pool, n_pages: int, block_table, table_stride: int, max_blocks_per_seq: int, seq_lens, new_lens, row_starts,
+                   n_rows: int, q, q_stride: int, slopes, prefix_lens, window: int, out, out_f32, n_seqs: int, T: int, stream: int = 0):
+    """Attention of a chunk of new tokens over the paged cache that holds them already."""
+    _check(lib().isv_chunk_attn(h, _ptr(pool), n_pages, _ptr(block_table), table_stride, max_blocks_per_seq, _ptr(seq_lens),
+                                _ptr(new_lens), _ptr(row_starts), n_rows, _ptr(q), q_stride, _ptr(slopes), _ptr(prefix_lens), window,
+                                _ptr(out), _ptr(out_f32), n_seqs, T, stream or None))
+
+
+def isv_chunk_status(h: int, stream: int = 0) -> int:
+    st = ctypes.c_uint32(0)
+    _check(lib().isv_chunk_status(h, stream or None, ctypes.byref(st)))
+    return st.value
+
+
+def isv_draft_verify(target, row_starts, n_rows: int, draft, vocab: int, dtype: int, drafted, n_draft, uniforms, seq_lens, n_seqs: int,
+                     max_draft: int, tokens, accepted, lens_out, status=None, stream: int = 0):
+    """Which drafted tokens stand, the token behind them, and the lengths that the cache keeps."""
+    _check(lib().isv_draft_verify(_ptr(target), _ptr(row_starts), n_rows, _ptr(draft), vocab, dtype, _ptr(drafted), _ptr(n_draft),
+                                  _ptr(uniforms), _ptr(seq_lens), n_seqs, max_draft, _ptr(tokens), _ptr(accepted), _ptr(lens_out),
+                                  _ptr(status), stream or None))
 
 
 def desc_from_workload(w, **overrides) -> dict:
