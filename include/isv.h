@@ -671,6 +671,12 @@ int isv_chunk_attn(isv_chunk *h, const void *pool_dev, int32_t n_pages, const in
 /* Waits for `stream` and returns ISV_EDEVICE_STATUS (and clears the status) if a call on this handle flagged a problem
  * since the last query. */
 int isv_chunk_status(isv_chunk *h, void *stream, uint32_t *status_out);
+/* As isv_set_wait_limit and isv_inject_lost_copy, for the attention's copies: `polls` of a barrier before a wait gives up
+ * (0 = the built-in default), and launches in which a page of the first CTA's first visit is expected and not copied.  A CTA
+ * in which a wait runs out gives the copies in flight one more bounded chance to land and leaves; the launch ends with
+ * incomplete outputs, isv_chunk_status reports it once, and the handle stays usable. */
+int isv_chunk_set_wait_limit(isv_chunk *h, uint32_t polls);
+int isv_chunk_inject_lost_copy(isv_chunk *h, int32_t launches);
 
 /* Which drafted tokens the target model's probabilities let stand, and the token behind them, so that the result is
  * distributed as the target's own tokens (given uniforms in [0, 1) that are independent of everything else).  With

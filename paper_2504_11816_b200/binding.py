@@ -55,7 +55,8 @@ EXPORTS = [
     "isv_pages_copy", "isv_pages_fork", "isv_pages_resize", "isv_pages_compact",
     "isv_linear4_create", "isv_linear4_forward", "isv_linear4_status",
     "isv_linear4_set_wait_limit", "isv_linear4_inject_lost_copy", "isv_linear4_free",
-    "isv_chunk_create", "isv_chunk_free", "isv_chunk_write", "isv_chunk_attn", "isv_chunk_status", "isv_draft_verify",
+    "isv_chunk_create", "isv_chunk_free", "isv_chunk_write", "isv_chunk_attn", "isv_chunk_status",
+    "isv_chunk_set_wait_limit", "isv_chunk_inject_lost_copy", "isv_draft_verify",
     "isv_last_error",
 ]
 
@@ -199,6 +200,8 @@ def lib():
     L.isv_chunk_write.argtypes = [vp, vp, i32, vp, i32, i32, vp, vp, vp, i32, vp, vp, i64, vp, i64, vp, vp, vp, vp, f32, i32, i32, vp]
     L.isv_chunk_attn.argtypes = [vp, vp, i32, vp, i32, i32, vp, vp, vp, i32, vp, i64, vp, vp, i32, vp, vp, i32, i32, vp]
     L.isv_chunk_status.argtypes = [vp, vp, P(ctypes.c_uint32)]
+    L.isv_chunk_set_wait_limit.argtypes = [vp, ctypes.c_uint32]
+    L.isv_chunk_inject_lost_copy.argtypes = [vp, i32]
     L.isv_draft_verify.argtypes = [vp, vp, i32, vp, i32, i32, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp, vp]
     L.isv_last_error.argtypes = []
     L.isv_last_error.restype = ctypes.c_char_p
@@ -549,6 +552,14 @@ def isv_chunk_status(h: int, stream: int = 0) -> int:
     st = ctypes.c_uint32(0)
     _check(lib().isv_chunk_status(h, stream or None, ctypes.byref(st)))
     return st.value
+
+
+def isv_chunk_set_wait_limit(h: int, polls: int):
+    _check(lib().isv_chunk_set_wait_limit(h, polls))
+
+
+def isv_chunk_inject_lost_copy(h: int, launches: int):
+    _check(lib().isv_chunk_inject_lost_copy(h, launches))
 
 
 def isv_draft_verify(target, row_starts, n_rows: int, draft, vocab: int, dtype: int, drafted, n_draft, uniforms, seq_lens, n_seqs: int,

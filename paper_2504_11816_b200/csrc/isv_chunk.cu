@@ -3,6 +3,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -44,6 +45,7 @@ struct OnDevice {
 // ---------------------------------------------------------------- storing a chunk
 
 constexpr int kWriteThreads = 256;
+constexpr uint32_t kSpinLimit = 1u << 22;   // polls before a wait of the attention kernel gives up, unless isv_chunk_set_wait_limit says otherwise
 
 struct WriteParams {
     CacheParams c;
@@ -132,98 +134,6 @@ __global__ void __launch_bounds__(kWriteThreads) write_kernel(const WriteParams 
     dst[place<D>(c1, slot)] = x[1];
 }
 
-// ---------------------------------------------------------------- attention, one row of one head after another
-
-// A warp per (new token, query head): lanes take the 32 tokens of two pages for the scores, and pairs of dims for the
-// sums, which are kept in 64 bits.
-template <int D, bool BF16>
-__device__ void attend_row(const AttnParams &a, int s, const Seq &q, int t, int h) {
-    constexpr int J = (D / 2 + 31) / 32;
-    const int lane = threadIdx.x & 31, kvh = h / (a.c.Hq / a.c.Hkv);
-    const int p = q.start + t;
-    const long long row = q.first + t;
-    const Sight v = sight_of(a, s, q, p);
-    const uint4 *qrow = reinterpret_cast<const uint4 *>(a.q + row * a.q_stride + h * D);
-    const float slope = a.slopes ? a.slopes[h] : 0.f;
-    float m = -INFINITY;
-    double l = 0, o[J][2] = {};
-    for (int j0 = (v.prefix ? 0 : v.low) / kBT * kBT; j0 < v.lim; j0 += 32) {
-        const int j = j0 + lane, slot = j % kBT;
-        int page = -1;
-        if (j < v.lim) {
-            page = a.c.table[(long long)s * a.c.table_stride + j / kBT];
-            if (page != ISV_BLOCK_NONE && (page < 0 || page >= a.c.n_pages)) {
-                atomicOr(a.c.status, ISV_STATUS_BAD_BLOCK_ID);
-                page = -1;
-            }
-        }
-        const bool seen = page >= 0 && v.sees(j);
-        float x = -INFINITY;
-        if (seen) {
-            const uint4 *krow = reinterpret_cast<const uint4 *>(a.c.pool + (((long long)page * 2 * a.c.Hkv + kvh) * kBT + slot) * D);
-            x = 0.f;
-            for (int c = 0; c < D / 8; ++c) {
-                const uint4 kw = krow[place<D>(c, slot)], qw = qrow[c];
-                const uint32_t *kk = reinterpret_cast<const uint32_t *>(&kw), *qq = reinterpret_cast<const uint32_t *>(&qw);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float2 e = widen<BF16>(kk[i]), f = widen<BF16>(qq[i]);
-                    x = fmaf(e.x, f.x, x);
-                    x = fmaf(e.y, f.y, x);
-                }
-            }
-            x *= a.scale;
-            if (a.cap > 0.f) x = a.cap * tanhf(x / a.cap);
-            x -= slope * fabsf((float)(p - j));
-        }
-        float top = x;
-        for (int i = 16; i; i >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, i));
-        unsigned left = __ballot_sync(~0u, seen);
-        const float before = m;
-        m = fmaxf(m, top);
-        const double keep = before == -INFINITY ? 0.0 : (double)expf(before - m);
-        const float e = seen ? expf(x - m) : 0.f;
-        l *= keep;
-#pragma unroll
-        for (int i = 0; i < J; ++i) { o[i][0] *= keep; o[i][1] *= keep; }
-        for (; left; left &= left - 1) {
-            const int y = __ffs(left) - 1, pg = __shfl_sync(~0u, page, y), sl = (j0 + y) % kBT;
-            const double w = (double)__shfl_sync(~0u, e, y);
-            l += w;
-            const uint32_t *vrow = reinterpret_cast<const uint32_t *>(a.c.pool + ((((long long)pg * 2 + 1) * a.c.Hkv + kvh) * kBT + sl) * D);
-#pragma unroll
-            for (int i = 0; i < J; ++i) {
-                const int x2 = lane + 32 * i;
-                if (x2 >= D / 2) continue;
-                const float2 z = widen<BF16>(vrow[place<D>(x2 / 4, sl) * 4 + x2 % 4]);
-                o[i][0] += w * z.x;
-                o[i][1] += w * z.y;
-            }
-        }
-    }
-    const double inv = l != 0 ? 1.0 / l : 0.0;
-#pragma unroll
-    for (int i = 0; i < J; ++i) {
-        const int x2 = lane + 32 * i;
-        if (x2 >= D / 2) continue;
-        const float e = l != 0 ? (float)(o[i][0] * inv) : 0.f, f = l != 0 ? (float)(o[i][1] * inv) : 0.f;
-        const long long at = (row * a.c.Hq + h) * (D / 2) + x2;
-        if (a.out) reinterpret_cast<uint32_t *>(a.out)[at] = narrow<BF16>(e, f);
-        if (a.out_f32) reinterpret_cast<float2 *>(a.out_f32)[at] = make_float2(e, f);
-    }
-}
-
-template <int D, bool BF16>
-__global__ void __launch_bounds__(256) attn_rows_kernel(const AttnParams a) {
-    const int s = blockIdx.y;
-    bool bad;
-    const Seq q = seq_of(a.c, s, bad);
-    if (bad && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(a.c.status, ISV_STATUS_BAD_LENGTH);
-    const long long at = (long long)blockIdx.x * 8 + threadIdx.x / 32;
-    const int t = (int)(at / a.c.Hq), h = (int)(at % a.c.Hq);
-    if (t < q.n) attend_row<D, BF16>(a, s, q, t, h);
-}
-
 bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 
 }  // namespace
@@ -231,7 +141,13 @@ bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) !
 struct isv_chunk {
     isv_chunk_desc d{};
     int device = 0;
+    int grid = 1;                       // of the attention kernel
+    int GT = 1, P = 1;                  // query heads per visit, passes
     uint32_t *status = nullptr;
+    float *part_o = nullptr, *part_ml = nullptr;
+    MergeRec *merges = nullptr;
+    std::atomic<uint32_t> wait_polls{kSpinLimit};
+    std::atomic<int32_t> lost_copies{0};
 };
 
 namespace {
@@ -271,13 +187,6 @@ cudaError_t launch_write(const WriteParams &p, bool bf16, dim3 grid, cudaStream_
     else write_kernel<D, false><<<grid, kWriteThreads, 0, st>>>(p);
     return cudaGetLastError();
 }
-template <int D>
-cudaError_t launch_rows(const AttnParams &p, bool bf16, dim3 grid, cudaStream_t st) {
-    if (bf16) attn_rows_kernel<D, true><<<grid, 256, 0, st>>>(p);
-    else attn_rows_kernel<D, false><<<grid, 256, 0, st>>>(p);
-    return cudaGetLastError();
-}
-
 }  // namespace
 
 extern "C" {
@@ -287,6 +196,9 @@ int isv_chunk_free(isv_chunk *h) {
     OnDevice on(h->device);
     cudaDeviceSynchronize();   // calls may have been made on any stream
     cudaFree(h->status);
+    cudaFree(h->part_o);
+    cudaFree(h->part_ml);
+    cudaFree(h->merges);
     delete h;
     return ISV_OK;
 }
@@ -313,9 +225,21 @@ int isv_chunk_create(isv_chunk **out, const isv_chunk_desc *desc) {
     isv_chunk *h = new (std::nothrow) isv_chunk();
     if (!h) return err(ISV_EINVAL, "out of host memory");
     h->d = *desc;
+    // a row tile holds tokens with GT heads each; more than a tile's rows of heads are served in equal passes
+    const int G = desc->q_heads / desc->kv_heads;
+    h->P = (G + 127) / 128;
+    h->GT = (G + h->P - 1) / h->P;
+    int sms = 0;
     cudaError_t e = cudaGetDevice(&h->device);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, h->device);
+    h->grid = desc->max_ctas > 0 ? std::min(desc->max_ctas, sms) : sms;   // one CTA per SM
+    const size_t rows = attn_part_rows(h->grid);
+    if (e == cudaSuccess) e = attn_configure(desc->head_dim, desc->dtype == ISV_BF16);
     if (e == cudaSuccess) e = cudaMalloc((void **)&h->status, 4);
     if (e == cudaSuccess) e = cudaMemset(h->status, 0, 4);
+    if (e == cudaSuccess) e = cudaMalloc((void **)&h->part_o, rows * desc->head_dim * 4);
+    if (e == cudaSuccess) e = cudaMalloc((void **)&h->part_ml, rows * 2 * 4);
+    if (e == cudaSuccess) e = cudaMalloc((void **)&h->merges, h->grid * sizeof(MergeRec));
     if (e == cudaSuccess) e = cudaDeviceSynchronize();   // the zeros are there before any stream's first call
     if (e != cudaSuccess) {
         cudaGetLastError();
@@ -394,15 +318,18 @@ int isv_chunk_attn(isv_chunk *h, const void *pool_dev, int32_t n_pages, const in
     p.out = static_cast<uint16_t *>(out_dev); p.out_f32 = out_f32_dev;
     p.scale = h->d.scale != 0.f ? h->d.scale : (float)(1.0 / std::sqrt((double)h->d.head_dim));
     p.cap = h->d.softcap;
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    p.GT = h->GT; p.P = h->P; p.TT = 128 / h->GT;
+    const int tokens = attn_tiles((long long)T * h->GT) * p.TT;
+    p.RT = (T + tokens - 1) / tokens;
+    if ((long long)n_seqs * p.RT >= (1ll << 31)) return err(ISV_EINVAL, "%s: n_seqs * T too large", who);
+    p.part_o = h->part_o; p.part_ml = h->part_ml; p.merges = h->merges;
+    p.spin_limit = h->wait_polls.load();
+    if (h->lost_copies.load() > 0) p.drop_first_copy = h->lost_copies.fetch_sub(1) > 0;
     OnDevice on(h->device);
     if (on.e != cudaSuccess) return err(ISV_ECUDA, "%s: %s", who, cudaGetErrorString(on.e));
-    const bool bf16 = h->d.dtype == ISV_BF16;
-    const dim3 grid((unsigned)(((long long)T * h->d.q_heads + 7) / 8), (unsigned)n_seqs);
-    const cudaError_t e = h->d.head_dim == 64   ? launch_rows<64>(p, bf16, grid, st)
-                          : h->d.head_dim == 80 ? launch_rows<80>(p, bf16, grid, st)
-                                                : launch_rows<128>(p, bf16, grid, st);
-    return e == cudaSuccess ? ISV_OK : err(ISV_ECUDA, "%s: %s", who, cudaGetErrorString(e));
+    const char *what = nullptr;
+    const cudaError_t e = launch_attn(p, h->d.head_dim, h->d.dtype == ISV_BF16, h->grid, static_cast<cudaStream_t>(stream), &what);
+    return e == cudaSuccess ? ISV_OK : err(ISV_ECUDA, "%s: %s", who, what ? what : cudaGetErrorString(e));
 }
 
 int isv_chunk_status(isv_chunk *h, void *stream, uint32_t *status_out) {
@@ -418,6 +345,19 @@ int isv_chunk_status(isv_chunk *h, void *stream, uint32_t *status_out) {
     }
     if (e != cudaSuccess) return err(ISV_ECUDA, "isv_chunk_status: %s", cudaGetErrorString(e));
     if (*status_out) return err(ISV_EDEVICE_STATUS, "a call on a chunk reported status 0x%x", *status_out);
+    return ISV_OK;
+}
+
+int isv_chunk_set_wait_limit(isv_chunk *h, uint32_t polls) {
+    if (!h) return err(ISV_EINVAL, "null handle");
+    h->wait_polls = polls ? polls : kSpinLimit;
+    return ISV_OK;
+}
+
+int isv_chunk_inject_lost_copy(isv_chunk *h, int32_t launches) {
+    if (!h) return err(ISV_EINVAL, "null handle");
+    if (launches < 0) return err(ISV_EINVAL, "launches must not be negative");
+    h->lost_copies = launches;
     return ISV_OK;
 }
 

@@ -25,6 +25,8 @@ struct CacheParams {
     int32_t table_stride, max_blocks, n_pages, n_seqs, n_rows, T, Hkv, Hq;
 };
 
+struct MergeRec;
+
 struct AttnParams {
     CacheParams c;
     const uint16_t *q;          // [n_rows] rows of q_stride elements: [Hq][D]
@@ -36,7 +38,27 @@ struct AttnParams {
     int32_t window;             // 0: no limit
     float scale;                // of the scores
     float cap;                  // 0: scores are not capped
+    // how the work is cut (attn_shape), and scratch
+    int32_t GT, P;              // a visit serves GT of a KV head's query heads; P passes serve all of them
+    int32_t TT, RT;             // tokens of a row tile; items that a chunk of T tokens has at most, per KV head and pass
+    float *part_o;              // partial results: [slot][D / 4][rows of an item] of four values, two slots a CTA
+    float *part_ml;             // [slot][rows of an item] of (reference, sum)
+    MergeRec *merges;           // [grid]: the item that begins in this CTA's range and ends in another's
+    uint32_t spin_limit;        // polls of a barrier before a wait gives up
+    int32_t drop_first_copy;    // failure injection: the first visit's barrier of CTA 0 is armed without issuing one of its copies
 };
+
+// Rows of an item (NT row tiles of 128), whose partial results are in slot 2 * first + 1 and in 2 * c for the CTAs c up to `last`.
+struct MergeRec {
+    int32_t n;                  // partial results, 0: none
+    int32_t last, s, token0, kvh, pass;
+};
+
+// The launchers.  NT: row tiles of an item; FINE: weights enter their product as two 16-bit numbers.
+int attn_tiles(long long rows);                                    // row tiles of an item, for that many rows per KV head
+size_t attn_part_rows(int grid);                                   // rows of partial results
+cudaError_t attn_configure(int D, bool bf16);
+cudaError_t launch_attn(const AttnParams &p, int D, bool bf16, int grid, cudaStream_t st, const char **what);
 
 // One sequence of a call, clamped to what the table row, T and the rows hold.
 struct Seq {
@@ -93,6 +115,85 @@ __device__ __forceinline__ uint32_t narrow(float lo, float hi) {
     }
     const __half2 h = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t *>(&h);
+}
+
+// A warp per (new token, query head): lanes take the 32 tokens of two pages for the scores, and pairs of dims for the
+// sums, which are kept in 64 bits.
+template <int D, bool BF16>
+__device__ __noinline__ void attend_row(const AttnParams &a, int s, const Seq &q, int t, int h) {
+    constexpr int J = (D / 2 + 31) / 32;
+    const int lane = threadIdx.x & 31, kvh = h / (a.c.Hq / a.c.Hkv);
+    const int p = q.start + t;
+    const long long row = q.first + t;
+    const Sight v = sight_of(a, s, q, p);
+    const uint4 *qrow = reinterpret_cast<const uint4 *>(a.q + row * a.q_stride + h * D);
+    const float slope = a.slopes ? a.slopes[h] : 0.f;
+    float m = -INFINITY;
+    double l = 0, o[J][2] = {};
+    for (int j0 = (v.prefix ? 0 : v.low) / kBT * kBT; j0 < v.lim; j0 += 32) {
+        const int j = j0 + lane, slot = j % kBT;
+        int page = -1;
+        if (j < v.lim) {
+            page = a.c.table[(long long)s * a.c.table_stride + j / kBT];
+            if (page != ISV_BLOCK_NONE && (page < 0 || page >= a.c.n_pages)) {
+                atomicOr(a.c.status, ISV_STATUS_BAD_BLOCK_ID);
+                page = -1;
+            }
+        }
+        const bool seen = page >= 0 && v.sees(j);
+        float x = -INFINITY;
+        if (seen) {
+            const uint4 *krow = reinterpret_cast<const uint4 *>(a.c.pool + (((long long)page * 2 * a.c.Hkv + kvh) * kBT + slot) * D);
+            x = 0.f;
+            for (int c = 0; c < D / 8; ++c) {
+                const uint4 kw = krow[place<D>(c, slot)], qw = qrow[c];
+                const uint32_t *kk = reinterpret_cast<const uint32_t *>(&kw), *qq = reinterpret_cast<const uint32_t *>(&qw);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 e = widen<BF16>(kk[i]), f = widen<BF16>(qq[i]);
+                    x = fmaf(e.x, f.x, x);
+                    x = fmaf(e.y, f.y, x);
+                }
+            }
+            x *= a.scale;
+            if (a.cap > 0.f) x = a.cap * tanhf(x / a.cap);
+            x -= slope * fabsf((float)(p - j));
+        }
+        float top = x;
+        for (int i = 16; i; i >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, i));
+        unsigned left = __ballot_sync(~0u, seen);
+        const float before = m;
+        m = fmaxf(m, top);
+        const double keep = before == -INFINITY ? 0.0 : (double)expf(before - m);
+        const float e = seen ? expf(x - m) : 0.f;
+        l *= keep;
+#pragma unroll
+        for (int i = 0; i < J; ++i) { o[i][0] *= keep; o[i][1] *= keep; }
+        for (; left; left &= left - 1) {
+            const int y = __ffs(left) - 1, pg = __shfl_sync(~0u, page, y), sl = (j0 + y) % kBT;
+            const double w = (double)__shfl_sync(~0u, e, y);
+            l += w;
+            const uint32_t *vrow = reinterpret_cast<const uint32_t *>(a.c.pool + ((((long long)pg * 2 + 1) * a.c.Hkv + kvh) * kBT + sl) * D);
+#pragma unroll
+            for (int i = 0; i < J; ++i) {
+                const int x2 = lane + 32 * i;
+                if (x2 >= D / 2) continue;
+                const float2 z = widen<BF16>(vrow[place<D>(x2 / 4, sl) * 4 + x2 % 4]);
+                o[i][0] += w * z.x;
+                o[i][1] += w * z.y;
+            }
+        }
+    }
+    const double inv = l != 0 ? 1.0 / l : 0.0;
+#pragma unroll
+    for (int i = 0; i < J; ++i) {
+        const int x2 = lane + 32 * i;
+        if (x2 >= D / 2) continue;
+        const float e = l != 0 ? (float)(o[i][0] * inv) : 0.f, f = l != 0 ? (float)(o[i][1] * inv) : 0.f;
+        const long long at = (row * a.c.Hq + h) * (D / 2) + x2;
+        if (a.out) reinterpret_cast<uint32_t *>(a.out)[at] = narrow<BF16>(e, f);
+        if (a.out_f32) reinterpret_cast<float2 *>(a.out_f32)[at] = make_float2(e, f);
+    }
 }
 
 }  // namespace chunk

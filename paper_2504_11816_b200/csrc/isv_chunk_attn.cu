@@ -1,0 +1,967 @@
+// Attention of chunks of new tokens over the paged cache (isv_chunk_attn, described in include/isv.h), on tcgen05.
+//
+// Mathematics: per KV head the rows are the chunk's (token, query head) pairs, S = Q K^T and O = P V with P = 2^(S' - r) for the
+// scaled, capped, biased and masked scores S' (base 2) and a row's running reference r; a row's sum l of P is kept in fp32, its
+// O in tensor memory, and O / l is the result.  r follows the row's maximum only when that has grown by 2^8 (then O and l are
+// scaled down once): the quotient does not depend on r, and P stays below 2^8 (fp16: times 2^7, so that weights down to 2^-21
+// of the largest are normal numbers).
+//
+// Work: an item is (sequence, NT tiles of 128 rows, KV head); its visits are the tiles of 128 tokens that some row of it sees.  All
+// visits of all items form one list that is cut into equal ranges, one per persistent CTA, whatever the lengths; an item that
+// crosses ranges leaves partial results, which a second small kernel merges in fixed order.
+//
+// A CTA: a producer warp copies a visit's pages (K, then V) into a ring by TMA; one thread issues the products; NT groups of four
+// warps turn scores into weights, one row per thread.  With NT = 2 the groups take turns with the tensor cores: while one
+// computes its weights, the other's products run.  With NT = 1 the scores of the next visit are computed meanwhile.
+//
+// Layout: the pool's rows hold their 16-byte chunks in the order that the 128-byte swizzle of tensor-core operands wants
+// (chunk c of token t at c XOR t mod 8), so a page's 64-element half rows are copied by an unswizzled box of {64, 16} each and
+// are operands as they land: K as the K-major B operand of Q K^T, V as the MN-major one of P V.  The last 16 elements of
+// head_dim 80 are a box of their own with the 32-byte swizzle.  P goes back into the scores' columns of tensor memory as 16-bit
+// numbers, the A operand of P V.
+//
+// Every wait is bounded; on expiry the kernel flags the status word, waits for its copies (bounded), frees its tensor memory
+// and returns.
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cfloat>
+
+#include "isv_chunk.cuh"
+
+namespace isv {
+namespace chunk {
+
+namespace {
+
+constexpr int kTile = 128;             // rows of a tile, tokens of a visit
+constexpr int kPages = kTile / kBT;
+constexpr int kRecs = 8;               // visit records in flight (a ring of at most 10 tiles is less than 6 visits ahead)
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kSlack = 8.f;          // how far a maximum may pass the reference before the reference follows
+
+__device__ __forceinline__ uint32_t s32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}\n"
+                 : "=r"(ok)
+                 : "r"(bar), "r"(parity)
+                 : "memory");
+    return ok;
+}
+// Whether the barrier's phase completed before the limit, and before another warp gave up.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, uint32_t limit, const volatile int *failed) {
+    if (bar_try(bar, parity)) return true;
+    for (uint32_t i = 0; i < limit; ++i) {
+        if (bar_try(bar, parity)) return true;
+        if ((i & 63) == 63 && *failed) return false;
+    }
+    return false;
+}
+
+__device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+                 "l"(map), "r"(x), "r"(y), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+                 "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+                 : "memory");
+}
+
+// Shared-memory matrix descriptors.  K-major operands: 8-row groups are `stride` bytes apart.  MN-major: blocks of a swizzle
+// row's elements are `lead` bytes apart, groups of 8 along K `stride` bytes.
+__device__ __forceinline__ uint64_t desc(uint32_t addr, uint32_t lead, uint32_t stride, uint64_t layout) {
+    return (uint64_t)((addr & 0x3ffffu) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(stride >> 4) << 32 | 1ull << 46 | layout << 61;
+}
+constexpr uint64_t kSwz128 = 2, kSwz32 = 6;
+
+__host__ __device__ constexpr uint32_t instr_desc(bool bf16, bool b_mn_major, int n) {
+    return (1u << 4) | ((bf16 ? 1u : 0u) << 7) | ((bf16 ? 1u : 0u) << 10) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) |
+           ((uint32_t)(kTile >> 4) << 24);
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a),
+                 "l"(b), "r"(idesc), "r"(accumulate)
+                 : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d), "r"(a),
+                 "l"(b), "r"(idesc), "r"(accumulate)
+                 : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+__device__ __forceinline__ void tmem_ld32(uint32_t a, uint32_t *r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, "
+        "%20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]),
+          "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]),
+          "=r"(r[30]), "=r"(r[31])
+        : "r"(a)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t a, uint32_t *r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(a)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t a, const uint32_t *r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(a),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+__device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float reciprocal(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint64_t pair(float x, float y) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ float2 unpair(uint64_t v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// ---------------------------------------------------------------- how the work is cut
+
+struct Item {
+    int s, token0, kvh, pass;   // first token of the chunk in it
+    int lo, hi;                 // its visits: tiles lo .. hi - 1 of 128 tokens
+};
+__device__ __forceinline__ void span_of(const AttnParams &a, int s, const Seq &q, int token0, int tokens, int &lo, int &hi) {
+    const int last = min(token0 + tokens, q.n) - 1;
+    const Sight first = sight_of(a, s, q, q.start + token0);
+    lo = first.prefix > 0 ? 0 : first.low / kTile;
+    hi = (min(q.len, max(q.start + last + 1, first.prefix)) + kTile - 1) / kTile;
+}
+
+// A visit's record, written by the producer for the warps that work on it.
+struct Visit {
+    int j0;                     // first token
+    int pages;                  // bit i: page i is there
+    int flags;
+    int partial;                // tokens of the last page, 0: all 16
+    int last_page;              // the page that is partial
+    int s, token0, kvh, pass;
+    int slot;                   // of the partial result, -1: the item is whole
+    Seq q;
+};
+enum { FIRST = 1, LAST = 2, TWO = 4, END = 8 };
+
+template <int D>
+struct Shape {
+    static constexpr int HALVES = D / 64, TAIL = D % 64;                          // of a row: 64 elements each, and the rest
+    static constexpr int HALF_BYTES = kTile * 128, TAIL_BYTES = kTile * TAIL * 2;
+    static constexpr int TILE = HALVES * HALF_BYTES + TAIL_BYTES;                 // a tile of Q, K or V
+    static constexpr int SLOTS = D == 128 ? 5 : D == 80 ? 9 : 10;
+};
+constexpr int kMisc = 1536;
+template <int D>
+constexpr size_t smem_bytes() { return 1024 + (size_t)(2 + Shape<D>::SLOTS) * Shape<D>::TILE + kMisc; }
+
+// warps: NT groups of four for the weights, then the producer, the issuer of products, and the loader of Q
+template <int NT>
+__host__ __device__ constexpr int threads_of() { return NT * 128 + 96; }
+
+template <int D, bool BF16, int NT, bool FINE>
+__global__ void __launch_bounds__(threads_of<NT>(), 1)
+attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ CUtensorMap map_kv_tail,
+            const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_q_tail, const __grid_constant__ AttnParams a) {
+    using SH = Shape<D>;
+    constexpr int SLOTS = SH::SLOTS, NTHREADS = threads_of<NT>(), NWARPS = NTHREADS / 32;
+    constexpr int kProducer = NT * 4, kIssuer = NT * 4 + 1, kLoader = NT * 4 + 2;
+    constexpr float kOffset = BF16 ? 0.f : 7.f;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = smem_raw + ((1024u - (s32(smem_raw) & 1023u)) & 1023u);
+    uint8_t *q_tiles = smem, *ring = smem + 2 * SH::TILE;
+    uint8_t *misc = ring + SLOTS * SH::TILE;
+    Visit *recs = reinterpret_cast<Visit *>(misc);
+    uint64_t *bars = reinterpret_cast<uint64_t *>(misc + kRecs * sizeof(Visit));
+    uint64_t *full = bars, *empty = full + SLOTS, *rec_full = empty + SLOTS, *q_full = rec_full + kRecs, *q_empty = q_full + 2;
+    uint64_t *s_full = q_empty + 2, *p_full = s_full + 2, *pv_done = p_full + 2, *drain = pv_done + 2;
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(drain + 1);
+    volatile int *failed = reinterpret_cast<volatile int *>(tmem_slot + 1);
+    static_assert(kRecs * sizeof(Visit) + (2 * SLOTS + kRecs + 11) * 8 + 8 <= kMisc, "");
+    long long *sums = reinterpret_cast<long long *>(ring + (SLOTS - 1) * SH::TILE);   // until the first copies
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < SLOTS; ++i) {
+            bar_init(s32(&full[i]), 1);
+            bar_init(s32(&empty[i]), 1);
+        }
+        for (int i = 0; i < kRecs; ++i) bar_init(s32(&rec_full[i]), 1);
+        for (int i = 0; i < 2; ++i) {
+            bar_init(s32(&q_full[i]), 1);
+            bar_init(s32(&q_empty[i]), 1);
+            bar_init(s32(&s_full[i]), 1);
+            bar_init(s32(&p_full[i]), 4);
+            bar_init(s32(&pv_done[i]), 1);
+        }
+        bar_init(s32(drain), 1);
+        *failed = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == kIssuer) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(s32(tmem_slot)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    if (warp == kProducer && lane == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_kv) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q) : "memory");
+        if (SH::TAIL) {
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&map_kv_tail) : "memory");
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&map_q_tail) : "memory");
+        }
+    }
+    // nothing in global memory is touched before what was launched ahead is complete; then the kernel behind may enter
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+    // ---- the list of visits: a unit is (sequence, row tiles), each thread sums a run of units; an item counts one visit more
+    // for what it costs by itself
+    const int units = a.c.n_seqs * a.RT, group = a.c.Hkv * a.P;
+    const int u_lo = (int)((long long)units * threadIdx.x / NTHREADS), u_hi = (int)((long long)units * (threadIdx.x + 1) / NTHREADS);
+    auto weight = [&](int u, Seq &q, int &lo, int &hi) {   // of an item of unit u, 0: there is none
+        const int s = u / a.RT, token0 = (u - s * a.RT) * NT * a.TT;
+        bool bad;
+        q = seq_of(a.c, s, bad);
+        if (bad && token0 == 0 && blockIdx.x == 0) atomicOr(a.c.status, ISV_STATUS_BAD_LENGTH);
+        if (token0 >= q.n) return 0;
+        span_of(a, s, q, token0, NT * a.TT, lo, hi);
+        return hi - lo + 1;
+    };
+    long long mine = 0;
+    for (int u = u_lo; u < u_hi; ++u) {
+        Seq q;
+        int lo, hi;
+        mine += weight(u, q, lo, hi);
+    }
+    mine *= group;
+    long long up = mine;
+#pragma unroll
+    for (int i = 1; i < 32; i *= 2) {
+        const long long z = __shfl_up_sync(~0u, up, i);
+        if (lane >= i) up += z;
+    }
+    if (lane == 31) sums[NTHREADS + warp] = up;
+    __syncthreads();
+    long long base = 0, total = 0;
+    for (int i = 0; i < NWARPS; ++i) {
+        if (i < warp) base += sums[NTHREADS + i];
+        total += sums[NTHREADS + i];
+    }
+    sums[threadIdx.x] = base + up - mine;
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = *tmem_slot;
+    const int n_ctas = (int)min((long long)gridDim.x, total);
+    const int cta = blockIdx.x;
+
+    if (warp == kProducer) {
+        // ---- walks the CTA's range, writes visit records, copies pages
+        const long long f0 = cta < n_ctas ? total * cta / n_ctas : 0, f1 = cta < n_ctas ? total * (cta + 1) / n_ctas : 0;
+        MergeRec rec{};
+        int v = 0;              // visits so far
+        uint32_t seq = 0;       // tiles so far: K and V of a visit
+        bool ok = true;
+        auto put_end = [&]() {
+            if (lane == 0) {
+                recs[v % kRecs].flags = END;
+                bar_arrive(s32(&rec_full[v % kRecs]));
+            }
+        };
+        if (f0 < f1) {
+            // the run that holds f0: the last one that begins at or before it and is not empty
+            int r = 0;
+            for (int i = lane; i < NTHREADS; i += 32)
+                if (sums[i] <= f0) r = max(r, i);
+            r = __reduce_max_sync(~0u, r);
+            long long at = sums[r];
+            __syncwarp();
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // `sums` is read; copies may overwrite it
+            bool recorded = false;
+            for (int u = (int)((long long)units * r / NTHREADS); at < f1 && u < units && ok; ++u) {
+                Seq q;
+                int lo, hi;
+                const int w = weight(u, q, lo, hi);
+                if (w == 0 || at + (long long)w * group <= f0) {
+                    at += (long long)w * group;
+                    continue;
+                }
+                const int s = u / a.RT, token0 = (u - s * a.RT) * NT * a.TT;
+                int i = at < f0 ? (int)((f0 - at) / w) : 0;
+                at += (long long)i * w;
+                for (; i < group && at < f1 && ok; ++i, at += w) {
+                    // position 0 of an item stands for what it costs by itself, position 1 + i for visit i
+                    const int b = (int)max(0ll, f0 - at - 1), e = (int)min((long long)w, f1 - at) - 1;
+                    if (e <= b) continue;
+                    const int kvh = i / a.P, pass = i - kvh * a.P;
+                    const bool begins = b == 0, ends = e == w - 1;
+                    const int slot = begins && ends ? -1 : 2 * cta + (begins ? 1 : 0);
+                    if (begins && !ends) {
+                        rec.last = (int)(((at + w) * n_ctas - 1) / total);
+                        rec.n = rec.last - cta + 1;
+                        rec.s = s; rec.token0 = token0; rec.kvh = kvh; rec.pass = pass;
+                        // now: the record is this launch's, whatever becomes of the visits
+                        if (lane == 0) a.merges[cta] = rec;
+                        recorded = true;
+                    }
+                    const int tiles_rows = min(q.n - token0, NT * a.TT) > a.TT ? TWO : 0;
+                    const int32_t *row = a.c.table + (long long)s * a.c.table_stride;
+                    // page ids of four visits at a time, one batch ahead
+                    auto page_at = [&](int tile) {
+                        const int j = (lo + tile) * kPages + (lane & 7);
+                        return tile < e && j * kBT < q.len ? row[j] : ISV_BLOCK_NONE;
+                    };
+                    int ids = page_at(b + lane / 8), next_ids = page_at(b + 4 + lane / 8);
+                    for (int x = b; x < e; ++x, ++v) {
+                        const int y = (x - b) & 3;
+                        if (y == 0 && x > b) {
+                            ids = next_ids;
+                            next_ids = page_at(x + 4 + lane / 8);
+                        }
+                        const int j0 = (lo + x) * kTile;
+                        const int id = __shfl_sync(~0u, ids, 8 * y + (lane & 7));
+                        const bool there = id >= 0 && id < a.c.n_pages;
+                        if (lane < 8 && !there && id != ISV_BLOCK_NONE) atomicOr(a.c.status, ISV_STATUS_BAD_BLOCK_ID);
+                        const uint32_t pages = __ballot_sync(~0u, there) & 0xff;
+                        // K
+                        const int ks = seq % SLOTS;
+                        ok = seq < SLOTS || bar_wait(s32(&empty[ks]), (seq / SLOTS - 1) & 1, a.spin_limit, failed);
+                        ok = __all_sync(~0u, ok);
+                        if (!ok) break;
+                        const uint32_t bytes = __popc(pages) * (SH::TILE / kPages);
+                        const bool drop = a.drop_first_copy && cta == 0 && v == 0;
+                        if (lane == 0) {
+                            Visit &z = recs[v % kRecs];
+                            z.j0 = j0; z.pages = pages;
+                            z.flags = (x == b ? FIRST : 0) | (x == e - 1 ? LAST : 0) | tiles_rows;
+                            const int left = q.len - j0;
+                            z.partial = left < kTile ? left % kBT : 0;
+                            z.last_page = left / kBT;
+                            z.s = s; z.token0 = token0; z.kvh = kvh; z.pass = pass; z.slot = slot; z.q = q;
+                            bar_arrive(s32(&rec_full[v % kRecs]));
+                            bar_expect(s32(&full[ks]), bytes);
+                        }
+                        __syncwarp();
+#pragma unroll
+                        for (int kv = 0; kv < 2; ++kv) {
+                            const int slot_i = seq % SLOTS;
+                            if (kv == 1) {
+                                ok = seq < SLOTS || bar_wait(s32(&empty[slot_i]), (seq / SLOTS - 1) & 1, a.spin_limit, failed);
+                                ok = __all_sync(~0u, ok);
+                                if (!ok) break;
+                                if (lane == 0) bar_expect(s32(&full[slot_i]), bytes);
+                                __syncwarp();
+                            }
+                            const uint32_t dst = s32(ring + (size_t)slot_i * SH::TILE), bar = s32(&full[slot_i]);
+                            const int page = lane & 7, part = lane >> 3;      // part: a half, or the tail
+                            const int trow = ((id * 2 + kv) * a.c.Hkv + kvh) * kBT;
+                            if ((pages >> page & 1) && !(drop && kv == 0 && page == 0)) {
+                                if (part < SH::HALVES) tma_2d(dst + part * SH::HALF_BYTES + page * (kBT * 128), &map_kv, 64 * part, trow, bar);
+                                else if (SH::TAIL && part == SH::HALVES)
+                                    tma_2d(dst + SH::HALVES * SH::HALF_BYTES + page * (kBT * SH::TAIL * 2), &map_kv_tail, 64 * SH::HALVES, trow, bar);
+                            }
+                            ++seq;
+                        }
+                        if (!ok) break;
+                    }
+                }
+            }
+            if (lane == 0 && !recorded) a.merges[cta] = rec;
+        } else if (lane == 0) {
+            a.merges[cta] = rec;
+        }
+        if (ok) put_end();
+        else *failed = 1;
+        if (!ok || *failed) {
+            // something gave up: the copies in flight land before the memory passes on
+            for (uint32_t i = seq > SLOTS ? seq - SLOTS : 0; i < seq; ++i)
+                for (uint32_t k = 0; k < 1u << 16 && !bar_try(s32(&full[i % SLOTS]), (i / SLOTS) & 1); ++k) {}
+        }
+    } else if (warp == kLoader) {
+        // ---- Q of each item: a box of the row tile's tokens and their GT heads
+        if (lane == 0) {
+            bool ok = true;
+            int used[2] = {0, 0}, item = 0;
+            for (int v = 0; ok; ++v) {
+                if (!bar_wait(s32(&rec_full[v % kRecs]), (v / kRecs) & 1, a.spin_limit, failed)) { ok = false; break; }
+                const Visit z = recs[v % kRecs];
+                if (z.flags & END) break;
+                if (!(z.flags & FIRST)) continue;
+                const int tiles = NT == 2 && (z.flags & TWO) ? 2 : 1;
+                for (int i = 0; i < tiles && ok; ++i) {
+                    const int buf = NT == 2 ? i : item & 1;
+                    if (used[buf] > 0 && !bar_wait(s32(&q_empty[buf]), (used[buf] - 1) & 1, a.spin_limit, failed)) { ok = false; break; }
+                    ++used[buf];
+                    const uint32_t dst = s32(q_tiles + buf * SH::TILE), bar = s32(&q_full[buf]);
+                    const int rows = a.GT * a.TT, head = z.kvh * (a.c.Hq / a.c.Hkv) + z.pass * a.GT, token = z.q.first + z.token0 + i * a.TT;
+                    bar_expect(bar, rows * D * 2);
+                    for (int h = 0; h < SH::HALVES; ++h) tma_3d(dst + h * SH::HALF_BYTES, &map_q, 64 * h, head, token, bar);
+                    if (SH::TAIL) tma_3d(dst + SH::HALVES * SH::HALF_BYTES, &map_q_tail, 64 * SH::HALVES, head, token, bar);
+                }
+                ++item;
+            }
+            if (!ok) *failed = 1;
+            if (!ok || *failed)
+                for (int buf = 0; buf < 2; ++buf)
+                    for (uint32_t k = 0; used[buf] > 0 && k < 1u << 16 && !bar_try(s32(&q_full[buf]), (used[buf] - 1) & 1); ++k) {}
+        }
+    } else if (warp == kIssuer) {
+        // ---- the products, all issued by one thread in the order in which they run
+        if (lane == 0) {
+            constexpr uint32_t idesc_s = instr_desc(BF16, false, kTile);
+            constexpr uint32_t idesc_o = instr_desc(BF16, true, 64 * SH::HALVES), idesc_t = instr_desc(BF16, true, 16);
+            bool ok = true;
+            int q_used[2] = {0, 0}, p_used[2] = {0, 0}, item = 0;
+            bool started[2] = {false, false};
+            // S of tile or buffer w of visit v
+            auto scores = [&](int v, const Visit &z, int w, bool release) {
+                const int qb = NT == 2 ? w : item & 1;
+                const uint32_t ks = (2u * v) % SLOTS;
+                const uint32_t qa = s32(q_tiles + qb * SH::TILE), ka = s32(ring + (size_t)ks * SH::TILE);
+                const uint32_t d = tmem + w * kTile;
+#pragma unroll
+                for (int h = 0; h < SH::HALVES; ++h)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        mma_ss(d, desc(qa + h * SH::HALF_BYTES, 16, 1024, kSwz128) + 2 * k, desc(ka + h * SH::HALF_BYTES, 16, 1024, kSwz128) + 2 * k,
+                               idesc_s, h + k > 0);
+                if (SH::TAIL)
+                    mma_ss(d, desc(qa + SH::HALVES * SH::HALF_BYTES, 16, 256, kSwz32), desc(ka + SH::HALVES * SH::HALF_BYTES, 16, 256, kSwz32),
+                           idesc_s, 1);
+                commit(s32(&s_full[w]));
+                if (z.flags & LAST) commit(s32(&q_empty[qb]));
+                if (release) commit(s32(&empty[ks]));
+            };
+            // O += P V of tile w of visit v
+            auto output = [&](int v, const Visit &z, int w, bool release) {
+                const uint32_t vs = (2u * v + 1) % SLOTS, va = s32(ring + (size_t)vs * SH::TILE);
+                const int ow = NT == 2 ? w : 0;
+                const uint32_t d = tmem + 2 * kTile + ow * kTile, p = tmem + w * kTile;
+                if (z.flags & FIRST) started[ow] = false;
+#pragma unroll
+                for (int i = 0; i < kPages; ++i) {
+                    if (!(z.pages >> i & 1)) continue;
+#pragma unroll
+                    for (int half = 0; half < (FINE ? 2 : 1); ++half) {
+                        const uint32_t pa = p + half * (kTile / 2) + i * 8;
+                        mma_ts(d, pa, desc(va + i * (kBT * 128), SH::HALF_BYTES, 1024, kSwz128), idesc_o, started[ow]);
+                        if (SH::TAIL)
+                            mma_ts(d + 64 * SH::HALVES, pa, desc(va + SH::HALVES * SH::HALF_BYTES + i * (kBT * SH::TAIL * 2), 16, 256, kSwz32),
+                                   idesc_t, started[ow]);
+                        started[ow] = true;
+                    }
+                }
+                commit(s32(&pv_done[w]));
+                if (release) commit(s32(&empty[vs]));
+            };
+            auto rec_of = [&](int v, Visit &z) {
+                ok = bar_wait(s32(&rec_full[v % kRecs]), (v / kRecs) & 1, a.spin_limit, failed);
+                if (ok) z = recs[v % kRecs];
+            };
+            auto k_ready = [&](int v) {
+                const uint32_t n = 2u * v;
+                ok = ok && bar_wait(s32(&full[n % SLOTS]), (n / SLOTS) & 1, a.spin_limit, failed);
+            };
+            auto v_ready = [&](int v) {
+                const uint32_t n = 2u * v + 1;
+                ok = ok && bar_wait(s32(&full[n % SLOTS]), (n / SLOTS) & 1, a.spin_limit, failed);
+            };
+            auto q_ready = [&](const Visit &z, int w) {
+                if (!(z.flags & FIRST)) return;
+                const int qb = NT == 2 ? w : item & 1;
+                ok = ok && bar_wait(s32(&q_full[qb]), q_used[qb] & 1, a.spin_limit, failed);
+                ++q_used[qb];
+            };
+            auto p_ready = [&](int w) {
+                ok = ok && bar_wait(s32(&p_full[w]), p_used[w] & 1, a.spin_limit, failed);
+                ++p_used[w];
+            };
+            Visit z, next;
+            rec_of(0, z);
+            if (ok && !(z.flags & END)) {
+                k_ready(0);
+                q_ready(z, 0);
+                if (ok) {
+                    fence_after();
+                    scores(0, z, 0, !(NT == 2 && (z.flags & TWO)));
+                }
+                if (NT == 2 && (z.flags & TWO)) {
+                    q_ready(z, 1);
+                    if (ok) { fence_after(); scores(0, z, 1, true); }
+                }
+                for (int v = 0; ok; ++v) {
+                    rec_of(v + 1, next);
+                    if (!ok) break;
+                    const bool more = !(next.flags & END);
+                    if (NT == 1) {
+                        const int w = v & 1;
+                        if (more) {
+                            if (z.flags & LAST) ++item;
+                            k_ready(v + 1);
+                            q_ready(next, w ^ 1);
+                            if (!ok) break;
+                            fence_after();
+                            scores(v + 1, next, w ^ 1, true);
+                        }
+                        v_ready(v);
+                        p_ready(w);
+                        if (!ok) break;
+                        fence_after();
+                        output(v, z, w, true);
+                    } else {
+                        const bool two = z.flags & TWO, next_two = more && (next.flags & TWO);
+                        v_ready(v);
+                        p_ready(0);
+                        if (!ok) break;
+                        fence_after();
+                        output(v, z, 0, !two);
+                        if (more) {
+                            k_ready(v + 1);
+                            q_ready(next, 0);
+                            if (!ok) break;
+                            fence_after();
+                            scores(v + 1, next, 0, !next_two);
+                        }
+                        if (two) {
+                            p_ready(1);
+                            if (!ok) break;
+                            fence_after();
+                            output(v, z, 1, true);
+                        }
+                        if (next_two) {
+                            q_ready(next, 1);
+                            if (!ok) break;
+                            fence_after();
+                            scores(v + 1, next, 1, true);
+                        }
+                    }
+                    if (!more) break;
+                    z = next;
+                }
+            }
+            if (!ok) {
+                *failed = 1;
+                atomicOr(a.c.status, ISV_STATUS_WAIT_EXPIRED);
+                commit(s32(drain));       // what was issued ends before tensor memory passes on
+                for (uint32_t k = 0; k < 1u << 16 && !bar_try(s32(drain), 0); ++k) {}
+            }
+        }
+    } else {
+        // ---- weights: group w of four warps, one row of its tile per thread
+        const int w = warp >> 2, r = threadIdx.x & 127;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const int row_t = r / a.GT, row_g = r - row_t * a.GT, G = a.c.Hq / a.c.Hkv;
+        const bool shaped = a.cap > 0.f || a.slopes || !(a.scale > 0.f);      // scores need more than a positive factor
+        const float c = shaped ? kLog2e : a.scale * kLog2e;
+        int used = 0;           // visits of this group
+        int tok = 0, head = 0, pos = 0;
+        bool live = false, any_live = false;
+        Sight sight{};
+        float ref = -INFINITY, l = 0.f, slope = 0.f;
+        bool ok = true;
+        for (int v = 0;; ++v) {
+            ok = __all_sync(~0u, bar_wait(s32(&rec_full[v % kRecs]), (v / kRecs) & 1, a.spin_limit, failed));
+            if (!ok) break;
+            const Visit &z = recs[v % kRecs];
+            const int flags = z.flags;
+            if (flags & END) break;
+            if (NT == 2 && w == 1 && !(flags & TWO)) continue;
+            const int b = NT == 2 ? w : v & 1;                                // buffer of the scores
+            const uint32_t phase = NT == 2 ? used & 1 : (v >> 1) & 1;
+            if (flags & FIRST) {
+                tok = z.token0 + w * a.TT + row_t;
+                head = z.kvh * G + z.pass * a.GT + row_g;
+                live = row_t < a.TT && tok < z.q.n && z.pass * a.GT + row_g < G;
+                pos = z.q.start + tok;
+                sight = sight_of(a, z.s, z.q, pos);
+                slope = a.slopes && live ? a.slopes[head] : 0.f;
+                ref = -INFINITY;
+                l = 0.f;
+                any_live = __any_sync(~0u, live);
+            }
+            const int j0 = z.j0;
+            const uint32_t pages = z.pages;
+            ok = __all_sync(~0u, bar_wait(s32(&s_full[b]), phase, a.spin_limit, failed));
+            if (!ok) break;
+            fence_after();
+            if (any_live) {
+                float x[kTile];
+                uint32_t *xw = reinterpret_cast<uint32_t *>(x);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) tmem_ld32(tmem + lanes + b * kTile + 32 * i, xw + 32 * i);
+                wait_ld();
+                if (shaped) {
+                    const float in = a.cap > 0.f ? 2.f * kLog2e * a.scale / a.cap : a.scale;
+                    const float distance = (float)(pos - j0);
+                    if (a.cap > 0.f) {
+                        // cap tanh(y) = cap - 2 cap / (e^2y + 1): off by a few 2^-24 of the cap
+#pragma unroll
+                        for (int i = 0; i < kTile; ++i) {
+                            const float e = exp2_fast(x[i] * in);
+                            x[i] = fmaf(-2.f * a.cap, reciprocal(e + 1.f), a.cap);
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < kTile; ++i) x[i] *= in;
+                    }
+                    if (a.slopes) {
+#pragma unroll
+                        for (int i = 0; i < kTile; ++i) x[i] = fmaf(-slope, fabsf(distance - (float)i), x[i]);
+                    }
+                }
+                const bool all = pages == 0xff && sight.lim >= j0 + kTile && (sight.low <= j0 || sight.prefix >= j0 + kTile);
+                if (!__all_sync(~0u, all || !live)) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        // bit i: token j0 + 32 k + i is seen
+                        auto below = [&](int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; };
+                        const int at = j0 + 32 * k;
+                        uint32_t seen = below(sight.lim - at) & (~below(sight.low - at) | below(sight.prefix - at));
+                        seen &= (pages >> (2 * k) & 1 ? 0xffffu : 0u) | (pages >> (2 * k + 1) & 1 ? 0xffff0000u : 0u);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) x[32 * k + i] = seen >> i & 1 ? x[32 * k + i] : -INFINITY;
+                    }
+                }
+                float top[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+                for (int i = 4; i < kTile; ++i) top[i & 3] = fmaxf(top[i & 3], x[i]);
+                const float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c;
+                float factor = 1.f;
+                if (ref == -INFINITY) {
+                    ref = high;
+                } else if (high > ref + kSlack) {
+                    factor = exp2_fast(ref - high);
+                    ref = high;
+                }
+                if (__any_sync(~0u, factor != 1.f)) {
+                    // O is scaled: the product before this one has to be in it
+                    l *= factor;
+                    const uint32_t before = NT == 2 ? used - 1 : v - 1;
+                    ok = __all_sync(~0u, bar_wait(s32(&pv_done[NT == 2 ? w : before & 1]), (NT == 2 ? before : before >> 1) & 1, a.spin_limit, failed));
+                    if (!ok) break;
+                    fence_after();
+                    const uint32_t o = tmem + lanes + 2 * kTile + (NT == 2 ? w : 0) * kTile;
+#pragma unroll 1
+                    for (int i = 0; i < D; i += 16) {
+                        uint32_t y[16];
+                        tmem_ld16(o + i, y);
+                        wait_ld();
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) y[k] = __float_as_uint(__uint_as_float(y[k]) * factor);
+                        tmem_st16(o + i, y);
+                    }
+                }
+                const float minus = ref == -INFINITY ? 0.f : kOffset - ref;
+                const uint64_t cc = pair(c, c), mm = pair(minus, minus);
+                uint64_t sum[2] = {pair(0.f, 0.f), pair(0.f, 0.f)};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    uint32_t hi[16], lo[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const float2 e = unpair(fma2(pair(x[32 * k + 2 * i], x[32 * k + 2 * i + 1]), cc, mm));
+                        const float p0 = exp2_fast(e.x), p1 = exp2_fast(e.y);
+                        sum[i & 1] = add2(sum[i & 1], pair(p0, p1));
+                        hi[i] = narrow<BF16>(p0, p1);
+                        if (FINE) {
+                            const float2 h = widen<BF16>(hi[i]);
+                            lo[i] = narrow<BF16>(p0 - h.x, p1 - h.y);
+                        }
+                    }
+                    tmem_st16(tmem + lanes + b * kTile + 16 * k, hi);
+                    if (FINE) tmem_st16(tmem + lanes + b * kTile + kTile / 2 + 16 * k, lo);
+                }
+                const float2 total2 = unpair(add2(sum[0], sum[1]));
+                l += total2.x + total2.y;
+                wait_st();
+            }
+            if (w == 0 && z.partial) {
+                // rows of V behind the sequence's last token meet weights of 0; what stands there may be no number
+                const uint32_t n = 2u * v + 1;
+                ok = __all_sync(~0u, bar_wait(s32(&full[n % SLOTS]), (n / SLOTS) & 1, a.spin_limit, failed));
+                if (!ok) break;
+                if (pages >> z.last_page & 1) {
+                    uint8_t *vt = ring + (size_t)(n % SLOTS) * SH::TILE;
+                    const int rows = kBT - z.partial, first = z.last_page * kBT + z.partial;
+                    for (int i = r; i < rows * 8 * SH::HALVES; i += 128)
+                        *reinterpret_cast<uint4 *>(vt + (i / (rows * 8)) * SH::HALF_BYTES + (first + i % (rows * 8) / 8) * 128 + i % 8 * 16) =
+                            make_uint4(0, 0, 0, 0);
+                    if (SH::TAIL)
+                        for (int i = r; i < rows * 2; i += 128)
+                            *reinterpret_cast<uint4 *>(vt + SH::HALVES * SH::HALF_BYTES + (first + i / 2) * (SH::TAIL * 2) + i % 2 * 16) =
+                                make_uint4(0, 0, 0, 0);
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                }
+            }
+            const int s = z.s, slot = z.slot;
+            const Seq q = z.q;
+            ++used;
+            fence_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive(s32(&p_full[b]));
+            if (!(flags & LAST)) continue;
+
+            // ---- the item's end: O / l, or a partial result
+            ok = __all_sync(~0u, bar_wait(s32(&pv_done[b]), phase, a.spin_limit, failed));
+            if (!ok) break;
+            if (!any_live) continue;
+            fence_after();
+            const uint32_t o = tmem + lanes + 2 * kTile + (NT == 2 ? w : 0) * kTile;
+            const bool some = l != 0.f;        // NaN is some
+            const long long at = ((long long)(q.first + tok) * a.c.Hq + head) * D;
+            const float inv = slot < 0 ? 1.f / l : 1.f;
+            bool fine = !some || fabsf(l) <= FLT_MAX;
+#pragma unroll 1
+            for (int i = 0; i < D; i += 16) {
+                uint32_t y[16];
+                tmem_ld16(o + i, y);
+                wait_ld();
+                float f[16];
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    f[k] = some ? __uint_as_float(y[k]) * inv : 0.f;
+                    fine = fine && fabsf(f[k]) <= FLT_MAX;
+                }
+                if (live && slot < 0) {
+                    if (a.out) {
+                        uint32_t h[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) h[k] = narrow<BF16>(f[2 * k], f[2 * k + 1]);
+                        uint4 *dst = reinterpret_cast<uint4 *>(a.out + at + i);
+                        dst[0] = make_uint4(h[0], h[1], h[2], h[3]);
+                        dst[1] = make_uint4(h[4], h[5], h[6], h[7]);
+                    }
+                    if (a.out_f32) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            reinterpret_cast<float4 *>(a.out_f32 + at + i)[k] = make_float4(f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3]);
+                    }
+                } else if (live) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        reinterpret_cast<float4 *>(a.part_o)[((long long)slot * (D / 4) + i / 4 + k) * (2 * kTile) + w * kTile + r] =
+                            make_float4(f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3]);
+                }
+                __syncwarp();
+            }
+            if (slot >= 0) {
+                if (live) reinterpret_cast<float2 *>(a.part_ml)[(long long)slot * (2 * kTile) + w * kTile + r] =
+                    make_float2(some ? ref : -INFINITY, l);
+            } else {
+                // sums that are no number: an infinity or NaN in a token that the row does not see (0 times that is NaN), or an
+                // overflow of values near the type's largest.  Such a row is computed token by token.
+                for (uint32_t odd = __ballot_sync(~0u, live && !fine); odd; odd &= odd - 1) {
+                    const int from = __ffs(odd) - 1;
+                    attend_row<D, BF16>(a, s, q, __shfl_sync(~0u, tok, from), __shfl_sync(~0u, head, from));
+                }
+            }
+            fence_before();
+        }
+        if (!ok) *failed = 1;
+    }
+
+    fence_before();
+    __syncthreads();
+    if (warp == kIssuer) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+}
+
+// ---------------------------------------------------------------- merging
+
+// Partial results of items that crossed ranges.  CTA (record, group of 32 rows, four-value columns): a lane has one row, a
+// warp every eighth column.
+constexpr int kMergeThreads = 256;
+template <int D, bool BF16>
+__global__ void __launch_bounds__(kMergeThreads) merge_kernel(const __grid_constant__ AttnParams a) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const MergeRec m = a.merges[blockIdx.x];
+    if (m.n == 0) return;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.y * 32 + lane;
+    const int w = row / kTile, r = row % kTile, row_t = r / a.GT, row_g = r - row_t * a.GT, G = a.c.Hq / a.c.Hkv;
+    const int tok = m.token0 + w * a.TT + row_t, head = m.kvh * G + m.pass * a.GT + row_g;
+    bool bad;
+    const Seq q = seq_of(a.c, m.s, bad);
+    const bool live = row_t < a.TT && tok < q.n && m.pass * a.GT + row_g < G;
+    if (!__any_sync(~0u, live)) return;
+    auto slot = [&](int i) { return (long long)(2 * ((int)blockIdx.x + i) + (i == 0 ? 1 : 0)); };
+    const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml);
+    float top = -INFINITY, l = 0.f;
+    if (live)
+        for (int i = 0; i < m.n; ++i) top = fmaxf(top, ml[slot(i) * (2 * kTile) + row].x);
+    const float at = top == -INFINITY ? 0.f : top;
+    if (live)
+        for (int i = 0; i < m.n; ++i) {
+            const float2 z = ml[slot(i) * (2 * kTile) + row];
+            l += z.y * exp2_fast(z.x - at);
+        }
+    const float inv = l != 0.f ? 1.f / l : 0.f;
+    bool fine = l == 0.f || fabsf(l) <= FLT_MAX;
+    for (int c = warp; c < D / 4; c += kMergeThreads / 32) {
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (!live) continue;
+#pragma unroll 4
+        for (int i = 0; i < m.n; ++i) {
+            const float f = exp2_fast(ml[slot(i) * (2 * kTile) + row].x - at);
+            const float4 y = reinterpret_cast<const float4 *>(a.part_o)[(slot(i) * (D / 4) + c) * (2 * kTile) + row];
+            o.x = fmaf(f, y.x, o.x); o.y = fmaf(f, y.y, o.y); o.z = fmaf(f, y.z, o.z); o.w = fmaf(f, y.w, o.w);
+        }
+        o.x *= inv; o.y *= inv; o.z *= inv; o.w *= inv;
+        fine = fine && fabsf(o.x) <= FLT_MAX && fabsf(o.y) <= FLT_MAX && fabsf(o.z) <= FLT_MAX && fabsf(o.w) <= FLT_MAX;
+        const long long to = ((long long)(q.first + tok) * a.c.Hq + head) * D + 4 * c;
+        if (a.out) *reinterpret_cast<uint2 *>(a.out + to) = make_uint2(narrow<BF16>(o.x, o.y), narrow<BF16>(o.z, o.w));
+        if (a.out_f32) *reinterpret_cast<float4 *>(a.out_f32 + to) = o;
+    }
+    // rows whose sums are no number (see the kernel above): every warp has its columns written before one recomputes the row
+    __shared__ uint32_t odd_s;
+    if (threadIdx.x == 0) odd_s = 0;
+    __syncthreads();
+    const uint32_t odd = __ballot_sync(~0u, live && !fine);
+    if (lane == 0 && odd) atomicOr(&odd_s, odd);
+    __syncthreads();
+    int i = 0;
+    for (uint32_t left = odd_s; left; left &= left - 1, ++i) {
+        const int from = __ffs(left) - 1;
+        const int t = __shfl_sync(~0u, tok, from), h = __shfl_sync(~0u, head, from);
+        if (i % (kMergeThreads / 32) == warp) attend_row<D, BF16>(a, m.s, q, t, h);
+    }
+}
+
+// ---------------------------------------------------------------- host side
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                                  CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_fn() {
+    static const EncodeTiledFn fn = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        const bool ok = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess;
+        return ok ? reinterpret_cast<EncodeTiledFn>(p) : nullptr;
+    }();
+    return fn;
+}
+
+bool encode(CUtensorMap *m, bool bf16, int rank, const void *base, const cuuint64_t *dims, const cuuint64_t *strides, const cuuint32_t *box,
+            CUtensorMapSwizzle swizzle) {
+    const cuuint32_t one[3] = {1, 1, 1};
+    return encode_fn()(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, rank, const_cast<void *>(base), dims, strides,
+                       box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, bool BF16, int NT, bool FINE>
+cudaError_t launch(const AttnParams &p, int grid, cudaStream_t st, const char **what) {
+    CUtensorMap kv{}, kv_tail{}, q{}, q_tail{};
+    if (!encode_fn()) { *what = "cuTensorMapEncodeTiled is not available from this driver"; return cudaErrorUnknown; }
+    const cuuint64_t kv_dims[2] = {D, (cuuint64_t)p.c.n_pages * 2 * p.c.Hkv * kBT}, kv_strides[1] = {D * 2};
+    const cuuint64_t q_dims[3] = {D, (cuuint64_t)p.c.Hq, (cuuint64_t)p.c.n_rows}, q_strides[2] = {D * 2, (cuuint64_t)p.q_stride * 2};
+    const cuuint32_t kv_box[2] = {64, kBT}, q_box[3] = {64, (cuuint32_t)p.GT, (cuuint32_t)p.TT};
+    const cuuint32_t kv_tail_box[2] = {16, kBT}, q_tail_box[3] = {16, (cuuint32_t)p.GT, (cuuint32_t)p.TT};
+    bool ok = encode(&kv, BF16, 2, p.c.pool, kv_dims, kv_strides, kv_box, CU_TENSOR_MAP_SWIZZLE_NONE) &&
+              encode(&q, BF16, 3, p.q, q_dims, q_strides, q_box, CU_TENSOR_MAP_SWIZZLE_128B);
+    if (Shape<D>::TAIL)
+        ok = ok && encode(&kv_tail, BF16, 2, p.c.pool, kv_dims, kv_strides, kv_tail_box, CU_TENSOR_MAP_SWIZZLE_32B) &&
+             encode(&q_tail, BF16, 3, p.q, q_dims, q_strides, q_tail_box, CU_TENSOR_MAP_SWIZZLE_32B);
+    if (!ok) { *what = "cuTensorMapEncodeTiled refused the pool or the rows of q"; return cudaErrorUnknown; }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(threads_of<NT>());
+    cfg.dynamicSmemBytes = smem_bytes<D>();
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    cudaError_t e = cudaLaunchKernelEx(&cfg, attn_kernel<D, BF16, NT, FINE>, kv, kv_tail, q, q_tail, p);
+    if (e != cudaSuccess) return e;
+    cfg.gridDim = dim3(grid, NT * kTile / 32);
+    cfg.blockDim = dim3(kMergeThreads);
+    cfg.dynamicSmemBytes = 0;
+    return cudaLaunchKernelEx(&cfg, merge_kernel<D, BF16>, p);
+}
+
+template <int D, bool BF16>
+cudaError_t configure() {
+    cudaError_t e = cudaFuncSetAttribute(attn_kernel<D, BF16, 1, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D>());
+    if (e == cudaSuccess)
+        e = cudaFuncSetAttribute(attn_kernel<D, BF16, 2, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D>());
+    if (e == cudaSuccess)
+        e = cudaFuncSetAttribute(attn_kernel<D, BF16, 2, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D>());
+    return e;
+}
+template <int D, bool BF16>
+cudaError_t pick(const AttnParams &p, int grid, cudaStream_t st, const char **what) {
+    if (attn_tiles((long long)p.c.T * p.GT) == 1) return launch<D, BF16, 1, true>(p, grid, st, what);
+    return p.out_f32 ? launch<D, BF16, 2, true>(p, grid, st, what) : launch<D, BF16, 2, false>(p, grid, st, what);
+}
+
+}  // namespace
+
+int attn_tiles(long long rows) { return rows <= kTile ? 1 : 2; }
+size_t attn_part_rows(int grid) { return (size_t)2 * grid * 2 * kTile; }
+
+cudaError_t attn_configure(int D, bool bf16) {
+    if (D == 64) return bf16 ? configure<64, true>() : configure<64, false>();
+    if (D == 80) return bf16 ? configure<80, true>() : configure<80, false>();
+    return bf16 ? configure<128, true>() : configure<128, false>();
+}
+cudaError_t launch_attn(const AttnParams &p, int D, bool bf16, int grid, cudaStream_t st, const char **what) {
+    if (D == 64) return bf16 ? pick<64, true>(p, grid, st, what) : pick<64, false>(p, grid, st, what);
+    if (D == 80) return bf16 ? pick<80, true>(p, grid, st, what) : pick<80, false>(p, grid, st, what);
+    return bf16 ? pick<128, true>(p, grid, st, what) : pick<128, false>(p, grid, st, what);
+}
+
+}  // namespace chunk
+}  // namespace isv
