@@ -2,9 +2,9 @@
 //
 // Mathematics: per KV head the rows are the chunk's (token, query head) pairs, S = Q K^T and O = P V with P = 2^(S' - r) for the
 // scaled, capped, biased and masked scores S' (base 2) and a row's running reference r; a row's sum l of P is kept in fp32, its
-// O in tensor memory, and O / l is the result.  r follows the row's maximum only when that has grown by 2^8 (then O and l are
-// scaled down once): the quotient does not depend on r, and P stays below 2^8 (fp16: times 2^7, so that weights down to 2^-21
-// of the largest are normal numbers).
+// O in tensor memory, and O / l is the result.  r follows the row's maximum only when that has passed it by 8 (fp16)
+// or 40 (bf16), then O and l are scaled down once: the quotient does not depend on r.  fp16 weights are 2^7 times as large, so
+// that they stay below 2^16 and down to 2^-21 of the largest are normal numbers.
 //
 // Work: an item is (sequence, NT tiles of 128 rows, KV head); its visits are the tiles of 128 tokens that some row of it sees.  All
 // visits of all items form one list that is cut into equal ranges, one per persistent CTA, whatever the lengths; an item that
@@ -39,7 +39,11 @@ constexpr int kTile = 128;             // rows of a tile, tokens of a visit
 constexpr int kPages = kTile / kBT;
 constexpr int kRecs = 8;               // visit records in flight (a ring of at most 10 tiles is less than 6 visits ahead)
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kSlack = 8.f;          // how far a maximum may pass the reference before the reference follows
+// How far a row's maximum may pass its reference before the reference follows (and O is scaled): fp16 weights have to stay below 2^16;
+// bf16's are as exact at 2^40 as at 1, and fp32 sums of 2^40 times values up to 2^70 do not overflow.  With heavy-tailed
+// scores some row of a warp passes 2^8 in every second visit.
+template <bool BF16>
+__host__ __device__ constexpr float slack_of() { return BF16 ? 40.f : 8.f; }
 
 __device__ __forceinline__ uint32_t s32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
@@ -70,6 +74,9 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, uint32_t
     return false;
 }
 
+// A value that all lanes have alike, told to the compiler so: what is computed from it, and the branches on it, are the warp's.
+__device__ __forceinline__ int same(int x) { return __shfl_sync(~0u, x, 0); }
+
 __device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
                  "l"(map), "r"(x), "r"(y), "r"(bar)
@@ -92,18 +99,25 @@ __host__ __device__ constexpr uint32_t instr_desc(bool bf16, bool b_mn_major, in
     return (1u << 4) | ((bf16 ? 1u : 0u) << 7) | ((bf16 ? 1u : 0u) << 10) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) |
            ((uint32_t)(kTile >> 4) << 24);
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a),
-                 "l"(b), "r"(idesc), "r"(accumulate)
-                 : "memory");
+// The issuing warp runs these as a whole, so that operands stay in uniform registers; the thread with `one` set issues.
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate, uint32_t one) {
+    asm volatile(
+        "{\n.reg .pred p, q;\nsetp.ne.b32 p, %4, 0;\nsetp.ne.b32 q, %5, 0;\n@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(one)
+        : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d), "r"(a),
-                 "l"(b), "r"(idesc), "r"(accumulate)
-                 : "memory");
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate, uint32_t one) {
+    asm volatile(
+        "{\n.reg .pred p, q;\nsetp.ne.b32 p, %4, 0;\nsetp.ne.b32 q, %5, 0;\n@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(
+            d),
+        "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(one)
+        : "memory");
 }
-__device__ __forceinline__ void commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+__device__ __forceinline__ void commit(uint32_t bar, uint32_t one) {
+    asm volatile(
+        "{\n.reg .pred q;\nsetp.ne.b32 q, %1, 0;\n@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(bar),
+        "r"(one)
+        : "memory");
 }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -141,6 +155,11 @@ __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+__device__ __forceinline__ float max3(float x, float y, float z) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
+    return r;
 }
 __device__ __forceinline__ float reciprocal(float x) {
     float y;
@@ -205,9 +224,12 @@ constexpr int kMisc = 1536;
 template <int D>
 constexpr size_t smem_bytes() { return 1024 + (size_t)(2 + Shape<D>::SLOTS) * Shape<D>::TILE + kMisc; }
 
-// warps: NT groups of four for the weights, then the producer, the issuer of products, and the loader of Q
+// warps: NT groups of four for the weights, then the producer, the issuer of products, the loader of Q, and one that rests
 template <int NT>
-__host__ __device__ constexpr int threads_of() { return NT * 128 + 96; }
+__host__ __device__ constexpr int threads_of() { return NT * 128 + 128; }
+// With NT = 2 a thread starts with 168 registers; the groups that hold a row of scores go up to 200, the other warps down to
+// 104: 2 * 128 * 200 + 128 * 104 = 384 * 168.
+constexpr int kMoreRegs = 200, kFewRegs = 104;
 
 template <int D, bool BF16, int NT, bool FINE>
 __global__ void __launch_bounds__(threads_of<NT>(), 1)
@@ -224,12 +246,12 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
     Visit *recs = reinterpret_cast<Visit *>(misc);
     uint64_t *bars = reinterpret_cast<uint64_t *>(misc + kRecs * sizeof(Visit));
     uint64_t *full = bars, *empty = full + SLOTS, *rec_full = empty + SLOTS, *q_full = rec_full + kRecs, *q_empty = q_full + 2;
-    uint64_t *s_full = q_empty + 2, *p_full = s_full + 2, *pv_done = p_full + 2, *drain = pv_done + 2;
+    uint64_t *s_full = q_empty + 2, *p_full = s_full + 2, *pv_done = p_full + 4, *drain = pv_done + 2;   // p_full: [half of the tokens][2]
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(drain + 1);
     volatile int *failed = reinterpret_cast<volatile int *>(tmem_slot + 1);
-    static_assert(kRecs * sizeof(Visit) + (2 * SLOTS + kRecs + 11) * 8 + 8 <= kMisc, "");
+    static_assert(kRecs * sizeof(Visit) + (2 * SLOTS + kRecs + 13) * 8 + 8 <= kMisc, "");
     long long *sums = reinterpret_cast<long long *>(ring + (SLOTS - 1) * SH::TILE);   // until the first copies
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = same(threadIdx.x >> 5), lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < SLOTS; ++i) {
@@ -242,6 +264,7 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
             bar_init(s32(&q_empty[i]), 1);
             bar_init(s32(&s_full[i]), 1);
             bar_init(s32(&p_full[i]), 4);
+            bar_init(s32(&p_full[2 + i]), 4);
             bar_init(s32(&pv_done[i]), 1);
         }
         bar_init(s32(drain), 1);
@@ -302,10 +325,11 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
     fence_before();
     __syncthreads();
     fence_after();
-    const uint32_t tmem = *tmem_slot;
     const int n_ctas = (int)min((long long)gridDim.x, total);
     const int cta = blockIdx.x;
 
+    if (warp >= kProducer) {
+    if (NT == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegs));
     if (warp == kProducer) {
         // ---- walks the CTA's range, writes visit records, copies pages
         const long long f0 = cta < n_ctas ? total * cta / n_ctas : 0, f1 = cta < n_ctas ? total * (cta + 1) / n_ctas : 0;
@@ -458,146 +482,151 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
         }
     } else if (warp == kIssuer) {
         // ---- the products, all issued by one thread in the order in which they run
-        if (lane == 0) {
-            constexpr uint32_t idesc_s = instr_desc(BF16, false, kTile);
-            constexpr uint32_t idesc_o = instr_desc(BF16, true, 64 * SH::HALVES), idesc_t = instr_desc(BF16, true, 16);
-            bool ok = true;
-            int q_used[2] = {0, 0}, p_used[2] = {0, 0}, item = 0;
-            bool started[2] = {false, false};
-            // S of tile or buffer w of visit v
-            auto scores = [&](int v, const Visit &z, int w, bool release) {
-                const int qb = NT == 2 ? w : item & 1;
-                const uint32_t ks = (2u * v) % SLOTS;
-                const uint32_t qa = s32(q_tiles + qb * SH::TILE), ka = s32(ring + (size_t)ks * SH::TILE);
-                const uint32_t d = tmem + w * kTile;
+        constexpr uint32_t idesc_s = instr_desc(BF16, false, kTile);
+        constexpr uint32_t idesc_o = instr_desc(BF16, true, 64 * SH::HALVES), idesc_t = instr_desc(BF16, true, 16);
+        constexpr uint32_t kTail = SH::HALVES * SH::HALF_BYTES;
+        const uint32_t one = lane == 0;
+        bool ok = true;
+        int q_used[2] = {0, 0}, p_used[2] = {0, 0}, item = 0;
+        uint32_t started[2] = {0, 0};
+        const uint32_t q_base = s32(q_tiles), ring_base = s32(ring);
+        auto wait = [&](uint64_t *bar, uint32_t parity) {
+            ok = ok && __all_sync(~0u, bar_wait(s32(bar), parity, a.spin_limit, failed));
+        };
+        // S of tile or buffer w of visit v
+        auto scores = [&](int v, int flags, int w, bool release) {
+            const int qb = NT == 2 ? w : item & 1;
+            const uint32_t ks = (2u * v) % SLOTS;
+            const uint32_t qa = q_base + qb * SH::TILE, ka = ring_base + ks * SH::TILE;
+            const uint64_t da = desc(qa, 16, 1024, kSwz128), db = desc(ka, 16, 1024, kSwz128);
 #pragma unroll
-                for (int h = 0; h < SH::HALVES; ++h)
+            for (int h = 0; h < SH::HALVES; ++h)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        mma_ss(d, desc(qa + h * SH::HALF_BYTES, 16, 1024, kSwz128) + 2 * k, desc(ka + h * SH::HALF_BYTES, 16, 1024, kSwz128) + 2 * k,
-                               idesc_s, h + k > 0);
-                if (SH::TAIL)
-                    mma_ss(d, desc(qa + SH::HALVES * SH::HALF_BYTES, 16, 256, kSwz32), desc(ka + SH::HALVES * SH::HALF_BYTES, 16, 256, kSwz32),
-                           idesc_s, 1);
-                commit(s32(&s_full[w]));
-                if (z.flags & LAST) commit(s32(&q_empty[qb]));
-                if (release) commit(s32(&empty[ks]));
-            };
-            // O += P V of tile w of visit v
-            auto output = [&](int v, const Visit &z, int w, bool release) {
-                const uint32_t vs = (2u * v + 1) % SLOTS, va = s32(ring + (size_t)vs * SH::TILE);
-                const int ow = NT == 2 ? w : 0;
-                const uint32_t d = tmem + 2 * kTile + ow * kTile, p = tmem + w * kTile;
-                if (z.flags & FIRST) started[ow] = false;
+                for (int k = 0; k < 4; ++k)
+                    mma_ss(w * kTile, da + (h * SH::HALF_BYTES / 16 + 2 * k), db + (h * SH::HALF_BYTES / 16 + 2 * k), idesc_s, h + k > 0, one);
+            if (SH::TAIL) mma_ss(w * kTile, desc(qa + kTail, 16, 256, kSwz32), desc(ka + kTail, 16, 256, kSwz32), idesc_s, 1, one);
+            commit(s32(&s_full[w]), one);
+            if (flags & LAST) commit(s32(&q_empty[qb]), one);
+            if (release) commit(s32(&empty[ks]), one);
+        };
+        // O += P V of tile w of visit v, page after page; the weights come in two halves
+        auto output = [&](int v, int flags, uint32_t pages, int w, bool release) {
+            wait(&p_full[w], p_used[w] & 1);
+            if (!ok) return;
+            fence_after();
+            const uint32_t vs = (2u * v + 1) % SLOTS, va = ring_base + vs * SH::TILE;
+            const int ow = NT == 2 ? w : 0;
+            const uint32_t d = 2 * kTile + ow * kTile, p = w * kTile;
+            const uint64_t db = desc(va, SH::HALF_BYTES, 1024, kSwz128), dt = desc(va + kTail, 16, 256, kSwz32);
+            uint32_t more = flags & FIRST ? 0 : started[ow];
+            auto page = [&](int i) {
 #pragma unroll
-                for (int i = 0; i < kPages; ++i) {
-                    if (!(z.pages >> i & 1)) continue;
-#pragma unroll
-                    for (int half = 0; half < (FINE ? 2 : 1); ++half) {
-                        const uint32_t pa = p + half * (kTile / 2) + i * 8;
-                        mma_ts(d, pa, desc(va + i * (kBT * 128), SH::HALF_BYTES, 1024, kSwz128), idesc_o, started[ow]);
-                        if (SH::TAIL)
-                            mma_ts(d + 64 * SH::HALVES, pa, desc(va + SH::HALVES * SH::HALF_BYTES + i * (kBT * SH::TAIL * 2), 16, 256, kSwz32),
-                                   idesc_t, started[ow]);
-                        started[ow] = true;
-                    }
+                for (int half = 0; half < (FINE ? 2 : 1); ++half) {
+                    const uint32_t pa = p + half * (kTile / 2) + i * 8;
+                    mma_ts(d, pa, db + i * (kBT * 128 / 16), idesc_o, more, one);
+                    if (SH::TAIL) mma_ts(d + 64 * SH::HALVES, pa, dt + i * (kBT * SH::TAIL * 2 / 16), idesc_t, more, one);
+                    more = 1;
                 }
-                commit(s32(&pv_done[w]));
-                if (release) commit(s32(&empty[vs]));
             };
-            auto rec_of = [&](int v, Visit &z) {
-                ok = bar_wait(s32(&rec_full[v % kRecs]), (v / kRecs) & 1, a.spin_limit, failed);
-                if (ok) z = recs[v % kRecs];
-            };
-            auto k_ready = [&](int v) {
-                const uint32_t n = 2u * v;
-                ok = ok && bar_wait(s32(&full[n % SLOTS]), (n / SLOTS) & 1, a.spin_limit, failed);
-            };
-            auto v_ready = [&](int v) {
-                const uint32_t n = 2u * v + 1;
-                ok = ok && bar_wait(s32(&full[n % SLOTS]), (n / SLOTS) & 1, a.spin_limit, failed);
-            };
-            auto q_ready = [&](const Visit &z, int w) {
-                if (!(z.flags & FIRST)) return;
-                const int qb = NT == 2 ? w : item & 1;
-                ok = ok && bar_wait(s32(&q_full[qb]), q_used[qb] & 1, a.spin_limit, failed);
-                ++q_used[qb];
-            };
-            auto p_ready = [&](int w) {
-                ok = ok && bar_wait(s32(&p_full[w]), p_used[w] & 1, a.spin_limit, failed);
-                ++p_used[w];
-            };
-            Visit z, next;
-            rec_of(0, z);
-            if (ok && !(z.flags & END)) {
-                k_ready(0);
-                q_ready(z, 0);
+            if (pages == 0xff) {
+#pragma unroll
+                for (int i = 0; i < kPages / 2; ++i) page(i);
+            } else {
+#pragma unroll 1
+                for (uint32_t left = pages & 0xf; left; left &= left - 1) page(__ffs(left) - 1);
+            }
+            wait(&p_full[2 + w], p_used[w]++ & 1);
+            if (!ok) return;
+            fence_after();
+            if (pages == 0xff) {
+#pragma unroll
+                for (int i = kPages / 2; i < kPages; ++i) page(i);
+            } else {
+#pragma unroll 1
+                for (uint32_t left = pages & 0xf0; left; left &= left - 1) page(__ffs(left) - 1);
+            }
+            started[ow] = more;
+            commit(s32(&pv_done[w]), one);
+            if (release) commit(s32(&empty[vs]), one);
+        };
+        auto tile_ready = [&](uint32_t n) { wait(&full[n % SLOTS], (n / SLOTS) & 1); };
+        auto q_ready = [&](int flags, int w) {
+            if (!(flags & FIRST)) return;
+            const int qb = NT == 2 ? w : item & 1;
+            wait(&q_full[qb], q_used[qb] & 1);
+            ++q_used[qb];
+        };
+        wait(&rec_full[0], 0);
+        int flags = same(ok ? recs[0].flags : END);
+        uint32_t pages = same(recs[0].pages);
+        ok = ok && same(*tmem_slot) == 0;       // all columns are ours: they are counted from 0
+        if (ok && !(flags & END)) {
+            tile_ready(0);
+            q_ready(flags, 0);
+            if (ok) {
+                fence_after();
+                scores(0, flags, 0, !(NT == 2 && (flags & TWO)));
+            }
+            if (NT == 2 && (flags & TWO)) {
+                q_ready(flags, 1);
                 if (ok) {
                     fence_after();
-                    scores(0, z, 0, !(NT == 2 && (z.flags & TWO)));
-                }
-                if (NT == 2 && (z.flags & TWO)) {
-                    q_ready(z, 1);
-                    if (ok) { fence_after(); scores(0, z, 1, true); }
-                }
-                for (int v = 0; ok; ++v) {
-                    rec_of(v + 1, next);
-                    if (!ok) break;
-                    const bool more = !(next.flags & END);
-                    if (NT == 1) {
-                        const int w = v & 1;
-                        if (more) {
-                            if (z.flags & LAST) ++item;
-                            k_ready(v + 1);
-                            q_ready(next, w ^ 1);
-                            if (!ok) break;
-                            fence_after();
-                            scores(v + 1, next, w ^ 1, true);
-                        }
-                        v_ready(v);
-                        p_ready(w);
-                        if (!ok) break;
-                        fence_after();
-                        output(v, z, w, true);
-                    } else {
-                        const bool two = z.flags & TWO, next_two = more && (next.flags & TWO);
-                        v_ready(v);
-                        p_ready(0);
-                        if (!ok) break;
-                        fence_after();
-                        output(v, z, 0, !two);
-                        if (more) {
-                            k_ready(v + 1);
-                            q_ready(next, 0);
-                            if (!ok) break;
-                            fence_after();
-                            scores(v + 1, next, 0, !next_two);
-                        }
-                        if (two) {
-                            p_ready(1);
-                            if (!ok) break;
-                            fence_after();
-                            output(v, z, 1, true);
-                        }
-                        if (next_two) {
-                            q_ready(next, 1);
-                            if (!ok) break;
-                            fence_after();
-                            scores(v + 1, next, 1, true);
-                        }
-                    }
-                    if (!more) break;
-                    z = next;
+                    scores(0, flags, 1, true);
                 }
             }
-            if (!ok) {
-                *failed = 1;
-                atomicOr(a.c.status, ISV_STATUS_WAIT_EXPIRED);
-                commit(s32(drain));       // what was issued ends before tensor memory passes on
-                for (uint32_t k = 0; k < 1u << 16 && !bar_try(s32(drain), 0); ++k) {}
+            for (int v = 0; ok; ++v) {
+                wait(&rec_full[(v + 1) % kRecs], ((v + 1) / kRecs) & 1);
+                if (!ok) break;
+                const int next = same(recs[(v + 1) % kRecs].flags);
+                const uint32_t next_pages = same(recs[(v + 1) % kRecs].pages);
+                const bool more = !(next & END);
+                if (NT == 1) {
+                    const int w = v & 1;
+                    if (more) {
+                        if (flags & LAST) ++item;
+                        tile_ready(2 * v + 2);
+                        q_ready(next, 0);
+                        if (!ok) break;
+                        fence_after();
+                        scores(v + 1, next, w ^ 1, true);
+                    }
+                    tile_ready(2 * v + 1);
+                    output(v, flags, pages, w, true);
+                } else {
+                    const bool two = flags & TWO, next_two = more && (next & TWO);
+                    tile_ready(2 * v + 1);
+                    output(v, flags, pages, 0, !two);
+                    if (more) {
+                        tile_ready(2 * v + 2);
+                        q_ready(next, 0);
+                        if (!ok) break;
+                        fence_after();
+                        scores(v + 1, next, 0, !next_two);
+                    }
+                    if (two) output(v, flags, pages, 1, true);
+                    if (next_two) {
+                        q_ready(next, 1);
+                        if (!ok) break;
+                        fence_after();
+                        scores(v + 1, next, 1, true);
+                    }
+                }
+                if (!more) break;
+                flags = next;
+                pages = next_pages;
             }
         }
+        if (!ok) {
+            if (lane == 0) {
+                *failed = 1;
+                atomicOr(a.c.status, ISV_STATUS_WAIT_EXPIRED);
+            }
+            commit(s32(drain), one);       // what was issued ends before tensor memory passes on
+            for (uint32_t k = 0; k < 1u << 16 && !bar_try(s32(drain), 0); ++k) {}
+        }
+    }
     } else {
+        if (NT == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kMoreRegs));
         // ---- weights: group w of four warps, one row of its tile per thread
         const int w = warp >> 2, r = threadIdx.x & 127;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
@@ -605,7 +634,8 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
         const bool shaped = a.cap > 0.f || a.slopes || !(a.scale > 0.f);      // scores need more than a positive factor
         const float c = shaped ? kLog2e : a.scale * kLog2e;
         int used = 0;           // visits of this group
-        int tok = 0, head = 0, pos = 0;
+        int tok = 0, head = 0, pos = 0, s = 0;
+        Seq q{};
         bool live = false, any_live = false;
         Sight sight{};
         float ref = -INFINITY, l = 0.f, slope = 0.f;
@@ -620,26 +650,46 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
             const int b = NT == 2 ? w : v & 1;                                // buffer of the scores
             const uint32_t phase = NT == 2 ? used & 1 : (v >> 1) & 1;
             if (flags & FIRST) {
+                q = z.q;
+                s = z.s;
                 tok = z.token0 + w * a.TT + row_t;
                 head = z.kvh * G + z.pass * a.GT + row_g;
-                live = row_t < a.TT && tok < z.q.n && z.pass * a.GT + row_g < G;
-                pos = z.q.start + tok;
-                sight = sight_of(a, z.s, z.q, pos);
+                live = row_t < a.TT && tok < q.n && z.pass * a.GT + row_g < G;
+                pos = q.start + tok;
+                sight = sight_of(a, s, q, pos);
                 slope = a.slopes && live ? a.slopes[head] : 0.f;
                 ref = -INFINITY;
                 l = 0.f;
                 any_live = __any_sync(~0u, live);
             }
-            const int j0 = z.j0;
+            const int j0 = z.j0, slot = z.slot, partial = w == 0 ? z.partial : 0, last_page = z.last_page;
             const uint32_t pages = z.pages;
             ok = __all_sync(~0u, bar_wait(s32(&s_full[b]), phase, a.spin_limit, failed));
             if (!ok) break;
             fence_after();
+            if (partial) {
+                // rows of V behind the sequence's last token meet weights of 0; what stands there may be no number
+                const uint32_t n = 2u * v + 1;
+                ok = __all_sync(~0u, bar_wait(s32(&full[n % SLOTS]), (n / SLOTS) & 1, a.spin_limit, failed));
+                if (!ok) break;
+                if (pages >> last_page & 1) {
+                    uint8_t *vt = ring + (size_t)(n % SLOTS) * SH::TILE;
+                    const int rows = kBT - partial, first = last_page * kBT + partial;
+                    for (int i = r; i < rows * 8 * SH::HALVES; i += 128)
+                        *reinterpret_cast<uint4 *>(vt + (i / (rows * 8)) * SH::HALF_BYTES + (first + i % (rows * 8) / 8) * 128 + i % 8 * 16) =
+                            make_uint4(0, 0, 0, 0);
+                    if (SH::TAIL)
+                        for (int i = r; i < rows * 2; i += 128)
+                            *reinterpret_cast<uint4 *>(vt + SH::HALVES * SH::HALF_BYTES + (first + i / 2) * (SH::TAIL * 2) + i % 2 * 16) =
+                                make_uint4(0, 0, 0, 0);
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                }
+            }
             if (any_live) {
                 float x[kTile];
                 uint32_t *xw = reinterpret_cast<uint32_t *>(x);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) tmem_ld32(tmem + lanes + b * kTile + 32 * i, xw + 32 * i);
+                for (int i = 0; i < 4; ++i) tmem_ld32(lanes + b * kTile + 32 * i, xw + 32 * i);
                 wait_ld();
                 if (shaped) {
                     const float in = a.cap > 0.f ? 2.f * kLog2e * a.scale / a.cap : a.scale;
@@ -675,12 +725,12 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                 }
                 float top[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
-                for (int i = 4; i < kTile; ++i) top[i & 3] = fmaxf(top[i & 3], x[i]);
-                const float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * c;
+                for (int i = 4; i < kTile - 4; i += 2) top[i / 2 & 3] = max3(top[i / 2 & 3], x[i], x[i + 1]);
+                const float high = fmaxf(max3(max3(top[0], x[kTile - 4], x[kTile - 3]), max3(top[1], x[kTile - 2], x[kTile - 1]), top[2]), top[3]) * c;
                 float factor = 1.f;
                 if (ref == -INFINITY) {
                     ref = high;
-                } else if (high > ref + kSlack) {
+                } else if (high > ref + slack_of<BF16>()) {
                     factor = exp2_fast(ref - high);
                     ref = high;
                 }
@@ -691,7 +741,7 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                     ok = __all_sync(~0u, bar_wait(s32(&pv_done[NT == 2 ? w : before & 1]), (NT == 2 ? before : before >> 1) & 1, a.spin_limit, failed));
                     if (!ok) break;
                     fence_after();
-                    const uint32_t o = tmem + lanes + 2 * kTile + (NT == 2 ? w : 0) * kTile;
+                    const uint32_t o = lanes + 2 * kTile + (NT == 2 ? w : 0) * kTile;
 #pragma unroll 1
                     for (int i = 0; i < D; i += 16) {
                         uint32_t y[16];
@@ -719,37 +769,26 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                             lo[i] = narrow<BF16>(p0 - h.x, p1 - h.y);
                         }
                     }
-                    tmem_st16(tmem + lanes + b * kTile + 16 * k, hi);
-                    if (FINE) tmem_st16(tmem + lanes + b * kTile + kTile / 2 + 16 * k, lo);
+                    tmem_st16(lanes + b * kTile + 16 * k, hi);
+                    if (FINE) tmem_st16(lanes + b * kTile + kTile / 2 + 16 * k, lo);
+                    if (k == 1) {
+                        wait_st();
+                        fence_before();
+                        __syncwarp();
+                        if (lane == 0) bar_arrive(s32(&p_full[b]));
+                    }
                 }
                 const float2 total2 = unpair(add2(sum[0], sum[1]));
                 l += total2.x + total2.y;
                 wait_st();
             }
-            if (w == 0 && z.partial) {
-                // rows of V behind the sequence's last token meet weights of 0; what stands there may be no number
-                const uint32_t n = 2u * v + 1;
-                ok = __all_sync(~0u, bar_wait(s32(&full[n % SLOTS]), (n / SLOTS) & 1, a.spin_limit, failed));
-                if (!ok) break;
-                if (pages >> z.last_page & 1) {
-                    uint8_t *vt = ring + (size_t)(n % SLOTS) * SH::TILE;
-                    const int rows = kBT - z.partial, first = z.last_page * kBT + z.partial;
-                    for (int i = r; i < rows * 8 * SH::HALVES; i += 128)
-                        *reinterpret_cast<uint4 *>(vt + (i / (rows * 8)) * SH::HALF_BYTES + (first + i % (rows * 8) / 8) * 128 + i % 8 * 16) =
-                            make_uint4(0, 0, 0, 0);
-                    if (SH::TAIL)
-                        for (int i = r; i < rows * 2; i += 128)
-                            *reinterpret_cast<uint4 *>(vt + SH::HALVES * SH::HALF_BYTES + (first + i / 2) * (SH::TAIL * 2) + i % 2 * 16) =
-                                make_uint4(0, 0, 0, 0);
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                }
-            }
-            const int s = z.s, slot = z.slot;
-            const Seq q = z.q;
             ++used;
             fence_before();
             __syncwarp();
-            if (lane == 0) bar_arrive(s32(&p_full[b]));
+            if (lane == 0) {
+                if (!any_live) bar_arrive(s32(&p_full[b]));
+                bar_arrive(s32(&p_full[2 + b]));
+            }
             if (!(flags & LAST)) continue;
 
             // ---- the item's end: O / l, or a partial result
@@ -757,7 +796,7 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
             if (!ok) break;
             if (!any_live) continue;
             fence_after();
-            const uint32_t o = tmem + lanes + 2 * kTile + (NT == 2 ? w : 0) * kTile;
+            const uint32_t o = lanes + 2 * kTile + (NT == 2 ? w : 0) * kTile;
             const bool some = l != 0.f;        // NaN is some
             const long long at = ((long long)(q.first + tok) * a.c.Hq + head) * D;
             const float inv = slot < 0 ? 1.f / l : 1.f;
@@ -813,7 +852,7 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
 
     fence_before();
     __syncthreads();
-    if (warp == kIssuer) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    if (warp == kIssuer) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(*tmem_slot) : "memory");
 }
 
 // ---------------------------------------------------------------- merging
