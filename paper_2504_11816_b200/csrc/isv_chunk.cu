@@ -318,8 +318,10 @@ int isv_chunk_attn(isv_chunk *h, const void *pool_dev, int32_t n_pages, const in
     p.out = static_cast<uint16_t *>(out_dev); p.out_f32 = out_f32_dev;
     p.scale = h->d.scale != 0.f ? h->d.scale : (float)(1.0 / std::sqrt((double)h->d.head_dim));
     p.cap = h->d.softcap;
-    p.GT = h->GT; p.P = h->P; p.TT = 128 / h->GT;
-    const int tokens = attn_tiles((long long)T * h->GT) * p.TT;
+    p.GT = h->GT; p.P = h->P;
+    p.tile_rows = attn_tile_rows((long long)T * h->GT);
+    p.TT = std::min(p.tile_rows, 128) / h->GT;
+    const int tokens = p.tile_rows / std::min(p.tile_rows, 128) * p.TT;
     p.RT = (T + tokens - 1) / tokens;
     if ((long long)n_seqs * p.RT >= (1ll << 31)) return err(ISV_EINVAL, "%s: n_seqs * T too large", who);
     p.part_o = h->part_o; p.part_ml = h->part_ml; p.merges = h->merges;

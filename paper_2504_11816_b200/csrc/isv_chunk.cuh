@@ -40,7 +40,8 @@ struct AttnParams {
     float cap;                  // 0: scores are not capped
     // how the work is cut (attn_shape), and scratch
     int32_t GT, P;              // a visit serves GT of a KV head's query heads; P passes serve all of them
-    int32_t TT, RT;             // tokens of a row tile; items that a chunk of T tokens has at most, per KV head and pass
+    int32_t tile_rows;          // rows of an item, as attn_tile_rows says
+    int32_t TT, RT;             // tokens of a tile of (at most) 128 rows; items that a chunk of T tokens has at most, per KV head and pass
     float *part_o;              // partial results: [slot][D / 4][rows of an item] of four values, two slots a CTA
     float *part_ml;             // [slot][rows of an item] of (reference, sum)
     MergeRec *merges;           // [grid]: the item that begins in this CTA's range and ends in another's
@@ -48,14 +49,14 @@ struct AttnParams {
     int32_t drop_first_copy;    // failure injection: the first visit's barrier of CTA 0 is armed without issuing one of its copies
 };
 
-// Rows of an item (NT row tiles of 128), whose partial results are in slot 2 * first + 1 and in 2 * c for the CTAs c up to `last`.
+// An item whose partial results are in slot 2 * first + 1 and in 2 * c for the CTAs c up to `last`.
 struct MergeRec {
     int32_t n;                  // partial results, 0: none
     int32_t last, s, token0, kvh, pass;
 };
 
-// The launchers.  NT: row tiles of an item; FINE: weights enter their product as two 16-bit numbers.
-int attn_tiles(long long rows);                                    // row tiles of an item, for that many rows per KV head
+// The launchers.
+int attn_tile_rows(long long rows);                                // rows of an item (32, 64, 128 or 256), for that many rows per KV head
 size_t attn_part_rows(int grid);                                   // rows of partial results
 cudaError_t attn_configure(int D, bool bf16);
 cudaError_t launch_attn(const AttnParams &p, int D, bool bf16, int grid, cudaStream_t st, const char **what);

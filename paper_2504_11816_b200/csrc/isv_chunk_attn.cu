@@ -12,7 +12,9 @@
 //
 // A CTA: a producer warp copies a visit's pages (K, then V) into a ring by TMA; one thread issues the products; NT groups of four
 // warps turn scores into weights, one row per thread.  With NT = 2 the groups take turns with the tensor cores: while one
-// computes its weights, the other's products run.  With NT = 1 the scores of the next visit are computed meanwhile.
+// computes its weights, the other's products run.  With NT = 1 the scores of the next visit are computed meanwhile.  Where a KV
+// head has no more than 64 or 32 rows, the tile holds R = 2 or 4 copies of them, each for its share of a visit's columns (a warp
+// reaches only its own quarter of tensor memory's lanes), and the weights meet as an operand in shared memory.
 //
 // Layout: the pool's rows hold their 16-byte chunks in the order that the 128-byte swizzle of tensor-core operands wants
 // (chunk c of token t at c XOR t mod 8), so a page's 64-element half rows are copied by an unswizzled box of {64, 16} each and
@@ -218,11 +220,16 @@ struct Shape {
     static constexpr int HALVES = D / 64, TAIL = D % 64;                          // of a row: 64 elements each, and the rest
     static constexpr int HALF_BYTES = kTile * 128, TAIL_BYTES = kTile * TAIL * 2;
     static constexpr int TILE = HALVES * HALF_BYTES + TAIL_BYTES;                 // a tile of Q, K or V
-    static constexpr int SLOTS = D == 128 ? 5 : D == 80 ? 9 : 10;
+    // tiles of the ring; where the weights are in shared memory (32 KB), 128 KB of it (deeper rings are no faster)
+    static __host__ __device__ constexpr int slots(int R) { return R > 1 ? (D == 128 ? 4 : D == 80 ? 6 : 8) : D == 128 ? 5 : D == 80 ? 9 : 10; }
 };
-constexpr int kMisc = 1536;
+constexpr int kMisc = 1024;
+constexpr int kWeights = 2 * 64 * 256;     // R > 1: weights of up to 64 rows as two 16-bit numbers each
+constexpr int kExchange = 2 * kTile * 4;   // R > 1: maxima and sums that the copies of a row exchange
 template <int D>
-constexpr size_t smem_bytes() { return 1024 + (size_t)(2 + Shape<D>::SLOTS) * Shape<D>::TILE + kMisc; }
+constexpr size_t smem_bytes(int R) {
+    return 1024 + (size_t)(2 + Shape<D>::slots(R)) * Shape<D>::TILE + kMisc + (R > 1 ? kWeights + kExchange : 0);
+}
 
 // warps: NT groups of four for the weights, then the producer, the issuer of products, the loader of Q, and one that rests
 template <int NT>
@@ -231,25 +238,27 @@ __host__ __device__ constexpr int threads_of() { return NT * 128 + 128; }
 // 104: 2 * 128 * 200 + 128 * 104 = 384 * 168.
 constexpr int kMoreRegs = 200, kFewRegs = 104;
 
-template <int D, bool BF16, int NT, bool FINE>
+template <int D, bool BF16, int NT, int R, bool FINE>
 __global__ void __launch_bounds__(threads_of<NT>(), 1)
 attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ CUtensorMap map_kv_tail,
             const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_q_tail, const __grid_constant__ AttnParams a) {
     using SH = Shape<D>;
-    constexpr int SLOTS = SH::SLOTS, NTHREADS = threads_of<NT>(), NWARPS = NTHREADS / 32;
+    constexpr int SLOTS = SH::slots(R), NTHREADS = threads_of<NT>(), NWARPS = NTHREADS / 32;
     constexpr int kProducer = NT * 4, kIssuer = NT * 4 + 1, kLoader = NT * 4 + 2;
     constexpr float kOffset = BF16 ? 0.f : 7.f;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (s32(smem_raw) & 1023u)) & 1023u);
-    uint8_t *q_tiles = smem, *ring = smem + 2 * SH::TILE;
+    // the weights come first: what their operand's unused rows read is still shared memory of this CTA
+    uint8_t *weights = smem, *q_tiles = smem + (R > 1 ? kWeights : 0), *ring = q_tiles + 2 * SH::TILE;
     uint8_t *misc = ring + SLOTS * SH::TILE;
+    float *exchange = reinterpret_cast<float *>(misc + kMisc);      // [2][copy of the rows][row]
     Visit *recs = reinterpret_cast<Visit *>(misc);
     uint64_t *bars = reinterpret_cast<uint64_t *>(misc + kRecs * sizeof(Visit));
     uint64_t *full = bars, *empty = full + SLOTS, *rec_full = empty + SLOTS, *q_full = rec_full + kRecs, *q_empty = q_full + 2;
-    uint64_t *s_full = q_empty + 2, *p_full = s_full + 2, *pv_done = p_full + 4, *drain = pv_done + 2;   // p_full: [half of the tokens][2]
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(drain + 1);
+    uint64_t *s_full = q_empty + 2, *p_full = s_full + 2, *pv_done = p_full + 4, *drain = pv_done + 2, *x_full = drain + 1;   // p_full: [half of the tokens][2]
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(x_full + 1);
     volatile int *failed = reinterpret_cast<volatile int *>(tmem_slot + 1);
-    static_assert(kRecs * sizeof(Visit) + (2 * SLOTS + kRecs + 13) * 8 + 8 <= kMisc, "");
+    static_assert(kRecs * sizeof(Visit) + (2 * SLOTS + kRecs + 14) * 8 + 8 <= kMisc, "");
     long long *sums = reinterpret_cast<long long *>(ring + (SLOTS - 1) * SH::TILE);   // until the first copies
     const int warp = same(threadIdx.x >> 5), lane = threadIdx.x & 31;
 
@@ -268,6 +277,7 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
             bar_init(s32(&pv_done[i]), 1);
         }
         bar_init(s32(drain), 1);
+        bar_init(s32(x_full), 4);
         *failed = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -469,9 +479,13 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                     ++used[buf];
                     const uint32_t dst = s32(q_tiles + buf * SH::TILE), bar = s32(&q_full[buf]);
                     const int rows = a.GT * a.TT, head = z.kvh * (a.c.Hq / a.c.Hkv) + z.pass * a.GT, token = z.q.first + z.token0 + i * a.TT;
-                    bar_expect(bar, rows * D * 2);
-                    for (int h = 0; h < SH::HALVES; ++h) tma_3d(dst + h * SH::HALF_BYTES, &map_q, 64 * h, head, token, bar);
-                    if (SH::TAIL) tma_3d(dst + SH::HALVES * SH::HALF_BYTES, &map_q_tail, 64 * SH::HALVES, head, token, bar);
+                    bar_expect(bar, R * rows * D * 2);
+                    for (int y = 0; y < R; ++y) {
+                        for (int h = 0; h < SH::HALVES; ++h)
+                            tma_3d(dst + h * SH::HALF_BYTES + y * (kTile / R * 128), &map_q, 64 * h, head, token, bar);
+                        if (SH::TAIL)
+                            tma_3d(dst + SH::HALVES * SH::HALF_BYTES + y * (kTile / R * SH::TAIL * 2), &map_q_tail, 64 * SH::HALVES, head, token, bar);
+                    }
                 }
                 ++item;
             }
@@ -518,13 +532,20 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
             const int ow = NT == 2 ? w : 0;
             const uint32_t d = 2 * kTile + ow * kTile, p = w * kTile;
             const uint64_t db = desc(va, SH::HALF_BYTES, 1024, kSwz128), dt = desc(va + kTail, 16, 256, kSwz32);
+            const uint64_t dp = desc(s32(weights), 16, 1024, kSwz128);
             uint32_t more = flags & FIRST ? 0 : started[ow];
             auto page = [&](int i) {
 #pragma unroll
                 for (int half = 0; half < (FINE ? 2 : 1); ++half) {
-                    const uint32_t pa = p + half * (kTile / 2) + i * 8;
-                    mma_ts(d, pa, db + i * (kBT * 128 / 16), idesc_o, more, one);
-                    if (SH::TAIL) mma_ts(d + 64 * SH::HALVES, pa, dt + i * (kBT * SH::TAIL * 2 / 16), idesc_t, more, one);
+                    if (R > 1) {
+                        const uint64_t pa = dp + half * (kWeights / 2 / 16) + (i / 4) * (kTile / R * 128 / 16) + 2 * (i % 4);
+                        mma_ss(d, pa, db + i * (kBT * 128 / 16), idesc_o, more, one);
+                        if (SH::TAIL) mma_ss(d + 64 * SH::HALVES, pa, dt + i * (kBT * SH::TAIL * 2 / 16), idesc_t, more, one);
+                    } else {
+                        const uint32_t pa = p + half * (kTile / 2) + i * 8;
+                        mma_ts(d, pa, db + i * (kBT * 128 / 16), idesc_o, more, one);
+                        if (SH::TAIL) mma_ts(d + 64 * SH::HALVES, pa, dt + i * (kBT * SH::TAIL * 2 / 16), idesc_t, more, one);
+                    }
                     more = 1;
                 }
             };
@@ -581,17 +602,24 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                 const uint32_t next_pages = same(recs[(v + 1) % kRecs].pages);
                 const bool more = !(next & END);
                 if (NT == 1) {
+                    // the next visit's scores go first if their tile is there
                     const int w = v & 1;
-                    if (more) {
+                    const uint32_t k_next = 2 * v + 2;
+                    bool early = more && __all_sync(~0u, bar_try(s32(&full[k_next % SLOTS]), (k_next / SLOTS) & 1));
+                    auto ahead = [&]() {
                         if (flags & LAST) ++item;
-                        tile_ready(2 * v + 2);
+                        tile_ready(k_next);
                         q_ready(next, 0);
-                        if (!ok) break;
+                        if (!ok) return;
                         fence_after();
                         scores(v + 1, next, w ^ 1, true);
-                    }
+                    };
+                    if (early) ahead();
+                    if (!ok) break;
                     tile_ready(2 * v + 1);
                     output(v, flags, pages, w, true);
+                    if (!ok) break;
+                    if (more && !early) ahead();
                 } else {
                     const bool two = flags & TWO, next_two = more && (next & TWO);
                     tile_ready(2 * v + 1);
@@ -630,7 +658,23 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
         // ---- weights: group w of four warps, one row of its tile per thread
         const int w = warp >> 2, r = threadIdx.x & 127;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const int row_t = r / a.GT, row_g = r - row_t * a.GT, G = a.c.Hq / a.c.Hkv;
+        bool ok = true;
+        constexpr int ROWS = kTile / R, COLS = kTile / R;                      // of a copy
+        const int rr = r % ROWS, part = r / ROWS, col0 = part * COLS;
+        const int row_t = rr / a.GT, row_g = rr - row_t * a.GT, G = a.c.Hq / a.c.Hkv;
+        uint32_t x_phase = 0;   // exchanges so far
+        // what the copies of this thread's row hold of x; every warp takes part
+        auto gather = [&](float x, float (&all)[R]) {
+            float *at = exchange + (x_phase & 1) * kTile;
+            at[r] = x;
+            __syncwarp();
+            if (lane == 0) bar_arrive(s32(x_full));
+            ok = __all_sync(~0u, bar_wait(s32(x_full), x_phase & 1, a.spin_limit, failed));
+            ++x_phase;
+            if (!ok) return;
+#pragma unroll
+            for (int i = 0; i < R; ++i) all[i] = at[i * ROWS + rr];
+        };
         const bool shaped = a.cap > 0.f || a.slopes || !(a.scale > 0.f);      // scores need more than a positive factor
         const float c = shaped ? kLog2e : a.scale * kLog2e;
         int used = 0;           // visits of this group
@@ -639,7 +683,6 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
         bool live = false, any_live = false;
         Sight sight{};
         float ref = -INFINITY, l = 0.f, slope = 0.f;
-        bool ok = true;
         for (int v = 0;; ++v) {
             ok = __all_sync(~0u, bar_wait(s32(&rec_full[v % kRecs]), (v / kRecs) & 1, a.spin_limit, failed));
             if (!ok) break;
@@ -686,47 +729,56 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                 }
             }
             if (any_live) {
-                float x[kTile];
+                float x[COLS];
                 uint32_t *xw = reinterpret_cast<uint32_t *>(x);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) tmem_ld32(lanes + b * kTile + 32 * i, xw + 32 * i);
+                for (int i = 0; i < COLS / 32; ++i) tmem_ld32(lanes + b * kTile + col0 + 32 * i, xw + 32 * i);
                 wait_ld();
+                const int j1 = j0 + col0;                                      // this thread's columns
                 if (shaped) {
                     const float in = a.cap > 0.f ? 2.f * kLog2e * a.scale / a.cap : a.scale;
-                    const float distance = (float)(pos - j0);
+                    const float distance = (float)(pos - j1);
                     if (a.cap > 0.f) {
                         // cap tanh(y) = cap - 2 cap / (e^2y + 1): off by a few 2^-24 of the cap
 #pragma unroll
-                        for (int i = 0; i < kTile; ++i) {
+                        for (int i = 0; i < COLS; ++i) {
                             const float e = exp2_fast(x[i] * in);
                             x[i] = fmaf(-2.f * a.cap, reciprocal(e + 1.f), a.cap);
                         }
                     } else {
 #pragma unroll
-                        for (int i = 0; i < kTile; ++i) x[i] *= in;
+                        for (int i = 0; i < COLS; ++i) x[i] *= in;
                     }
                     if (a.slopes) {
 #pragma unroll
-                        for (int i = 0; i < kTile; ++i) x[i] = fmaf(-slope, fabsf(distance - (float)i), x[i]);
+                        for (int i = 0; i < COLS; ++i) x[i] = fmaf(-slope, fabsf(distance - (float)i), x[i]);
                     }
                 }
                 const bool all = pages == 0xff && sight.lim >= j0 + kTile && (sight.low <= j0 || sight.prefix >= j0 + kTile);
                 if (!__all_sync(~0u, all || !live)) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        // bit i: token j0 + 32 k + i is seen
+                    for (int k = 0; k < COLS / 32; ++k) {
+                        // bit i: token j1 + 32 k + i is seen
                         auto below = [&](int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; };
-                        const int at = j0 + 32 * k;
+                        const int at = j1 + 32 * k;
+                        const uint32_t here = pages >> (2 * k + col0 / kBT);
                         uint32_t seen = below(sight.lim - at) & (~below(sight.low - at) | below(sight.prefix - at));
-                        seen &= (pages >> (2 * k) & 1 ? 0xffffu : 0u) | (pages >> (2 * k + 1) & 1 ? 0xffff0000u : 0u);
+                        seen &= (here & 1 ? 0xffffu : 0u) | (here & 2 ? 0xffff0000u : 0u);
 #pragma unroll
                         for (int i = 0; i < 32; ++i) x[32 * k + i] = seen >> i & 1 ? x[32 * k + i] : -INFINITY;
                     }
                 }
                 float top[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
-                for (int i = 4; i < kTile - 4; i += 2) top[i / 2 & 3] = max3(top[i / 2 & 3], x[i], x[i + 1]);
-                const float high = fmaxf(max3(max3(top[0], x[kTile - 4], x[kTile - 3]), max3(top[1], x[kTile - 2], x[kTile - 1]), top[2]), top[3]) * c;
+                for (int i = 4; i < COLS - 4; i += 2) top[i / 2 & 3] = max3(top[i / 2 & 3], x[i], x[i + 1]);
+                float high = fmaxf(max3(max3(top[0], x[COLS - 4], x[COLS - 3]), max3(top[1], x[COLS - 2], x[COLS - 1]), top[2]), top[3]) * c;
+                if (R > 1) {
+                    float of[R];
+                    gather(high, of);
+                    if (!ok) break;
+#pragma unroll
+                    for (int i = 0; i < R; ++i) high = fmaxf(high, of[i]);
+                }
                 float factor = 1.f;
                 if (ref == -INFINITY) {
                     ref = high;
@@ -734,29 +786,37 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                     factor = exp2_fast(ref - high);
                     ref = high;
                 }
+                const uint32_t before = NT == 2 ? used - 1 : v - 1;            // the product before this one
+                if (R > 1 && v > 0) {
+                    // it has read the weights that are overwritten now
+                    ok = __all_sync(~0u, bar_wait(s32(&pv_done[before & 1]), (before >> 1) & 1, a.spin_limit, failed));
+                    if (!ok) break;
+                }
                 if (__any_sync(~0u, factor != 1.f)) {
                     // O is scaled: the product before this one has to be in it
                     l *= factor;
-                    const uint32_t before = NT == 2 ? used - 1 : v - 1;
                     ok = __all_sync(~0u, bar_wait(s32(&pv_done[NT == 2 ? w : before & 1]), (NT == 2 ? before : before >> 1) & 1, a.spin_limit, failed));
                     if (!ok) break;
                     fence_after();
                     const uint32_t o = lanes + 2 * kTile + (NT == 2 ? w : 0) * kTile;
+                    if (part == 0) {
 #pragma unroll 1
-                    for (int i = 0; i < D; i += 16) {
-                        uint32_t y[16];
-                        tmem_ld16(o + i, y);
-                        wait_ld();
+                        for (int i = 0; i < D; i += 16) {
+                            uint32_t y[16];
+                            tmem_ld16(o + i, y);
+                            wait_ld();
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) y[k] = __float_as_uint(__uint_as_float(y[k]) * factor);
-                        tmem_st16(o + i, y);
+                            for (int k = 0; k < 16; ++k) y[k] = __float_as_uint(__uint_as_float(y[k]) * factor);
+                            tmem_st16(o + i, y);
+                        }
+                        wait_st();
                     }
                 }
                 const float minus = ref == -INFINITY ? 0.f : kOffset - ref;
                 const uint64_t cc = pair(c, c), mm = pair(minus, minus);
                 uint64_t sum[2] = {pair(0.f, 0.f), pair(0.f, 0.f)};
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
+                for (int k = 0; k < COLS / 32; ++k) {
                     uint32_t hi[16], lo[16];
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
@@ -769,6 +829,18 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                             lo[i] = narrow<BF16>(p0 - h.x, p1 - h.y);
                         }
                     }
+                    if (R > 1) {
+                        // rows of 64 columns with the 128-byte swizzle
+                        const int col = col0 + 32 * k;
+                        uint8_t *row = weights + (col / 64) * (ROWS * 128) + rr * 128;
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) {
+                            const int chunk = (col % 64 / 8 + y) ^ (rr & 7);
+                            *reinterpret_cast<uint4 *>(row + chunk * 16) = make_uint4(hi[4 * y], hi[4 * y + 1], hi[4 * y + 2], hi[4 * y + 3]);
+                            *reinterpret_cast<uint4 *>(row + kWeights / 2 + chunk * 16) = make_uint4(lo[4 * y], lo[4 * y + 1], lo[4 * y + 2], lo[4 * y + 3]);
+                        }
+                        continue;
+                    }
                     tmem_st16(lanes + b * kTile + 16 * k, hi);
                     if (FINE) tmem_st16(lanes + b * kTile + kTile / 2 + 16 * k, lo);
                     if (k == 1) {
@@ -780,13 +852,18 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                 }
                 const float2 total2 = unpair(add2(sum[0], sum[1]));
                 l += total2.x + total2.y;
-                wait_st();
+                if (R > 1) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                else wait_st();
+            } else if (R > 1) {
+                float of[R];
+                gather(-INFINITY, of);
+                if (!ok) break;
             }
             ++used;
             fence_before();
             __syncwarp();
             if (lane == 0) {
-                if (!any_live) bar_arrive(s32(&p_full[b]));
+                if (R > 1 || !any_live) bar_arrive(s32(&p_full[b]));
                 bar_arrive(s32(&p_full[2 + b]));
             }
             if (!(flags & LAST)) continue;
@@ -794,7 +871,17 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
             // ---- the item's end: O / l, or a partial result
             ok = __all_sync(~0u, bar_wait(s32(&pv_done[b]), phase, a.spin_limit, failed));
             if (!ok) break;
-            if (!any_live) continue;
+            if (R > 1) {
+                float of[R];
+                gather(l, of);
+                if (!ok) break;
+                if (any_live) {
+                    l = 0.f;
+#pragma unroll
+                    for (int i = 0; i < R; ++i) l += of[i];
+                }
+            }
+            if (!any_live || part > 0) continue;
             fence_after();
             const uint32_t o = lanes + 2 * kTile + (NT == 2 ? w : 0) * kTile;
             const bool some = l != 0.f;        // NaN is some
@@ -939,7 +1026,7 @@ bool encode(CUtensorMap *m, bool bf16, int rank, const void *base, const cuuint6
                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, bool BF16, int NT, bool FINE>
+template <int D, bool BF16, int NT, int R, bool FINE>
 cudaError_t launch(const AttnParams &p, int grid, cudaStream_t st, const char **what) {
     CUtensorMap kv{}, kv_tail{}, q{}, q_tail{};
     if (!encode_fn()) { *what = "cuTensorMapEncodeTiled is not available from this driver"; return cudaErrorUnknown; }
@@ -956,39 +1043,50 @@ cudaError_t launch(const AttnParams &p, int grid, cudaStream_t st, const char **
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(grid);
     cfg.blockDim = dim3(threads_of<NT>());
-    cfg.dynamicSmemBytes = smem_bytes<D>();
+    cfg.dynamicSmemBytes = smem_bytes<D>(R);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    cudaError_t e = cudaLaunchKernelEx(&cfg, attn_kernel<D, BF16, NT, FINE>, kv, kv_tail, q, q_tail, p);
+    cudaError_t e = cudaLaunchKernelEx(&cfg, attn_kernel<D, BF16, NT, R, FINE>, kv, kv_tail, q, q_tail, p);
     if (e != cudaSuccess) return e;
-    cfg.gridDim = dim3(grid, NT * kTile / 32);
+    cfg.gridDim = dim3(grid, NT * kTile / R / 32);
     cfg.blockDim = dim3(kMergeThreads);
     cfg.dynamicSmemBytes = 0;
     return cudaLaunchKernelEx(&cfg, merge_kernel<D, BF16>, p);
 }
 
-template <int D, bool BF16>
-cudaError_t configure() {
-    cudaError_t e = cudaFuncSetAttribute(attn_kernel<D, BF16, 1, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D>());
-    if (e == cudaSuccess)
-        e = cudaFuncSetAttribute(attn_kernel<D, BF16, 2, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D>());
-    if (e == cudaSuccess)
-        e = cudaFuncSetAttribute(attn_kernel<D, BF16, 2, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D>());
-    return e;
+template <int D, bool BF16, int NT, int R, bool FINE>
+cudaError_t allow() {
+    return cudaFuncSetAttribute(attn_kernel<D, BF16, NT, R, FINE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D>(R));
 }
 template <int D, bool BF16>
+cudaError_t configure() {
+    cudaError_t e = allow<D, BF16, 1, 4, true>();
+    if (e == cudaSuccess) e = allow<D, BF16, 1, 2, true>();
+    if (e == cudaSuccess) e = allow<D, BF16, 1, 1, true>();
+    if (e == cudaSuccess) e = allow<D, BF16, 2, 1, true>();
+    if (e == cudaSuccess) e = allow<D, BF16, 2, 1, false>();
+    return e;
+}
+// Weights enter their product as two 16-bit numbers (fp32's precision, one product more) wherever that costs little: with up to
+// 128 rows per KV head the call is bound by reading the cache.  Beyond that the tensor cores bound it, and a 16-bit output gets
+// weights rounded to 16 bits, an error of the order of its own rounding; with an fp32 output they stay exact.
+template <int D, bool BF16>
 cudaError_t pick(const AttnParams &p, int grid, cudaStream_t st, const char **what) {
-    if (attn_tiles((long long)p.c.T * p.GT) == 1) return launch<D, BF16, 1, true>(p, grid, st, what);
-    return p.out_f32 ? launch<D, BF16, 2, true>(p, grid, st, what) : launch<D, BF16, 2, false>(p, grid, st, what);
+    switch (p.tile_rows) {
+    case 32: return launch<D, BF16, 1, 4, true>(p, grid, st, what);
+    case 64: return launch<D, BF16, 1, 2, true>(p, grid, st, what);
+    case 128: return launch<D, BF16, 1, 1, true>(p, grid, st, what);
+    default: return p.out_f32 ? launch<D, BF16, 2, 1, true>(p, grid, st, what) : launch<D, BF16, 2, 1, false>(p, grid, st, what);
+    }
 }
 
 }  // namespace
 
-int attn_tiles(long long rows) { return rows <= kTile ? 1 : 2; }
+int attn_tile_rows(long long rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= kTile ? kTile : 2 * kTile; }
 size_t attn_part_rows(int grid) { return (size_t)2 * grid * 2 * kTile; }
 
 cudaError_t attn_configure(int D, bool bf16) {
