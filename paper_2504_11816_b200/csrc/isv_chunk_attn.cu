@@ -40,6 +40,10 @@ namespace {
 constexpr int kTile = 128;             // rows of a tile, tokens of a visit
 constexpr int kPages = kTile / kBT;
 constexpr int kRecs = 8;               // visit records in flight (a ring of at most 10 tiles is less than 6 visits ahead)
+#ifndef POLY
+#define POLY 0
+#endif
+constexpr int kPoly = POLY;               // of 16 powers of two, those that are taken by a polynomial where weights are rounded to 16 bits
 constexpr float kLog2e = 1.4426950408889634f;
 // How far a row's maximum may pass its reference before the reference follows (and O is scaled): fp16 weights have to stay below 2^16;
 // bf16's are as exact at 2^40 as at 1, and fp32 sums of 2^40 times values up to 2^70 do not overflow.  With heavy-tailed
@@ -101,24 +105,25 @@ __host__ __device__ constexpr uint32_t instr_desc(bool bf16, bool b_mn_major, in
     return (1u << 4) | ((bf16 ? 1u : 0u) << 7) | ((bf16 ? 1u : 0u) << 10) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) |
            ((uint32_t)(kTile >> 4) << 24);
 }
-// The issuing warp runs these as a whole, so that operands stay in uniform registers; the thread with `one` set issues.
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate, uint32_t one) {
+// The issuing warp runs these as a whole, so that operands stay in uniform registers, and each elects the thread that issues (a
+// predicate of the lane's number instead costs 40 cycles an instruction: 64 users' drafts 156 us instead of 141, single tokens 118
+// instead of 93).
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
-        "{\n.reg .pred p, q;\nsetp.ne.b32 p, %4, 0;\nsetp.ne.b32 q, %5, 0;\n@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(one)
+        "{\n.reg .pred p, q;\nsetp.ne.b32 p, %4, 0;\nelect.sync _|q, 0xffffffff;\n@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
         : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate, uint32_t one) {
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
-        "{\n.reg .pred p, q;\nsetp.ne.b32 p, %4, 0;\nsetp.ne.b32 q, %5, 0;\n@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(
+        "{\n.reg .pred p, q;\nsetp.ne.b32 p, %4, 0;\nelect.sync _|q, 0xffffffff;\n@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(
             d),
-        "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(one)
+        "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
         : "memory");
 }
-__device__ __forceinline__ void commit(uint32_t bar, uint32_t one) {
+__device__ __forceinline__ void commit(uint32_t bar) {
     asm volatile(
-        "{\n.reg .pred q;\nsetp.ne.b32 q, %1, 0;\n@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(bar),
-        "r"(one)
+        "{\n.reg .pred q;\nelect.sync _|q, 0xffffffff;\n@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(bar)
         : "memory");
 }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -150,6 +155,15 @@ __device__ __forceinline__ void tmem_st16(uint32_t a, const uint32_t *r) {
         "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
+__device__ __forceinline__ void tmem_st32(uint32_t a, const uint32_t *r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, "
+        "%20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(a),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
+        "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
 __device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -158,9 +172,10 @@ __device__ __forceinline__ float exp2_fast(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// NaN if one of them is
 __device__ __forceinline__ float max3(float x, float y, float z) {
     float r;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
     return r;
 }
 __device__ __forceinline__ float reciprocal(float x) {
@@ -188,8 +203,67 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t both(float x) { return pair(x, x); }
+
+// 2^x of two numbers without the special-function unit: x = n + f with |f| <= 1/2, a polynomial for 2^f whose constant is 1 (least
+// largest relative error on that range, fitted: degree 3 1.0e-4, degree 4 2.8e-6), n added to its exponent.  For weights that are
+// rounded to 16 bits next (2^-9 and 2^-12 of themselves).  -infinity gives 0; x is not above 127, and no NaN.
+template <int DEGREE>
+__device__ __forceinline__ float2 exp2_poly(uint64_t x) {
+    const uint64_t magic = both(12582912.f);             // 1.5 * 2^23: a sum with it has the rounded x in its low bits
+    const float2 v = unpair(x);
+    x = pair(fmaxf(v.x, -127.f), fmaxf(v.y, -127.f));
+    const uint64_t t = add2(x, magic);
+    const uint64_t f = fma2(add2(t, both(-12582912.f)), both(-1.f), x);
+    uint64_t y;
+    if (DEGREE == 3) {
+        y = fma2(both(0.05500892922282219f), f, both(0.24221095442771912f));
+        y = fma2(y, f, both(0.6932829022407532f));
+    } else {
+        y = fma2(both(0.009582852944731712f), f, both(0.055906426161527634f));
+        y = fma2(y, f, both(0.24024099111557007f));
+        y = fma2(y, f, both(0.6931241750717163f));
+    }
+    y = fma2(y, f, both(1.f));
+    const float2 z = unpair(y), n = unpair(t);
+    return make_float2(__int_as_float(__float_as_int(z.x) + (__float_as_int(n.x) << 23)), __int_as_float(__float_as_int(z.y) + (__float_as_int(n.y) << 23)));
+}
+// tanh for |x| <= 1: an odd polynomial of degree 13 (least largest error, fitted: 2.0e-8)
+__device__ __forceinline__ uint64_t tanh_poly(uint64_t x) {
+    const uint64_t z = mul2(x, x);
+    uint64_t y = fma2(both(0.0009637724724598229f), z, both(-0.005951281636953354f));
+    y = fma2(y, z, both(0.019973283633589745f));
+    y = fma2(y, z, both(-0.05326583608984947f));
+    y = fma2(y, z, both(0.13319583237171173f));
+    y = fma2(y, z, both(-0.33332130312919617f));
+    y = fma2(y, z, both(0.9999997019767761f));
+    return mul2(y, x);
+}
 
 // ---------------------------------------------------------------- how the work is cut
+
+// `total` positions over n CTAs, the first `total mod n` of which get one more.
+struct Cut {
+    long long each, more;       // more: CTAs with each + 1
+    __device__ Cut(long long total, int n) {
+        // 64-bit division is a long way; nearly every total fits in 32
+        if (total >> 31) each = total / n;
+        else each = (int)total / n;
+        more = total - each * n;
+    }
+    __device__ long long first(int c) const { return c * each + min((long long)c, more); }
+    __device__ int cta_of(long long x) const {
+        const long long border = more * (each + 1);
+        if (x < border) return x >> 31 ? (int)(x / (each + 1)) : (int)x / (int)(each + 1);
+        const long long y = x - border;
+        return (int)more + (y >> 31 || each >> 31 ? (int)(y / each) : (int)y / (int)each);
+    }
+};
 
 struct Item {
     int s, token0, kvh, pass;   // first token of the chunk in it
@@ -234,11 +308,7 @@ constexpr size_t smem_bytes(int R) {
 // warps: NT groups of four for the weights, then the producer, the issuer of products, the loader of Q, and one that rests
 template <int NT>
 __host__ __device__ constexpr int threads_of() { return NT * 128 + 128; }
-// With NT = 2 a thread starts with 168 registers; the groups that hold a row of scores go up to 200, the other warps down to
-// 104: 2 * 128 * 200 + 128 * 104 = 384 * 168.
-constexpr int kMoreRegs = 200, kFewRegs = 104;
-
-template <int D, bool BF16, int NT, int R, bool FINE>
+template <int D, bool BF16, int NT, int R, bool FINE, bool SHAPED>
 __global__ void __launch_bounds__(threads_of<NT>(), 1)
 attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ CUtensorMap map_kv_tail,
             const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_q_tail, const __grid_constant__ AttnParams a) {
@@ -338,11 +408,10 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
     const int n_ctas = (int)min((long long)gridDim.x, total);
     const int cta = blockIdx.x;
 
-    if (warp >= kProducer) {
-    if (NT == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegs));
     if (warp == kProducer) {
         // ---- walks the CTA's range, writes visit records, copies pages
-        const long long f0 = cta < n_ctas ? total * cta / n_ctas : 0, f1 = cta < n_ctas ? total * (cta + 1) / n_ctas : 0;
+        const Cut cut(total, max(n_ctas, 1));
+        const long long f0 = cta < n_ctas ? cut.first(cta) : 0, f1 = cta < n_ctas ? cut.first(cta + 1) : 0;
         MergeRec rec{};
         int v = 0;              // visits so far
         uint32_t seq = 0;       // tiles so far: K and V of a visit
@@ -382,7 +451,7 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                     const bool begins = b == 0, ends = e == w - 1;
                     const int slot = begins && ends ? -1 : 2 * cta + (begins ? 1 : 0);
                     if (begins && !ends) {
-                        rec.last = (int)(((at + w) * n_ctas - 1) / total);
+                        rec.last = cut.cta_of(at + w - 1);
                         rec.n = rec.last - cta + 1;
                         rec.s = s; rec.token0 = token0; rec.kvh = kvh; rec.pass = pass;
                         // now: the record is this launch's, whatever becomes of the visits
@@ -437,12 +506,13 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                                 if (lane == 0) bar_expect(s32(&full[slot_i]), bytes);
                                 __syncwarp();
                             }
+                            // a lane per copy (one lane for all takes twice as long)
                             const uint32_t dst = s32(ring + (size_t)slot_i * SH::TILE), bar = s32(&full[slot_i]);
-                            const int page = lane & 7, part = lane >> 3;      // part: a half, or the tail
+                            const int page = lane & 7, piece = lane >> 3;     // piece: a half, or the tail
                             const int trow = ((id * 2 + kv) * a.c.Hkv + kvh) * kBT;
                             if ((pages >> page & 1) && !(drop && kv == 0 && page == 0)) {
-                                if (part < SH::HALVES) tma_2d(dst + part * SH::HALF_BYTES + page * (kBT * 128), &map_kv, 64 * part, trow, bar);
-                                else if (SH::TAIL && part == SH::HALVES)
+                                if (piece < SH::HALVES) tma_2d(dst + piece * SH::HALF_BYTES + page * (kBT * 128), &map_kv, 64 * piece, trow, bar);
+                                else if (SH::TAIL && piece == SH::HALVES)
                                     tma_2d(dst + SH::HALVES * SH::HALF_BYTES + page * (kBT * SH::TAIL * 2), &map_kv_tail, 64 * SH::HALVES, trow, bar);
                             }
                             ++seq;
@@ -499,7 +569,6 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
         constexpr uint32_t idesc_s = instr_desc(BF16, false, kTile);
         constexpr uint32_t idesc_o = instr_desc(BF16, true, 64 * SH::HALVES), idesc_t = instr_desc(BF16, true, 16);
         constexpr uint32_t kTail = SH::HALVES * SH::HALF_BYTES;
-        const uint32_t one = lane == 0;
         bool ok = true;
         int q_used[2] = {0, 0}, p_used[2] = {0, 0}, item = 0;
         uint32_t started[2] = {0, 0};
@@ -517,11 +586,11 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
             for (int h = 0; h < SH::HALVES; ++h)
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                    mma_ss(w * kTile, da + (h * SH::HALF_BYTES / 16 + 2 * k), db + (h * SH::HALF_BYTES / 16 + 2 * k), idesc_s, h + k > 0, one);
-            if (SH::TAIL) mma_ss(w * kTile, desc(qa + kTail, 16, 256, kSwz32), desc(ka + kTail, 16, 256, kSwz32), idesc_s, 1, one);
-            commit(s32(&s_full[w]), one);
-            if (flags & LAST) commit(s32(&q_empty[qb]), one);
-            if (release) commit(s32(&empty[ks]), one);
+                    mma_ss(w * kTile, da + (h * SH::HALF_BYTES / 16 + 2 * k), db + (h * SH::HALF_BYTES / 16 + 2 * k), idesc_s, h + k > 0);
+            if (SH::TAIL) mma_ss(w * kTile, desc(qa + kTail, 16, 256, kSwz32), desc(ka + kTail, 16, 256, kSwz32), idesc_s, 1);
+            commit(s32(&s_full[w]));
+            if (flags & LAST) commit(s32(&q_empty[qb]));
+            if (release) commit(s32(&empty[ks]));
         };
         // O += P V of tile w of visit v, page after page; the weights come in two halves
         auto output = [&](int v, int flags, uint32_t pages, int w, bool release) {
@@ -539,12 +608,12 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                 for (int half = 0; half < (FINE ? 2 : 1); ++half) {
                     if (R > 1) {
                         const uint64_t pa = dp + half * (kWeights / 2 / 16) + (i / 4) * (kTile / R * 128 / 16) + 2 * (i % 4);
-                        mma_ss(d, pa, db + i * (kBT * 128 / 16), idesc_o, more, one);
-                        if (SH::TAIL) mma_ss(d + 64 * SH::HALVES, pa, dt + i * (kBT * SH::TAIL * 2 / 16), idesc_t, more, one);
+                        mma_ss(d, pa, db + i * (kBT * 128 / 16), idesc_o, more);
+                        if (SH::TAIL) mma_ss(d + 64 * SH::HALVES, pa, dt + i * (kBT * SH::TAIL * 2 / 16), idesc_t, more);
                     } else {
-                        const uint32_t pa = p + half * (kTile / 2) + i * 8;
-                        mma_ts(d, pa, db + i * (kBT * 128 / 16), idesc_o, more, one);
-                        if (SH::TAIL) mma_ts(d + 64 * SH::HALVES, pa, dt + i * (kBT * SH::TAIL * 2 / 16), idesc_t, more, one);
+                        const uint32_t pa = p + (i / 2) * 32 + (i % 2) * 8 + half * 16;
+                        mma_ts(d, pa, db + i * (kBT * 128 / 16), idesc_o, more);
+                        if (SH::TAIL) mma_ts(d + 64 * SH::HALVES, pa, dt + i * (kBT * SH::TAIL * 2 / 16), idesc_t, more);
                     }
                     more = 1;
                 }
@@ -567,8 +636,8 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                 for (uint32_t left = pages & 0xf0; left; left &= left - 1) page(__ffs(left) - 1);
             }
             started[ow] = more;
-            commit(s32(&pv_done[w]), one);
-            if (release) commit(s32(&empty[vs]), one);
+            commit(s32(&pv_done[w]));
+            if (release) commit(s32(&empty[vs]));
         };
         auto tile_ready = [&](uint32_t n) { wait(&full[n % SLOTS], (n / SLOTS) & 1); };
         auto q_ready = [&](int flags, int w) {
@@ -649,12 +718,10 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                 *failed = 1;
                 atomicOr(a.c.status, ISV_STATUS_WAIT_EXPIRED);
             }
-            commit(s32(drain), one);       // what was issued ends before tensor memory passes on
+            commit(s32(drain));       // what was issued ends before tensor memory passes on
             for (uint32_t k = 0; k < 1u << 16 && !bar_try(s32(drain), 0); ++k) {}
         }
-    }
-    } else {
-        if (NT == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kMoreRegs));
+    } else if (warp < NT * 4) {
         // ---- weights: group w of four warps, one row of its tile per thread
         const int w = warp >> 2, r = threadIdx.x & 127;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
@@ -675,8 +742,7 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
 #pragma unroll
             for (int i = 0; i < R; ++i) all[i] = at[i * ROWS + rr];
         };
-        const bool shaped = a.cap > 0.f || a.slopes || !(a.scale > 0.f);      // scores need more than a positive factor
-        const float c = shaped ? kLog2e : a.scale * kLog2e;
+        const float c = SHAPED ? kLog2e : a.scale * kLog2e;
         int used = 0;           // visits of this group
         int tok = 0, head = 0, pos = 0, s = 0;
         Seq q{};
@@ -729,58 +795,88 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                 }
             }
             if (any_live) {
-                float x[COLS];
-                uint32_t *xw = reinterpret_cast<uint32_t *>(x);
-#pragma unroll
-                for (int i = 0; i < COLS / 32; ++i) tmem_ld32(lanes + b * kTile + col0 + 32 * i, xw + 32 * i);
-                wait_ld();
+                // two passes over the scores, a few columns at a time (a loop that holds a row's 128 scores in registers is so
+                // long that fetching its instructions bounds it: 930 us against 590 on a prompt of 8192 tokens)
+                const uint32_t cols = lanes + b * kTile + col0;
                 const int j1 = j0 + col0;                                      // this thread's columns
-                if (shaped) {
-                    const float in = a.cap > 0.f ? 2.f * kLog2e * a.scale / a.cap : a.scale;
-                    const float distance = (float)(pos - j1);
-                    if (a.cap > 0.f) {
-                        // cap tanh(y) = cap - 2 cap / (e^2y + 1): off by a few 2^-24 of the cap
-#pragma unroll
-                        for (int i = 0; i < COLS; ++i) {
-                            const float e = exp2_fast(x[i] * in);
-                            x[i] = fmaf(-2.f * a.cap, reciprocal(e + 1.f), a.cap);
-                        }
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < COLS; ++i) x[i] *= in;
-                    }
-                    if (a.slopes) {
-#pragma unroll
-                        for (int i = 0; i < COLS; ++i) x[i] = fmaf(-slope, fabsf(distance - (float)i), x[i]);
-                    }
-                }
                 const bool all = pages == 0xff && sight.lim >= j0 + kTile && (sight.low <= j0 || sight.prefix >= j0 + kTile);
-                if (!__all_sync(~0u, all || !live)) {
+                const bool masked = !__all_sync(~0u, all || !live);
+                float xa[32], xb[32];
+                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                auto look = [&](float (&y)[32], int k) {
+                    const int at = j1 + 32 * k;
+                    if (SHAPED) {
+                        if (a.cap > 0.f) {
+                            const float in = a.scale / a.cap;
+                            float most = 0.f;
 #pragma unroll
-                    for (int k = 0; k < COLS / 32; ++k) {
-                        // bit i: token j1 + 32 k + i is seen
+                            for (int i = 0; i < 32; i += 2) most = max3(most, fabsf(y[i]), fabsf(y[i + 1]));
+                            if (__all_sync(~0u, most * fabsf(in) <= 1.f || !live)) {
+#pragma unroll
+                                for (int i = 0; i < 32; i += 2) {
+                                    const float2 z = unpair(mul2(tanh_poly(mul2(pair(y[i], y[i + 1]), both(in))), both(a.cap)));
+                                    y[i] = z.x;
+                                    y[i + 1] = z.y;
+                                }
+                            } else {
+                                // cap tanh(z) = cap - 2 cap / (e^2z + 1): off by a few 2^-24 of the cap
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) {
+                                    const float e = exp2_fast(y[i] * (2.f * kLog2e * in));
+                                    y[i] = fmaf(-2.f * a.cap, reciprocal(e + 1.f), a.cap);
+                                }
+                            }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) y[i] *= a.scale;
+                        }
+                        if (a.slopes) {
+                            const float distance = (float)(pos - at);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) y[i] = fmaf(-slope, fabsf(distance - (float)i), y[i]);
+                        }
+                    }
+                    if (masked) {
+                        // bit i: token at + i is seen
                         auto below = [&](int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; };
-                        const int at = j1 + 32 * k;
                         const uint32_t here = pages >> (2 * k + col0 / kBT);
                         uint32_t seen = below(sight.lim - at) & (~below(sight.low - at) | below(sight.prefix - at));
                         seen &= (here & 1 ? 0xffffu : 0u) | (here & 2 ? 0xffff0000u : 0u);
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) x[32 * k + i] = seen >> i & 1 ? x[32 * k + i] : -INFINITY;
+                        for (int i = 0; i < 32; ++i) y[i] = seen >> i & 1 ? y[i] : -INFINITY;
+                    }
+                    if (COLS > 32 && (SHAPED || masked)) tmem_st32(cols + 32 * k, reinterpret_cast<uint32_t *>(y));
+#pragma unroll
+                    for (int i = 0; i < 32; i += 2) top[i / 2 & 3] = max3(top[i / 2 & 3], y[i], y[i + 1]);
+                };
+                tmem_ld32(cols, reinterpret_cast<uint32_t *>(xa));
+#pragma unroll 1
+                for (int k = 0; k < COLS / 32; k += 2) {
+                    wait_ld();
+                    if (COLS > 32) tmem_ld32(cols + 32 * (k + 1), reinterpret_cast<uint32_t *>(xb));
+                    look(xa, k);
+                    if (COLS > 32) {
+                        wait_ld();
+                        if (k + 2 < COLS / 32) tmem_ld32(cols + 32 * (k + 2), reinterpret_cast<uint32_t *>(xa));
+                        look(xb, k + 1);
                     }
                 }
-                float top[4] = {x[0], x[1], x[2], x[3]};
-#pragma unroll
-                for (int i = 4; i < COLS - 4; i += 2) top[i / 2 & 3] = max3(top[i / 2 & 3], x[i], x[i + 1]);
-                float high = fmaxf(max3(max3(top[0], x[COLS - 4], x[COLS - 3]), max3(top[1], x[COLS - 2], x[COLS - 1]), top[2]), top[3]) * c;
+                if (COLS > 32) {
+                    if (SHAPED || masked) wait_st();
+                    tmem_ld32(cols, reinterpret_cast<uint32_t *>(xa));
+                }
+                float high = max3(top[0], top[1], max3(top[2], top[3], top[3])) * c;
                 if (R > 1) {
                     float of[R];
                     gather(high, of);
                     if (!ok) break;
 #pragma unroll
-                    for (int i = 0; i < R; ++i) high = fmaxf(high, of[i]);
+                    for (int i = 0; i < R; ++i) high = max3(high, high, of[i]);
                 }
                 float factor = 1.f;
-                if (ref == -INFINITY) {
+                if (!(high <= FLT_MAX)) {
+                    l = NAN;        // a score that is NaN or infinite: the row is computed token by token at the end
+                } else if (ref == -INFINITY) {
                     ref = high;
                 } else if (high > ref + slack_of<BF16>()) {
                     factor = exp2_fast(ref - high);
@@ -815,18 +911,20 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                 const float minus = ref == -INFINITY ? 0.f : kOffset - ref;
                 const uint64_t cc = pair(c, c), mm = pair(minus, minus);
                 uint64_t sum[2] = {pair(0.f, 0.f), pair(0.f, 0.f)};
-#pragma unroll
-                for (int k = 0; k < COLS / 32; ++k) {
+                auto weigh = [&](const float (&y)[32], int k) {
                     uint32_t hi[16], lo[16];
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const float2 e = unpair(fma2(pair(x[32 * k + 2 * i], x[32 * k + 2 * i + 1]), cc, mm));
-                        const float p0 = exp2_fast(e.x), p1 = exp2_fast(e.y);
-                        sum[i & 1] = add2(sum[i & 1], pair(p0, p1));
-                        hi[i] = narrow<BF16>(p0, p1);
+                        const uint64_t e2 = fma2(pair(y[2 * i], y[2 * i + 1]), cc, mm);
+                        const float2 e = unpair(e2);
+                        // the special-function unit bounds this loop: some of the powers are taken by polynomials
+                        const bool poly = !FINE && i * kPoly % 16 < kPoly;
+                        const float2 p = poly ? exp2_poly<BF16 ? 3 : 4>(e2) : make_float2(exp2_fast(e.x), exp2_fast(e.y));
+                        sum[i & 1] = add2(sum[i & 1], pair(p.x, p.y));
+                        hi[i] = narrow<BF16>(p.x, p.y);
                         if (FINE) {
                             const float2 h = widen<BF16>(hi[i]);
-                            lo[i] = narrow<BF16>(p0 - h.x, p1 - h.y);
+                            lo[i] = narrow<BF16>(p.x - h.x, p.y - h.y);
                         }
                     }
                     if (R > 1) {
@@ -834,16 +932,31 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                         const int col = col0 + 32 * k;
                         uint8_t *row = weights + (col / 64) * (ROWS * 128) + rr * 128;
 #pragma unroll
-                        for (int y = 0; y < 4; ++y) {
-                            const int chunk = (col % 64 / 8 + y) ^ (rr & 7);
-                            *reinterpret_cast<uint4 *>(row + chunk * 16) = make_uint4(hi[4 * y], hi[4 * y + 1], hi[4 * y + 2], hi[4 * y + 3]);
-                            *reinterpret_cast<uint4 *>(row + kWeights / 2 + chunk * 16) = make_uint4(lo[4 * y], lo[4 * y + 1], lo[4 * y + 2], lo[4 * y + 3]);
+                        for (int y4 = 0; y4 < 4; ++y4) {
+                            const int chunk = (col % 64 / 8 + y4) ^ (rr & 7);
+                            *reinterpret_cast<uint4 *>(row + chunk * 16) = make_uint4(hi[4 * y4], hi[4 * y4 + 1], hi[4 * y4 + 2], hi[4 * y4 + 3]);
+                            *reinterpret_cast<uint4 *>(row + kWeights / 2 + chunk * 16) =
+                                make_uint4(lo[4 * y4], lo[4 * y4 + 1], lo[4 * y4 + 2], lo[4 * y4 + 3]);
                         }
-                        continue;
+                    } else {
+                        // in place of their scores
+                        tmem_st16(cols + 32 * k, hi);
+                        if (FINE) tmem_st16(cols + 32 * k + 16, lo);
                     }
-                    tmem_st16(lanes + b * kTile + 16 * k, hi);
-                    if (FINE) tmem_st16(lanes + b * kTile + kTile / 2 + 16 * k, lo);
-                    if (k == 1) {
+                };
+#pragma unroll 1
+                for (int k = 0; k < COLS / 32; k += 2) {
+                    if (COLS > 32) {
+                        wait_ld();
+                        tmem_ld32(cols + 32 * (k + 1), reinterpret_cast<uint32_t *>(xb));
+                    }
+                    weigh(xa, k);
+                    if (COLS > 32) {
+                        wait_ld();
+                        if (k + 2 < COLS / 32) tmem_ld32(cols + 32 * (k + 2), reinterpret_cast<uint32_t *>(xa));
+                        weigh(xb, k + 1);
+                    }
+                    if (R == 1 && k == 0) {
                         wait_st();
                         fence_before();
                         __syncwarp();
@@ -888,42 +1001,40 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
             const long long at = ((long long)(q.first + tok) * a.c.Hq + head) * D;
             const float inv = slot < 0 ? 1.f / l : 1.f;
             bool fine = !some || fabsf(l) <= FLT_MAX;
+            constexpr int STEP = D == 80 ? 16 : 32;
 #pragma unroll 1
-            for (int i = 0; i < D; i += 16) {
-                uint32_t y[16];
-                tmem_ld16(o + i, y);
-                wait_ld();
-                float f[16];
+            for (int i = 0; i < D; i += STEP) {
+                uint32_t y[STEP];
 #pragma unroll
-                for (int k = 0; k < 16; ++k) {
+                for (int k = 0; k < STEP; k += 16) tmem_ld16(o + i + k, y + k);
+                wait_ld();
+                float f[STEP];
+#pragma unroll
+                for (int k = 0; k < STEP; ++k) {
                     f[k] = some ? __uint_as_float(y[k]) * inv : 0.f;
                     fine = fine && fabsf(f[k]) <= FLT_MAX;
                 }
-                if (live && slot < 0) {
-                    if (a.out) {
-                        uint32_t h[8];
+                if (live && slot >= 0) {
+                    float4 *dst = reinterpret_cast<float4 *>(a.part_o) + ((long long)slot * (D / 4) + i / 4) * (2 * kTile) + w * kTile + r;
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) h[k] = narrow<BF16>(f[2 * k], f[2 * k + 1]);
-                        uint4 *dst = reinterpret_cast<uint4 *>(a.out + at + i);
-                        dst[0] = make_uint4(h[0], h[1], h[2], h[3]);
-                        dst[1] = make_uint4(h[4], h[5], h[6], h[7]);
-                    }
-                    if (a.out_f32) {
+                    for (int k = 0; k < STEP / 4; ++k) dst[k * (2 * kTile)] = make_float4(f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3]);
+                }
+                if (live && slot < 0 && a.out_f32) {
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            reinterpret_cast<float4 *>(a.out_f32 + at + i)[k] = make_float4(f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3]);
-                    }
-                } else if (live) {
+                    for (int k = 0; k < STEP / 4; ++k)
+                        reinterpret_cast<float4 *>(a.out_f32 + at + i)[k] = make_float4(f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3]);
+                }
+                if (live && slot < 0 && a.out) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        reinterpret_cast<float4 *>(a.part_o)[((long long)slot * (D / 4) + i / 4 + k) * (2 * kTile) + w * kTile + r] =
-                            make_float4(f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3]);
+                    for (int k = 0; k < STEP / 8; ++k)
+                        reinterpret_cast<uint4 *>(a.out + at + i)[k] = make_uint4(narrow<BF16>(f[8 * k], f[8 * k + 1]), narrow<BF16>(f[8 * k + 2], f[8 * k + 3]),
+                                                                                  narrow<BF16>(f[8 * k + 4], f[8 * k + 5]), narrow<BF16>(f[8 * k + 6], f[8 * k + 7]));
                 }
                 __syncwarp();
             }
             if (slot >= 0) {
                 if (live) reinterpret_cast<float2 *>(a.part_ml)[(long long)slot * (2 * kTile) + w * kTile + r] =
-                    make_float2(some ? ref : -INFINITY, l);
+                    make_float2(!some ? -INFINITY : fabsf(l) <= FLT_MAX ? ref : INFINITY, l);   // what is no number outweighs the rest
             } else {
                 // sums that are no number: an infinity or NaN in a token that the row does not see (0 times that is NaN), or an
                 // overflow of values near the type's largest.  Such a row is computed token by token.
@@ -944,11 +1055,14 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
 
 // ---------------------------------------------------------------- merging
 
-// Partial results of items that crossed ranges.  CTA (record, group of 32 rows, four-value columns): a lane has one row, a
-// warp every eighth column.
-constexpr int kMergeThreads = 256;
-template <int D, bool BF16>
-__global__ void __launch_bounds__(kMergeThreads) merge_kernel(const __grid_constant__ AttnParams a) {
+// Partial results of items that crossed ranges.  CTA (record, group of 32 rows): a lane has one row, a warp four of its values at a
+// time, and kFly partial results are in flight together (bound by the latency of those rounds).  Items of few rows are cut into
+// many partial results: a warp for every four values.  Items of 256 rows have two or three, in many CTAs: eight warps.
+constexpr int kFly = 8;
+template <int D, int NT>
+__host__ __device__ constexpr int merge_warps() { return NT == 1 ? D / 4 : 8; }
+template <int D, bool BF16, int NT>
+__global__ void __launch_bounds__(merge_warps<D, NT>() * 32) merge_kernel(const __grid_constant__ AttnParams a) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const MergeRec m = a.merges[blockIdx.x];
@@ -962,31 +1076,46 @@ __global__ void __launch_bounds__(kMergeThreads) merge_kernel(const __grid_const
     if (!__any_sync(~0u, live)) return;
     auto slot = [&](int i) { return (long long)(2 * ((int)blockIdx.x + i) + (i == 0 ? 1 : 0)); };
     const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml);
+    // references first: the records of kFly partial results are in flight together
     float top = -INFINITY, l = 0.f;
-    if (live)
-        for (int i = 0; i < m.n; ++i) top = fmaxf(top, ml[slot(i) * (2 * kTile) + row].x);
+    for (int i = 0; i < m.n; i += kFly) {
+        float z[kFly];
+#pragma unroll
+        for (int y = 0; y < kFly; ++y) z[y] = ml[slot(min(i + y, m.n - 1)) * (2 * kTile) + row].x;
+#pragma unroll
+        for (int y = 0; y < kFly; ++y) top = fmaxf(top, z[y]);
+    }
     const float at = top == -INFINITY ? 0.f : top;
-    if (live)
-        for (int i = 0; i < m.n; ++i) {
-            const float2 z = ml[slot(i) * (2 * kTile) + row];
-            l += z.y * exp2_fast(z.x - at);
-        }
-    const float inv = l != 0.f ? 1.f / l : 0.f;
-    bool fine = l == 0.f || fabsf(l) <= FLT_MAX;
-    for (int c = warp; c < D / 4; c += kMergeThreads / 32) {
+    bool fine = true;
+    for (int c = warp; c < D / 4; c += merge_warps<D, NT>()) {
+        l = 0.f;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (!live) continue;
-#pragma unroll 4
-        for (int i = 0; i < m.n; ++i) {
-            const float f = exp2_fast(ml[slot(i) * (2 * kTile) + row].x - at);
-            const float4 y = reinterpret_cast<const float4 *>(a.part_o)[(slot(i) * (D / 4) + c) * (2 * kTile) + row];
-            o.x = fmaf(f, y.x, o.x); o.y = fmaf(f, y.y, o.y); o.z = fmaf(f, y.z, o.z); o.w = fmaf(f, y.w, o.w);
+        for (int i = 0; i < m.n; i += kFly) {
+            float4 y[kFly];
+            float2 z[kFly];
+#pragma unroll
+            for (int k = 0; k < kFly; ++k) {
+                const long long from = slot(min(i + k, m.n - 1));
+                z[k] = ml[from * (2 * kTile) + row];
+                y[k] = reinterpret_cast<const float4 *>(a.part_o)[(from * (D / 4) + c) * (2 * kTile) + row];
+            }
+#pragma unroll
+            for (int k = 0; k < kFly; ++k) {
+                const float f = exp2_fast(z[k].x - at);
+                if (i + k < m.n && f != 0.f) {
+                    l = fmaf(f, z[k].y, l);
+                    o.x = fmaf(f, y[k].x, o.x); o.y = fmaf(f, y[k].y, o.y); o.z = fmaf(f, y[k].z, o.z); o.w = fmaf(f, y[k].w, o.w);
+                }
+            }
         }
+        const float inv = l != 0.f ? 1.f / l : 0.f;
         o.x *= inv; o.y *= inv; o.z *= inv; o.w *= inv;
-        fine = fine && fabsf(o.x) <= FLT_MAX && fabsf(o.y) <= FLT_MAX && fabsf(o.z) <= FLT_MAX && fabsf(o.w) <= FLT_MAX;
+        fine = fine && fabsf(l) <= FLT_MAX && fabsf(o.x) <= FLT_MAX && fabsf(o.y) <= FLT_MAX && fabsf(o.z) <= FLT_MAX && fabsf(o.w) <= FLT_MAX;
         const long long to = ((long long)(q.first + tok) * a.c.Hq + head) * D + 4 * c;
-        if (a.out) *reinterpret_cast<uint2 *>(a.out + to) = make_uint2(narrow<BF16>(o.x, o.y), narrow<BF16>(o.z, o.w));
-        if (a.out_f32) *reinterpret_cast<float4 *>(a.out_f32 + to) = o;
+        if (live) {
+            if (a.out) *reinterpret_cast<uint2 *>(a.out + to) = make_uint2(narrow<BF16>(o.x, o.y), narrow<BF16>(o.z, o.w));
+            if (a.out_f32) *reinterpret_cast<float4 *>(a.out_f32 + to) = o;
+        }
     }
     // rows whose sums are no number (see the kernel above): every warp has its columns written before one recomputes the row
     __shared__ uint32_t odd_s;
@@ -999,7 +1128,7 @@ __global__ void __launch_bounds__(kMergeThreads) merge_kernel(const __grid_const
     for (uint32_t left = odd_s; left; left &= left - 1, ++i) {
         const int from = __ffs(left) - 1;
         const int t = __shfl_sync(~0u, tok, from), h = __shfl_sync(~0u, head, from);
-        if (i % (kMergeThreads / 32) == warp) attend_row<D, BF16>(a, m.s, q, t, h);
+        if (i % merge_warps<D, NT>() == warp) attend_row<D, BF16>(a, m.s, q, t, h);
     }
 }
 
@@ -1026,7 +1155,7 @@ bool encode(CUtensorMap *m, bool bf16, int rank, const void *base, const cuuint6
                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, bool BF16, int NT, int R, bool FINE>
+template <int D, bool BF16, int NT, int R, bool FINE, bool SHAPED>
 cudaError_t launch(const AttnParams &p, int grid, cudaStream_t st, const char **what) {
     CUtensorMap kv{}, kv_tail{}, q{}, q_tail{};
     if (!encode_fn()) { *what = "cuTensorMapEncodeTiled is not available from this driver"; return cudaErrorUnknown; }
@@ -1050,17 +1179,20 @@ cudaError_t launch(const AttnParams &p, int grid, cudaStream_t st, const char **
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    cudaError_t e = cudaLaunchKernelEx(&cfg, attn_kernel<D, BF16, NT, R, FINE>, kv, kv_tail, q, q_tail, p);
+    cudaError_t e = cudaLaunchKernelEx(&cfg, attn_kernel<D, BF16, NT, R, FINE, SHAPED>, kv, kv_tail, q, q_tail, p);
     if (e != cudaSuccess) return e;
     cfg.gridDim = dim3(grid, NT * kTile / R / 32);
-    cfg.blockDim = dim3(kMergeThreads);
+    cfg.blockDim = dim3(merge_warps<D, NT>() * 32);
     cfg.dynamicSmemBytes = 0;
-    return cudaLaunchKernelEx(&cfg, merge_kernel<D, BF16>, p);
+    return cudaLaunchKernelEx(&cfg, merge_kernel<D, BF16, NT>, p);
 }
 
 template <int D, bool BF16, int NT, int R, bool FINE>
 cudaError_t allow() {
-    return cudaFuncSetAttribute(attn_kernel<D, BF16, NT, R, FINE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D>(R));
+    cudaError_t e = cudaFuncSetAttribute(attn_kernel<D, BF16, NT, R, FINE, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D>(R));
+    if (e == cudaSuccess)
+        e = cudaFuncSetAttribute(attn_kernel<D, BF16, NT, R, FINE, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D>(R));
+    return e;
 }
 template <int D, bool BF16>
 cudaError_t configure() {
@@ -1074,14 +1206,19 @@ cudaError_t configure() {
 // Weights enter their product as two 16-bit numbers (fp32's precision, one product more) wherever that costs little: with up to
 // 128 rows per KV head the call is bound by reading the cache.  Beyond that the tensor cores bound it, and a 16-bit output gets
 // weights rounded to 16 bits, an error of the order of its own rounding; with an fp32 output they stay exact.
+template <int D, bool BF16, bool SHAPED>
+cudaError_t pick_shape(const AttnParams &p, int grid, cudaStream_t st, const char **what) {
+    switch (p.tile_rows) {
+    case 32: return launch<D, BF16, 1, 4, true, SHAPED>(p, grid, st, what);
+    case 64: return launch<D, BF16, 1, 2, true, SHAPED>(p, grid, st, what);
+    case 128: return launch<D, BF16, 1, 1, true, SHAPED>(p, grid, st, what);
+    default: return p.out_f32 ? launch<D, BF16, 2, 1, true, SHAPED>(p, grid, st, what) : launch<D, BF16, 2, 1, false, SHAPED>(p, grid, st, what);
+    }
+}
+// SHAPED: the scores need more than a positive factor.
 template <int D, bool BF16>
 cudaError_t pick(const AttnParams &p, int grid, cudaStream_t st, const char **what) {
-    switch (p.tile_rows) {
-    case 32: return launch<D, BF16, 1, 4, true>(p, grid, st, what);
-    case 64: return launch<D, BF16, 1, 2, true>(p, grid, st, what);
-    case 128: return launch<D, BF16, 1, 1, true>(p, grid, st, what);
-    default: return p.out_f32 ? launch<D, BF16, 2, 1, true>(p, grid, st, what) : launch<D, BF16, 2, 1, false>(p, grid, st, what);
-    }
+    return p.cap > 0.f || p.slopes || !(p.scale > 0.f) ? pick_shape<D, BF16, true>(p, grid, st, what) : pick_shape<D, BF16, false>(p, grid, st, what);
 }
 
 }  // namespace
