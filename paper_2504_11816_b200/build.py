@@ -14,8 +14,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libisv.so")
 SOURCES = ["isv_kernels.cu", "isv_api.cu", "isv_static.cu", "isv_linear.cu", "isv_q8.cu", "isv_q8_attn.cu", "isv_pages.cu",
-           "isv_linear4.cu", "isv_chunk.cu", "isv_chunk_attn.cu", "isv_draft.cu"]
-HEADERS = ["isv_kernels.cuh", "isv_q8.cuh", "isv_chunk.cuh", "isv_host.hpp", os.path.join("..", "..", "include", "isv.h")]
+           "isv_linear4.cu", "isv_chunk.cu", "isv_chunk_attn_64.cu", "isv_chunk_attn_80.cu", "isv_chunk_attn_128.cu", "isv_draft.cu"]
+HEADERS = ["isv_kernels.cuh", "isv_q8.cuh", "isv_chunk.cuh", "isv_chunk_attn.cuh", "isv_host.hpp", os.path.join("..", "..", "include", "isv.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC"]
 

@@ -45,6 +45,8 @@ struct OnDevice {
 // ---------------------------------------------------------------- storing a chunk
 
 constexpr int kWriteThreads = 256;
+constexpr int kWriteTokens = 16;       // of a CTA, at most
+constexpr int kWriteAhead = 4;         // units of a thread whose loads are in flight
 constexpr uint32_t kSpinLimit = 1u << 22;   // polls before a wait of the attention kernel gives up, unless isv_chunk_set_wait_limit says otherwise
 
 struct WriteParams {
@@ -56,6 +58,7 @@ struct WriteParams {
     const int32_t *positions;       // [axes][n_rows] or NULL: the place in the sequence
     const uint8_t *axis;            // [rotary / 2] or NULL: axis 0
     int32_t rotary, adjacent, axes;
+    int32_t tokens;                 // of a CTA
     float magnitude;
 };
 
@@ -69,69 +72,112 @@ __device__ __forceinline__ float2 turn(int position, float freq, float magnitude
     return make_float2(c * magnitude, s * magnitude);
 }
 
-// One thread of the grid per 32 bytes of a token's head: the two 16-byte chunks that the rotation pairs (or, behind the
-// rotated part and in V, two adjacent ones).
+// A CTA takes a few tokens of one sequence.  The unit of work is 32 bytes of a token's head: the two 16-byte chunks that the rotation
+// pairs (or, behind the rotated part and in V, two adjacent ones).  The first units' loads are in flight while the tokens' sines
+// and cosines are computed, once for all heads, into shared memory.  Bound by HBM on prompts, by one chain of loads (lengths, rows,
+// page) on single tokens.
 template <int D, bool BF16>
 __global__ void __launch_bounds__(kWriteThreads) write_kernel(const WriteParams p) {
     constexpr int UNITS = D / 16;
-    const int s = blockIdx.y;
+    __shared__ float2 turns[kWriteTokens * D / 2];      // [token][pair]
+    __shared__ int pages[kWriteTokens];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int s = blockIdx.y, t0 = blockIdx.x * p.tokens;
     bool bad;
     const Seq q = seq_of(p.c, s, bad);
     if (bad && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(p.c.status, ISV_STATUS_BAD_LENGTH);
-    const int heads = (p.q ? p.c.Hq : 0) + 2 * p.c.Hkv;
-    const long long at = (long long)blockIdx.x * kWriteThreads + threadIdx.x;
-    const int u = (int)(at % UNITS);
-    const long long th = at / UNITS;
-    const int t = (int)(th / heads), h = (int)(th % heads);
-    if (t >= q.n) return;
-    const int pos = q.start + t, row = q.first + t, slot = pos % kBT;
-    const bool is_v = h >= p.c.Hkv && h < 2 * p.c.Hkv, is_q = h >= 2 * p.c.Hkv;
-    const bool turned = !is_v && u < p.rotary / 16;
-    const int c0 = turned && !p.adjacent ? u : 2 * u, c1 = turned && !p.adjacent ? u + p.rotary / 16 : 2 * u + 1;
-    const uint16_t *src = is_q   ? p.q + row * p.q_stride + (h - 2 * p.c.Hkv) * D
-                          : is_v ? p.v + row * p.kv_stride + (h - p.c.Hkv) * D
-                                 : p.k + row * p.kv_stride + h * D;
-    uint4 x[2] = {reinterpret_cast<const uint4 *>(src)[c0], reinterpret_cast<const uint4 *>(src)[c1]};
-    if (turned) {
-        uint32_t *w0 = reinterpret_cast<uint32_t *>(&x[0]), *w1 = reinterpret_cast<uint32_t *>(&x[1]);
-        float2 cs[8];
+    const int n = min(p.tokens, q.n - t0);
+    if (n <= 0) return;
+    const int heads = (p.q ? p.c.Hq : 0) + 2 * p.c.Hkv, per_token = heads * UNITS, units = n * per_token;
+    const int row0 = q.first + t0, pos0 = q.start + t0;
+
+    struct Unit {
+        int t, h, c0, c1;       // token, head (of K, V, Q in this order), chunks
+        bool turned;
+    };
+    auto unit_at = [&](int i) {
+        Unit z;
+        z.t = i / per_token;
+        const int y = i - z.t * per_token, u = y % UNITS;
+        z.h = y / UNITS;
+        z.turned = (z.h < p.c.Hkv || z.h >= 2 * p.c.Hkv) && u < p.rotary / 16;
+        const bool halves = z.turned && !p.adjacent;
+        z.c0 = halves ? u : 2 * u;
+        z.c1 = halves ? u + p.rotary / 16 : 2 * u + 1;
+        return z;
+    };
+    auto load = [&](int i, uint4 (&x)[2]) {
+        const Unit z = unit_at(i);
+        const long long row = row0 + z.t;
+        const uint16_t *src = z.h >= 2 * p.c.Hkv ? p.q + row * p.q_stride + (z.h - 2 * p.c.Hkv) * D
+                              : z.h >= p.c.Hkv   ? p.v + row * p.kv_stride + (z.h - p.c.Hkv) * D
+                                                 : p.k + row * p.kv_stride + z.h * D;
+        x[0] = reinterpret_cast<const uint4 *>(src)[z.c0];
+        x[1] = reinterpret_cast<const uint4 *>(src)[z.c1];
+    };
+    uint4 x[kWriteAhead][2];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int pair = 8 * u + i;
-            const int axis = p.axis ? min((int)p.axis[pair], p.axes - 1) : 0;
-            cs[i] = turn(p.positions ? p.positions[(long long)axis * p.c.n_rows + row] : pos, p.freq[pair], p.magnitude);
-        }
-        if (p.adjacent) {
+    for (int k = 0; k < kWriteAhead; ++k)
+        if (threadIdx.x + k * kWriteThreads < units) load(threadIdx.x + k * kWriteThreads, x[k]);
+
+    const int pairs = p.rotary / 2;
+    for (int i = threadIdx.x; i < n * pairs; i += kWriteThreads) {
+        const int t = i / pairs, y = i - t * pairs;
+        const int axis = p.axis ? min((int)p.axis[y], p.axes - 1) : 0;
+        turns[t * (D / 2) + y] = turn(p.positions ? p.positions[(long long)axis * p.c.n_rows + row0 + t] : pos0 + t, p.freq[y], p.magnitude);
+    }
+    if (threadIdx.x < n) {
+        const int page = p.c.table[(long long)s * p.c.table_stride + (pos0 + threadIdx.x) / kBT];
+        const bool there = page >= 0 && page < p.c.n_pages;
+        if (!there) atomicOr(p.c.status, ISV_STATUS_BAD_BLOCK_ID);
+        pages[threadIdx.x] = there ? page : -1;
+    }
+    __syncthreads();
+
+    for (int base = threadIdx.x; base < units; base += kWriteAhead * kWriteThreads) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                uint32_t &w = i < 4 ? w0[i] : w1[i - 4];
-                const float2 v = widen<BF16>(w);
-                w = narrow<BF16>(v.x * cs[i].x - v.y * cs[i].y, v.y * cs[i].x + v.x * cs[i].y);
+        for (int k = 0; k < kWriteAhead; ++k) {
+            const int i = base + k * kWriteThreads;
+            if (i >= units) break;
+            const Unit z = unit_at(i);
+            uint4 y[2] = {x[k][0], x[k][1]};
+            if (i + kWriteAhead * kWriteThreads < units) load(i + kWriteAhead * kWriteThreads, x[k]);
+            if (z.turned) {
+                uint32_t *w0 = reinterpret_cast<uint32_t *>(&y[0]), *w1 = reinterpret_cast<uint32_t *>(&y[1]);
+                const int u = p.adjacent ? z.c0 / 2 : z.c0;
+                const float4 *cs = reinterpret_cast<const float4 *>(turns + z.t * (D / 2) + 8 * u);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float4 f = cs[e];                 // cos, sin of two pairs
+                    if (p.adjacent) {
+                        uint32_t &a = e < 2 ? w0[2 * e] : w1[2 * e - 4], &b = e < 2 ? w0[2 * e + 1] : w1[2 * e - 3];
+                        const float2 v = widen<BF16>(a), w = widen<BF16>(b);
+                        a = narrow<BF16>(v.x * f.x - v.y * f.y, v.y * f.x + v.x * f.y);
+                        b = narrow<BF16>(w.x * f.z - w.y * f.w, w.y * f.z + w.x * f.w);
+                    } else {
+                        const float2 v = widen<BF16>(w0[e]), w = widen<BF16>(w1[e]);
+                        w0[e] = narrow<BF16>(v.x * f.x - w.x * f.y, v.y * f.z - w.y * f.w);
+                        w1[e] = narrow<BF16>(w.x * f.x + v.x * f.y, w.y * f.z + v.y * f.w);
+                    }
+                }
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 a = widen<BF16>(w0[i]), b = widen<BF16>(w1[i]), e = cs[2 * i], f = cs[2 * i + 1];
-                w0[i] = narrow<BF16>(a.x * e.x - b.x * e.y, a.y * f.x - b.y * f.y);
-                w1[i] = narrow<BF16>(b.x * e.x + a.x * e.y, b.y * f.x + a.y * f.y);
+            uint4 *dst;
+            int c0 = z.c0, c1 = z.c1;
+            if (z.h >= 2 * p.c.Hkv) {
+                dst = reinterpret_cast<uint4 *>(p.q_out + (long long)(row0 + z.t) * p.q_out_stride + (z.h - 2 * p.c.Hkv) * D);
+            } else {
+                if (pages[z.t] < 0) continue;
+                // heads of K, then of V: the order of a page's tiles
+                const int slot = (pos0 + z.t) % kBT;
+                dst = reinterpret_cast<uint4 *>(p.c.pool + (((long long)pages[z.t] * 2 * p.c.Hkv + z.h) * kBT + slot) * D);
+                c0 = place<D>(c0, slot);
+                c1 = place<D>(c1, slot);
             }
+            dst[c0] = y[0];
+            dst[c1] = y[1];
         }
     }
-    if (is_q) {
-        uint4 *dst = reinterpret_cast<uint4 *>(p.q_out + row * p.q_out_stride + (h - 2 * p.c.Hkv) * D);
-        dst[c0] = x[0];
-        dst[c1] = x[1];
-        return;
-    }
-    const int page = p.c.table[(long long)s * p.c.table_stride + pos / kBT];
-    if (page < 0 || page >= p.c.n_pages) {
-        if (h == 0 && u == 0) atomicOr(p.c.status, ISV_STATUS_BAD_BLOCK_ID);
-        return;
-    }
-    // heads of K, then of V: the order of a page's tiles
-    uint4 *dst = reinterpret_cast<uint4 *>(p.c.pool + (((long long)page * 2 * p.c.Hkv + h) * kBT + slot) * D);
-    dst[place<D>(c0, slot)] = x[0];
-    dst[place<D>(c1, slot)] = x[1];
 }
 
 bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
@@ -181,12 +227,24 @@ CacheParams cache_params(const isv_chunk *h, const void *pool, int32_t n_pages, 
     return c;
 }
 
+template <int D, bool BF16>
+cudaError_t launch_write_as(const WriteParams &p, dim3 grid, cudaStream_t st) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(kWriteThreads);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;   // see the kernel's griddepcontrol pair
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, write_kernel<D, BF16>, p);
+}
 template <int D>
 cudaError_t launch_write(const WriteParams &p, bool bf16, dim3 grid, cudaStream_t st) {
-    if (bf16) write_kernel<D, true><<<grid, kWriteThreads, 0, st>>>(p);
-    else write_kernel<D, false><<<grid, kWriteThreads, 0, st>>>(p);
-    return cudaGetLastError();
+    return bf16 ? launch_write_as<D, true>(p, grid, st) : launch_write_as<D, false>(p, grid, st);
 }
+
 }  // namespace
 
 extern "C" {
@@ -234,7 +292,9 @@ int isv_chunk_create(isv_chunk **out, const isv_chunk_desc *desc) {
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, h->device);
     h->grid = desc->max_ctas > 0 ? std::min(desc->max_ctas, sms) : sms;   // one CTA per SM
     const size_t rows = attn_part_rows(h->grid);
-    if (e == cudaSuccess) e = attn_configure(desc->head_dim, desc->dtype == ISV_BF16);
+    const bool bf16 = desc->dtype == ISV_BF16;
+    if (e == cudaSuccess)
+        e = desc->head_dim == 64 ? attn_configure<64>(bf16) : desc->head_dim == 80 ? attn_configure<80>(bf16) : attn_configure<128>(bf16);
     if (e == cudaSuccess) e = cudaMalloc((void **)&h->status, 4);
     if (e == cudaSuccess) e = cudaMemset(h->status, 0, 4);
     if (e == cudaSuccess) e = cudaMalloc((void **)&h->part_o, rows * desc->head_dim * 4);
@@ -281,8 +341,10 @@ int isv_chunk_write(isv_chunk *h, void *pool_dev, int32_t n_pages, const int32_t
     p.freq = inv_freq_dev; p.positions = positions_dev; p.axis = pair_axis_dev;
     p.rotary = h->d.rotary_dim; p.adjacent = h->d.rotary_pairs == ISV_ROTARY_ADJACENT; p.axes = h->d.rotary_axes;
     p.magnitude = magnitude;
-    const long long units = (long long)T * ((q_dev ? h->d.q_heads : 0) + 2 * h->d.kv_heads) * (h->d.head_dim / 16);
-    const dim3 grid((unsigned)((units + kWriteThreads - 1) / kWriteThreads), (unsigned)n_seqs);
+    // about six units a thread: fewer and the tokens' sines weigh, more and few CTAs are left
+    const long long per_token = (long long)((q_dev ? h->d.q_heads : 0) + 2 * h->d.kv_heads) * (h->d.head_dim / 16);
+    p.tokens = (int)std::min<long long>(kWriteTokens, std::max<long long>(1, 6 * kWriteThreads / per_token));
+    const dim3 grid((unsigned)((T + p.tokens - 1) / p.tokens), (unsigned)n_seqs);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     OnDevice on(h->device);
     if (on.e != cudaSuccess) return err(ISV_ECUDA, "%s: %s", who, cudaGetErrorString(on.e));
@@ -330,7 +392,11 @@ int isv_chunk_attn(isv_chunk *h, const void *pool_dev, int32_t n_pages, const in
     OnDevice on(h->device);
     if (on.e != cudaSuccess) return err(ISV_ECUDA, "%s: %s", who, cudaGetErrorString(on.e));
     const char *what = nullptr;
-    const cudaError_t e = launch_attn(p, h->d.head_dim, h->d.dtype == ISV_BF16, h->grid, static_cast<cudaStream_t>(stream), &what);
+    const bool bf16 = h->d.dtype == ISV_BF16;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const cudaError_t e = h->d.head_dim == 64   ? launch_attn<64>(p, bf16, h->grid, st, &what)
+                          : h->d.head_dim == 80 ? launch_attn<80>(p, bf16, h->grid, st, &what)
+                                                : launch_attn<128>(p, bf16, h->grid, st, &what);
     return e == cudaSuccess ? ISV_OK : err(ISV_ECUDA, "%s: %s", who, what ? what : cudaGetErrorString(e));
 }
 

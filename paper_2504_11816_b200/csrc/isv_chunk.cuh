@@ -55,11 +55,14 @@ struct MergeRec {
     int32_t last, s, token0, kvh, pass;
 };
 
-// The launchers.
-int attn_tile_rows(long long rows);                                // rows of an item (32, 64, 128 or 256), for that many rows per KV head
-size_t attn_part_rows(int grid);                                   // rows of partial results
-cudaError_t attn_configure(int D, bool bf16);
-cudaError_t launch_attn(const AttnParams &p, int D, bool bf16, int grid, cudaStream_t st, const char **what);
+// Rows of an item for that many rows per KV head: a quarter, a half or the whole of a tile of 128, or two tiles.
+inline int attn_tile_rows(long long rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
+// Rows of partial results: two items of 256 rows a CTA.
+inline size_t attn_part_rows(int grid) { return (size_t)2 * grid * 256; }
+template <int D>
+cudaError_t attn_configure(bool bf16);
+template <int D>
+cudaError_t launch_attn(const AttnParams &p, bool bf16, int grid, cudaStream_t st, const char **what);
 
 // One sequence of a call, clamped to what the table row, T and the rows hold.
 struct Seq {

@@ -133,6 +133,7 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const Params p) {
     __syncthreads();
     const int took = took_s;
     const bool refused = refused_s, some = row_s >= 0;
+    const float u_last = p.u[(long long)s * (p.K + 1) + p.K];
     const int x = refused ? p.drafted[(long long)s * p.K + took] : -1;
     const T *prow = some ? target + (long long)row_s * p.V : nullptr;
     const T *qrow = refused && draft ? draft + ((long long)s * p.K + took) * p.V : nullptr;
@@ -164,22 +165,35 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const Params p) {
     }
     cluster.sync();
 
-    // every warp knows all totals: which part holds the crossing is the same answer for all
-    double all = 0, all_p = 0;
-    for (int i = 0; i < parts; ++i) { all += totals[i][0]; all_p += totals[i][1]; }
-    const int kind = refused && all > 0 ? 0 : 1;
-    const double total = kind == 0 ? all : all_p;
-    const double border = (double)p.u[(long long)s * (p.K + 1) + p.K] * total;
-    double before = 0, at = 0;
-    int owner = -1;
-    for (int i = 0; i < parts; ++i) {
-        if (totals[i][kind] > 0) {
-            owner = i;                  // the last part with any weight, if rounding (or u >= 1) lets none cross
-            before = at;
-        }
-        at += totals[i][kind];
-        if (at > border && owner == i) break;
+    // every warp works out, from all parts' totals, which part holds the crossing: a lane has `each` parts in a row
+    const int each = (parts + 31) / 32;
+    double mine = 0, mine_p = 0;
+    for (int i = lane * each; i < min(parts, (lane + 1) * each); ++i) { mine += totals[i][0]; mine_p += totals[i][1]; }
+    const int kind = refused && warp_sum(mine) > 0 ? 0 : 1;
+    if (kind == 1) mine = mine_p;
+    const double total = warp_sum(mine);
+    const double border = (double)u_last * total;
+    double up = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const double z = __shfl_up_sync(~0u, up, d);
+        if (lane >= d) up += z;
     }
+    // the first part whose sum passes the border; the last one with any weight, if rounding (or u >= 1) lets none do so
+    double at = up - mine, before = 0;
+    int hit = 0x7fffffff, any = -1;
+    for (int i = lane * each; i < min(parts, (lane + 1) * each); ++i) {
+        const double w = totals[i][kind];
+        if (w > 0) {
+            any = i;
+            if (at + w > border && hit == 0x7fffffff) { hit = i; before = at; }
+            else if (hit == 0x7fffffff) before = at;
+        }
+        at += w;
+    }
+    const int first = __reduce_min_sync(~0u, hit), last_any = __reduce_max_sync(~0u, any);
+    const int owner = first != 0x7fffffff ? first : last_any;
+    before = __shfl_sync(~0u, before, owner < 0 ? 0 : owner / each);
     if (part == owner) {
         int token = -1, last = -1;
         double run = before;
