@@ -46,7 +46,7 @@ struct OnDevice {
 
 constexpr int kWriteThreads = 256;
 constexpr int kWriteTokens = 16;       // of a CTA, at most
-constexpr int kWriteAhead = 4;         // units of a thread whose loads are in flight
+constexpr int kWriteAhead = 2;         // units of a thread whose loads are in flight (4: more registers, fewer CTAs, 194 us instead of 143)
 constexpr uint32_t kSpinLimit = 1u << 22;   // polls before a wait of the attention kernel gives up, unless isv_chunk_set_wait_limit says otherwise
 
 struct WriteParams {
@@ -187,7 +187,7 @@ bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) !
 struct isv_chunk {
     isv_chunk_desc d{};
     int device = 0;
-    int grid = 1;                       // of the attention kernel
+    int sms = 1, grid = 1;              // of the device, of the attention kernel
     int GT = 1, P = 1;                  // query heads per visit, passes
     uint32_t *status = nullptr;
     float *part_o = nullptr, *part_ml = nullptr;
@@ -290,7 +290,8 @@ int isv_chunk_create(isv_chunk **out, const isv_chunk_desc *desc) {
     int sms = 0;
     cudaError_t e = cudaGetDevice(&h->device);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, h->device);
-    h->grid = desc->max_ctas > 0 ? std::min(desc->max_ctas, sms) : sms;   // one CTA per SM
+    h->sms = std::max(1, sms);
+    h->grid = desc->max_ctas > 0 ? std::min(desc->max_ctas, h->sms) : h->sms;   // one CTA per SM
     const size_t rows = attn_part_rows(h->grid);
     const bool bf16 = desc->dtype == ISV_BF16;
     if (e == cudaSuccess)
@@ -341,9 +342,10 @@ int isv_chunk_write(isv_chunk *h, void *pool_dev, int32_t n_pages, const int32_t
     p.freq = inv_freq_dev; p.positions = positions_dev; p.axis = pair_axis_dev;
     p.rotary = h->d.rotary_dim; p.adjacent = h->d.rotary_pairs == ISV_ROTARY_ADJACENT; p.axes = h->d.rotary_axes;
     p.magnitude = magnitude;
-    // about six units a thread: fewer and the tokens' sines weigh, more and few CTAs are left
+    // about six units a thread (fewer, and the tokens' sines weigh), but not less than six CTAs an SM
     const long long per_token = (long long)((q_dev ? h->d.q_heads : 0) + 2 * h->d.kv_heads) * (h->d.head_dim / 16);
-    p.tokens = (int)std::min<long long>(kWriteTokens, std::max<long long>(1, 6 * kWriteThreads / per_token));
+    const long long most = std::min<long long>(6 * kWriteThreads / per_token, (long long)n_seqs * T / (6 * h->sms));
+    p.tokens = (int)std::min<long long>(kWriteTokens, std::max<long long>(1, most));
     const dim3 grid((unsigned)((T + p.tokens - 1) / p.tokens), (unsigned)n_seqs);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     OnDevice on(h->device);

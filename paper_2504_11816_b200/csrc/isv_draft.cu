@@ -5,9 +5,10 @@
 // whose running sum exceeds u times the total.  Which index that is hangs on sums over a whole vocabulary, so these are
 // taken in 64 bits (in 32 bits, neighbouring tokens of probability 1e-5 would trade places in one call of a hundred).
 //
-// A cluster of up to eight CTAs does a sequence.  Every warp owns a contiguous part of the row and sums it once; the
-// parts' totals are exchanged through distributed shared memory; the warp whose part holds the crossing walks that part
-// again.  So the row is read from HBM once, and nothing is kept but one total per warp.
+// A cluster of up to eight CTAs does a sequence.  Every warp owns a contiguous part of the row and sums it once, group by group;
+// the parts' totals are exchanged through distributed shared memory; the warp whose part holds the crossing finds the group
+// in its sums and walks that group alone again.  So the row is read from HBM once, and nothing is kept but the groups' sums.
+// Bound by a chain of dependent loads (counts, drafts, their probabilities, the row, the group), then by HBM.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -29,6 +30,7 @@ namespace {
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kMaxCtas = 8;            // of a cluster (the portable maximum)
 constexpr int kMaxDraft = 1024;
+constexpr int kGroups = 64;            // groups of a warp's part, at most
 
 int err(int code, const char *fmt, ...) {
     char buf[512];
@@ -73,10 +75,68 @@ __device__ __forceinline__ void load(const T *row, int i, int end, float (&x)[E]
     for (int y = 0; y < E; ++y) x[y] = i + y < end ? number<T>(row[i + y]) : 0.f;
 }
 
+// What a lane holds of a row before it is used: 16 bytes of adjacent probabilities, or (rows that are not aligned) elements that
+// lie 32 apart, so that a warp's loads are contiguous either way.
+template <typename T, bool VEC>
+struct Batch {
+    static constexpr int E = 16 / sizeof(T), DEEP = VEC ? 4 : 16 / E;       // loads in flight: 4 of 16 bytes, or 16 of an element
+    static constexpr int STEP = 32 * E * DEEP;                              // elements of a warp's batch
+    uint4 w[VEC ? DEEP : 1];
+    T e[VEC ? 1 : DEEP * E];
+    __device__ __forceinline__ static int index(int i0, int lane, int d, int y) {
+        return VEC ? i0 + (d * 32 + lane) * E + y : i0 + (d * E + y) * 32 + lane;
+    }
+    __device__ __forceinline__ void load(const T *row, int i0, int lane, int end) {
+#pragma unroll
+        for (int d = 0; d < DEEP; ++d) {
+            if constexpr (VEC) {
+                // a row's length is a multiple of E here: a vector is inside or behind
+                w[d] = index(i0, lane, d, 0) < end ? *reinterpret_cast<const uint4 *>(row + index(i0, lane, d, 0)) : make_uint4(0, 0, 0, 0);
+            } else {
+#pragma unroll
+                for (int y = 0; y < E; ++y) e[d * E + y] = index(i0, lane, d, y) < end ? row[index(i0, lane, d, y)] : T(0.f);
+            }
+        }
+    }
+    __device__ __forceinline__ float at(int d, int y) const {
+        return number<T>(VEC ? reinterpret_cast<const T *>(&w[d])[y] : e[d * E + y]);
+    }
+};
+
 // Weight of one token in the residual: what the target gives it beyond the draft.  What is not a positive number weighs nothing.
 __device__ __forceinline__ double beyond(float p, float q) {
     const double r = (double)p - (double)q;
     return r > 0 ? r : 0.0;
+}
+
+// A sum as an fp32 number and what its roundings left.
+struct Sum {
+    float hi = 0.f, lo = 0.f;
+    // x + rest, |rest| far below |x|
+    __device__ __forceinline__ void add(float x, float rest) {
+        const float t = __fadd_rn(hi, x), z = __fsub_rn(t, hi);
+        lo = __fadd_rn(lo, __fadd_rn(__fadd_rn(__fsub_rn(hi, __fsub_rn(t, z)), __fsub_rn(x, z)), rest));
+        hi = t;
+    }
+    // what the target gives beyond the draft, exactly: the difference and its rounding
+    __device__ __forceinline__ void add_beyond(float p, float q) {
+        const bool more = p > q;
+        const float d = __fsub_rn(p, q), rest = __fsub_rn(__fsub_rn(p, d), q);
+        add(more ? d : 0.f, more ? rest : 0.f);
+    }
+};
+__device__ __forceinline__ double warp_sum(Sum x) {
+#pragma unroll
+    for (int i = 16; i; i >>= 1) {
+        const float hi = __shfl_xor_sync(~0u, x.hi, i), lo = __shfl_xor_sync(~0u, x.lo, i);
+        // both lanes add the smaller number to the larger, so that they get the same bits
+        Sum y;
+        y.hi = fmaxf(x.hi, hi);
+        y.lo = __fadd_rn(x.lo, lo);
+        y.add(fminf(x.hi, hi), 0.f);
+        x = y;
+    }
+    return (double)x.hi + (double)x.lo;
 }
 
 __device__ __forceinline__ double warp_sum(double x) {
@@ -85,12 +145,44 @@ __device__ __forceinline__ double warp_sum(double x) {
     return x;
 }
 
+// Of n weights get(0) .. get(n - 1): the first whose running sum, from `start` on, passes the border; the last one with any weight, if
+// rounding (or u >= 1) lets none do so; -1 if there is none.  `before` becomes the sum ahead of it.  A lane has a few in a row.
+template <typename Get>
+__device__ __forceinline__ int crossing(int n, Get get, double start, double border, double &before) {
+    const int lane = threadIdx.x & 31, each = (n + 31) / 32, lo = lane * each, hi = min(n, lo + each);
+    double mine = 0;
+    for (int i = lo; i < hi; ++i) mine += get(i);
+    double up = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const double z = __shfl_up_sync(~0u, up, d);
+        if (lane >= d) up += z;
+    }
+    double at = start + (up - mine), ahead = 0;
+    int hit = 0x7fffffff, any = -1;
+    for (int i = lo; i < hi; ++i) {
+        const double w = get(i);
+        if (w > 0 && hit == 0x7fffffff) {
+            any = i;
+            ahead = at;
+            if (at + w > border) hit = i;
+        }
+        at += w;
+    }
+    const int first = __reduce_min_sync(~0u, hit), last = __reduce_max_sync(~0u, any);
+    const int found = first != 0x7fffffff ? first : last;
+    before = __shfl_sync(~0u, ahead, found < 0 ? 0 : found / each);
+    return found;
+}
+
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(kThreads) verify_kernel(const Params p) {
+__global__ void __launch_bounds__(kThreads, 2) verify_kernel(const Params p) {
     constexpr int E = 16 / sizeof(T);
     cg::cluster_group cluster = cg::this_cluster();
-    __shared__ int took_s, refused_s, row_s, bad_s;
+    __shared__ int took_s, refused_s, row_s, bad_s, owner_s;
+    __shared__ double border_s, before_s;
     __shared__ double totals[kMaxCtas * kWarps][2];   // of each warp's part: residual, target
+    __shared__ double groups[kWarps][kGroups];        // of each group of this CTA's parts
     const int s = blockIdx.x / p.ctas, rank = blockIdx.x % p.ctas;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const T *target = static_cast<const T *>(p.target), *draft = static_cast<const T *>(p.draft);
@@ -142,93 +234,100 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const Params p) {
     const int parts = p.ctas * kWarps, steps = (p.V + 32 * E - 1) / (32 * E);
     const int part = rank * kWarps + warp;
     const int lo = (int)((long long)steps * part / parts) * 32 * E, hi = min(p.V, (int)((long long)steps * (part + 1) / parts) * 32 * E);
-    double sum = 0, whole = 0;
-    if (some) {
-#pragma unroll 4
-        for (int i = lo + lane * E; i < hi; i += 32 * E) {
-            float a[E], b[E];
-            load<T, VEC, E>(prow, i, hi, a);
-            if (qrow) load<T, VEC, E>(qrow, i, hi, b);
+    using Rows = Batch<T, VEC>;
+    int kind = refused ? 0 : 1;         // 0: from the residual, 1: from the target
+    auto weight = [&](float target, float draft_, int i) {
+        return kind == 1 ? beyond(target, 0.f) : qrow ? beyond(target, draft_) : i == x ? 0.0 : beyond(target, 0.f);
+    };
+    const int batches = (hi - lo + Rows::STEP - 1) / Rows::STEP, per_group = max(1, (batches + kGroups - 1) / kGroups) * Rows::STEP;
+    for (;; kind = 1) {
+        double part_sum = 0;
+        for (int g = 0; lo + g * per_group < hi && some; ++g) {
+            const int end = min(hi, lo + (g + 1) * per_group);
+            Sum sum;
+            for (int i0 = lo + g * per_group; i0 < end; i0 += Rows::STEP) {
+                Rows a, b;
+                a.load(prow, i0, lane, hi);
+                if (kind == 0 && qrow) b.load(qrow, i0, lane, hi);
 #pragma unroll
-            for (int y = 0; y < E; ++y) {
-                whole += beyond(a[y], 0.f);
-                sum += qrow ? beyond(a[y], b[y]) : i + y == x ? 0.0 : beyond(a[y], 0.f);
+                for (int d = 0; d < Rows::DEEP; ++d)
+#pragma unroll
+                    for (int y = 0; y < E; ++y) {
+                        const bool left_out = kind == 0 && !qrow && Rows::index(i0, lane, d, y) == x;
+                        sum.add_beyond(left_out ? 0.f : a.at(d, y), kind == 0 && qrow ? b.at(d, y) : 0.f);
+                    }
+            }
+            const double group_sum = warp_sum(sum);
+            if (lane == 0) groups[warp][g] = group_sum;
+            part_sum += group_sum;
+        }
+        if (lane < p.ctas) cluster.map_shared_rank(totals, lane)[part][kind] = part_sum;
+        cluster.sync();
+        // one warp adds up, and finds the part that holds the crossing
+        if (warp == 0) {
+            double mine = 0;
+            for (int i = lane; i < parts; i += 32) mine += totals[i][kind];
+            const double total = warp_sum(mine);
+            double before = 0;
+            const double border = (double)u_last * total;
+            const int owner = total > 0 ? crossing(parts, [&](int i) { return totals[i][kind]; }, 0.0, border, before) : -1;
+            if (lane == 0) {
+                owner_s = owner;
+                border_s = border;
+                before_s = before;
             }
         }
+        __syncthreads();
+        if (kind == 1 || owner_s >= 0) break;
+        // nothing is left of the target beyond the draft: the same with the target alone
     }
-    sum = warp_sum(sum);
-    whole = warp_sum(whole);
-    if (lane < p.ctas) {
-        double(*there)[2] = cluster.map_shared_rank(totals, lane);
-        there[part][0] = sum;
-        there[part][1] = whole;
-    }
-    cluster.sync();
-
-    // every warp works out, from all parts' totals, which part holds the crossing: a lane has `each` parts in a row
-    const int each = (parts + 31) / 32;
-    double mine = 0, mine_p = 0;
-    for (int i = lane * each; i < min(parts, (lane + 1) * each); ++i) { mine += totals[i][0]; mine_p += totals[i][1]; }
-    const int kind = refused && warp_sum(mine) > 0 ? 0 : 1;
-    if (kind == 1) mine = mine_p;
-    const double total = warp_sum(mine);
-    const double border = (double)u_last * total;
-    double up = mine;
-#pragma unroll
-    for (int d = 1; d < 32; d *= 2) {
-        const double z = __shfl_up_sync(~0u, up, d);
-        if (lane >= d) up += z;
-    }
-    // the first part whose sum passes the border; the last one with any weight, if rounding (or u >= 1) lets none do so
-    double at = up - mine, before = 0;
-    int hit = 0x7fffffff, any = -1;
-    for (int i = lane * each; i < min(parts, (lane + 1) * each); ++i) {
-        const double w = totals[i][kind];
-        if (w > 0) {
-            any = i;
-            if (at + w > border && hit == 0x7fffffff) { hit = i; before = at; }
-            else if (hit == 0x7fffffff) before = at;
-        }
-        at += w;
-    }
-    const int first = __reduce_min_sync(~0u, hit), last_any = __reduce_max_sync(~0u, any);
-    const int owner = first != 0x7fffffff ? first : last_any;
-    before = __shfl_sync(~0u, before, owner < 0 ? 0 : owner / each);
+    const double border = border_s, before = before_s;
+    const int owner = owner_s;
     if (part == owner) {
-        int token = -1, last = -1;
+        const int n = (hi - lo + per_group - 1) / per_group;
         double run = before;
-        for (int i0 = lo; i0 < hi && token < 0; i0 += 32 * E) {
-            const int i = i0 + lane * E;
-            float a[E], b[E];
-            load<T, VEC, E>(prow, i, hi, a);
-            if (qrow && kind == 0) load<T, VEC, E>(qrow, i, hi, b);
-            double w[E], mine = 0;
+        const int g = n > 1 ? crossing(n, [&](int i) { return groups[warp][i]; }, before, border, run) : 0;
+        const int end = min(hi, lo + (g + 1) * per_group);
+        constexpr int W = 16 / E;       // steps whose loads are in flight
+        int token = -1, last = -1;
+        for (int i0 = lo + g * per_group; i0 < end && token < 0; i0 += W * 32 * E) {
+            float a[W][E], b[W][E];
 #pragma unroll
-            for (int y = 0; y < E; ++y) {
-                w[y] = kind == 1 ? beyond(a[y], 0.f) : qrow ? beyond(a[y], b[y]) : i + y == x ? 0.0 : beyond(a[y], 0.f);
-                mine += w[y];
+            for (int k = 0; k < W; ++k) {
+                load<T, VEC, E>(prow, i0 + (k * 32 + lane) * E, end, a[k]);
+                if (qrow && kind == 0) load<T, VEC, E>(qrow, i0 + (k * 32 + lane) * E, end, b[k]);
             }
-            double up = mine;
 #pragma unroll
-            for (int d = 1; d < 32; d *= 2) {
-                const double z = __shfl_up_sync(~0u, up, d);
-                if (lane >= d) up += z;
-            }
-            const double next = run + __shfl_sync(~0u, up, 31);
-            double c = run + (up - mine);
-            int hit = 0x7fffffff, any = -1;
+            for (int k = 0; k < W; ++k) {
+                if (token >= 0 || i0 + k * 32 * E >= end) continue;
+                const int i = i0 + (k * 32 + lane) * E;
+                double w[E], mine = 0;
 #pragma unroll
-            for (int y = 0; y < E; ++y) {
-                c += w[y];
-                if (w[y] > 0) {
-                    any = i + y;
-                    if (c > border) hit = min(hit, i + y);
+                for (int y = 0; y < E; ++y) {
+                    w[y] = i + y < end ? weight(a[k][y], qrow && kind == 0 ? b[k][y] : 0.f, i + y) : 0.0;
+                    mine += w[y];
                 }
+                double up = mine;
+#pragma unroll
+                for (int d = 1; d < 32; d *= 2) {
+                    const double z = __shfl_up_sync(~0u, up, d);
+                    if (lane >= d) up += z;
+                }
+                double c = run + (up - mine);
+                run += __shfl_sync(~0u, up, 31);
+                int hit = 0x7fffffff, any = -1;
+#pragma unroll
+                for (int y = 0; y < E; ++y) {
+                    c += w[y];
+                    if (w[y] > 0) {
+                        any = i + y;
+                        if (c > border) hit = min(hit, i + y);
+                    }
+                }
+                hit = __reduce_min_sync(~0u, hit);
+                last = max(last, __reduce_max_sync(~0u, any));
+                if (hit != 0x7fffffff) token = hit;
             }
-            hit = __reduce_min_sync(~0u, hit);
-            last = max(last, __reduce_max_sync(~0u, any));
-            if (hit != 0x7fffffff) token = hit;
-            run = next;
         }
         if (lane == 0) p.tokens[(long long)s * (p.K + 1) + took] = token >= 0 ? token : last;
     }
