@@ -216,10 +216,12 @@ def lib():
 def _ptr(x) -> Optional[int]:
     if x is None:
         return None
+    try:
+        return x.data_ptr()          # a tensor: by far the most frequent, and a call has a dozen of them
+    except AttributeError:
+        pass
     if isinstance(x, int):
         return x
-    if hasattr(x, "data_ptr"):
-        return x.data_ptr()
     if isinstance(x, np.ndarray):
         return x.ctypes.data
     raise TypeError(f"cannot take a pointer from {type(x)!r}")

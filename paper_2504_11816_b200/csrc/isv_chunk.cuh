@@ -49,10 +49,19 @@ struct AttnParams {
     int32_t drop_first_copy;    // failure injection: the first visit's barrier of CTA 0 is armed without issuing one of its copies
 };
 
+// One sequence of a call, clamped to what the table row, T and the rows hold.
+struct Seq {
+    int len;                    // tokens in the cache
+    int start;                  // position of the chunk's first token
+    int n;                      // new tokens
+    int first;                  // row of the first of them
+};
+
 // An item whose partial results are in slot 2 * first + 1 and in 2 * c for the CTAs c up to `last`.
 struct MergeRec {
     int32_t n;                  // partial results, 0: none
     int32_t last, s, token0, kvh, pass;
+    Seq q;
 };
 
 // Rows of an item for that many rows per KV head: a quarter, a half or the whole of a tile of 128, or two tiles.
@@ -64,13 +73,6 @@ cudaError_t attn_configure(bool bf16);
 template <int D>
 cudaError_t launch_attn(const AttnParams &p, bool bf16, int grid, cudaStream_t st, const char **what);
 
-// One sequence of a call, clamped to what the table row, T and the rows hold.
-struct Seq {
-    int len;                    // tokens in the cache
-    int start;                  // position of the chunk's first token
-    int n;                      // new tokens
-    int first;                  // row of the first of them
-};
 __device__ __forceinline__ Seq seq_of(const CacheParams &c, int s, bool &bad) {
     Seq q;
     const int n = c.lens[s], most = c.max_blocks * kBT;

@@ -296,15 +296,15 @@ struct Shape {
     static constexpr int HALVES = D / 64, TAIL = D % 64;                          // of a row: 64 elements each, and the rest
     static constexpr int HALF_BYTES = kTile * 128, TAIL_BYTES = kTile * TAIL * 2;
     static constexpr int TILE = HALVES * HALF_BYTES + TAIL_BYTES;                 // a tile of Q, K or V
-    // tiles of the ring; where the weights are in shared memory (32 KB), 128 KB of it (deeper rings are no faster)
-    static __host__ __device__ constexpr int slots(int R) { return R > 1 ? (D == 128 ? 4 : D == 80 ? 6 : 8) : D == 128 ? 5 : D == 80 ? 9 : 10; }
+    // tiles of the ring: what fits beside two tiles of Q, or (R > 1) one and the weights
+    static __host__ __device__ constexpr int slots(int R) { return D == 128 ? 5 : D == 80 ? (R > 1 ? 8 : 9) : 10; }
 };
 constexpr int kMisc = 1024;
 constexpr int kWeights = 2 * 64 * 256;     // R > 1: weights of up to 64 rows as two 16-bit numbers each
 constexpr int kExchange = 2 * kTile * 4;   // R > 1: maxima and sums that the copies of a row exchange
 template <int D>
 constexpr size_t smem_bytes(int R) {
-    return 1024 + (size_t)(2 + Shape<D>::slots(R)) * Shape<D>::TILE + kMisc + (R > 1 ? kWeights + kExchange : 0);
+    return 1024 + (size_t)((R > 1 ? 1 : 2) + Shape<D>::slots(R)) * Shape<D>::TILE + kMisc + (R > 1 ? kWeights + kExchange : 0);
 }
 
 // warps: NT groups of four for the weights, then the producer, the issuer of products, the loader of Q, and one that rests
@@ -321,7 +321,7 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (s32(smem_raw) & 1023u)) & 1023u);
     // the weights come first: what their operand's unused rows read is still shared memory of this CTA
-    uint8_t *weights = smem, *q_tiles = smem + (R > 1 ? kWeights : 0), *ring = q_tiles + 2 * SH::TILE;
+    uint8_t *weights = smem, *q_tiles = smem + (R > 1 ? kWeights : 0), *ring = q_tiles + (R > 1 ? 1 : 2) * SH::TILE;
     uint8_t *misc = ring + SLOTS * SH::TILE;
     float *exchange = reinterpret_cast<float *>(misc + kMisc);      // [2][copy of the rows][row]
     Visit *recs = reinterpret_cast<Visit *>(misc);
@@ -333,6 +333,10 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
     static_assert(kRecs * sizeof(Visit) + (2 * SLOTS + kRecs + 14) * 8 + 8 <= kMisc, "");
     long long *sums = reinterpret_cast<long long *>(ring + (SLOTS - 1) * SH::TILE);   // until the first copies
     const int warp = same(threadIdx.x >> 5), lane = threadIdx.x & 31;
+    // Tiles in the order in which they are consumed.  NT = 2: K and V of a visit in turn.  NT = 1: the next visit's K before this one's V
+    // (K0 K1 V0 K2 V1 ..), so that V does not wait in the ring for its weights.
+    auto k_index = [](int v) -> uint32_t { return NT == 2 ? 2 * v : v == 0 ? 0 : 2 * v - 1; };
+    auto v_index = [](int v) -> uint32_t { return NT == 2 ? 2 * v + 1 : 2 * v + 2; };
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < SLOTS; ++i) {
@@ -416,8 +420,27 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
         const long long f0 = cta < n_ctas ? cut.first(cta) : 0, f1 = cta < n_ctas ? cut.first(cta + 1) : 0;
         MergeRec rec{};
         int v = 0;              // visits so far
-        uint32_t seq = 0;       // tiles so far: K and V of a visit
+        uint32_t top = 0;       // tiles so far
         bool ok = true;
+        int before_id = 0, before_kvh = 0;
+        uint32_t before_pages = 0;
+        auto slot_free = [&](uint32_t n) {
+            ok = __all_sync(~0u, n < SLOTS || bar_wait(s32(&empty[n % SLOTS]), (n / SLOTS - 1) & 1, a.spin_limit, failed));
+        };
+        // copies the pages of K (kv = 0) or V of a visit as tile n: a lane per copy (one lane for all takes twice as long)
+        auto fetch = [&](uint32_t n, int kv, int id, uint32_t pages, int kvh, bool drop) {
+            const uint32_t dst = s32(ring + (size_t)(n % SLOTS) * SH::TILE), bar = s32(&full[n % SLOTS]);
+            if (lane == 0) bar_expect(bar, __popc(pages) * (SH::TILE / kPages));
+            __syncwarp();
+            const int page = lane & 7, piece = lane >> 3;     // piece: a half, or the tail
+            const int trow = ((id * 2 + kv) * a.c.Hkv + kvh) * kBT;
+            if ((pages >> page & 1) && !(drop && page == 0)) {
+                if (piece < SH::HALVES) tma_2d(dst + piece * SH::HALF_BYTES + page * (kBT * 128), &map_kv, 64 * piece, trow, bar);
+                else if (SH::TAIL && piece == SH::HALVES)
+                    tma_2d(dst + SH::HALVES * SH::HALF_BYTES + page * (kBT * SH::TAIL * 2), &map_kv_tail, 64 * SH::HALVES, trow, bar);
+            }
+            top = n + 1;
+        };
         auto put_end = [&]() {
             if (lane == 0) {
                 recs[v % kRecs].flags = END;
@@ -455,7 +478,7 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                     if (begins && !ends) {
                         rec.last = cut.cta_of(at + w - 1);
                         rec.n = rec.last - cta + 1;
-                        rec.s = s; rec.token0 = token0; rec.kvh = kvh; rec.pass = pass;
+                        rec.s = s; rec.token0 = token0; rec.kvh = kvh; rec.pass = pass; rec.q = q;
                         // now: the record is this launch's, whatever becomes of the visits
                         if (lane == 0) a.merges[cta] = rec;
                         recorded = true;
@@ -479,13 +502,8 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                         const bool there = id >= 0 && id < a.c.n_pages;
                         if (lane < 8 && !there && id != ISV_BLOCK_NONE) atomicOr(a.c.status, ISV_STATUS_BAD_BLOCK_ID);
                         const uint32_t pages = __ballot_sync(~0u, there) & 0xff;
-                        // K
-                        const int ks = seq % SLOTS;
-                        ok = seq < SLOTS || bar_wait(s32(&empty[ks]), (seq / SLOTS - 1) & 1, a.spin_limit, failed);
-                        ok = __all_sync(~0u, ok);
+                        slot_free(k_index(v));
                         if (!ok) break;
-                        const uint32_t bytes = __popc(pages) * (SH::TILE / kPages);
-                        const bool drop = a.drop_first_copy && cta == 0 && v == 0;
                         if (lane == 0) {
                             Visit &z = recs[v % kRecs];
                             z.j0 = j0; z.pages = pages;
@@ -495,33 +513,26 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                             z.last_page = left / kBT;
                             z.s = s; z.token0 = token0; z.kvh = kvh; z.pass = pass; z.slot = slot; z.q = q;
                             bar_arrive(s32(&rec_full[v % kRecs]));
-                            bar_expect(s32(&full[ks]), bytes);
                         }
-                        __syncwarp();
-#pragma unroll
-                        for (int kv = 0; kv < 2; ++kv) {
-                            const int slot_i = seq % SLOTS;
-                            if (kv == 1) {
-                                ok = seq < SLOTS || bar_wait(s32(&empty[slot_i]), (seq / SLOTS - 1) & 1, a.spin_limit, failed);
-                                ok = __all_sync(~0u, ok);
+                        fetch(k_index(v), 0, id, pages, kvh, a.drop_first_copy && cta == 0 && v == 0);
+                        if (NT == 1) {
+                            if (v > 0) {
+                                slot_free(v_index(v - 1));
                                 if (!ok) break;
-                                if (lane == 0) bar_expect(s32(&full[slot_i]), bytes);
-                                __syncwarp();
+                                fetch(v_index(v - 1), 1, before_id, before_pages, before_kvh, false);
                             }
-                            // a lane per copy (one lane for all takes twice as long)
-                            const uint32_t dst = s32(ring + (size_t)slot_i * SH::TILE), bar = s32(&full[slot_i]);
-                            const int page = lane & 7, piece = lane >> 3;     // piece: a half, or the tail
-                            const int trow = ((id * 2 + kv) * a.c.Hkv + kvh) * kBT;
-                            if ((pages >> page & 1) && !(drop && kv == 0 && page == 0)) {
-                                if (piece < SH::HALVES) tma_2d(dst + piece * SH::HALF_BYTES + page * (kBT * 128), &map_kv, 64 * piece, trow, bar);
-                                else if (SH::TAIL && piece == SH::HALVES)
-                                    tma_2d(dst + SH::HALVES * SH::HALF_BYTES + page * (kBT * SH::TAIL * 2), &map_kv_tail, 64 * SH::HALVES, trow, bar);
-                            }
-                            ++seq;
+                            before_id = id; before_pages = pages; before_kvh = kvh;
+                        } else {
+                            slot_free(v_index(v));
+                            if (!ok) break;
+                            fetch(v_index(v), 1, id, pages, kvh, false);
                         }
-                        if (!ok) break;
                     }
                 }
+            }
+            if (NT == 1 && ok && v > 0) {
+                slot_free(v_index(v - 1));
+                if (ok) fetch(v_index(v - 1), 1, before_id, before_pages, before_kvh, false);
             }
             if (lane == 0 && !recorded) a.merges[cta] = rec;
         } else if (lane == 0) {
@@ -531,7 +542,7 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
         else *failed = 1;
         if (!ok || *failed) {
             // something gave up: the copies in flight land before the memory passes on
-            for (uint32_t i = seq > SLOTS ? seq - SLOTS : 0; i < seq; ++i)
+            for (uint32_t i = top > SLOTS ? top - SLOTS : 0; i < top; ++i)
                 for (uint32_t k = 0; k < 1u << 16 && !bar_try(s32(&full[i % SLOTS]), (i / SLOTS) & 1); ++k) {}
         }
     } else if (warp == kLoader) {
@@ -546,7 +557,7 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                 if (!(z.flags & FIRST)) continue;
                 const int tiles = NT == 2 && (z.flags & TWO) ? 2 : 1;
                 for (int i = 0; i < tiles && ok; ++i) {
-                    const int buf = NT == 2 ? i : item & 1;
+                    const int buf = NT == 2 ? i : R > 1 ? 0 : item & 1;
                     if (used[buf] > 0 && !bar_wait(s32(&q_empty[buf]), (used[buf] - 1) & 1, a.spin_limit, failed)) { ok = false; break; }
                     ++used[buf];
                     const uint32_t dst = s32(q_tiles + buf * SH::TILE), bar = s32(&q_full[buf]);
@@ -580,8 +591,8 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
         };
         // S of tile or buffer w of visit v
         auto scores = [&](int v, int flags, int w, bool release) {
-            const int qb = NT == 2 ? w : item & 1;
-            const uint32_t ks = (2u * v) % SLOTS;
+            const int qb = NT == 2 ? w : R > 1 ? 0 : item & 1;
+            const uint32_t ks = k_index(v) % SLOTS;
             const uint32_t qa = q_base + qb * SH::TILE, ka = ring_base + ks * SH::TILE;
             const uint64_t da = desc(qa, 16, 1024, kSwz128), db = desc(ka, 16, 1024, kSwz128);
 #pragma unroll
@@ -599,7 +610,7 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
             wait(&p_full[w], p_used[w] & 1);
             if (!ok) return;
             fence_after();
-            const uint32_t vs = (2u * v + 1) % SLOTS, va = ring_base + vs * SH::TILE;
+            const uint32_t vs = v_index(v) % SLOTS, va = ring_base + vs * SH::TILE;
             const int ow = NT == 2 ? w : 0;
             const uint32_t d = 2 * kTile + ow * kTile, p = w * kTile;
             const uint64_t db = desc(va, SH::HALF_BYTES, 1024, kSwz128), dt = desc(va + kTail, 16, 256, kSwz32);
@@ -644,7 +655,7 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
         auto tile_ready = [&](uint32_t n) { wait(&full[n % SLOTS], (n / SLOTS) & 1); };
         auto q_ready = [&](int flags, int w) {
             if (!(flags & FIRST)) return;
-            const int qb = NT == 2 ? w : item & 1;
+            const int qb = NT == 2 ? w : R > 1 ? 0 : item & 1;
             wait(&q_full[qb], q_used[qb] & 1);
             ++q_used[qb];
         };
@@ -675,7 +686,7 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                 if (NT == 1) {
                     // the next visit's scores go first if their tile is there
                     const int w = v & 1;
-                    const uint32_t k_next = 2 * v + 2;
+                    const uint32_t k_next = k_index(v + 1);
                     bool early = more && __all_sync(~0u, bar_try(s32(&full[k_next % SLOTS]), (k_next / SLOTS) & 1));
                     auto ahead = [&]() {
                         if (flags & LAST) ++item;
@@ -687,16 +698,16 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                     };
                     if (early) ahead();
                     if (!ok) break;
-                    tile_ready(2 * v + 1);
+                    tile_ready(v_index(v));
                     output(v, flags, pages, w, true);
                     if (!ok) break;
                     if (more && !early) ahead();
                 } else {
                     const bool two = flags & TWO, next_two = more && (next & TWO);
-                    tile_ready(2 * v + 1);
+                    tile_ready(v_index(v));
                     output(v, flags, pages, 0, !two);
                     if (more) {
-                        tile_ready(2 * v + 2);
+                        tile_ready(k_index(v + 1));
                         q_ready(next, 0);
                         if (!ok) break;
                         fence_after();
@@ -780,7 +791,7 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
             fence_after();
             if (partial) {
                 // rows of V behind the sequence's last token meet weights of 0; what stands there may be no number
-                const uint32_t n = 2u * v + 1;
+                const uint32_t n = v_index(v);
                 ok = __all_sync(~0u, bar_wait(s32(&full[n % SLOTS]), (n / SLOTS) & 1, a.spin_limit, failed));
                 if (!ok) break;
                 if (pages >> last_page & 1) {
@@ -1068,28 +1079,17 @@ __global__ void __launch_bounds__(merge_warps<D, NT>() * 32) merge_kernel(const 
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const MergeRec m = a.merges[blockIdx.x];
     if (m.n == 0) return;
+    const Seq q = m.q;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.y * 32 + lane;
     const int w = row / kTile, r = row % kTile, row_t = r / a.GT, row_g = r - row_t * a.GT, G = a.c.Hq / a.c.Hkv;
     const int tok = m.token0 + w * a.TT + row_t, head = m.kvh * G + m.pass * a.GT + row_g;
-    bool bad;
-    const Seq q = seq_of(a.c, m.s, bad);
     const bool live = row_t < a.TT && tok < q.n && m.pass * a.GT + row_g < G;
     if (!__any_sync(~0u, live)) return;
     auto slot = [&](int i) { return (long long)(2 * ((int)blockIdx.x + i) + (i == 0 ? 1 : 0)); };
     const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml);
-    // references first: the records of kFly partial results are in flight together
-    float top = -INFINITY, l = 0.f;
-    for (int i = 0; i < m.n; i += kFly) {
-        float z[kFly];
-#pragma unroll
-        for (int y = 0; y < kFly; ++y) z[y] = ml[slot(min(i + y, m.n - 1)) * (2 * kTile) + row].x;
-#pragma unroll
-        for (int y = 0; y < kFly; ++y) top = fmaxf(top, z[y]);
-    }
-    const float at = top == -INFINITY ? 0.f : top;
     bool fine = true;
     for (int c = warp; c < D / 4; c += merge_warps<D, NT>()) {
-        l = 0.f;
+        float at = -INFINITY, l = 0.f;        // the largest reference so far; sums relative to it
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int i = 0; i < m.n; i += kFly) {
             float4 y[kFly];
@@ -1100,9 +1100,17 @@ __global__ void __launch_bounds__(merge_warps<D, NT>() * 32) merge_kernel(const 
                 z[k] = ml[from * (2 * kTile) + row];
                 y[k] = reinterpret_cast<const float4 *>(a.part_o)[(from * (D / 4) + c) * (2 * kTile) + row];
             }
+            float top = at;
+#pragma unroll
+            for (int k = 0; k < kFly; ++k) top = fmaxf(top, z[k].x);
+            const float keep = at == -INFINITY ? 0.f : exp2_fast(at - top);
+            const float to = top == -INFINITY ? 0.f : top;
+            at = top;
+            l *= keep;
+            o.x *= keep; o.y *= keep; o.z *= keep; o.w *= keep;
 #pragma unroll
             for (int k = 0; k < kFly; ++k) {
-                const float f = exp2_fast(z[k].x - at);
+                const float f = exp2_fast(z[k].x - to);
                 if (i + k < m.n && f != 0.f) {
                     l = fmaf(f, z[k].y, l);
                     o.x = fmaf(f, y[k].x, o.x); o.y = fmaf(f, y[k].y, o.y); o.z = fmaf(f, y[k].z, o.z); o.w = fmaf(f, y[k].w, o.w);
