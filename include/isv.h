@@ -661,6 +661,8 @@ int isv_chunk_write(isv_chunk *h, void *pool_dev, int32_t n_pages, const int32_t
  * out_f32_dev (fp32) are [n_rows][q_heads][head_dim] and may each be NULL, not both.  A block without a page
  * (ISV_BLOCK_NONE) is left out and not flagged; other ids outside [0, n_pages) are left out and flagged.  A query that
  * sees nothing yields zeros.  What stands in invisible tokens, infinities and NaN too, changes nothing.
+ * Scores, sums and statistics are fp32.  The softmax weights meet V as 16-bit numbers (an error of the order of the output's own
+ * rounding) if out_f32_dev is NULL, and with fp32's precision if it is given.  The same inputs give the same bits.
  * Asynchronous on `stream`; may be captured. */
 int isv_chunk_attn(isv_chunk *h, const void *pool_dev, int32_t n_pages, const int32_t *block_table_dev, int32_t table_stride,
                    int32_t max_blocks_per_seq, const int32_t *seq_lens_dev, const int32_t *new_lens_dev,
@@ -684,7 +686,8 @@ int isv_chunk_inject_lost_copy(isv_chunk *h, int32_t launches);
  *     a = the first i < n for which u_i * q_i(x_i) < p_i(x_i) does not hold, or n
  *     next token: drawn from max(p_a - q_a, 0) where a < n (from p_a if that is 0 everywhere), from p_n where a = n
  * A draw takes the lowest index whose running sum exceeds u * total, with u = uniforms[s][max_draft].  Sums are taken in
- * 64 bits; probabilities that are negative or NaN count as 0, and need not sum to 1.
+ * 64 bits (long ones as pairs of fp32 numbers); probabilities that are negative or NaN count as 0, and need not sum to 1.  They
+ * are finite.
  *   target_dev     rows of vocab probabilities: rows row_starts_dev[s] .. + n (NULL = from s * (max_draft + 1) on) of n_rows
  *   draft_dev      [n_seqs][max_draft][vocab]; NULL = the drafts were certain (looked up, or the draft's best token):
  *                  q_i is 1 at x_i and 0 elsewhere.  dtype of both: ISV_F32, ISV_F16 or ISV_BF16

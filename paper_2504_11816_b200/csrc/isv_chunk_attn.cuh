@@ -930,7 +930,7 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                     for (int i = 0; i < 16; ++i) {
                         const uint64_t e2 = fma2(pair(y[2 * i], y[2 * i + 1]), cc, mm);
                         const float2 e = unpair(e2);
-                        const bool poly = !FINE && !SHAPED && i * kPoly % 16 < kPoly;
+                        const bool poly = NT == 2 && !FINE && !SHAPED && i * kPoly % 16 < kPoly;
                         const float2 p = poly ? exp2_poly<BF16 ? 3 : 4>(e2) : make_float2(exp2_fast(e.x), exp2_fast(e.y));
                         sum[i & 1] = add2(sum[i & 1], pair(p.x, p.y));
                         hi[i] = narrow<BF16>(p.x, p.y);
@@ -947,8 +947,9 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                         for (int y4 = 0; y4 < 4; ++y4) {
                             const int chunk = (col % 64 / 8 + y4) ^ (rr & 7);
                             *reinterpret_cast<uint4 *>(row + chunk * 16) = make_uint4(hi[4 * y4], hi[4 * y4 + 1], hi[4 * y4 + 2], hi[4 * y4 + 3]);
-                            *reinterpret_cast<uint4 *>(row + kWeights / 2 + chunk * 16) =
-                                make_uint4(lo[4 * y4], lo[4 * y4 + 1], lo[4 * y4 + 2], lo[4 * y4 + 3]);
+                            if (FINE)
+                                *reinterpret_cast<uint4 *>(row + kWeights / 2 + chunk * 16) =
+                                    make_uint4(lo[4 * y4], lo[4 * y4 + 1], lo[4 * y4 + 2], lo[4 * y4 + 3]);
                         }
                     } else {
                         // in place of their scores
@@ -1197,32 +1198,40 @@ cudaError_t launch(const AttnParams &p, int grid, cudaStream_t st, const char **
 }
 
 template <int D, bool BF16, int NT, int R, bool FINE>
-cudaError_t allow() {
+cudaError_t allow_as() {
     cudaError_t e = cudaFuncSetAttribute(attn_kernel<D, BF16, NT, R, FINE, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D>(R));
     if (e == cudaSuccess)
         e = cudaFuncSetAttribute(attn_kernel<D, BF16, NT, R, FINE, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D>(R));
     return e;
 }
+template <int D, bool BF16, int NT, int R>
+cudaError_t allow() {
+    const cudaError_t e = allow_as<D, BF16, NT, R, false>();
+    return e == cudaSuccess ? allow_as<D, BF16, NT, R, true>() : e;
+}
 template <int D, bool BF16>
 cudaError_t configure() {
-    cudaError_t e = allow<D, BF16, 1, 4, true>();
-    if (e == cudaSuccess) e = allow<D, BF16, 1, 2, true>();
-    if (e == cudaSuccess) e = allow<D, BF16, 1, 1, true>();
-    if (e == cudaSuccess) e = allow<D, BF16, 2, 1, true>();
-    if (e == cudaSuccess) e = allow<D, BF16, 2, 1, false>();
+    cudaError_t e = allow<D, BF16, 1, 4>();
+    if (e == cudaSuccess) e = allow<D, BF16, 1, 2>();
+    if (e == cudaSuccess) e = allow<D, BF16, 1, 1>();
+    if (e == cudaSuccess) e = allow<D, BF16, 2, 1>();
     return e;
 }
-// Weights enter their product as two 16-bit numbers (fp32's precision, one product more) wherever that costs little: with up to
-// 128 rows per KV head the call is bound by reading the cache.  Beyond that the tensor cores bound it, and a 16-bit output gets
-// weights rounded to 16 bits, an error of the order of its own rounding; with an fp32 output they stay exact.
+// FINE: weights enter their product as two 16-bit numbers, which keeps fp32's precision for one product more.  An fp32 output gets
+// that.  A 16-bit output alone gets weights rounded to 16 bits, an error of the order of its own rounding: 64 users' drafts 131 ->
+// 118 us, single tokens 90 -> 86; on prompts the tensor cores have half as much again to do for it.
+template <int D, bool BF16, bool FINE, bool SHAPED>
+cudaError_t pick_rows(const AttnParams &p, int grid, cudaStream_t st, const char **what) {
+    switch (p.tile_rows) {
+    case 32: return launch<D, BF16, 1, 4, FINE, SHAPED>(p, grid, st, what);
+    case 64: return launch<D, BF16, 1, 2, FINE, SHAPED>(p, grid, st, what);
+    case 128: return launch<D, BF16, 1, 1, FINE, SHAPED>(p, grid, st, what);
+    default: return launch<D, BF16, 2, 1, FINE, SHAPED>(p, grid, st, what);
+    }
+}
 template <int D, bool BF16, bool SHAPED>
 cudaError_t pick_shape(const AttnParams &p, int grid, cudaStream_t st, const char **what) {
-    switch (p.tile_rows) {
-    case 32: return launch<D, BF16, 1, 4, true, SHAPED>(p, grid, st, what);
-    case 64: return launch<D, BF16, 1, 2, true, SHAPED>(p, grid, st, what);
-    case 128: return launch<D, BF16, 1, 1, true, SHAPED>(p, grid, st, what);
-    default: return p.out_f32 ? launch<D, BF16, 2, 1, true, SHAPED>(p, grid, st, what) : launch<D, BF16, 2, 1, false, SHAPED>(p, grid, st, what);
-    }
+    return p.out_f32 ? pick_rows<D, BF16, true, SHAPED>(p, grid, st, what) : pick_rows<D, BF16, false, SHAPED>(p, grid, st, what);
 }
 // SHAPED: the scores need more than a positive factor.
 template <int D, bool BF16>
