@@ -1068,10 +1068,9 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
 
 // ---------------------------------------------------------------- merging
 
-// Partial results of items that crossed ranges.  CTA (record, group of 32 rows): a lane has one row, a warp four of its values at a
-// time, and kFly partial results are in flight together (bound by the latency of those rounds).  Items of few rows are cut into
+// Partial results of items that crossed ranges.  CTA (record, group of 32 rows): a lane has one row, a warp kWide times four of its
+// values, and kFly partial results are in flight together (bound by the latency of those rounds).  Items of few rows are cut into
 // many partial results: a warp for every four values.  Items of 256 rows have two or three, in many CTAs: eight warps.
-constexpr int kFly = 8;
 template <int D, int NT>
 __host__ __device__ constexpr int merge_warps() { return NT == 1 ? D / 4 : 8; }
 template <int D, bool BF16, int NT>
@@ -1088,43 +1087,56 @@ __global__ void __launch_bounds__(merge_warps<D, NT>() * 32) merge_kernel(const 
     if (!__any_sync(~0u, live)) return;
     auto slot = [&](int i) { return (long long)(2 * ((int)blockIdx.x + i) + (i == 0 ? 1 : 0)); };
     const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml);
-    bool fine = true;
-    for (int c = warp; c < D / 4; c += merge_warps<D, NT>()) {
-        float at = -INFINITY, l = 0.f;        // the largest reference so far; sums relative to it
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int i = 0; i < m.n; i += kFly) {
-            float4 y[kFly];
-            float2 z[kFly];
+    constexpr int WARPS = merge_warps<D, NT>(), kWide = (D / 4 + WARPS - 1) / WARPS, kFly = NT == 1 ? 8 : 2;
+    float at = -INFINITY, l = 0.f;        // the largest reference so far; sums relative to it
+    float4 o[kWide];
 #pragma unroll
-            for (int k = 0; k < kFly; ++k) {
-                const long long from = slot(min(i + k, m.n - 1));
-                z[k] = ml[from * (2 * kTile) + row];
-                y[k] = reinterpret_cast<const float4 *>(a.part_o)[(from * (D / 4) + c) * (2 * kTile) + row];
-            }
-            float top = at;
+    for (int c = 0; c < kWide; ++c) o[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i < m.n; i += kFly) {
+        float4 y[kFly][kWide];
+        float2 z[kFly];
 #pragma unroll
-            for (int k = 0; k < kFly; ++k) top = fmaxf(top, z[k].x);
-            const float keep = at == -INFINITY ? 0.f : exp2_fast(at - top);
-            const float to = top == -INFINITY ? 0.f : top;
-            at = top;
-            l *= keep;
-            o.x *= keep; o.y *= keep; o.z *= keep; o.w *= keep;
+        for (int k = 0; k < kFly; ++k) {
+            const long long from = slot(min(i + k, m.n - 1));
+            z[k] = ml[from * (2 * kTile) + row];
 #pragma unroll
-            for (int k = 0; k < kFly; ++k) {
-                const float f = exp2_fast(z[k].x - to);
-                if (i + k < m.n && f != 0.f) {
-                    l = fmaf(f, z[k].y, l);
-                    o.x = fmaf(f, y[k].x, o.x); o.y = fmaf(f, y[k].y, o.y); o.z = fmaf(f, y[k].z, o.z); o.w = fmaf(f, y[k].w, o.w);
+            for (int c = 0; c < kWide; ++c)
+                y[k][c] = reinterpret_cast<const float4 *>(a.part_o)[(from * (D / 4) + min(warp + c * WARPS, D / 4 - 1)) * (2 * kTile) + row];
+        }
+        float top = at;
+#pragma unroll
+        for (int k = 0; k < kFly; ++k) top = fmaxf(top, z[k].x);
+        const float keep = at == -INFINITY ? 0.f : exp2_fast(at - top);
+        const float to = top == -INFINITY ? 0.f : top;
+        at = top;
+        l *= keep;
+#pragma unroll
+        for (int c = 0; c < kWide; ++c) { o[c].x *= keep; o[c].y *= keep; o[c].z *= keep; o[c].w *= keep; }
+#pragma unroll
+        for (int k = 0; k < kFly; ++k) {
+            const float f = exp2_fast(z[k].x - to);
+            if (i + k < m.n && f != 0.f) {
+                l = fmaf(f, z[k].y, l);
+#pragma unroll
+                for (int c = 0; c < kWide; ++c) {
+                    o[c].x = fmaf(f, y[k][c].x, o[c].x); o[c].y = fmaf(f, y[k][c].y, o[c].y);
+                    o[c].z = fmaf(f, y[k][c].z, o[c].z); o[c].w = fmaf(f, y[k][c].w, o[c].w);
                 }
             }
         }
-        const float inv = l != 0.f ? 1.f / l : 0.f;
-        o.x *= inv; o.y *= inv; o.z *= inv; o.w *= inv;
-        fine = fine && fabsf(l) <= FLT_MAX && fabsf(o.x) <= FLT_MAX && fabsf(o.y) <= FLT_MAX && fabsf(o.z) <= FLT_MAX && fabsf(o.w) <= FLT_MAX;
-        const long long to = ((long long)(q.first + tok) * a.c.Hq + head) * D + 4 * c;
+    }
+    const float inv = l != 0.f ? 1.f / l : 0.f;
+    bool fine = fabsf(l) <= FLT_MAX;
+#pragma unroll
+    for (int c = 0; c < kWide; ++c) {
+        if (warp + c * WARPS >= D / 4) continue;
+        float4 r4 = o[c];
+        r4.x *= inv; r4.y *= inv; r4.z *= inv; r4.w *= inv;
+        fine = fine && fabsf(r4.x) <= FLT_MAX && fabsf(r4.y) <= FLT_MAX && fabsf(r4.z) <= FLT_MAX && fabsf(r4.w) <= FLT_MAX;
+        const long long to = ((long long)(q.first + tok) * a.c.Hq + head) * D + 4 * (warp + c * WARPS);
         if (live) {
-            if (a.out) *reinterpret_cast<uint2 *>(a.out + to) = make_uint2(narrow<BF16>(o.x, o.y), narrow<BF16>(o.z, o.w));
-            if (a.out_f32) *reinterpret_cast<float4 *>(a.out_f32 + to) = o;
+            if (a.out) *reinterpret_cast<uint2 *>(a.out + to) = make_uint2(narrow<BF16>(r4.x, r4.y), narrow<BF16>(r4.z, r4.w));
+            if (a.out_f32) *reinterpret_cast<float4 *>(a.out_f32 + to) = r4;
         }
     }
     // rows whose sums are no number (see the kernel above): every warp has its columns written before one recomputes the row
