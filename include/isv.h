@@ -597,8 +597,8 @@ int isv_linear4_free(isv_linear4 *l);
  * The pool is [n_pages][K|V][kv_heads][16 tokens][head_dim] 16-bit in the order described under "KV pool layout" above,
  * one layer of it.  Sequence s has seq_lens_dev[s] tokens, the new ones included; its last new_lens_dev[s] <= T of them
  * (NULL = T of every sequence) are the chunk, at positions seq_lens_dev[s] - new_lens_dev[s] and on.  Their q, k, v and
- * outputs are rows row_starts_dev[s] and on (NULL = s * T) of arrays of n_rows rows; rows of no sequence are neither read
- * nor written.  Row strides are in elements, multiples of 8, and hold at least a token's heads: q, k and v may be parts
+ * outputs are rows row_starts_dev[s] and on (NULL = s * T) of arrays of n_rows rows, which no two sequences share; rows of no
+ * sequence have no influence and are not written.  Row strides are in elements, multiples of 8, and hold at least a token's heads: q, k and v may be parts
  * of one array.
  * Lengths are clamped to what the table row holds (16 * max_blocks_per_seq), new lengths to [0, min(T, length)] and to the
  * rows there are, and flagged (ISV_STATUS_BAD_LENGTH).  All pointers but block tables, lengths, starts, prefixes, slopes,
@@ -643,7 +643,8 @@ int isv_chunk_free(isv_chunk *h);
  *                    beyond the last axis mean the last); NULL = axis 0
  *   magnitude        factor on the turned elements, 1 for none
  * A token whose block has no page (ISV_BLOCK_NONE or an id outside [0, n_pages)) is not stored, and flagged
- * (ISV_STATUS_BAD_BLOCK_ID); its query is turned all the same.  The inputs and the pool must not overlap.
+ * (ISV_STATUS_BAD_BLOCK_ID); its query is turned all the same.  Inputs, pool and q_out must not overlap, and no two sequences
+ * store into one page.
  * Asynchronous on `stream`; may be captured into a CUDA graph; calls may overlap. */
 int isv_chunk_write(isv_chunk *h, void *pool_dev, int32_t n_pages, const int32_t *block_table_dev, int32_t table_stride,
                     int32_t max_blocks_per_seq, const int32_t *seq_lens_dev, const int32_t *new_lens_dev,
@@ -663,6 +664,8 @@ int isv_chunk_write(isv_chunk *h, void *pool_dev, int32_t n_pages, const int32_t
  * sees nothing yields zeros.  What stands in invisible tokens, infinities and NaN too, changes nothing.
  * Scores, sums and statistics are fp32.  The softmax weights meet V as 16-bit numbers (an error of the order of the output's own
  * rounding) if out_f32_dev is NULL, and with fp32's precision if it is given.  The same inputs give the same bits.
+ * A row whose sums are not finite (an infinity or NaN among the tokens of its tile, values near the type's largest) is computed
+ * again, token by token: correctly, but slowly.
  * Asynchronous on `stream`; may be captured. */
 int isv_chunk_attn(isv_chunk *h, const void *pool_dev, int32_t n_pages, const int32_t *block_table_dev, int32_t table_stride,
                    int32_t max_blocks_per_seq, const int32_t *seq_lens_dev, const int32_t *new_lens_dev,
@@ -674,7 +677,7 @@ int isv_chunk_attn(isv_chunk *h, const void *pool_dev, int32_t n_pages, const in
  * since the last query. */
 int isv_chunk_status(isv_chunk *h, void *stream, uint32_t *status_out);
 /* As isv_set_wait_limit and isv_inject_lost_copy, for the attention's copies: `polls` of a barrier before a wait gives up
- * (0 = the built-in default), and launches in which a page of the first CTA's first visit is expected and not copied.  A CTA
+ * (0 = the built-in default), and launches in which the first page that is to be read is expected and not copied.  A CTA
  * in which a wait runs out gives the copies in flight one more bounded chance to land and leaves; the launch ends with
  * incomplete outputs, isv_chunk_status reports it once, and the handle stays usable. */
 int isv_chunk_set_wait_limit(isv_chunk *h, uint32_t polls);
@@ -700,7 +703,7 @@ int isv_chunk_inject_lost_copy(isv_chunk *h, int32_t launches);
  * A drafted token outside [0, vocab) does not stand (ISV_STATUS_BAD_TOKEN).  Where all of a row's probabilities are 0 the
  * next token is -1 (ISV_STATUS_BAD_TOKEN).  Counts outside [0, max_draft] and rows that are not there are clamped and
  * flagged (ISV_STATUS_BAD_LENGTH); a sequence without any row gets no token.  max_draft <= 1024.  Probabilities are aligned
- * to their elements.  Uses no memory but what it is given and runs on the current device; asynchronous on `stream`; may be
+ * to their elements; outputs overlap nothing, but lens_out_dev may be seq_lens_dev.  Uses no memory but what it is given and runs on the current device; asynchronous on `stream`; may be
  * captured; results do not depend on scheduling. */
 int isv_draft_verify(const void *target_dev, const int32_t *row_starts_dev, int32_t n_rows, const void *draft_dev,
                      int32_t vocab, int32_t dtype, const int32_t *drafted_dev, const int32_t *n_draft_dev,

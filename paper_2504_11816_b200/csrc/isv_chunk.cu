@@ -327,6 +327,7 @@ int isv_chunk_write(isv_chunk *h, void *pool_dev, int32_t n_pages, const int32_t
     const int64_t kv_row = (int64_t)h->d.kv_heads * h->d.head_dim, q_row = (int64_t)h->d.q_heads * h->d.head_dim;
     if (kv_stride % 8 || kv_stride < kv_row || (q_dev && (q_stride % 8 || q_stride < q_row)))
         return err(ISV_EINVAL, "%s: strides must be multiples of 8 elements that hold a token's heads", who);
+    if (q_dev && q_out_dev == q_dev && q_stride != q_row) return err(ISV_EINVAL, "%s: q_out is q, but q has another stride (NULL turns q in place)", who);
     if (h->d.rotary_dim > 0 && !inv_freq_dev) return err(ISV_EINVAL, "%s: inv_freq is required", who);
     if (!positions_dev && pair_axis_dev) return err(ISV_EINVAL, "%s: pair_axis without positions", who);
     if (!std::isfinite(magnitude)) return err(ISV_EINVAL, "%s: magnitude must be finite", who);
@@ -372,7 +373,7 @@ int isv_chunk_attn(isv_chunk *h, const void *pool_dev, int32_t n_pages, const in
     if (q_stride % 8 || q_stride < (int64_t)h->d.q_heads * h->d.head_dim)
         return err(ISV_EINVAL, "%s: the stride of q must be a multiple of 8 elements that holds a token's heads", who);
     if (window < 0) return err(ISV_EINVAL, "%s: window must not be negative", who);
-    if (n_seqs == 0 || T == 0) return ISV_OK;
+    if (n_seqs == 0 || T == 0 || n_rows == 0) return ISV_OK;
     AttnParams p{};
     p.c = cache_params(h, pool_dev, n_pages, block_table_dev, table_stride, max_blocks_per_seq, seq_lens_dev, new_lens_dev, row_starts_dev,
                        n_rows, n_seqs, T);

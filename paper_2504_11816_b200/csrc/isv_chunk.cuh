@@ -46,7 +46,7 @@ struct AttnParams {
     float *part_ml;             // [slot][rows of an item] of (reference, sum)
     MergeRec *merges;           // [grid]: the item that begins in this CTA's range and ends in another's
     uint32_t spin_limit;        // polls of a barrier before a wait gives up
-    int32_t drop_first_copy;    // failure injection: the first visit's barrier of CTA 0 is armed without issuing one of its copies
+    int32_t drop_first_copy;    // failure injection: the first item's first barrier is armed without issuing one of its copies
 };
 
 // One sequence of a call, clamped to what the table row, T and the rows hold.

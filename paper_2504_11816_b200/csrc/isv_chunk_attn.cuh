@@ -514,7 +514,7 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                             z.s = s; z.token0 = token0; z.kvh = kvh; z.pass = pass; z.slot = slot; z.q = q;
                             bar_arrive(s32(&rec_full[v % kRecs]));
                         }
-                        fetch(k_index(v), 0, id, pages, kvh, a.drop_first_copy && cta == 0 && v == 0);
+                        fetch(k_index(v), 0, id, pages, kvh, a.drop_first_copy && at == 0 && x == 0);
                         if (NT == 1) {
                             if (v > 0) {
                                 slot_free(v_index(v - 1));
@@ -1075,8 +1075,8 @@ template <int D, int NT>
 __host__ __device__ constexpr int merge_warps() { return NT == 1 ? D / 4 : 8; }
 template <int D, bool BF16, int NT>
 __global__ void __launch_bounds__(merge_warps<D, NT>() * 32) merge_kernel(const __grid_constant__ AttnParams a) {
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const MergeRec m = a.merges[blockIdx.x];
     if (m.n == 0) return;
     const Seq q = m.q;
@@ -1202,7 +1202,8 @@ cudaError_t launch(const AttnParams &p, int grid, cudaStream_t st, const char **
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     cudaError_t e = cudaLaunchKernelEx(&cfg, attn_kernel<D, BF16, NT, R, FINE, SHAPED>, kv, kv_tail, q, q_tail, p);
-    if (e != cudaSuccess) return e;
+    // a table row that covers one visit: no item is cut
+    if (e != cudaSuccess || p.c.max_blocks <= kPages) return e;
     cfg.gridDim = dim3(grid, NT * kTile / R / 32);
     cfg.blockDim = dim3(merge_warps<D, NT>() * 32);
     cfg.dynamicSmemBytes = 0;
