@@ -815,10 +815,14 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                 const bool all = pages == 0xff && sight.lim >= j0 + kTile && (sight.low <= j0 || sight.prefix >= j0 + kTile);
                 const bool masked = !__all_sync(~0u, all || !live);
                 float xa[32], xb[32];
-                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                auto look = [&](float (&y)[32], int k) {
-                    const int at = j1 + 32 * k;
-                    if (SHAPED) {
+                if (SHAPED) {
+                    // scores that need more than a factor are made ready first, in place: a loop of its own is the least code
+#pragma unroll 1
+                    for (int k = 0; k < COLS / 32; ++k) {
+                        const int at = j1 + 32 * k;
+                        float (&y)[32] = xa;
+                        tmem_ld32(cols + 32 * k, reinterpret_cast<uint32_t *>(y));
+                        wait_ld();
                         if (a.cap > 0.f) {
                             const float in = a.scale / a.cap;
                             float most = 0.f;
@@ -839,17 +843,34 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                                     y[i] = fmaf(-2.f * a.cap, reciprocal(e + 1.f), a.cap);
                                 }
                             }
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) y[i] *= a.scale;
                         }
-                        if (a.slopes) {
+                        if (a.slopes || !(a.cap > 0.f)) {
+                            const uint64_t by = both(a.cap > 0.f ? 1.f : a.scale);
                             const float distance = (float)(pos - at);
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) y[i] = fmaf(-slope, fabsf(distance - (float)i), y[i]);
+                            for (int i = 0; i < 32; i += 2) {
+                                const float2 z = unpair(mul2(pair(y[i], y[i + 1]), by));
+                                y[i] = fmaf(-slope, fabsf(distance - (float)i), z.x);
+                                y[i + 1] = fmaf(-slope, fabsf(distance - (float)(i + 1)), z.y);
+                            }
                         }
+                        if (masked) {
+                            // bit i: token at + i is seen
+                            auto below = [&](int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; };
+                            const uint32_t here = pages >> ((at - j0) / kBT);
+                            uint32_t seen = below(sight.lim - at) & (~below(sight.low - at) | below(sight.prefix - at));
+                            seen &= (here & 1 ? 0xffffu : 0u) | (here & 2 ? 0xffff0000u : 0u);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) y[i] = seen >> i & 1 ? y[i] : -INFINITY;
+                        }
+                        tmem_st32(cols + 32 * k, reinterpret_cast<uint32_t *>(y));
                     }
-                    if (masked) {
+                    wait_st();
+                }
+                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                auto look = [&](float (&y)[32], int k) {
+                    const int at = j1 + 32 * k;
+                    if (!SHAPED && masked) {
                         // bit i: token at + i is seen
                         auto below = [&](int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; };
                         const uint32_t here = pages >> (2 * k + col0 / kBT);
@@ -858,7 +879,7 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
 #pragma unroll
                         for (int i = 0; i < 32; ++i) y[i] = seen >> i & 1 ? y[i] : -INFINITY;
                     }
-                    if (COLS > 32 && (SHAPED || masked)) tmem_st32(cols + 32 * k, reinterpret_cast<uint32_t *>(y));
+                    if (COLS > 32 && !SHAPED && masked) tmem_st32(cols + 32 * k, reinterpret_cast<uint32_t *>(y));
 #pragma unroll
                     for (int i = 0; i < 32; i += 2) top[i / 2 & 3] = max3(top[i / 2 & 3], y[i], y[i + 1]);
                 };
@@ -875,7 +896,7 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                     }
                 }
                 if (COLS > 32) {
-                    if (SHAPED || masked) wait_st();
+                    if (!SHAPED && masked) wait_st();
                     tmem_ld32(cols, reinterpret_cast<uint32_t *>(xa));
                 }
                 float high = max3(top[0], top[1], max3(top[2], top[3], top[3])) * c;
