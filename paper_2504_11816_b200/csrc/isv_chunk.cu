@@ -189,6 +189,7 @@ struct isv_chunk {
     int device = 0;
     int sms = 1, grid = 1;              // of the device, of the attention kernel
     int GT = 1, P = 1;                  // query heads per visit, passes
+    char *memory = nullptr;             // all of what follows
     uint32_t *status = nullptr;
     float *part_o = nullptr, *part_ml = nullptr;
     MergeRec *merges = nullptr;
@@ -253,10 +254,7 @@ int isv_chunk_free(isv_chunk *h) {
     if (!h) return err(ISV_EINVAL, "null handle");
     OnDevice on(h->device);
     cudaDeviceSynchronize();   // calls may have been made on any stream
-    cudaFree(h->status);
-    cudaFree(h->part_o);
-    cudaFree(h->part_ml);
-    cudaFree(h->merges);
+    cudaFree(h->memory);
     delete h;
     return ISV_OK;
 }
@@ -296,11 +294,15 @@ int isv_chunk_create(isv_chunk **out, const isv_chunk_desc *desc) {
     const bool bf16 = desc->dtype == ISV_BF16;
     if (e == cudaSuccess)
         e = desc->head_dim == 64 ? attn_configure<64>(bf16) : desc->head_dim == 80 ? attn_configure<80>(bf16) : attn_configure<128>(bf16);
-    if (e == cudaSuccess) e = cudaMalloc((void **)&h->status, 4);
-    if (e == cudaSuccess) e = cudaMemset(h->status, 0, 4);
-    if (e == cudaSuccess) e = cudaMalloc((void **)&h->part_o, rows * desc->head_dim * 4);
-    if (e == cudaSuccess) e = cudaMalloc((void **)&h->part_ml, rows * 2 * 4);
-    if (e == cudaSuccess) e = cudaMalloc((void **)&h->merges, h->grid * sizeof(MergeRec));
+    const size_t o_bytes = rows * desc->head_dim * 4, ml_bytes = rows * 2 * 4, rec_bytes = (h->grid * sizeof(MergeRec) + 255) / 256 * 256;
+    if (e == cudaSuccess) e = cudaMalloc((void **)&h->memory, o_bytes + ml_bytes + rec_bytes + 256);
+    if (e == cudaSuccess) {
+        h->part_o = reinterpret_cast<float *>(h->memory);
+        h->part_ml = reinterpret_cast<float *>(h->memory + o_bytes);
+        h->merges = reinterpret_cast<MergeRec *>(h->memory + o_bytes + ml_bytes);
+        h->status = reinterpret_cast<uint32_t *>(h->memory + o_bytes + ml_bytes + rec_bytes);
+        e = cudaMemset(h->status, 0, 4);
+    }
     if (e == cudaSuccess) e = cudaDeviceSynchronize();   // the zeros are there before any stream's first call
     if (e != cudaSuccess) {
         cudaGetLastError();

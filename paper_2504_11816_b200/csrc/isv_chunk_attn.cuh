@@ -953,12 +953,11 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                         const float2 e = unpair(e2);
                         const bool poly = NT == 2 && !FINE && !SHAPED && i * kPoly % 16 < kPoly;
                         const float2 p = poly ? exp2_poly<BF16 ? 3 : 4>(e2) : make_float2(exp2_fast(e.x), exp2_fast(e.y));
-                        sum[i & 1] = add2(sum[i & 1], pair(p.x, p.y));
                         hi[i] = narrow<BF16>(p.x, p.y);
-                        if (FINE) {
-                            const float2 h = widen<BF16>(hi[i]);
-                            lo[i] = narrow<BF16>(p.x - h.x, p.y - h.y);
-                        }
+                        // the sum is that of the weights as they are used: a weight that is most of a row has no error then
+                        const float2 h = widen<BF16>(hi[i]);
+                        sum[i & 1] = add2(sum[i & 1], FINE ? pair(p.x, p.y) : pair(h.x, h.y));
+                        if (FINE) lo[i] = narrow<BF16>(p.x - h.x, p.y - h.y);
                     }
                     if (R > 1) {
                         // rows of 64 columns with the 128-byte swizzle
