@@ -38,7 +38,7 @@ struct AttnParams {
     int32_t window;             // 0: no limit
     float scale;                // of the scores
     float cap;                  // 0: scores are not capped
-    // how the work is cut (attn_shape), and scratch
+    // how the work is cut, and scratch
     int32_t GT, P;              // a visit serves GT of a KV head's query heads; P passes serve all of them
     int32_t tile_rows;          // rows of an item, as attn_tile_rows says
     int32_t TT, RT;             // tokens of a tile of (at most) 128 rows; items that a chunk of T tokens has at most, per KV head and pass

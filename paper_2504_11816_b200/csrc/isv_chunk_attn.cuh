@@ -11,7 +11,7 @@
 // visits of all items form one list that is cut into equal ranges, one per persistent CTA, whatever the lengths; an item that
 // crosses ranges leaves partial results, which a second small kernel merges in fixed order.
 //
-// A CTA: a producer warp copies a visit's pages (K, then V) into a ring by TMA; one thread issues the products; NT groups of four
+// A CTA: a producer warp copies the pages of K and V into a ring of tiles by TMA; one thread issues the products; NT groups of four
 // warps turn scores into weights, one row per thread.  With NT = 2 the groups take turns with the tensor cores: while one
 // computes its weights, the other's products run.  With NT = 1 the scores of the next visit are computed meanwhile.  Where a KV
 // head has no more than 64 or 32 rows, the tile holds R = 2 or 4 copies of them, each for its share of a visit's columns (a warp
@@ -23,8 +23,8 @@
 // head_dim 80 are a box of their own with the 32-byte swizzle.  P goes back into the scores' columns of tensor memory as 16-bit
 // numbers, the A operand of P V.
 //
-// Every wait is bounded; on expiry the kernel flags the status word, waits for its copies (bounded), frees its tensor memory
-// and returns.
+// Every wait is bounded (while a warp computes rows token by token, which ends, the count stops); on expiry the kernel flags the
+// status word, waits for its copies (bounded), frees its tensor memory and returns.
 #pragma once
 
 #include <cuda.h>
@@ -32,6 +32,7 @@
 
 #include <algorithm>
 #include <cfloat>
+#include <climits>
 
 #include "isv_chunk.cuh"
 
@@ -42,9 +43,10 @@ namespace {
 
 constexpr int kTile = 128;             // rows of a tile, tokens of a visit
 constexpr int kPages = kTile / kBT;
-constexpr int kRecs = 8;               // visit records in flight (a ring of at most 10 tiles is less than 6 visits ahead)
+constexpr int kRecs = 8;               // visit records in flight (a ring of at most 10 tiles is less than 6 visits ahead of the products)
 // Of 16 powers of two, those that are taken by a polynomial where weights are rounded to 16 bits and scores come as they are: the
-// special-function unit does 4 a cycle and quarter of an SM.  A prompt of 8192 tokens: 0 625 us, 3 593, 5 594.
+// special-function unit does 4 a cycle and quarter of an SM.  A prompt of 8192 tokens, when this was
+// settled: 0 625 us, 3 593, 5 594.
 constexpr int kPoly = 3;
 constexpr float kLog2e = 1.4426950408889634f;
 // How far a row's maximum may pass its reference before the reference follows (and O is scaled): fp16 weights have to stay below 2^16;
@@ -72,12 +74,17 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
                  : "memory");
     return ok;
 }
-// Whether the barrier's phase completed before the limit, and before another warp gave up.
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, uint32_t limit, const volatile int *failed) {
+// Whether the barrier's phase completed before the limit, and before another warp gave up (state below 0).  While warps compute rows
+// token by token (their number above 0), which ends but may take long, a wait is not counted.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, uint32_t limit, const volatile int *state) {
     if (bar_try(bar, parity)) return true;
     for (uint32_t i = 0; i < limit; ++i) {
         if (bar_try(bar, parity)) return true;
-        if ((i & 63) == 63 && *failed) return false;
+        if ((i & 63) == 63) {
+            const int now = *state;
+            if (now < 0) return false;
+            if (now > 0) i = 0;
+        }
     }
     return false;
 }
@@ -326,13 +333,15 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
     float *exchange = reinterpret_cast<float *>(misc + kMisc);      // [2][copy of the rows][row]
     Visit *recs = reinterpret_cast<Visit *>(misc);
     uint64_t *bars = reinterpret_cast<uint64_t *>(misc + kRecs * sizeof(Visit));
-    uint64_t *full = bars, *empty = full + SLOTS, *rec_full = empty + SLOTS, *q_full = rec_full + kRecs, *q_empty = q_full + 2;
+    uint64_t *full = bars, *empty = full + SLOTS, *rec_full = empty + SLOTS, *rec_read = rec_full + kRecs, *q_full = rec_read + kRecs, *q_empty = q_full + 2;
     uint64_t *s_full = q_empty + 2, *p_full = s_full + 2, *pv_done = p_full + 4, *drain = pv_done + 2, *x_full = drain + 1;   // p_full: [half of the tokens][2]
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(x_full + 1);
-    volatile int *failed = reinterpret_cast<volatile int *>(tmem_slot + 1);
-    static_assert(kRecs * sizeof(Visit) + (2 * SLOTS + kRecs + 14) * 8 + 8 <= kMisc, "");
+    int *state = reinterpret_cast<int *>(tmem_slot + 1);      // below 0: a wait ran out; above: warps that others wait for, however long
+    static_assert(kRecs * sizeof(Visit) + (2 * SLOTS + 2 * kRecs + 14) * 8 + 8 <= kMisc, "");
     long long *sums = reinterpret_cast<long long *>(ring + (SLOTS - 1) * SH::TILE);   // until the first copies
     const int warp = same(threadIdx.x >> 5), lane = threadIdx.x & 31;
+    auto give_up = [&]() { atomicOr(state, INT_MIN); };
+    auto gave_up = [&]() { return *reinterpret_cast<const volatile int *>(state) < 0; };
     // Tiles in the order in which they are consumed.  NT = 2: K and V of a visit in turn.  NT = 1: the next visit's K before this one's V
     // (K0 K1 V0 K2 V1 ..), so that V does not wait in the ring for its weights.
     auto k_index = [](int v) -> uint32_t { return NT == 2 ? 2 * v : v == 0 ? 0 : 2 * v - 1; };
@@ -343,7 +352,10 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
             bar_init(s32(&full[i]), 1);
             bar_init(s32(&empty[i]), 1);
         }
-        for (int i = 0; i < kRecs; ++i) bar_init(s32(&rec_full[i]), 1);
+        for (int i = 0; i < kRecs; ++i) {
+            bar_init(s32(&rec_full[i]), 1);
+            bar_init(s32(&rec_read[i]), NT == 2 ? 5 : 1);
+        }
         for (int i = 0; i < 2; ++i) {
             bar_init(s32(&q_full[i]), 1);
             bar_init(s32(&q_empty[i]), 1);
@@ -354,7 +366,7 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
         }
         bar_init(s32(drain), 1);
         bar_init(s32(x_full), 4);
-        *failed = 0;
+        *state = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -425,7 +437,7 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
         int before_id = 0, before_kvh = 0;
         uint32_t before_pages = 0;
         auto slot_free = [&](uint32_t n) {
-            ok = __all_sync(~0u, n < SLOTS || bar_wait(s32(&empty[n % SLOTS]), (n / SLOTS - 1) & 1, a.spin_limit, failed));
+            ok = __all_sync(~0u, n < SLOTS || bar_wait(s32(&empty[n % SLOTS]), (n / SLOTS - 1) & 1, a.spin_limit, state));
         };
         // copies the pages of K (kv = 0) or V of a visit as tile n: a lane per copy (one lane for all takes twice as long)
         auto fetch = [&](uint32_t n, int kv, int id, uint32_t pages, int kvh, bool drop) {
@@ -441,8 +453,15 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
             }
             top = n + 1;
         };
+        // Record v may be written: the one before it in its place is read.  A visit whose tiles are used up has been read by those
+        // who work on it; these may lag behind the ring: the loader, which only works at an item's begin, and the second group of
+        // warps, which passes over items of one row tile.
+        auto rec_free = [&]() {
+            ok = ok && __all_sync(~0u, v < kRecs || bar_wait(s32(&rec_read[v % kRecs]), (v / kRecs - 1) & 1, a.spin_limit, state));
+        };
         auto put_end = [&]() {
-            if (lane == 0) {
+            rec_free();
+            if (ok && lane == 0) {
                 recs[v % kRecs].flags = END;
                 bar_arrive(s32(&rec_full[v % kRecs]));
             }
@@ -503,6 +522,7 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                         if (lane < 8 && !there && id != ISV_BLOCK_NONE) atomicOr(a.c.status, ISV_STATUS_BAD_BLOCK_ID);
                         const uint32_t pages = __ballot_sync(~0u, there) & 0xff;
                         slot_free(k_index(v));
+                        rec_free();
                         if (!ok) break;
                         if (lane == 0) {
                             Visit &z = recs[v % kRecs];
@@ -539,8 +559,8 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
             a.merges[cta] = rec;
         }
         if (ok) put_end();
-        else *failed = 1;
-        if (!ok || *failed) {
+        if (!ok) give_up();
+        if (!ok || gave_up()) {
             // something gave up: the copies in flight land before the memory passes on
             for (uint32_t i = top > SLOTS ? top - SLOTS : 0; i < top; ++i)
                 for (uint32_t k = 0; k < 1u << 16 && !bar_try(s32(&full[i % SLOTS]), (i / SLOTS) & 1); ++k) {}
@@ -551,14 +571,15 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
             bool ok = true;
             int used[2] = {0, 0}, item = 0;
             for (int v = 0; ok; ++v) {
-                if (!bar_wait(s32(&rec_full[v % kRecs]), (v / kRecs) & 1, a.spin_limit, failed)) { ok = false; break; }
+                if (!bar_wait(s32(&rec_full[v % kRecs]), (v / kRecs) & 1, a.spin_limit, state)) { ok = false; break; }
                 const Visit z = recs[v % kRecs];
+                bar_arrive(s32(&rec_read[v % kRecs]));
                 if (z.flags & END) break;
                 if (!(z.flags & FIRST)) continue;
                 const int tiles = NT == 2 && (z.flags & TWO) ? 2 : 1;
                 for (int i = 0; i < tiles && ok; ++i) {
                     const int buf = NT == 2 ? i : R > 1 ? 0 : item & 1;
-                    if (used[buf] > 0 && !bar_wait(s32(&q_empty[buf]), (used[buf] - 1) & 1, a.spin_limit, failed)) { ok = false; break; }
+                    if (used[buf] > 0 && !bar_wait(s32(&q_empty[buf]), (used[buf] - 1) & 1, a.spin_limit, state)) { ok = false; break; }
                     ++used[buf];
                     const uint32_t dst = s32(q_tiles + buf * SH::TILE), bar = s32(&q_full[buf]);
                     const int rows = a.GT * a.TT, head = z.kvh * (a.c.Hq / a.c.Hkv) + z.pass * a.GT, token = z.q.first + z.token0 + i * a.TT;
@@ -572,8 +593,8 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                 }
                 ++item;
             }
-            if (!ok) *failed = 1;
-            if (!ok || *failed)
+            if (!ok) give_up();
+            if (!ok || gave_up())
                 for (int buf = 0; buf < 2; ++buf)
                     for (uint32_t k = 0; used[buf] > 0 && k < 1u << 16 && !bar_try(s32(&q_full[buf]), (used[buf] - 1) & 1); ++k) {}
         }
@@ -587,7 +608,7 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
         uint32_t started[2] = {0, 0};
         const uint32_t q_base = s32(q_tiles), ring_base = s32(ring);
         auto wait = [&](uint64_t *bar, uint32_t parity) {
-            ok = ok && __all_sync(~0u, bar_wait(s32(bar), parity, a.spin_limit, failed));
+            ok = ok && __all_sync(~0u, bar_wait(s32(bar), parity, a.spin_limit, state));
         };
         // S of tile or buffer w of visit v
         auto scores = [&](int v, int flags, int w, bool release) {
@@ -727,10 +748,7 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
             }
         }
         if (!ok) {
-            if (lane == 0) {
-                *failed = 1;
-                atomicOr(a.c.status, ISV_STATUS_WAIT_EXPIRED);
-            }
+            give_up();
             commit(s32(drain));       // what was issued ends before tensor memory passes on
             for (uint32_t k = 0; k < 1u << 16 && !bar_try(s32(drain), 0); ++k) {}
         }
@@ -749,7 +767,7 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
             at[r] = x;
             __syncwarp();
             if (lane == 0) bar_arrive(s32(x_full));
-            ok = __all_sync(~0u, bar_wait(s32(x_full), x_phase & 1, a.spin_limit, failed));
+            ok = __all_sync(~0u, bar_wait(s32(x_full), x_phase & 1, a.spin_limit, state));
             ++x_phase;
             if (!ok) return;
 #pragma unroll
@@ -763,12 +781,20 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
         Sight sight{};
         float ref = -INFINITY, l = 0.f, slope = 0.f;
         for (int v = 0;; ++v) {
-            ok = __all_sync(~0u, bar_wait(s32(&rec_full[v % kRecs]), (v / kRecs) & 1, a.spin_limit, failed));
+            ok = __all_sync(~0u, bar_wait(s32(&rec_full[v % kRecs]), (v / kRecs) & 1, a.spin_limit, state));
             if (!ok) break;
             const Visit &z = recs[v % kRecs];
             const int flags = z.flags;
             if (flags & END) break;
-            if (NT == 2 && w == 1 && !(flags & TWO)) continue;
+            auto read = [&]() {
+                if (NT == 1 || w == 0) return;
+                __syncwarp();
+                if (lane == 0) bar_arrive(s32(&rec_read[v % kRecs]));
+            };
+            if (NT == 2 && w == 1 && !(flags & TWO)) {
+                read();
+                continue;
+            }
             const int b = NT == 2 ? w : v & 1;                                // buffer of the scores
             const uint32_t phase = NT == 2 ? used & 1 : (v >> 1) & 1;
             if (flags & FIRST) {
@@ -786,13 +812,14 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
             }
             const int j0 = z.j0, slot = z.slot, partial = w == 0 ? z.partial : 0, last_page = z.last_page;
             const uint32_t pages = z.pages;
-            ok = __all_sync(~0u, bar_wait(s32(&s_full[b]), phase, a.spin_limit, failed));
+            read();
+            ok = __all_sync(~0u, bar_wait(s32(&s_full[b]), phase, a.spin_limit, state));
             if (!ok) break;
             fence_after();
             if (partial) {
                 // rows of V behind the sequence's last token meet weights of 0; what stands there may be no number
                 const uint32_t n = v_index(v);
-                ok = __all_sync(~0u, bar_wait(s32(&full[n % SLOTS]), (n / SLOTS) & 1, a.spin_limit, failed));
+                ok = __all_sync(~0u, bar_wait(s32(&full[n % SLOTS]), (n / SLOTS) & 1, a.spin_limit, state));
                 if (!ok) break;
                 if (pages >> last_page & 1) {
                     uint8_t *vt = ring + (size_t)(n % SLOTS) * SH::TILE;
@@ -919,13 +946,13 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
                 const uint32_t before = NT == 2 ? used - 1 : v - 1;            // the product before this one
                 if (R > 1 && v > 0) {
                     // it has read the weights that are overwritten now
-                    ok = __all_sync(~0u, bar_wait(s32(&pv_done[before & 1]), (before >> 1) & 1, a.spin_limit, failed));
+                    ok = __all_sync(~0u, bar_wait(s32(&pv_done[before & 1]), (before >> 1) & 1, a.spin_limit, state));
                     if (!ok) break;
                 }
                 if (__any_sync(~0u, factor != 1.f)) {
                     // O is scaled: the product before this one has to be in it
                     l *= factor;
-                    ok = __all_sync(~0u, bar_wait(s32(&pv_done[NT == 2 ? w : before & 1]), (NT == 2 ? before : before >> 1) & 1, a.spin_limit, failed));
+                    ok = __all_sync(~0u, bar_wait(s32(&pv_done[NT == 2 ? w : before & 1]), (NT == 2 ? before : before >> 1) & 1, a.spin_limit, state));
                     if (!ok) break;
                     fence_after();
                     const uint32_t o = lanes + 2 * kTile + (NT == 2 ? w : 0) * kTile;
@@ -1015,7 +1042,7 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
             if (!(flags & LAST)) continue;
 
             // ---- the item's end: O / l, or a partial result
-            ok = __all_sync(~0u, bar_wait(s32(&pv_done[b]), phase, a.spin_limit, failed));
+            ok = __all_sync(~0u, bar_wait(s32(&pv_done[b]), phase, a.spin_limit, state));
             if (!ok) break;
             if (R > 1) {
                 float of[R];
@@ -1071,18 +1098,24 @@ attn_kernel(const __grid_constant__ CUtensorMap map_kv, const __grid_constant__ 
             } else {
                 // sums that are no number: an infinity or NaN in a token that the row does not see (0 times that is NaN), or an
                 // overflow of values near the type's largest.  Such a row is computed token by token.
-                for (uint32_t odd = __ballot_sync(~0u, live && !fine); odd; odd &= odd - 1) {
-                    const int from = __ffs(odd) - 1;
-                    attend_row<D, BF16>(a, s, q, __shfl_sync(~0u, tok, from), __shfl_sync(~0u, head, from));
+                uint32_t odd = __ballot_sync(~0u, live && !fine);
+                if (odd) {
+                    if (lane == 0) atomicAdd(state, 1);
+                    for (; odd; odd &= odd - 1) {
+                        const int from = __ffs(odd) - 1;
+                        attend_row<D, BF16>(a, s, q, __shfl_sync(~0u, tok, from), __shfl_sync(~0u, head, from));
+                    }
+                    if (lane == 0) atomicSub(state, 1);
                 }
             }
             fence_before();
         }
-        if (!ok) *failed = 1;
+        if (!ok) give_up();
     }
 
     fence_before();
     __syncthreads();
+    if (threadIdx.x == 0 && gave_up()) atomicOr(a.c.status, ISV_STATUS_WAIT_EXPIRED);
     if (warp == kIssuer) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(*tmem_slot) : "memory");
 }
 

@@ -95,6 +95,25 @@ def test_a_lost_copy_ends_in_a_status_not_a_hang(news, d, dtype):
         B.isv_chunk_free(h)
 
 
+@pytest.mark.parametrize("news,d", [(48, 128), (20, 64), (6, 80)])
+def test_rows_that_take_long_do_not_run_out_the_waits_of_others(news, d):
+    """The value of the last token is infinite: every other row is computed token by token, while the rest of the CTA waits."""
+    n = 4000 + news
+    c = Case([4000], [news], 16, 2, d, "f16")
+    c.pool[c.table[0, (n - 1) // 16], 1, :, (n - 1) % 16] = float("inf")
+    want, tol = c.want(weight_step=2.0 ** -16)
+    c.to_gpu()
+    h = c.handle(max_ctas=1)
+    f32 = torch.full((c.rows, c.Hq, c.d), 7.0, device="cuda")
+    try:
+        B.isv_chunk_set_wait_limit(h, 2000)
+        c.attend(h, None, f32)
+        assert B.isv_chunk_status(h) == 0
+        c.check(f32, want, tol)
+    finally:
+        B.isv_chunk_free(h)
+
+
 def test_knobs_validate_their_arguments(handle):
     _refused("negative", B.isv_chunk_inject_lost_copy, handle, -1)
     _refused("null", B.isv_chunk_set_wait_limit, None, 5)
