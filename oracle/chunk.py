@@ -115,7 +115,13 @@ def attend(q, K, V, pos, seen, scale: float, cap: float = 0.0, slopes=None, weig
 
 
 def verify(target, draft, drafted, u):
-    """target [n + 1, V], draft [n, V] or None, drafted [n], u [n + 1] (the last one for the draw) -> (a, next token)."""
+    """target [n + 1, V], draft [n, V] or None, drafted [n], u [n + 1] (the last one for the draw) -> (a, next token).
+    Probabilities that are negative or NaN count as 0."""
+    def positive(z):
+        z = np.asarray(z, np.float64)
+        return np.where(z > 0, z, 0.0)
+
+    target, draft = positive(target), None if draft is None else positive(draft)
     n = len(drafted)
     a = n
     for i in range(n):
@@ -128,18 +134,15 @@ def verify(target, draft, drafted, u):
             a = i
             break
 
-    def positive(z):
-        return np.where(z > 0, z, 0.0)
-
-    p = np.asarray(target[a], np.float64)
-    w = positive(p)
+    p = target[a]
+    w = p
     if a < n:
         if draft is None:
-            r = positive(p)
+            r = p.copy()
             if 0 <= int(drafted[a]) < len(r):
                 r[int(drafted[a])] = 0.0
         else:
-            r = positive(p - np.asarray(draft[a], np.float64))
+            r = positive(p - draft[a])
         if r.sum() > 0:
             w = r
     if not w.sum() > 0:

@@ -61,6 +61,10 @@ __device__ __forceinline__ float number<__half>(__half x) { return __half2float(
 template <>
 __device__ __forceinline__ float number<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
 
+// A probability: what is negative or no number counts as 0.
+template <typename T>
+__device__ __forceinline__ float chance(T x) { return fmaxf(number<T>(x), 0.f); }
+
 // E adjacent probabilities from index i on; those at `end` and behind it are 0.
 template <typename T, bool VEC, int E>
 __device__ __forceinline__ void load(const T *row, int i, int end, float (&x)[E]) {
@@ -68,11 +72,11 @@ __device__ __forceinline__ void load(const T *row, int i, int end, float (&x)[E]
         const uint4 w = *reinterpret_cast<const uint4 *>(row + i);
         const T *e = reinterpret_cast<const T *>(&w);
 #pragma unroll
-        for (int y = 0; y < E; ++y) x[y] = number<T>(e[y]);
+        for (int y = 0; y < E; ++y) x[y] = chance<T>(e[y]);
         return;
     }
 #pragma unroll
-    for (int y = 0; y < E; ++y) x[y] = i + y < end ? number<T>(row[i + y]) : 0.f;
+    for (int y = 0; y < E; ++y) x[y] = i + y < end ? chance<T>(row[i + y]) : 0.f;
 }
 
 // What a lane holds of a row before it is used: 16 bytes of adjacent probabilities, or (rows that are not aligned) elements that
@@ -99,11 +103,11 @@ struct Batch {
         }
     }
     __device__ __forceinline__ float at(int d, int y) const {
-        return number<T>(VEC ? reinterpret_cast<const T *>(&w[d])[y] : e[d * E + y]);
+        return chance<T>(VEC ? reinterpret_cast<const T *>(&w[d])[y] : e[d * E + y]);
     }
 };
 
-// Weight of one token in the residual: what the target gives it beyond the draft.  What is not a positive number weighs nothing.
+// Weight of one token in the residual: what the target gives it beyond the draft.
 __device__ __forceinline__ double beyond(float p, float q) {
     const double r = (double)p - (double)q;
     return r > 0 ? r : 0.0;
@@ -204,8 +208,8 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const Params p) {
                 if (x < 0 || x >= p.V) {
                     bad |= ISV_STATUS_BAD_TOKEN;
                 } else {
-                    const double px = number<T>(target[(first + i) * p.V + x]);
-                    const double qx = draft ? (double)number<T>(draft[((long long)s * p.K + i) * p.V + x]) : 1.0;
+                    const double px = chance<T>(target[(first + i) * p.V + x]);
+                    const double qx = draft ? (double)chance<T>(draft[((long long)s * p.K + i) * p.V + x]) : 1.0;
                     keep = (double)u * qx < px;
                 }
             }

@@ -246,6 +246,25 @@ def test_zero_probabilities_bad_tokens_and_counts():
         _hold(again, target, draft, drafted, counts, u)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("V", [64, 1003])
+def test_probabilities_that_are_negative_or_no_number_count_as_zero(V, dtype):
+    S, K = 60, 3
+    target, draft, drafted, counts, u = _drafts(S, K, V, dtype, V)
+    g = torch.Generator().manual_seed(V)
+    for x in (target, draft):
+        odd = torch.rand(x.shape, generator=g)
+        x[odd < 0.2] *= -1
+        x[odd > 0.9] = float("nan")
+    for s in range(0, S, 2):                                                   # drafts that their model gave nothing
+        draft[s, 0, drafted[s, 0]] = (-1.0, float("nan"))[s // 2 % 2]
+    counts[:30] = K
+    got = _verify(target.cuda(), draft.cuda(), drafted.cuda(), dev(counts), u.cuda(), V, dtype)
+    _hold(got, target, draft, drafted, counts, u)
+    got = _verify(target.cuda(), None, drafted.cuda(), dev(counts), u.cuda(), V, dtype)
+    _hold(got, target, None, drafted, counts, u)
+
+
 def test_target_rows_at_their_starts():
     """Rows of sequences one behind the other; rows that are not there cost their drafts, or the token."""
     S, K, V = 5, 3, 1001

@@ -108,4 +108,8 @@ def test_verification_rules():
     assert oc.verify(p[:1], None, [], [0.5]) == (0, 1)
     assert oc.verify(p, p[:1], [2], [0.5, 0.7]) == (0, 1)               # an empty residual: the target itself
     assert oc.verify(np.zeros((2, 3)), q, [0], [0.5, 0.5]) == (0, -1)
+    odd = np.array([[np.nan, -0.5, 0.75]])                              # count as 0: the residual of the target beyond them is all of it
+    assert oc.verify(p, odd, [2], [0.0, 0.0]) == (0, 0) and oc.verify(p, odd, [2], [0.0, 0.5]) == (0, 1)
+    assert oc.verify(p, odd, [0], [0.9, 0.0]) == (1, 0) and oc.verify(p, odd, [1], [0.9, 0.0]) == (1, 0)
+    assert oc.verify(np.stack([-p[0], p[1]]), odd, [1], [0.9, 0.0]) == (0, -1)
     assert oc.verify(p, q, [7], [0.0, 0.0]) == (0, 1)
