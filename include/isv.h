@@ -598,8 +598,8 @@ int isv_linear4_free(isv_linear4 *l);
  * one layer of it.  Sequence s has seq_lens_dev[s] tokens, the new ones included; its last new_lens_dev[s] <= T of them
  * (NULL = T of every sequence) are the chunk, at positions seq_lens_dev[s] - new_lens_dev[s] and on.  Their q, k, v and
  * outputs are rows row_starts_dev[s] and on (NULL = s * T) of arrays of n_rows rows, which no two sequences share; rows of no
- * sequence have no influence and are not written.  Row strides are in elements, multiples of 8, and hold at least a token's heads: q, k and v may be parts
- * of one array.
+ * sequence have no influence and are not written.  Row strides are in elements, multiples of 8, and hold at least a token's
+ * heads: q, k and v may be parts of one array.
  * Lengths are clamped to what the table row holds (16 * max_blocks_per_seq), new lengths to [0, min(T, length)] and to the
  * rows there are, and flagged (ISV_STATUS_BAD_LENGTH).  All pointers but block tables, lengths, starts, prefixes, slopes,
  * frequencies and positions (aligned to their elements) are 16-byte aligned. */
@@ -659,7 +659,7 @@ int isv_chunk_write(isv_chunk *h, void *pool_dev, int32_t n_pages, const int32_t
  *     j <= p and (window = 0 or p - j < window), and those with j < prefix_lens_dev[s]
  * (a prefix that all queries see, later ones too), as far as they exist.  slopes_dev: fp32 [q_heads], or NULL;
  * prefix_lens_dev: int32 [n_seqs], or NULL.  Query head h reads KV head h / (q_heads / kv_heads).  out_dev (16-bit) and
- * out_f32_dev (fp32) are [n_rows][q_heads][head_dim] and may each be NULL, not both.  A block without a page
+ * out_f32_dev (fp32) are [n_rows][q_heads][head_dim], may each be NULL, not both, and overlap nothing.  A block without a page
  * (ISV_BLOCK_NONE) is left out and not flagged; other ids outside [0, n_pages) are left out and flagged.  A query that
  * sees nothing yields zeros.  What stands in invisible tokens, infinities and NaN too, changes nothing.
  * Scores, sums and statistics are fp32.  The softmax weights meet V as 16-bit numbers (an error of the order of the output's own
@@ -703,8 +703,8 @@ int isv_chunk_inject_lost_copy(isv_chunk *h, int32_t launches);
  * A drafted token outside [0, vocab) does not stand (ISV_STATUS_BAD_TOKEN).  Where all of a row's probabilities are 0 the
  * next token is -1 (ISV_STATUS_BAD_TOKEN).  Counts outside [0, max_draft] and rows that are not there are clamped and
  * flagged (ISV_STATUS_BAD_LENGTH); a sequence without any row gets no token.  max_draft <= 1024.  Probabilities are aligned
- * to their elements; outputs overlap nothing, but lens_out_dev may be seq_lens_dev.  Uses no memory but what it is given and runs on the current device; asynchronous on `stream`; may be
- * captured; results do not depend on scheduling. */
+ * to their elements; outputs overlap nothing, but lens_out_dev may be seq_lens_dev.  Uses no memory but what it is given and
+ * runs on the current device; asynchronous on `stream`; may be captured; results do not depend on scheduling. */
 int isv_draft_verify(const void *target_dev, const int32_t *row_starts_dev, int32_t n_rows, const void *draft_dev,
                      int32_t vocab, int32_t dtype, const int32_t *drafted_dev, const int32_t *n_draft_dev,
                      const float *uniforms_dev, const int32_t *seq_lens_dev, int32_t n_seqs, int32_t max_draft,

@@ -372,6 +372,7 @@ int isv_chunk_attn(isv_chunk *h, const void *pool_dev, int32_t n_pages, const in
     if (!q_dev || (!out_dev && !out_f32_dev)) return err(ISV_EINVAL, "%s: q and one output are required", who);
     if (misaligned(q_dev) || misaligned(out_dev) || misaligned(out_f32_dev))
         return err(ISV_EINVAL, "%s: q and outputs must be 16-byte aligned", who);
+    if (out_dev == q_dev || out_f32_dev == q_dev || out_dev == out_f32_dev) return err(ISV_EINVAL, "%s: outputs overlap nothing", who);
     if (q_stride % 8 || q_stride < (int64_t)h->d.q_heads * h->d.head_dim)
         return err(ISV_EINVAL, "%s: the stride of q must be a multiple of 8 elements that holds a token's heads", who);
     if (window < 0) return err(ISV_EINVAL, "%s: window must not be negative", who);

@@ -28,7 +28,7 @@ def handle():
 
 def _attn(**kw):
     d = dict(pool=A, n_pages=10, block_table=A, table_stride=4, max_blocks_per_seq=4, seq_lens=A, new_lens=A, row_starts=A, n_rows=8, q=A,
-             q_stride=512, slopes=None, prefix_lens=None, window=0, out=A, out_f32=None, n_seqs=2, T=4)
+             q_stride=512, slopes=None, prefix_lens=None, window=0, out=2 * A, out_f32=None, n_seqs=2, T=4)
     d.update(kw)
     return d
 
@@ -48,7 +48,8 @@ COMMON = [(dict(pool=None), "required"), (dict(block_table=None), "required"), (
 
 @pytest.mark.parametrize("kw,text", COMMON + [
     (dict(q=None), "q and one output"), (dict(out=None), "q and one output"), (dict(q=A + 8), "16-byte"), (dict(out=A + 2), "16-byte"),
-    (dict(out_f32=A + 4), "16-byte"), (dict(q_stride=511), "stride"), (dict(q_stride=504), "stride"), (dict(window=-1), "window")])
+    (dict(out_f32=A + 4), "16-byte"), (dict(q_stride=511), "stride"), (dict(q_stride=504), "stride"), (dict(window=-1), "window"),
+    (dict(out=A), "overlap"), (dict(out_f32=A), "overlap"), (dict(out_f32=2 * A), "overlap")])
 def test_attn_refuses(handle, kw, text):
     _refused(text, B.isv_chunk_attn, handle, **_attn(**kw))
 
